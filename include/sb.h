@@ -466,6 +466,78 @@ sb_status sb_sgd_update(int count, float *const *w, const float *const *g,
                         const size_t *n, const float *scale, float lr,
                         void *stream);
 
+/* AdamW step on `count` tensors (Adam with decoupled weight decay: in place of
+ * the SGD step).  For every element, with g = grad_scale * gradient and t the
+ * number of this update:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *   w = (1 - lr decay) w - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * in fp32; m and v of the update are those before they become bytes.
+ *
+ * Moments (`moments` of the descriptor):
+ *   32  fp32, zero before the first update;
+ *   8   bytes.  The rank of a value is its fp32 pattern's exponent and upper
+ *       three mantissa bits, as a whole number: 8 ranks an octave.  Each block
+ *       of 256 consecutive elements of a tensor has a reference, the largest
+ *       rank in it (m_top, v_top: ceil(n / 256) int16 values).  The byte of v is
+ *       255 - (reference - rank), at least 1 unless v is 0; that of m has the
+ *       sign in its highest bit and 127 - (reference - rank) below it, 0 where
+ *       that is negative: 31 octaves below the block's largest v, 15 below its
+ *       largest m.  A value is rounded to one of its two neighbours at random,
+ *       up with the probability that makes its mean right (a moment that a
+ *       step changes by less than half a rank would otherwise stay as it is),
+ *       from 16 bits of a hash of seed, t and the element's number `first` + i;
+ *       results are the same in every run.  All bytes zero before the first
+ *       update, the references too.  Infinities and NaN stay what they are, the
+ *       other values of their block are lost.
+ *
+ * Tensors: w, g (and m, v of 32 bits) fp32; copy, if not NULL, gets w's new value
+ * in bfloat16.  first: the number of the tensor's first element among the random
+ * numbers; tensors of one model take ranges of their own (unused with 32).  n may
+ * be 0 (nothing to do).  The array is host memory, read before the call returns;
+ * more than 40 tensors take a launch per 40.
+ *
+ * The number of the update is step + *steps_done, where steps_done is a device
+ * counter (int32, 0 at the start) for callers that replay the call from a graph
+ * and advance it there with sb_adamw_advance, or NULL: then it is step.
+ *
+ * SB_ERR_INVALID_ARG for a count outside 1..SB_ADAMW_MAX_TENSORS, betas outside
+ * [0, 1), values that are not finite, a negative eps, step < 1 (< 0 would be with a
+ * counter: the sum has to be at least 1), moments other than 8 and 32, NULL
+ * pointers, pointers that are not multiples of their elements' size, and for
+ * an output (w, copy, moments, references) that overlaps any other tensor of the
+ * call.  Gradients may overlap each other. */
+enum { SB_ADAMW_MAX_TENSORS = 512, SB_ADAMW_BLOCK = 256 };
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int step;              /* >= 1: the update's number, or 1 + what is added
+                              to the counter's value                       */
+    int moments;           /* 32 or 8                                      */
+    uint32_t seed;
+} sb_adamw_desc;
+typedef struct {
+    float *w;
+    void *copy;            /* bfloat16, or NULL                            */
+    const float *g;
+    void *m, *v;           /* fp32, or bytes                               */
+    int16_t *m_top, *v_top; /* references (8), unused (32)                 */
+    uint64_t first;
+    size_t n;
+    float grad_scale;      /* 1/K for FC shards                            */
+    float decay;
+} sb_adamw_tensor;
+sb_status sb_adamw_update(const sb_adamw_desc *desc, int count,
+                          const sb_adamw_tensor *tensors,
+                          const int32_t *steps_done, void *stream);
+
+/* *steps_done += 1, on the stream. */
+sb_status sb_adamw_advance(int32_t *steps_done, void *stream);
+
+/* The values that n moments in bytes stand for, in fp32 (to store, inspect or go
+ * on with in 32 bits).  m_out and v_out may each be NULL (with its inputs). */
+sb_status sb_adamw_unpack(size_t n, const uint8_t *m, const int16_t *m_top,
+                          const uint8_t *v, const int16_t *v_top, float *m_out,
+                          float *v_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

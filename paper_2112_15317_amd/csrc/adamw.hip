@@ -1,0 +1,413 @@
+// adamw.hip -- the AdamW step over many tensors, moments in fp32 or in bytes
+// (in place of the SGD step of sec. 4: what an MP group's worker does with the
+// gradients of its conv layers and FC shards).
+//
+// Per element, in fp32 and in this order:
+//   m = b1 m + (1 - b1) g,   v = b2 v + (1 - b2) g^2,   g = scale * gradient
+//   w = keep w - (lr / (1 - b1^t)) m / (sqrt(v) (1 - b2^t)^-1/2 + eps)
+// keep = 1 - lr * decay; the host forms the factors in fp64.  The products of m
+// and v are rounded before their sum (no fused multiply-add), so that the bytes
+// below are the same wherever they are formed.
+//
+// Moments in bytes.  A positive fp32 pattern's upper 11 bits below the sign are
+// a rank: 8 ranks an octave, equally spaced within one.  A byte says how far a
+// value's rank lies below the largest one of its block of 256 elements, so that a
+// block needs one reference and no division: coding is a shift, an addition and
+// a subtraction.  7 bits of it (m, with the sign) reach 15 octaves down, 8 (v)
+// reach 31, the same as 15 of sqrt(v); a v below that takes the lowest code and
+// not zero, which would turn m / sqrt(v) into m / eps.
+//
+// Rounding is random (up with the probability of the bits left out, so its mean
+// is the value), because b2 = 0.999 changes v by 0.1 % a step and ranks are 6 to
+// 12 % apart: rounded to nearest, v would never move.  The 16 random bits of each
+// moment are halves of a hash of seed, step and element number.
+//
+// The kernel is a stream: 28 bytes an element (16 with moments in bytes), 2 more
+// for the bf16 copy.  A wave takes 256 consecutive elements at a time, four a
+// lane in 16-byte pieces, so that a block of bytes is one wave's and its largest
+// rank a reduction over the lanes; a lane has all its loads under way before the
+// first store.  Blocks of tensor t are block0[t] .. block0[t+1]-1; the block's
+// tensor is found by bisection.
+#include "sb_internal.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+namespace sb {
+
+constexpr int kAdamwLaunch = 40;             // tensors per launch (kernel arguments end at 4 KB)
+constexpr int kAdamwGroups = 4;              // groups of 4 elements per lane
+constexpr int kAdamwBlock = 1024 * kAdamwGroups;
+
+struct AdamwTensor {
+  float* w;
+  u16* copy;
+  const float* g;
+  void *m, *v;
+  int16_t *m_top, *v_top;
+  uint64_t first;
+  size_t n;
+  float scale, keep;
+  int block0, vec;
+};
+
+struct AdamwBatch {
+  AdamwTensor t[kAdamwLaunch];
+  const int32_t* steps_done;
+  double lr, beta1, beta2;
+  float b1, c1, b2, c2, eps, rate, vscale;   // rate, vscale: of step, without a counter
+  uint32_t seed;
+  int step, count;
+};
+static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
+
+__host__ __device__ inline uint32_t mix32(uint32_t x) {
+  x ^= x >> 16;
+  x *= 0x9e3779b9u;
+  x ^= x >> 15;
+  x *= 0xb7e15163u;
+  return x ^ (x >> 16);
+}
+
+// beta^t by squaring.
+__host__ __device__ inline double int_power(double b, uint32_t t) {
+  double p = 1.0;
+  for (; t; t >>= 1) {
+    if (t & 1) p *= b;
+    b *= b;
+  }
+  return p;
+}
+
+__device__ __forceinline__ float rank_value(int rank) {
+  return rank > 0 ? __uint_as_float((uint32_t)rank << 20) : 0.f;
+}
+
+// The rank a magnitude's pattern is rounded to: up if the 20 bits below it and
+// the random ones carry.  Finite values stay finite.
+__device__ __forceinline__ int rank_of(uint32_t bits, uint32_t noise) {
+  const int r = min((int)((bits + noise * 16 + 8) >> 20), 0x7f7);
+  return bits < 0x7f800000u ? r : (bits > 0x7f800000u ? 0x7fc : 0x7f8);
+}
+
+// The largest of both halves over the wave.
+__device__ __forceinline__ uint32_t wave_max2(uint32_t v) {
+  typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    const uint32_t u = (uint32_t)__shfl_xor((int)v, o, 64);
+    v = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(us2, v),
+                                                               __builtin_bit_cast(us2, u)));
+  }
+  return v;
+}
+
+template <class T, class V>
+__device__ __forceinline__ V adamw_load4(const T* p, size_t i, size_t n, bool whole) {
+  if (whole) return *reinterpret_cast<const V*>(p + i);
+  V v{};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) v[e] = p[i + e];
+  return v;
+}
+template <class T, class V>
+__device__ __forceinline__ void adamw_store4(T* p, size_t i, size_t n, bool whole, V v) {
+  if (whole) {
+    *reinterpret_cast<V*>(p + i) = v;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (i + e < n) p[i + e] = v[e];
+}
+
+typedef uint8_t b4 __attribute__((ext_vector_type(4)));
+typedef u16 h4 __attribute__((ext_vector_type(4)));
+
+template <bool BYTES>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch b) {
+  typedef typename std::conditional<BYTES, uint8_t, float>::type S;
+  typedef typename std::conditional<BYTES, b4, f4>::type S4;
+  constexpr int U = kAdamwGroups;
+  const int blk = blockIdx.x;
+  int ti = 0, hi = b.count;                  // the last tensor whose blocks start by blk
+  while (hi - ti > 1) {
+    const int mid = (ti + hi) / 2;
+    if (b.t[mid].block0 <= blk) ti = mid;
+    else hi = mid;
+  }
+  const AdamwTensor& t = b.t[ti];
+  const size_t n = t.n;
+  const size_t base = (size_t)(blk - t.block0) * kAdamwBlock + threadIdx.x * 4;
+  const S *m = (const S*)t.m, *v = (const S*)t.v;
+  f4 w4[U], g4[U];
+  S4 m4[U], v4[U];
+  int mtop[U], vtop[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const size_t i = base + u * 1024;
+    const bool whole = t.vec && i + 4 <= n;
+    g4[u] = adamw_load4<float, f4>(t.g, i, n, whole);
+    m4[u] = adamw_load4<S, S4>(m, i, n, whole);
+    v4[u] = adamw_load4<S, S4>(v, i, n, whole);
+    w4[u] = adamw_load4<float, f4>(t.w, i, n, whole);
+    if constexpr (BYTES) {
+      mtop[u] = i < n ? t.m_top[i / 256] : 0;
+      vtop[u] = i < n ? t.v_top[i / 256] : 0;
+    }
+  }
+  float rate = b.rate, vscale = b.vscale;
+  uint32_t step = (uint32_t)b.step;
+  if (b.steps_done) {
+    step = (uint32_t)max(1, b.step + *b.steps_done);
+    rate = (float)(b.lr / (1.0 - int_power(b.beta1, step)));
+    vscale = (float)(1.0 / sqrt(1.0 - int_power(b.beta2, step)));
+  }
+  const uint32_t key = mix32(b.seed + step * 0x9e3779b9u);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const size_t i = base + u * 1024;
+    if (i - threadIdx.x % 64 * 4 >= n) return;   // whole waves leave together
+    const bool whole = t.vec && i + 4 <= n;
+    f4 nm, nv, nw;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+#pragma clang fp contract(off)
+      float om, ov;
+      if constexpr (BYTES) {
+        const int mc = m4[u][e] & 127, vc = v4[u][e];
+        om = rank_value(mc ? mtop[u] + mc - 127 : 0);
+        om = m4[u][e] > 127 ? -om : om;
+        ov = rank_value(vc ? vtop[u] + vc - 255 : 0);
+      } else {
+        om = m4[u][e];
+        ov = v4[u][e];
+      }
+      const float g = g4[u][e] * t.scale;
+      nm[e] = om * b.b1 + g * b.c1;
+      nv[e] = ov * b.b2 + (g * g) * b.c2;
+      nw[e] = w4[u][e] * t.keep - rate * (nm[e] / (sqrtf(nv[e]) * vscale + b.eps));
+    }
+    adamw_store4<float, f4>(t.w, i, n, whole, nw);
+    if (t.copy) {
+      h4 c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) c[e] = f32_to_bf16(nw[e]);
+      adamw_store4<u16, h4>(t.copy, i, n, whole, c);
+    }
+    if constexpr (!BYTES) {
+      adamw_store4<float, f4>((float*)t.m, i, n, whole, nm);
+      adamw_store4<float, f4>((float*)t.v, i, n, whole, nv);
+    } else {
+      const uint64_t at = t.first + i;
+      int mr[4], vr[4];
+      uint32_t top = 0;                      // m's largest rank above v's
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint64_t id = at + e;
+        const uint32_t h = mix32((uint32_t)id ^ key ^ (uint32_t)(id >> 32) * 0x9e3779b9u);
+        mr[e] = rank_of(__float_as_uint(nm[e]) & 0x7fffffffu, h & 0xffffu);
+        vr[e] = rank_of(__float_as_uint(nv[e]) & 0x7fffffffu, h >> 16);
+        if (i + e >= n) mr[e] = vr[e] = 0;
+      }
+      top = (uint32_t)max(max(mr[0], mr[1]), max(mr[2], mr[3])) << 16 |
+            (uint32_t)max(max(vr[0], vr[1]), max(vr[2], vr[3]));
+      top = wave_max2(top);
+      const int mt = (int)(top >> 16), vt = (int)(top & 0xffffu);
+      b4 mb, vb;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int mc = max(mr[e] - mt + 127, 0), vc = max(vr[e] - vt + 255, 1);
+        mb[e] = (uint8_t)(mc | (mc > 0 && nm[e] < 0.f ? 128 : 0));
+        vb[e] = (uint8_t)(nv[e] == 0.f ? 0 : vc);
+      }
+      adamw_store4<uint8_t, b4>((uint8_t*)t.m, i, n, whole, mb);
+      adamw_store4<uint8_t, b4>((uint8_t*)t.v, i, n, whole, vb);
+      if (threadIdx.x % 64 == 0) {
+        t.m_top[i / 256] = (int16_t)mt;
+        t.v_top[i / 256] = (int16_t)vt;
+      }
+    }
+  }
+}
+
+__global__ void adamw_advance_kernel(int32_t* steps_done) { *steps_done += 1; }
+
+// Four bytes of both moments a lane; a wave has one block's 256.
+__global__ __launch_bounds__(256) void adamw_unpack_kernel(size_t n, const uint8_t* __restrict__ m,
+                                                           const int16_t* __restrict__ m_top,
+                                                           const uint8_t* __restrict__ v,
+                                                           const int16_t* __restrict__ v_top,
+                                                           float* __restrict__ m_out,
+                                                           float* __restrict__ v_out, int vec) {
+  constexpr int U = kAdamwGroups;
+  const size_t base = (size_t)blockIdx.x * kAdamwBlock + threadIdx.x * 4;
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const size_t i = base + u * 1024;
+    if (i >= n) return;
+    const bool whole = vec && i + 4 <= n;
+    if (m_out) {
+      const b4 c = adamw_load4<uint8_t, b4>(m, i, n, whole);
+      const int top = m_top[i / 256];
+      f4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x = rank_value((c[e] & 127) ? top + (c[e] & 127) - 127 : 0);
+        o[e] = c[e] > 127 ? -x : x;
+      }
+      adamw_store4<float, f4>(m_out, i, n, whole, o);
+    }
+    if (v_out) {
+      const b4 c = adamw_load4<uint8_t, b4>(v, i, n, whole);
+      const int top = v_top[i / 256];
+      f4 o;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = rank_value(c[e] ? top + c[e] - 255 : 0);
+      adamw_store4<float, f4>(v_out, i, n, whole, o);
+    }
+  }
+}
+
+}  // namespace sb
+
+namespace {
+
+struct Range {
+  uintptr_t at, end;
+  bool out;
+};
+
+// Whether an output's range meets another one.  Sorted by their starts, a range
+// meets an earlier one exactly if it starts before the furthest end so far.
+bool outputs_meet(Range* r, int count) {
+  std::sort(r, r + count, [](const Range& a, const Range& b) { return a.at < b.at; });
+  uintptr_t in_end = 0, out_end = 0;
+  for (int i = 0; i < count; ++i) {
+    if (r[i].at < out_end || (r[i].out && r[i].at < in_end)) return true;
+    uintptr_t& end = r[i].out ? out_end : in_end;
+    end = std::max(end, r[i].end);
+  }
+  return false;
+}
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+}  // namespace
+
+extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, int count,
+                                     const sb_adamw_tensor* tensors, const int32_t* steps_done,
+                                     void* stream) {
+  if (!d || !tensors || count < 1 || count > SB_ADAMW_MAX_TENSORS) return SB_ERR_INVALID_ARG;
+  if (!std::isfinite(d->lr) || !std::isfinite(d->eps) || !(d->eps >= 0.0)) return SB_ERR_INVALID_ARG;
+  if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0))
+    return SB_ERR_INVALID_ARG;
+  if (d->step < 1 || (d->moments != 8 && d->moments != 32)) return SB_ERR_INVALID_ARG;
+  if (!aligned(steps_done, 4)) return SB_ERR_INVALID_ARG;
+  const bool bytes = d->moments == 8;
+  Range r[7 * SB_ADAMW_MAX_TENSORS + 1];
+  int ranges = 0;
+  auto add = [&](const void* p, size_t size, bool out) {
+    r[ranges++] = Range{(uintptr_t)p, (uintptr_t)p + size, out};
+  };
+  if (steps_done) add(steps_done, 4, false);
+  long blocks = 0;
+  for (int i = 0; i < count; ++i) {
+    const sb_adamw_tensor& t = tensors[i];
+    if (!std::isfinite(t.grad_scale) || !std::isfinite(t.decay) ||
+        !std::isfinite((float)(1.0 - d->lr * t.decay)))
+      return SB_ERR_INVALID_ARG;
+    if (t.n == 0) continue;
+    if (!t.w || !t.g || !t.m || !t.v || t.n >= (1ull << 40)) return SB_ERR_INVALID_ARG;
+    if (!aligned(t.w, 4) || !aligned(t.g, 4) || !aligned(t.copy, 2)) return SB_ERR_INVALID_ARG;
+    const size_t tops = (t.n + SB_ADAMW_BLOCK - 1) / SB_ADAMW_BLOCK;
+    if (bytes) {
+      if (!t.m_top || !t.v_top || !aligned(t.m_top, 2) || !aligned(t.v_top, 2))
+        return SB_ERR_INVALID_ARG;
+      add(t.m_top, tops * 2, true);
+      add(t.v_top, tops * 2, true);
+    } else if (!aligned(t.m, 4) || !aligned(t.v, 4)) {
+      return SB_ERR_INVALID_ARG;
+    }
+    add(t.w, t.n * 4, true);
+    add(t.g, t.n * 4, false);
+    add(t.m, t.n * (bytes ? 1 : 4), true);
+    add(t.v, t.n * (bytes ? 1 : 4), true);
+    if (t.copy) add(t.copy, t.n * 2, true);
+    blocks += (long)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
+    if (blocks >= (1l << 31)) return SB_ERR_UNSUPPORTED;
+  }
+  if (outputs_meet(r, ranges)) return SB_ERR_INVALID_ARG;
+  const double lr1 = d->lr / (1.0 - sb::int_power(d->beta1, (uint32_t)d->step));
+  const double vs = 1.0 / std::sqrt(1.0 - sb::int_power(d->beta2, (uint32_t)d->step));
+  if (!std::isfinite((float)lr1) || !std::isfinite((float)vs)) return SB_ERR_INVALID_ARG;
+  sb::AdamwBatch b{};
+  b.steps_done = steps_done;
+  b.lr = d->lr; b.beta1 = d->beta1; b.beta2 = d->beta2;
+  b.b1 = (float)d->beta1; b.c1 = (float)(1.0 - d->beta1);
+  b.b2 = (float)d->beta2; b.c2 = (float)(1.0 - d->beta2);
+  b.eps = (float)d->eps; b.rate = (float)lr1; b.vscale = (float)vs;
+  b.seed = d->seed; b.step = d->step;
+  blocks = 0;
+  for (int i = 0; i <= count; ++i) {
+    if (b.count == sb::kAdamwLaunch || i == count) {
+      if (b.count) {
+        if (bytes)
+          sb::adamw_kernel<true><<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(b);
+        else
+          sb::adamw_kernel<false><<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(b);
+        const sb_status s = sbh::launch_status();
+        if (s != SB_OK) return s;
+      }
+      b.count = 0;
+      blocks = 0;
+      if (i == count) break;
+    }
+    const sb_adamw_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    sb::AdamwTensor& o = b.t[b.count++];
+    o.w = t.w; o.copy = (sb::u16*)t.copy; o.g = t.g; o.m = t.m; o.v = t.v;
+    o.m_top = t.m_top; o.v_top = t.v_top; o.first = t.first; o.n = t.n;
+    o.scale = t.grad_scale;
+    o.keep = (float)(1.0 - d->lr * t.decay);
+    o.block0 = (int)blocks;
+    // Four elements at a time: 16, 8 and 4 bytes of fp32, bf16 and bytes.
+    o.vec = aligned(t.w, 16) && aligned(t.g, 16) && aligned(t.copy, 8) &&
+            aligned(t.m, bytes ? 4 : 16) && aligned(t.v, bytes ? 4 : 16);
+    blocks += (long)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
+  }
+  return SB_OK;
+}
+
+extern "C" sb_status sb_adamw_advance(int32_t* steps_done, void* stream) {
+  if (!steps_done || !aligned(steps_done, 4)) return SB_ERR_INVALID_ARG;
+  sb::adamw_advance_kernel<<<1, 1, 0, sbh::stream_of(stream)>>>(steps_done);
+  return sbh::launch_status();
+}
+
+extern "C" sb_status sb_adamw_unpack(size_t n, const uint8_t* m, const int16_t* m_top,
+                                     const uint8_t* v, const int16_t* v_top, float* m_out,
+                                     float* v_out, void* stream) {
+  if (n == 0) return SB_OK;
+  if (n >= (1ull << 40)) return SB_ERR_INVALID_ARG;
+  if ((m_out && (!m || !m_top)) || (v_out && (!v || !v_top))) return SB_ERR_INVALID_ARG;
+  if (!aligned(m_out, 4) || !aligned(v_out, 4) || !aligned(m_top, 2) || !aligned(v_top, 2))
+    return SB_ERR_INVALID_ARG;
+  if (!m_out && !v_out) return SB_OK;
+  const size_t tops = (n + SB_ADAMW_BLOCK - 1) / SB_ADAMW_BLOCK * 2;
+  const void* in[4] = {m_out ? m : nullptr, m_out ? m_top : nullptr, v_out ? v : nullptr,
+                       v_out ? v_top : nullptr};
+  const size_t inb[4] = {n, tops, n, tops};
+  for (int i = 0; i < 4; ++i)
+    if (sbh::overlaps(m_out, n * 4, in[i], inb[i]) || sbh::overlaps(v_out, n * 4, in[i], inb[i]))
+      return SB_ERR_INVALID_ARG;
+  if (sbh::overlaps(m_out, n * 4, v_out, n * 4)) return SB_ERR_INVALID_ARG;
+  const size_t blocks = (n + sb::kAdamwBlock - 1) / sb::kAdamwBlock;
+  if (blocks >= (1ull << 31)) return SB_ERR_UNSUPPORTED;
+  const int vec = aligned(m_out, 16) && aligned(v_out, 16) && (!m_out || aligned(m, 4)) &&
+                  (!v_out || aligned(v, 4));
+  sb::adamw_unpack_kernel<<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(
+      n, m, m_top, v, v_top, m_out, v_out, vec);
+  return sbh::launch_status();
+}

@@ -28,6 +28,7 @@ SB_PASS_FWD, SB_PASS_BWD_DATA, SB_PASS_BWD_WEIGHT, SB_PASS_FWD_POOL = 0, 1, 2, 3
 SIZE_MAX = 2 ** 64 - 1          # (size_t)-1: the workspace queries' "not supported"
 SB_FC_FWD, SB_FC_BWD = 0, 1
 SB_SGD_MAX_TENSORS = 64
+SB_ADAMW_MAX_TENSORS, SB_ADAMW_BLOCK = 512, 256
 SB_NOALLOC_SCRATCH_BYTES = 40 << 20
 
 _vp = ctypes.c_void_p
@@ -43,6 +44,18 @@ class sb_conv3x3_desc(ctypes.Structure):
 class sb_fc_desc(ctypes.Structure):
     _fields_ = [("m", _i), ("k_in", _i), ("n_shard", _i), ("dtype", _i),
                 ("ldx", _i), ("ldy", _i), ("flags", ctypes.c_uint)]
+
+
+class sb_adamw_desc(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", _i), ("moments", _i),
+                ("seed", ctypes.c_uint32)]
+
+
+class sb_adamw_tensor(ctypes.Structure):
+    _fields_ = [("w", _vp), ("copy", _vp), ("g", _vp), ("m", _vp), ("v", _vp), ("m_top", _vp),
+                ("v_top", _vp), ("first", ctypes.c_uint64), ("n", _sz),
+                ("grad_scale", ctypes.c_float), ("decay", ctypes.c_float)]
 
 
 class sb_modulo_desc(ctypes.Structure):
@@ -90,6 +103,10 @@ SIGNATURES = {
     "sb_log_softmax_nll": (_i, [_i, _i, _i, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
     "sb_sgd_update": (_i, [_i, ctypes.POINTER(_vp), ctypes.POINTER(_vp), ctypes.POINTER(_sz),
                            ctypes.POINTER(ctypes.c_float), ctypes.c_float, _vp]),
+    "sb_adamw_update": (_i, [ctypes.POINTER(sb_adamw_desc), _i, ctypes.POINTER(sb_adamw_tensor),
+                             _vp, _vp]),
+    "sb_adamw_advance": (_i, [_vp, _vp]),
+    "sb_adamw_unpack": (_i, [_sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
 
 _lock = threading.Lock()
@@ -414,3 +431,90 @@ class SgdList:
 def sb_sgd_update(slist, lr, stream=None):
     _check("sb_sgd_update", load().sb_sgd_update(
         slist.count, slist.w, slist.g, slist.n, slist.scale, float(lr), _stream(stream)))
+
+
+# ------------------------------------------------------------------- AdamW --
+class AdamwList:
+    """Marshalled arguments of sb_adamw_update for a fixed list of tensors:
+    built once, passed to every call (the tensors must stay alive).
+
+    items: dicts of a parameter ``w``, its gradient ``g`` (fp32) and moments
+    ``m`` and ``v`` (fp32; or uint8, with their references ``m_top`` and
+    ``v_top``, int16, one for each SB_ADAMW_BLOCK elements), and, if wanted,
+    ``copy`` (bfloat16, gets the new w), ``scale`` (of the gradient, 1),
+    ``decay`` (0) and ``first`` (the number of the tensor's first element
+    among the random numbers; by default the tensors follow one another).
+    ``adamw_moments`` makes zero moments."""
+
+    def __init__(self, items):
+        import torch
+        n = len(items)
+        if not 1 <= n <= SB_ADAMW_MAX_TENSORS:
+            raise ValueError("1 to %d tensors per update" % SB_ADAMW_MAX_TENSORS)
+        self.moments = 8 if items[0]["m"].dtype == torch.uint8 else 32
+        kind = torch.uint8 if self.moments == 8 else torch.float32
+        self.count = n
+        self.tensors = (sb_adamw_tensor * n)()
+        first = 0
+        for t, it in zip(self.tensors, items):
+            w, g, m, v = it["w"], it["g"], it["m"], it["v"]
+            size = w.numel()
+            copy, m_top, v_top = it.get("copy"), it.get("m_top"), it.get("v_top")
+            if (w.dtype != torch.float32 or g.dtype != torch.float32 or m.dtype != kind
+                    or v.dtype != kind or not size == g.numel() == m.numel() == v.numel()):
+                raise ValueError("fp32 parameter and gradient, moments of one type, of equal size")
+            if copy is not None and (copy.dtype != torch.bfloat16 or copy.numel() != size):
+                raise ValueError("the copy is bfloat16, of the parameter's size")
+            if self.moments == 8:
+                tops = (size + SB_ADAMW_BLOCK - 1) // SB_ADAMW_BLOCK
+                for top in (m_top, v_top):
+                    if top is None or top.dtype != torch.int16 or top.numel() != tops:
+                        raise ValueError("int16 references, one for each %d elements"
+                                         % SB_ADAMW_BLOCK)
+            t.w, t.copy, t.g, t.m, t.v = _ptr(w), _ptr(copy), _ptr(g), _ptr(m), _ptr(v)
+            t.m_top, t.v_top = _ptr(m_top), _ptr(v_top)
+            t.first = it.get("first", first)
+            t.n = size
+            t.grad_scale, t.decay = it.get("scale", 1.0), it.get("decay", 0.0)
+            first = t.first + size
+
+
+def adamw_moments(w, moments=32):
+    """Zero moments for parameter w as AdamwList takes them (a dict)."""
+    import torch
+    n = w.numel()
+    if moments == 32:
+        return {k: torch.zeros(n, dtype=torch.float32, device=w.device) for k in ("m", "v")}
+    if moments != 8:
+        raise ValueError("moments of 32 or 8 bits")
+    tops = (n + SB_ADAMW_BLOCK - 1) // SB_ADAMW_BLOCK
+    d = {k: torch.zeros(n, dtype=torch.uint8, device=w.device) for k in ("m", "v")}
+    d.update({k: torch.zeros(tops, dtype=torch.int16, device=w.device) for k in ("m_top", "v_top")})
+    return d
+
+
+def sb_adamw_update(alist, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, steps_done=None,
+                    stream=None):
+    """step: the number of this update (from 1), or, with the int32 device
+    counter steps_done, what is added to its value."""
+    d = sb_adamw_desc(float(lr), float(beta1), float(beta2), float(eps), int(step), alist.moments,
+                      int(seed) & 0xffffffff)
+    _check("sb_adamw_update", load().sb_adamw_update(
+        ctypes.byref(d), alist.count, alist.tensors, _counter(steps_done), _stream(stream)))
+
+
+def _counter(t):
+    if t is not None and not isinstance(t, int) and str(t.dtype) != "torch.int32":
+        raise ValueError("the counter is int32")
+    return _ptr(t)
+
+
+def sb_adamw_advance(steps_done, stream=None):
+    _check("sb_adamw_advance", load().sb_adamw_advance(_counter(steps_done), _stream(stream)))
+
+
+def sb_adamw_unpack(n, m, m_top, v, v_top, m_out, v_out, stream=None):
+    """The fp32 values of n moments in bytes (either pair may be None)."""
+    _check("sb_adamw_unpack", load().sb_adamw_unpack(
+        int(n), _ptr(m), _ptr(m_top), _ptr(v), _ptr(v_top), _ptr(m_out), _ptr(v_out),
+        _stream(stream)))
