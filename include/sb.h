@@ -330,6 +330,67 @@ sb_status sb_fc_shard_bwd(const sb_fc_desc *desc, const void *x,
                           void *workspace, size_t workspace_bytes, void *stream);
 
 /* ------------------------------------------------------------------------
+ * Gated FC column shard: a dense layer with a gate in place of the ReLU (one
+ * projection of the input, through an activation, multiplies another), split
+ * along its outputs like the FC shard above and run on the same gathered
+ * batch:
+ *   a = x * w_gate + b_gate,  u = x * w_up + b_up,  y = act(a) * u
+ *
+ *   x               [m][k_in]      gathered activations, row stride ldx
+ *   w_gate, w_up    [k_in][n_shard] this worker's columns, dense
+ *   b_gate, b_up    [n_shard]       fp32, each may be NULL (zero)
+ *   y, dy           [m][n_shard]    row stride ldy
+ *   pre             [2][m][n_shard] fp32, dense: a, then u
+ * Types as for the FC shard: SB_F32, or SB_BF16 (x, the weights, y, dy and
+ * dx_partial bfloat16; biases, pre and the parameters' gradients fp32).  a, u,
+ * the activation and its product with u are fp32 in both.
+ * ---------------------------------------------------------------------- */
+typedef enum {
+    SB_ACT_SIGMOID = 0,    /* 1 / (1 + exp(-a))                              */
+    SB_ACT_SILU = 1,       /* a / (1 + exp(-a))                              */
+    SB_ACT_GELU = 2,       /* a * (1 + erf(a / sqrt(2))) / 2                 */
+    SB_ACT_GELU_TANH = 3,  /* a * (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))) / 2 */
+    SB_ACT_RELU = 4        /* max(a, 0); its derivative at 0 is 0            */
+} sb_act;
+
+typedef struct {
+    int m, k_in, n_shard;  /* gathered rows, input features, shard columns */
+    int dtype;             /* sb_dtype                                     */
+    int act;               /* sb_act                                       */
+    int ldx;               /* row stride of x and dx_partial (>= k_in)     */
+    int ldy;               /* row stride of y and dy (>= n_shard)          */
+} sb_gated_desc;
+
+/* Workspace bytes for `pass` (SB_FC_FWD, SB_FC_BWD); (size_t)-1 for an invalid
+ * descriptor, and for one whose x, y or weights reach 2^31 bytes. */
+size_t sb_gated_workspace_bytes(const sb_gated_desc *desc, int pass);
+
+/* y as above.  pre may be NULL (inference); the backward needs it. */
+sb_status sb_gated_shard_fwd(const sb_gated_desc *desc, const void *x,
+                             const void *w_gate, const void *w_up,
+                             const float *b_gate, const float *b_up, void *y,
+                             float *pre, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/* From the forward's pre and the gradient dy of y, with
+ *   da = dy * u * act'(a),  du = dy * act(a)   (fp32):
+ *   dx_partial[i,k] = sum_j da[i,j] w_gate[k,j] + du[i,j] w_up[k,j]
+ *                                              (may be NULL: skipped)
+ *   dw_gate[k,j]    = (accumulate ? dw_gate[k,j] : 0) + sum_i x[i,k] da[i,j]
+ *   db_gate[j]      = (accumulate ? db_gate[j]   : 0) + sum_i da[i,j]
+ * and dw_up, db_up likewise with du (db_gate, db_up may each be NULL).  The
+ * parameters' gradients are fp32 and carry da and du in full; SB_BF16's
+ * dx_partial, itself rounded to bf16, is summed from da and du rounded to
+ * bf16.  As for the FC shard the division by K is the optimiser's.
+ * The summation order is fixed: repeated calls give bit-identical results. */
+sb_status sb_gated_shard_bwd(const sb_gated_desc *desc, const void *x,
+                             const void *w_gate, const void *w_up,
+                             const float *pre, const void *dy, void *dx_partial,
+                             float *dw_gate, float *dw_up, float *db_gate,
+                             float *db_up, int accumulate, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
  * Modulo and shard layers on one device (sec. 3.1, Modulo Layer and Shard
  * Layer; sec. 3.2, Group MP Extension).
  *

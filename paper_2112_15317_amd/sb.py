@@ -27,6 +27,7 @@ SB_PACKED_FILTERS = 2
 SB_PASS_FWD, SB_PASS_BWD_DATA, SB_PASS_BWD_WEIGHT, SB_PASS_FWD_POOL = 0, 1, 2, 3
 SIZE_MAX = 2 ** 64 - 1          # (size_t)-1: the workspace queries' "not supported"
 SB_FC_FWD, SB_FC_BWD = 0, 1
+SB_ACT_SIGMOID, SB_ACT_SILU, SB_ACT_GELU, SB_ACT_GELU_TANH, SB_ACT_RELU = range(5)
 SB_SGD_MAX_TENSORS = 64
 SB_ADAMW_MAX_TENSORS, SB_ADAMW_BLOCK = 512, 256
 SB_NOALLOC_SCRATCH_BYTES = 40 << 20
@@ -56,6 +57,11 @@ class sb_adamw_tensor(ctypes.Structure):
     _fields_ = [("w", _vp), ("copy", _vp), ("g", _vp), ("m", _vp), ("v", _vp), ("m_top", _vp),
                 ("v_top", _vp), ("first", ctypes.c_uint64), ("n", _sz),
                 ("grad_scale", ctypes.c_float), ("decay", ctypes.c_float)]
+
+
+class sb_gated_desc(ctypes.Structure):
+    _fields_ = [("m", _i), ("k_in", _i), ("n_shard", _i), ("dtype", _i), ("act", _i),
+                ("ldx", _i), ("ldy", _i)]
 
 
 class sb_modulo_desc(ctypes.Structure):
@@ -94,6 +100,11 @@ SIGNATURES = {
     "sb_fc_shard_fwd": (_i, [ctypes.POINTER(sb_fc_desc), _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "sb_fc_shard_bwd": (_i, [ctypes.POINTER(sb_fc_desc), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i,
                              _vp, _sz, _vp]),
+    "sb_gated_workspace_bytes": (_sz, [ctypes.POINTER(sb_gated_desc), _i]),
+    "sb_gated_shard_fwd": (_i, [ctypes.POINTER(sb_gated_desc), _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                _vp, _sz, _vp]),
+    "sb_gated_shard_bwd": (_i, [ctypes.POINTER(sb_gated_desc), _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                _vp, _vp, _vp, _i, _vp, _sz, _vp]),
     "sb_modulo_fwd": (_i, [ctypes.POINTER(sb_modulo_desc), _i, _i, _vp, _sz, _vp, _vp]),
     "sb_modulo_bwd": (_i, [ctypes.POINTER(sb_modulo_desc), _i, _i, _vp, _sz, _vp, _sz, _vp]),
     "sb_shard_fwd": (_i, [ctypes.POINTER(sb_shard_desc), _i, _vp, _sz, _vp, _vp]),
@@ -192,6 +203,10 @@ def conv_desc(n, c, h, w, k, dtype=SB_F32, relu=False, packed=False, layout=SB_N
 def fc_desc(m, k_in, n_shard, dtype=SB_F32, ldx=None, ldy=None, relu=False):
     return sb_fc_desc(m, k_in, n_shard, dtype, ldx or k_in, ldy or n_shard,
                       SB_FUSE_RELU if relu else 0)
+
+
+def gated_desc(m, k_in, n_shard, dtype=SB_F32, act=SB_ACT_SILU, ldx=None, ldy=None):
+    return sb_gated_desc(m, k_in, n_shard, dtype, act, ldx or k_in, ldy or n_shard)
 
 
 # --------------------------------------------------------- entry points --
@@ -325,6 +340,28 @@ def sb_fc_shard_bwd(desc, x, w_shard, dy, relu_mask_src, dx_partial, dw_shard, d
         ctypes.byref(desc), _ptr(x), _ptr(w_shard), _ptr(dy), _ptr(relu_mask_src),
         _ptr(dx_partial), _ptr(dw_shard), _ptr(db_shard), 1 if accumulate else 0, p, nb,
         _stream(stream)))
+
+
+# ---------------------------------------------------------- gated FC shard --
+def sb_gated_workspace_bytes(desc, pass_):
+    return load().sb_gated_workspace_bytes(ctypes.byref(desc), pass_)
+
+
+def sb_gated_shard_fwd(desc, x, w_gate, w_up, b_gate, b_up, y, pre=None, ws=None, stream=None):
+    """pre: fp32 [2][m][n_shard], kept for the backward, or None."""
+    p, nb = _ws(ws)
+    _check("sb_gated_shard_fwd", load().sb_gated_shard_fwd(
+        ctypes.byref(desc), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(b_gate), _ptr(b_up), _ptr(y),
+        _ptr(pre), p, nb, _stream(stream)))
+
+
+def sb_gated_shard_bwd(desc, x, w_gate, w_up, pre, dy, dx_partial, dw_gate, dw_up, db_gate, db_up,
+                       accumulate=False, ws=None, stream=None):
+    p, nb = _ws(ws)
+    _check("sb_gated_shard_bwd", load().sb_gated_shard_bwd(
+        ctypes.byref(desc), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(pre), _ptr(dy),
+        _ptr(dx_partial), _ptr(dw_gate), _ptr(dw_up), _ptr(db_gate), _ptr(db_up),
+        1 if accumulate else 0, p, nb, _stream(stream)))
 
 
 # ------------------------------------------------ modulo and shard layers --
