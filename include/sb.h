@@ -75,6 +75,7 @@ typedef enum { SB_NCHW = 0, SB_NCHW8C = 1 } sb_layout;
 #define SB_FUSE_RELU 1u       /* apply ReLU to the output (conv fwd, FC fwd) */
 #define SB_PACKED_FILTERS 2u  /* conv fwd / data gradient: `w` holds filters
                                  packed by sb_conv3x3_pack_filters */
+#define SB_UNALIGNED 4u       /* gated FC: x or weights off 16-byte boundaries */
 
 /* Returns a static string naming the status. */
 const char *sb_status_string(sb_status s);
@@ -359,10 +360,15 @@ typedef struct {
     int act;               /* sb_act                                       */
     int ldx;               /* row stride of x and dx_partial (>= k_in)     */
     int ldy;               /* row stride of y and dy (>= n_shard)          */
+    unsigned flags;        /* SB_UNALIGNED (workspace query)               */
 } sb_gated_desc;
 
 /* Workspace bytes for `pass` (SB_FC_FWD, SB_FC_BWD); (size_t)-1 for an invalid
- * descriptor, and for one whose x, y or weights reach 2^31 bytes. */
+ * descriptor, and for one whose x, y or weights reach 2^31 bytes.  The workspace
+ * starts at a multiple of 16.  bf16 operands that no 16-byte access fits are laid
+ * out anew in it: those of odd sizes or strides always have their room; for x or
+ * weights whose addresses are not multiples of 16 the query is asked with
+ * SB_UNALIGNED (a call with less returns SB_ERR_WORKSPACE). */
 size_t sb_gated_workspace_bytes(const sb_gated_desc *desc, int pass);
 
 /* y as above.  pre may be NULL (inference); the backward needs it. */

@@ -1,0 +1,366 @@
+// gemm_dual.hpp -- bf16 products of the gated FC shard (gated.hip) on the
+// 32x32x16 MFMA, two weight matrices (or their gradients) at a time.
+//
+//   FWD   gate and up = x * Wg, x * Wu          x [m][k], W [k][n]
+//   DX    sum over q of d_q * W_q^T             d_q [m][n], W_q [kin][n]
+//   DW    x^T * da and x^T * du                 x [m][kin], d [m][n]
+//
+// A block has 64 F rows (M) by 64 F columns: of FWD and DW 32 F columns of each
+// of the two outputs (N), so the operand they share is staged once and the gate's
+// value and the other projection's for one output element end in one lane.  Four
+// waves, 2 x 2, each F x F blocks of 32 x 32 in registers.  The reduction is a
+// list of segments of equal length (DX: one per weight matrix; DW: one per bf16
+// part of da and du), each in stages of 32.
+//
+// Three stages are in LDS: while stage t is multiplied, t + 2 is written from
+// registers and t + 3 loaded, and t + 1 can already be read, so that the operands
+// of the next 16 k are in registers before the current ones are used up.  An
+// operand that is contiguous along k (x of FWD, both of DX) lies in LDS as rows
+// of four 16-byte pieces and is read as such; one that is contiguous along its
+// rows keeps its layout, and the transposing LDS read (ds_read_b64_tr_b16) gives a
+// lane its column's four k.  Pieces are permuted so that neither the writes nor
+// the reads meet in a bank: piece p of row r at p ^ r / 4 % 4, a column
+// block of 16 of line k at block ^ k % 4.
+//
+// The weight (or d) is the MFMA's first operand, so a lane has four consecutive
+// output columns of a row in four registers and stores them at once.
+#pragma once
+
+#include "gate.hpp"
+
+namespace sb {
+
+typedef short s8v __attribute__((ext_vector_type(8)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+
+enum DualKind { kDualFwd, kDualDx, kDualDw };
+
+template <int F_>
+struct DualTile {
+  static constexpr int F = F_;
+  static constexpr int BM = 64 * F, RC = 32 * F;     // rows; columns of a region
+  static constexpr int OPER = BM * 32;               // elements of an operand's stage
+  static constexpr int STAGE = 2 * OPER;
+  static constexpr size_t LDS_BYTES = 3 * (size_t)STAGE * sizeof(u16);
+};
+
+struct DualArgs {
+  const u16* a[3];                 // per segment
+  const u16* b[2][3];              // per region (DX: region 0) and segment
+  uint32_t a_bytes, b_bytes;       // ranges of the operands
+  int lda, ldb;
+  int M, N, K, segs;               // K: of a segment
+  int mt, nt, splits, stages;      // stages per split
+  float* part;                     // splits > 1: [split][2][M][N] (DX [split][M][N])
+  void* c[2]; int ldc;             // DX: dx (bf16); DW: fp32 gradients; FWD: y in c[0]
+  const float* bias[2];            // FWD
+  float* pre;                      // FWD, may be null: [2][M][N]
+  int accumulate;
+};
+
+__device__ __forceinline__ f16v mfma32(s8v a, s8v b, f16v c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ u4v load16(rsrc_t r, uint32_t off) {
+  return __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+}
+
+// A staged operand: KC contiguous along k, otherwise two regions of RC columns.
+template <class T, bool KC>
+struct DualStage {
+  uint32_t off[T::F];              // byte offset of this lane's pieces at k = 0, or kOOB
+  int lds[T::F];                   // their place (elements)
+  uint32_t step;                   // bytes per k
+  int k;                           // KC: the first k of all of them within a stage
+  // Rows (KC) or columns from r0 on, `rows` of them; region 1 starts at r1.
+  __device__ __forceinline__ void init(int tid, int ld, int rows, int r0, int r1) {
+    step = KC ? 2u : (uint32_t)ld * 2u;
+    k = KC ? tid % 4 * 8 : 0;
+#pragma unroll
+    for (int i = 0; i < T::F; ++i) {
+      if constexpr (KC) {
+        const int row = (tid + 256 * i) / 4, p = tid % 4;
+        lds[i] = row * 32 + (p ^ (row >> 2 & 3)) * 8;
+        off[i] = r0 + row < rows ? (uint32_t)((r0 + row) * ld + p * 8) * 2u : kOOB;
+      } else {
+        constexpr int PR = T::RC / 8;                // pieces a line
+        const int region = i / (T::F / 2);
+        const int w = tid + 256 * (i % (T::F / 2)), line = w / PR, p = w % PR;
+        const int col = (region ? r1 : r0) + p * 8;
+        lds[i] = region * (T::RC * 32) + line * T::RC + ((p / 2 ^ (line & 3)) * 2 + p % 2) * 8;
+        off[i] = col < rows ? (uint32_t)(line * ld + col) * 2u : kOOB;
+      }
+    }
+  }
+  // Piece i of the stage from k0 on (k0 < K); r: its region's resource.  Lines at
+  // and past K lie behind the operand and read 0 by its range, as kOOB does at
+  // any k; a row's pieces past K are left out here.
+  __device__ __forceinline__ void load_one(rsrc_t r, int k0, int K, u4v (&v)[T::F], int i) const {
+    uint32_t o = off[i] + (uint32_t)k0 * step;
+    if constexpr (KC) o = k0 + k < K ? o : kOOB;
+    v[i] = load16(r, o);
+  }
+  __device__ __forceinline__ void store_one(u16* S, const u4v (&v)[T::F], int i) const {
+    *reinterpret_cast<u4v*>(S + lds[i]) = v[i];
+  }
+};
+
+// The two blocks of 16 columns of a region that fragment q (0 .. F - 1) takes.
+template <int F>
+__device__ __forceinline__ int pair_block(int q, int half) {
+  return F == 4 ? q + 4 * half : 2 * q + half;
+}
+
+// Fragment of 32 rows (or columns) by 16 k.  place: this lane's first element
+// for k = 0 of the stage (frag_place); step s of the stage.
+template <class T, bool KC>
+__device__ __forceinline__ int frag_place(int q, int lane, int row0) {
+  if constexpr (KC) {
+    const int row = row0 + q * 32 + lane % 32;
+    return row * 32 + (((lane / 32) ^ (row >> 2 & 3)) * 8);
+  } else {
+    const int g = lane / 16, i = lane % 16;
+    const int line = 8 * (g >> 1) + i / 4, block = pair_block<T::F>(q, g & 1);
+    return line * T::RC + (block ^ (line & 3)) * 16 + (i % 4) * 4;
+  }
+}
+template <class T, bool KC>
+__device__ __forceinline__ s8v frag_read(const u16* S, int place, int s) {
+  if constexpr (KC) {
+    return *reinterpret_cast<const s8v*>(S + (place ^ (s * 16)));    // piece + 2 of 4
+  } else {
+    typedef __attribute__((address_space(3))) s4v* lds4;
+    const u16* p = S + place + s * 16 * T::RC;
+    const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p));
+    const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(p + 4 * T::RC));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+}
+
+// ACT: FWD's activation (its code is unrolled over all the outputs of a lane).
+template <class T, DualKind KIND, int ACT>
+__global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) {
+  extern __shared__ u16 lds[];
+  constexpr int F = T::F;
+  constexpr bool AKC = KIND != kDualDw, BKC = KIND == kDualDx;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave & 1, wn = wave >> 1;
+
+  // Blocks are dealt to the 8 XCDs in contiguous ranges of an order in which 8 row
+  // tiles take turns under one column tile, so what an XCD runs at a time is a
+  // patch of the output that shares rows and columns in its L2.
+  const int tiles = g.mt * g.nt, nb = tiles * g.splits;
+  int h = blockIdx.x;
+  if (nb % 8 == 0) h = (h % 8) * (nb / 8) + h / 8;
+  const int split = h / tiles;
+  h -= split * tiles;
+  const int group = h / (8 * g.nt), in = h - group * 8 * g.nt;
+  const int gm = min(8, g.mt - group * 8);
+  const int mtile = group * 8 + in % gm, ntile = in / gm;
+  const int m0 = mtile * T::BM, n0 = ntile * (KIND == kDualDx ? T::BM : T::RC);
+
+  const int per_seg = cdiv(g.K, 32);
+  const int t0 = split * g.stages, t1 = min(t0 + g.stages, per_seg * g.segs);
+  const int nk = t1 - t0;
+
+  DualStage<T, AKC> sa;
+  DualStage<T, BKC> sb;
+  sa.init(tid, g.lda, g.M, m0, m0 + T::RC);
+  sb.init(tid, g.ldb, g.N, n0, n0);
+  // The next stage to load.
+  int seg = t0 / per_seg, k0 = (t0 - seg * per_seg) * 32;
+  u4v va[2][F], vb[2][F];
+  // The operands of its segment; its first k.  Stages past the last segment, which
+  // nothing multiplies, load the last one again.
+  rsrc_t ra, rb, rc;
+  auto segment = [&]() {
+    const int s = min(seg, g.segs - 1);
+    ra = make_rsrc(g.a[s], g.a_bytes);
+    rb = make_rsrc(g.b[0][s], g.b_bytes);
+    rc = make_rsrc(g.b[1][s], g.b_bytes);
+  };
+  segment();
+  int ka;
+  auto next = [&]() {
+    ka = k0;
+    k0 += 32;
+    if (k0 >= g.K) {
+      k0 = 0;
+      ++seg;
+    }
+  };
+  auto load_a = [&](u4v (&x)[F], int i) { sa.load_one(ra, ka, g.K, x, i); };
+  auto load_b = [&](u4v (&x)[F], int i) {
+    sb.load_one(!BKC && i >= F / 2 ? rc : rb, ka, g.K, x, i);
+  };
+  auto load = [&](u4v (&xa)[F], u4v (&xb)[F]) {
+    next();
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+      load_a(xa, i);
+      load_b(xb, i);
+    }
+    if (k0 == 0) segment();
+  };
+  auto store = [&](u16* S, const u4v (&xa)[F], const u4v (&xb)[F]) {
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+      sa.store_one(S, xa, i);
+      sb.store_one(S + T::OPER, xb, i);
+    }
+  };
+
+  int pa[F], pb[F];
+#pragma unroll
+  for (int i = 0; i < F; ++i) {
+    pa[i] = frag_place<T, AKC>(i, lane, wm * T::RC) + (AKC ? 0 : wm * T::RC * 32);
+    if constexpr (BKC) pb[i] = T::OPER + frag_place<T, true>(i, lane, wn * T::RC);
+    else pb[i] = T::OPER + (i / (F / 2)) * T::RC * 32 +
+                 frag_place<T, false>(wn * (F / 2) + i % (F / 2), lane, 0);
+  }
+  f16v acc[F][F];                                    // [column block][row block]
+#pragma unroll
+  for (int j = 0; j < F; ++j)
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[j][i][v] = 0.f;
+
+  load(va[0], vb[0]);
+  load(va[1], vb[1]);
+  store(lds, va[0], vb[0]);
+  store(lds + T::STAGE, va[1], vb[1]);
+  load(va[0], vb[0]);
+  load(va[1], vb[1]);
+  __syncthreads();
+
+  s8v fa[2][F], fb[2][F];
+#pragma unroll
+  for (int i = 0; i < F; ++i) {
+    fa[0][i] = frag_read<T, AKC>(lds, pa[i], 0);
+    fb[0][i] = frag_read<T, BKC>(lds, pb[i], 0);
+  }
+  // 16 k out of fragment set P: F * F MFMAs, and between them the reads of the next
+  // 16 k from S (one fragment behind each of the first 2 F MFMAs, in the order of their
+  // use), and in a stage's first half, behind the others, the pieces of the stage
+  // after the next one to LDS and the loads that take their registers' place.
+  auto step = [&](auto P, auto W, const u16* S, int s, u16* to) {
+    constexpr int c = decltype(P)::value, r = decltype(W)::value;   // r < 0: nothing to write
+#pragma unroll
+    for (int n = 0; n < F * F; ++n) {
+      const int j = n / F, i = n % F;
+      acc[j][i] = mfma32(fb[c][j], fa[c][i], acc[j][i]);
+      if (n == 0) fb[c ^ 1][0] = frag_read<T, BKC>(S, pb[0], s);
+      else if (n <= F) fa[c ^ 1][n - 1] = frag_read<T, AKC>(S, pa[n - 1], s);
+      else if (n < 2 * F) fb[c ^ 1][n - F] = frag_read<T, BKC>(S, pb[n - F], s);
+      if constexpr (r >= 0) {
+        // The pieces of A, then of B: 2 F of them over the last MFMAs.
+        constexpr int first = F == 4 ? 8 : 0, each = F == 4 ? 1 : 1;
+        const int x = (n - first) * each;
+        if (x >= 0 && x < F) {
+          sa.store_one(to, va[r], x);
+          load_a(va[r], x);
+        } else if (x >= F && x < 2 * F) {
+          sb.store_one(to + T::OPER, vb[r], x - F);
+          load_b(vb[r], x - F);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // A stage in buffer b0; b2 gets the stage after the next one.
+  auto stage = [&](auto R, u16* b0, u16* b1, u16* b2) {
+    next();
+    step(std::integral_constant<int, 0>{}, R, b0, 1, b2);
+    if (k0 == 0) segment();
+    step(std::integral_constant<int, 1>{}, std::integral_constant<int, -1>{}, b1, 0, nullptr);
+    __syncthreads();
+  };
+  u16 *b0 = lds, *b1 = lds + T::STAGE, *b2 = lds + 2 * T::STAGE;
+  int t = 0;
+  for (; t + 2 <= nk; t += 2) {
+    stage(std::integral_constant<int, 0>{}, b0, b1, b2);
+    stage(std::integral_constant<int, 1>{}, b1, b2, b0);
+    u16* x = b0;
+    b0 = b2;
+    b2 = b1;
+    b1 = x;
+  }
+  if (t < nk) stage(std::integral_constant<int, 0>{}, b0, b1, b2);
+
+  // acc[j][i] element v: output row m of fragment i, column 8 (v / 4) + 4 (lane / 32) + v % 4
+  // of fragment j.
+#pragma unroll
+  for (int i = 0; i < F; ++i) {
+    const int c = lane % 32;
+    const int m = m0 + wm * T::RC +
+                  (AKC ? i * 32 + c : pair_block<F>(i, c / 16) * 16 + c % 16);
+    if (m >= g.M) continue;
+#pragma unroll
+    for (int v4 = 0; v4 < 4; ++v4) {
+      const int d = 8 * v4 + 4 * (lane / 32);
+      if constexpr (KIND == kDualDx) {
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+          const int n = n0 + wn * T::RC + j * 32 + d;
+          if (n >= g.N) continue;
+          f4 s;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[e] = acc[j][i][v4 * 4 + e];
+          if (g.splits > 1) {
+            float* p = g.part + ((size_t)split * g.M + m) * g.N + n;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (n + e < g.N) p[e] = s[e];
+          } else {
+            u16* p = (u16*)g.c[0] + (size_t)m * g.ldc + n;
+            if (n + 4 <= g.N && ((uintptr_t)p & 7) == 0) Elem<u16>::store4(p, s);
+            else
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (n + e < g.N) p[e] = f32_to_bf16(s[e]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < F / 2; ++j) {
+          const int n = n0 + pair_block<F>(wn * (F / 2) + j, d / 16) * 16 + d % 16;
+          if (n >= g.N) continue;
+          f4 s[2];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            s[0][e] = acc[j][i][v4 * 4 + e];
+            s[1][e] = acc[j + F / 2][i][v4 * 4 + e];
+          }
+          if (KIND == kDualFwd && g.splits == 1) {
+            gate_store<u16>(ACT, s[0], s[1], n, g.N, g.bias[0], g.bias[1],
+                            g.pre ? g.pre + (size_t)m * g.N : nullptr, (size_t)g.M * g.N,
+                            (u16*)g.c[0] + (size_t)m * g.ldc);
+          } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              float* p = g.splits > 1 ? g.part + (((size_t)split * 2 + q) * g.M + m) * g.N + n
+                                      : (float*)g.c[q] + (size_t)m * g.ldc + n;
+              const bool add = g.splits == 1 && g.accumulate;
+              if (n + 4 <= g.N && ((uintptr_t)p & 15) == 0) {
+                if (add) s[q] += *reinterpret_cast<const f4*>(p);
+                *reinterpret_cast<f4*>(p) = s[q];
+              } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (n + e < g.N) p[e] = add ? p[e] + s[q][e] : s[q][e];
+              }
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
+}  // namespace sb

@@ -24,6 +24,7 @@ SB_F32, SB_BF16 = 0, 1
 SB_NCHW, SB_NCHW8C = 0, 1
 SB_FUSE_RELU = 1
 SB_PACKED_FILTERS = 2
+SB_UNALIGNED = 4
 SB_PASS_FWD, SB_PASS_BWD_DATA, SB_PASS_BWD_WEIGHT, SB_PASS_FWD_POOL = 0, 1, 2, 3
 SIZE_MAX = 2 ** 64 - 1          # (size_t)-1: the workspace queries' "not supported"
 SB_FC_FWD, SB_FC_BWD = 0, 1
@@ -61,7 +62,7 @@ class sb_adamw_tensor(ctypes.Structure):
 
 class sb_gated_desc(ctypes.Structure):
     _fields_ = [("m", _i), ("k_in", _i), ("n_shard", _i), ("dtype", _i), ("act", _i),
-                ("ldx", _i), ("ldy", _i)]
+                ("ldx", _i), ("ldy", _i), ("flags", ctypes.c_uint)]
 
 
 class sb_modulo_desc(ctypes.Structure):
@@ -205,8 +206,11 @@ def fc_desc(m, k_in, n_shard, dtype=SB_F32, ldx=None, ldy=None, relu=False):
                       SB_FUSE_RELU if relu else 0)
 
 
-def gated_desc(m, k_in, n_shard, dtype=SB_F32, act=SB_ACT_SILU, ldx=None, ldy=None):
-    return sb_gated_desc(m, k_in, n_shard, dtype, act, ldx or k_in, ldy or n_shard)
+def gated_desc(m, k_in, n_shard, dtype=SB_F32, act=SB_ACT_SILU, ldx=None, ldy=None,
+               unaligned=False):
+    """unaligned: the workspace query includes room for x and weights at any address."""
+    return sb_gated_desc(m, k_in, n_shard, dtype, act, ldx or k_in, ldy or n_shard,
+                         SB_UNALIGNED if unaligned else 0)
 
 
 # --------------------------------------------------------- entry points --

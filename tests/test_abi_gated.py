@@ -103,6 +103,19 @@ def test_workspace_overlaps_backward(t):
     assert _bwd(ws=P + ORDER_B.index(t) * GAP) == BAD
 
 
-def test_short_and_missing_workspaces():
+def test_short_missing_and_unaligned_workspaces():
     assert _bwd(short=1) == sb.SB_ERR_WORKSPACE
     assert _bwd(ws=None) == sb.SB_ERR_WORKSPACE
+    assert _bwd(ws=P + 20 * GAP + 8) == BAD
+
+
+def test_operands_off_16_bytes_ask_for_room():
+    """The size asked for without SB_UNALIGNED does not cover them."""
+    for p in (sb.SB_FC_FWD, sb.SB_FC_BWD):
+        assert sb.sb_gated_workspace_bytes(_desc(unaligned=True), p) > sb.sb_gated_workspace_bytes(
+            _desc(), p)
+    assert _fwd(x=P + 2) == sb.SB_ERR_WORKSPACE
+    assert _bwd(w_up=P + 2 * GAP + 8) == sb.SB_ERR_WORKSPACE
+    d = _desc()
+    d.flags = 8
+    assert _fwd(d) == BAD and _bwd(d) == BAD

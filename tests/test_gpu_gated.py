@@ -38,7 +38,8 @@ class Case:
         if dtype == "bf16":
             for t in ("x", "dy", "wg", "wu"):
                 setattr(self, t, torch.from_numpy(getattr(self, t)).bfloat16().float().numpy())
-        self.desc = sb.gated_desc(m, k, n, CODE[dtype], ACT[act], self.ldx, self.ldy)
+        self.desc = sb.gated_desc(m, k, n, CODE[dtype], ACT[act], self.ldx, self.ldy,
+                                  unaligned=shift % 8 != 0)
         self.d = {t: self.put(getattr(self, t)) for t in ("x", "dy", "wg", "wu")}
         self.d.update({t: None if getattr(self, t) is None else self.put(getattr(self, t), "f32")
                        for t in ("bg", "bu")})
