@@ -364,11 +364,12 @@ typedef struct {
 } sb_gated_desc;
 
 /* Workspace bytes for `pass` (SB_FC_FWD, SB_FC_BWD); (size_t)-1 for an invalid
- * descriptor, and for one whose x, y or weights reach 2^31 bytes.  The workspace
- * starts at a multiple of 16.  bf16 operands that no 16-byte access fits are laid
- * out anew in it: those of odd sizes or strides always have their room; for x or
- * weights whose addresses are not multiples of 16 the query is asked with
- * SB_UNALIGNED (a call with less returns SB_ERR_WORKSPACE). */
+ * descriptor, and for one whose x, y or weights reach 2^31 bytes.  (size_t)-1 too where
+ * 32 rows of x or of a weight do.  The workspace starts at a multiple of 16.
+ * Operands that no 16-byte access fits are laid out anew in it: those of odd sizes
+ * or strides always have their room; for x or weights whose addresses are not
+ * multiples of 16 the query is asked with SB_UNALIGNED (a call with less returns
+ * SB_ERR_WORKSPACE). */
 size_t sb_gated_workspace_bytes(const sb_gated_desc *desc, int pass);
 
 /* y as above.  pre may be NULL (inference); the backward needs it. */

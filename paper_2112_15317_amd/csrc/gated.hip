@@ -7,60 +7,34 @@
 //             dx  = da Wg^T + du Wu^T                       [m x kin]
 //             dWg = x^T da,  dWu = x^T du,  db their column sums
 //
-// bf16 runs on gemm_dual (gemm_dual.hpp): both projections, the activation and the
-// product are one kernel, dx and the two weight gradients one each.  fp32 runs on
-// gemm_split (fc_gemm.hpp).  a and u are kept in fp32.  The weight gradients are fp32
-// also where x is bf16: da and du go into their products as three bf16 parts, which
-// hold all 24 bits, so a gradient is off by the rounding of its fp32 sums and not by
-// 2^-9 of every term.  dx of the bf16 path is rounded to bf16 itself and takes their
-// first parts.
-#include "fc_gemm.hpp"
+// The products run on gemm_dual (gemm_dual.hpp): both projections, the activation
+// and the product with it are one kernel, dx another, both weight gradients a third;
+// da, du and the bias gradients come from a pass over dy and the kept a and u.
+//
+// The weight gradients are fp32 also where x is bf16: da and du go into their
+// products as three bf16 parts, which hold all 24 bits, so a gradient is off by the
+// rounding of its fp32 sums and not by 2^-9 of every term (measured against 64 bits:
+// 3e-7 of the gradient; with two parts 2.6e-6, with one 1.7e-3).  dx of the bf16 path
+// is rounded to bf16 itself and takes their first parts.
 #include "gemm_dual.hpp"
 
-#include <cmath>
+#include <algorithm>
+#include <mutex>
 
 namespace sb {
 
-__global__ __launch_bounds__(256) void gated_act_fwd(int m, int n, int act,
-                                                     const float* __restrict__ pre, float* y,
-                                                     int ldy) {
-  const size_t mn = (size_t)m * n;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < mn; i += (size_t)gridDim.x * 256) {
-    float f, df;
-    gate_act(act, pre[i], f, df);
-    const size_t r = i / n;
-    y[r * ldy + (i - r * n)] = f * pre[mn + i];
-  }
-}
-
-// da and du, dense [m][n] each.
-__global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int act,
-                                                     const float* __restrict__ pre,
-                                                     const float* __restrict__ dy, int ldy,
-                                                     float* d) {
-  const size_t mn = (size_t)m * n;
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < mn; i += (size_t)gridDim.x * 256) {
-    float f, df;
-    gate_act(act, pre[i], f, df);
-    const size_t r = i / n;
-    const float g = dy[r * ldy + (i - r * n)];
-    d[i] = g * pre[mn + i] * df;
-    d[mn + i] = g * f;
-  }
-}
-
-// ---- bf16 -----------------------------------------------------------------
-// da and du as three parts each, rows of np (n rounded up to 8, zeros behind n): part
-// p of da at p * m * np, of du at (3 + p) * m * np.  A block has 256 columns of
-// kActRows rows, a lane four columns of every fourth row, and leaves its columns' sums
-// (of the whole values) in sums [row block][2][np].
+// da and du in rows of np (n rounded up to 8, zeros behind n).  fp32: da, then du,
+// m * np elements each.  bf16: three parts of each, part p of da at p * m * np, of du at
+// (3 + p) * m * np.  A block has 256 columns of kActRows rows, a lane four columns of
+// every fourth row, and leaves its columns' sums in sums [row block][2][np].
 constexpr int kActRows = 32;
 
-__global__ __launch_bounds__(256) void gated_act_bwd_parts(int m, int n, int np, int act,
-                                                           const float* __restrict__ pre,
-                                                           const u16* __restrict__ dy, int ldy,
-                                                           u16* __restrict__ d,
-                                                           float* __restrict__ sums, int vec) {
+template <class E>
+__global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int act,
+                                                     const float* __restrict__ pre,
+                                                     const E* __restrict__ dy, int ldy,
+                                                     E* __restrict__ d, float* __restrict__ sums,
+                                                     int vec) {
   __shared__ f4 part[2][4][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int c = blockIdx.x * 256 + lane * 4;
@@ -69,19 +43,19 @@ __global__ __launch_bounds__(256) void gated_act_bwd_parts(int m, int n, int np,
   f4 s[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
   for (int r = blockIdx.y * kActRows + w; r < r1 && c < np; r += 4) {
     const float* pa = pre + (size_t)r * n + c;
-    const u16* pd = dy + (size_t)r * ldy + c;
+    const E* pd = dy + (size_t)r * ldy + c;
     f4 a = f4{0.f, 0.f, 0.f, 0.f}, u = a, g = a;
     if (vec && c < n) {                              // n a multiple of 4
       a = *reinterpret_cast<const f4*>(pa);
       u = *reinterpret_cast<const f4*>(pa + mn);
-      g = Elem<u16>::load4(pd);
+      g = Elem<E>::load4(pd);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (c + e < n) {
           a[e] = pa[e];
           u[e] = pa[mn + e];
-          g[e] = bf16_to_f32(pd[e]);
+          g[e] = Elem<E>::load(pd, e);
         }
     }
     f4 v[2];
@@ -95,20 +69,25 @@ __global__ __launch_bounds__(256) void gated_act_bwd_parts(int m, int n, int np,
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       s[q] += v[q];
-      f4 rest = v[q];
+      const size_t at = (size_t)r * np + c;
+      if constexpr (sizeof(E) == 4) {
+        *reinterpret_cast<f4*>(d + q * plane + at) = v[q];
+      } else {
+        f4 rest = v[q];
 #pragma unroll
-      for (int p = 0; p < 3; ++p) {
-        u16* o = d + (3 * q + p) * plane + (size_t)r * np + c;
-        uint2 b;
-        b.x = f32x2_to_bf16x2(rest[0], rest[1]);
-        b.y = f32x2_to_bf16x2(rest[2], rest[3]);
-        *reinterpret_cast<uint2*>(o) = b;
-        const f4 h = Elem<u16>::load4(reinterpret_cast<const u16*>(&b));
+        for (int p = 0; p < 3; ++p) {
+          uint2 b;
+          b.x = f32x2_to_bf16x2(rest[0], rest[1]);
+          b.y = f32x2_to_bf16x2(rest[2], rest[3]);
+          *reinterpret_cast<uint2*>(d + (3 * q + p) * plane + at) = b;
+          const f4 h = f4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u),
+                          __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xffff0000u)};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          // An infinite or NaN first part is the whole value.
-          const bool whole = (__float_as_uint(h[e]) & 0x7f800000u) == 0x7f800000u;
-          rest[e] = whole ? 0.f : rest[e] - h[e];
+          for (int e = 0; e < 4; ++e) {
+            // An infinite or NaN first part is the whole value.
+            const bool whole = (__float_as_uint(h[e]) & 0x7f800000u) == 0x7f800000u;
+            rest[e] = whole ? 0.f : rest[e] - h[e];
+          }
         }
       }
     }
@@ -143,22 +122,20 @@ __global__ __launch_bounds__(256) void gated_bias_sums(const float* __restrict__
 }
 
 // Rows of `cols` elements, `ld` apart, to rows of cp (a multiple of 8), zeros behind.
-// grid.y: up to two matrices.
-__global__ __launch_bounds__(256) void gated_pack(const u16* a, const u16* b, size_t rows, int cols,
-                                                  int ld, int cp, u16* to) {
-  const u16* from = blockIdx.y ? b : a;
-  u16* out = to + blockIdx.y * rows * cp;
-  const size_t pieces = rows * (cp / 8);
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (size_t)gridDim.x * 256) {
-    const size_t r = i / (cp / 8);
-    const int c = (int)(i - r * (cp / 8)) * 8;
-    u16 v[8];
+// Block rows: two matrices.
+template <class E>
+__global__ __launch_bounds__(256) void gated_pack(const E* a, const E* b, size_t rows, int cols,
+                                                  int ld, int cp, E* to) {
+  const E* from = blockIdx.y ? b : a;
+  E* out = to + blockIdx.y * rows * cp;
+  const size_t quads = rows * (cp / 4);
+  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (size_t)gridDim.x * 256) {
+    const size_t r = i / (cp / 4);
+    const int c = (int)(i - r * (cp / 4)) * 4;
+    f4 v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? from[r * ld + c + e] : (u16)0;
-    u4v o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = (uint32_t)v[2 * e] | (uint32_t)v[2 * e + 1] << 16;
-    *reinterpret_cast<u4v*>(out + r * cp + c) = o;
+    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? Elem<E>::load(from, r * ld + c + e) : 0.f;
+    Elem<E>::store4(out + r * cp + c, v);
   }
 }
 
@@ -174,7 +151,7 @@ __device__ __forceinline__ f4 split_quad(const float* p, int splits, size_t stri
   return v;
 }
 
-template <DualKind KIND>
+template <DualKind KIND, class E>
 __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
   const int quads = cdiv(g.N, 4);
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -183,17 +160,16 @@ __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
   const size_t plane = (size_t)g.M * g.N, at = (size_t)m * g.N + n;
   if constexpr (KIND == kDualDx) {
     const f4 v = split_quad(g.part + at, g.splits, plane, n, g.N);
-    u16* o = (u16*)g.c[0] + (size_t)m * g.ldc + n;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (n + e < g.N) o[e] = f32_to_bf16(v[e]);
+      if (n + e < g.N) Elem<E>::store((E*)g.c[0], (size_t)m * g.ldc + n + e, v[e]);
   } else {
     const f4 a = split_quad(g.part + at, g.splits, 2 * plane, n, g.N);
     const f4 u = split_quad(g.part + plane + at, g.splits, 2 * plane, n, g.N);
     if constexpr (KIND == kDualFwd) {
-      gate_store<u16>(act, a, u, n, g.N, g.bias[0], g.bias[1],
-                      g.pre ? g.pre + (size_t)m * g.N : nullptr, plane,
-                      (u16*)g.c[0] + (size_t)m * g.ldc);
+      gate_store<E>(act, a, u, n, g.N, g.bias[0], g.bias[1],
+                    g.pre ? g.pre + (size_t)m * g.N : nullptr, plane,
+                    (E*)g.c[0] + (size_t)m * g.ldc);
     } else {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
@@ -208,25 +184,26 @@ __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
   }
 }
 
-// Tile and split of a product: the least estimated time.
+// Tile and split of a product: the least estimated time (us).
 struct DualPlan { int f, mt, nt, splits, stages; size_t ws_bytes; };
 
-static DualPlan dual_plan(DualKind kind, int M, int N, int K, int segs) {
+static DualPlan dual_plan(DualKind kind, bool b16, int M, int N, int K, int segs) {
   DualPlan best{};
   double best_t = 0;
   const int total = cdiv(K, 32) * segs;
-  for (int f = 4; f >= 2; f -= 2) {
+  for (int f = b16 ? 4 : 2; f >= 2; f -= 2) {
     const int mt = cdiv(M, 64 * f), nt = cdiv(N, kind == kDualDx ? 64 * f : 32 * f);
     const int64_t tiles = (int64_t)mt * nt;
     for (int s = 1; s <= 16 && s <= total; ++s) {
       const int stages = cdiv(total, s);
       if (cdiv(total, stages) != s) continue;
       const int64_t blocks = tiles * s;
-      const int64_t per_cu = (blocks + 255) / 256;
+      const double per_cu = (double)((blocks + 255) / 256);
       const double bytes = (double)M * N * (kind == kDualDx ? 4 : 8);
       double t = s > 1 ? 4.0 + bytes * (2 * s + 1) / 5e6 : 0.0;
-      t += f == 4 ? per_cu * (5.0 + stages * (blocks > 192 ? 1.04 : 0.75))
-                  : 3.0 * ((per_cu + 2) / 3) + stages * (per_cu > 1 ? 0.33 * per_cu : 0.29);
+      if (!b16) t += per_cu * (5.0 + stages * (blocks > 128 ? 1.8 : 1.4));
+      else if (f == 4) t += per_cu * (5.0 + stages * (blocks > 192 ? 1.04 : 0.75));
+      else t += 3.0 * (double)(((int64_t)per_cu + 2) / 3) + stages * (per_cu > 1 ? 0.33 * per_cu : 0.29);
       if (best_t == 0 || t < best_t) {
         best_t = t;
         best = DualPlan{f, mt, nt, s, stages, s > 1 ? (size_t)s * (size_t)bytes : 0};
@@ -236,9 +213,9 @@ static DualPlan dual_plan(DualKind kind, int M, int N, int K, int segs) {
   return best;
 }
 
-template <int F, DualKind KIND, int ACT>
-static void dual_launch_t(const DualArgs& g, hipStream_t st) {
-  typedef DualTile<F> T;
+template <int F, DualKind KIND, int ACT, class E>
+static void dual_launch(const DualArgs& g, hipStream_t st) {
+  typedef DualTile<F, E> T;
   static std::once_flag once;
   std::call_once(once, [] {
     (void)hipFuncSetAttribute((const void*)gemm_dual<T, KIND, ACT>,
@@ -246,96 +223,83 @@ static void dual_launch_t(const DualArgs& g, hipStream_t st) {
   });
   gemm_dual<T, KIND, ACT><<<(unsigned)(g.mt * g.nt * g.splits), 256, T::LDS_BYTES, st>>>(g);
 }
-template <DualKind KIND, int ACT>
-static void dual_launch(int f, const DualArgs& g, hipStream_t st) {
-  if (f == 4) dual_launch_t<4, KIND, ACT>(g, st);
-  else dual_launch_t<2, KIND, ACT>(g, st);
+template <DualKind KIND, int ACT, class E>
+static void dual_launch_f(int f, const DualArgs& g, hipStream_t st) {
+  if constexpr (sizeof(E) == 2) {
+    if (f == 4) {
+      dual_launch<4, KIND, ACT, E>(g, st);
+      return;
+    }
+  }
+  dual_launch<2, KIND, ACT, E>(g, st);
 }
 
 // One product under its plan: unsplit it ends in its outputs, split in the workspace,
 // from where gated_split_sum takes it.
-template <DualKind KIND>
+template <DualKind KIND, class E>
 static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStream_t st) {
   g.mt = p.mt; g.nt = p.nt; g.splits = p.splits; g.stages = p.stages;
   g.part = part;
   if (KIND != kDualFwd || p.splits > 1) {
-    dual_launch<KIND, 0>(p.f, g, st);
+    dual_launch_f<KIND, 0, E>(p.f, g, st);
   } else {
     switch (act) {
-      case SB_ACT_SIGMOID: dual_launch<kDualFwd, SB_ACT_SIGMOID>(p.f, g, st); break;
-      case SB_ACT_SILU: dual_launch<kDualFwd, SB_ACT_SILU>(p.f, g, st); break;
-      case SB_ACT_GELU: dual_launch<kDualFwd, SB_ACT_GELU>(p.f, g, st); break;
-      case SB_ACT_GELU_TANH: dual_launch<kDualFwd, SB_ACT_GELU_TANH>(p.f, g, st); break;
-      default: dual_launch<kDualFwd, SB_ACT_RELU>(p.f, g, st);
+      case SB_ACT_SIGMOID: dual_launch_f<kDualFwd, SB_ACT_SIGMOID, E>(p.f, g, st); break;
+      case SB_ACT_SILU: dual_launch_f<kDualFwd, SB_ACT_SILU, E>(p.f, g, st); break;
+      case SB_ACT_GELU: dual_launch_f<kDualFwd, SB_ACT_GELU, E>(p.f, g, st); break;
+      case SB_ACT_GELU_TANH: dual_launch_f<kDualFwd, SB_ACT_GELU_TANH, E>(p.f, g, st); break;
+      default: dual_launch_f<kDualFwd, SB_ACT_RELU, E>(p.f, g, st);
     }
   }
   if (p.splits > 1) {
     const size_t quads = (size_t)g.M * cdiv(g.N, 4);
-    gated_split_sum<KIND><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, act);
+    gated_split_sum<KIND, E><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, act);
   }
 }
 
 static unsigned gated_blocks(size_t count) {
   return (unsigned)std::min<size_t>((count + 255) / 256, 65536);
 }
-
 static int up8(int n) { return (n + 7) / 8 * 8; }
 static bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
-// Which bf16 operands have to be laid out anew for 16-byte pieces: x as rows of the
-// forward's reduction, x as lines of the weight gradient's, the weights.
+// Which operands have to be laid out anew for 16-byte pieces of whole eights: x as
+// rows of the forward's reduction, x as lines of the weight gradient's, the weights.
 struct GatedPacks { bool x, lines, w; };
 static GatedPacks gated_packs(const sb_gated_desc* d, bool x_at16, bool w_at16) {
-  // (An odd k_in would end the last line inside the 4 bytes that ranges count in.)
-  const bool lines = d->ldx % 8 != 0 || d->k_in % 2 != 0 || !x_at16;
+  const bool b16 = d->dtype == SB_BF16;
+  // (An odd bf16 k_in would end the last line inside the 4 bytes that ranges count in.)
+  const bool lines = d->ldx % (b16 ? 8 : 4) != 0 || (b16 && d->k_in % 2 != 0) || !x_at16;
   return GatedPacks{lines || d->k_in % 8 != 0, lines, d->n_shard % 8 != 0 || !w_at16};
 }
 
-// A workspace's parts, each from a multiple of 256 bytes on (offsets).
-struct GatedSpace {
-  size_t d, x, w, sums, split, bytes;
-};
-
 static DualPlan gated_plan(const sb_gated_desc* d, DualKind kind) {
-  if (kind == kDualFwd) return dual_plan(kind, d->m, d->n_shard, d->k_in, 1);
-  if (kind == kDualDx) return dual_plan(kind, d->m, d->k_in, up8(d->n_shard), 2);
-  return dual_plan(kind, d->k_in, d->n_shard, d->m, 3);
+  const bool b16 = d->dtype == SB_BF16;
+  if (kind == kDualFwd) return dual_plan(kind, b16, d->m, d->n_shard, d->k_in, 1);
+  if (kind == kDualDx) return dual_plan(kind, b16, d->m, d->k_in, up8(d->n_shard), 2);
+  return dual_plan(kind, b16, d->k_in, d->n_shard, d->m, b16 ? 3 : 1);
 }
 
-static GemmPlan gated_plan_y(const sb_gated_desc* d) {
-  return product_plan(d->m, d->n_shard, d->k_in, d->ldx, true, d->n_shard, false, 4);
-}
-static GemmPlan gated_plan_dx(const sb_gated_desc* d) {
-  return product_plan(d->m, d->k_in, d->n_shard, d->n_shard, true, d->n_shard, true, 4);
-}
-static GemmPlan gated_plan_dw(const sb_gated_desc* d) {
-  return product_plan(d->k_in, d->n_shard, d->m, d->ldx, false, d->n_shard, false, 4);
-}
+// A workspace's parts, each from a multiple of 256 bytes on (offsets).
+struct GatedSpace { size_t d, sums, x, w, split, bytes; };
 
-// pre: whether the forward has a place for a and u of the caller's.
-static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks& k, bool pre) {
-  const size_t m = d->m, mn = m * d->n_shard, np = up8(d->n_shard);
+static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks& k) {
+  const size_t m = d->m, np = up8(d->n_shard), es = sbh::dsize(d->dtype);
   GatedSpace s{};
   size_t at = 0;
   auto take = [&](size_t& part, size_t bytes) {
     part = at;
     at += round_up(bytes, 256);
   };
-  if (d->dtype == SB_F32) {
-    take(s.d, pass == SB_FC_FWD && pre ? 0 : mn * 8);
-    take(s.split, pass == SB_FC_FWD ? gated_plan_y(d).ws_bytes
-                                    : std::max(gated_plan_dx(d).ws_bytes, gated_plan_dw(d).ws_bytes));
-  } else {
-    if (pass == SB_FC_BWD) {
-      take(s.d, m * np * 12);
-      take(s.sums, (size_t)cdiv(d->m, kActRows) * np * 8);
-    }
-    if (pass == SB_FC_FWD ? k.x : k.lines) take(s.x, m * up8(d->k_in) * 2);
-    if (k.w) take(s.w, (size_t)d->k_in * np * 4);
-    take(s.split, pass == SB_FC_FWD
-                      ? gated_plan(d, kDualFwd).ws_bytes
-                      : std::max(gated_plan(d, kDualDx).ws_bytes, gated_plan(d, kDualDw).ws_bytes));
+  if (pass == SB_FC_BWD) {
+    take(s.d, m * np * (d->dtype == SB_BF16 ? 12 : 8));
+    take(s.sums, (size_t)cdiv(d->m, kActRows) * np * 8);
   }
+  if (pass == SB_FC_FWD ? k.x : k.lines) take(s.x, m * up8(d->k_in) * es);
+  if (k.w) take(s.w, 2 * (size_t)d->k_in * np * es);
+  take(s.split, pass == SB_FC_FWD
+                    ? gated_plan(d, kDualFwd).ws_bytes
+                    : std::max(gated_plan(d, kDualDx).ws_bytes, gated_plan(d, kDualDw).ws_bytes));
   s.bytes = at;
   return s;
 }
@@ -347,11 +311,12 @@ static sb_status gated_check(const sb_gated_desc* d) {
   if (d->dtype != SB_F32 && d->dtype != SB_BF16) return SB_ERR_INVALID_ARG;
   if (d->flags & ~SB_UNALIGNED) return SB_ERR_INVALID_ARG;
   if (d->act < SB_ACT_SIGMOID || d->act > SB_ACT_RELU) return SB_ERR_INVALID_ARG;
-  // The kernels' ranges are below 2^31 bytes.
+  // The kernels' ranges are below 2^31 bytes, and so are 32 lines, by which a
+  // stage may pass the end of one (its offsets must not wrap).
   const int64_t es = (int64_t)sbh::dsize(d->dtype), top = 1ll << 31;
-  if (((int64_t)(d->m - 1) * d->ldx + d->k_in) * es >= top ||
-      ((int64_t)(d->m - 1) * d->ldy + d->n_shard) * es >= top ||
-      (int64_t)d->k_in * d->n_shard * es >= top)
+  const int64_t m = d->m, kp = ((int64_t)d->k_in + 7) / 8 * 8, np = ((int64_t)d->n_shard + 7) / 8 * 8;
+  if (m * std::max<int64_t>(d->ldx, kp) * es >= top || m * std::max<int64_t>(d->ldy, np) * es >= top ||
+      d->k_in * np * es >= top || 32 * std::max<int64_t>({d->ldx, kp, np}) * es >= top)
     return SB_ERR_UNSUPPORTED;
   return SB_OK;
 }
@@ -365,146 +330,101 @@ static bool spans_meet(const Span* a, int na, const Span* b, int nb) {
   return false;
 }
 
-static sb_status gated_fwd_f32(const sb_gated_desc* d, const void* x, const void* const* w,
-                               const float* const* b, void* y, float* pre, char* ws,
-                               const GatedSpace& sp, hipStream_t st) {
-  const size_t mn = (size_t)d->m * d->n_shard;
-  if (!pre) pre = (float*)(ws + sp.d);
-  for (int q = 0; q < 2; ++q) {
-    GemmArgs g{};
-    g.a = x; g.lda = d->ldx;
-    g.b = w[q]; g.ldb = d->n_shard;
-    g.c = pre + q * mn; g.ldc = d->n_shard;
-    g.M = d->m; g.N = d->n_shard; g.K = d->k_in;
-    g.bias = b[q];
-    const sb_status s = gemm_run<true, false, float, float>(
-        g, gated_plan_y(d), (float*)(ws + sp.split), sp.bytes - sp.split, st);
-    if (s != SB_OK) return s;
-  }
-  gated_act_fwd<<<gated_blocks(mn), 256, 0, st>>>(d->m, d->n_shard, d->act, pre, (float*)y, d->ldy);
-  return SB_OK;
-}
-
-static sb_status gated_bwd_f32(const sb_gated_desc* d, const void* x, const void* const* w,
-                               const float* pre, const void* dy, void* dx, float* const* dw,
-                               float* const* db, int accumulate, char* ws, const GatedSpace& sp,
-                               hipStream_t st) {
-  const size_t mn = (size_t)d->m * d->n_shard, split_bytes = sp.bytes - sp.split;
-  float* split = (float*)(ws + sp.split);
-  float* dd = (float*)(ws + sp.d);
-  gated_act_bwd<<<gated_blocks(mn), 256, 0, st>>>(d->m, d->n_shard, d->act, pre, (const float*)dy,
-                                                  d->ldy, dd);
-  for (int q = 0; q < 2 && dx; ++q) {
-    GemmArgs g{};
-    g.a = dd + q * mn; g.lda = d->n_shard;
-    g.b = w[q]; g.ldb = d->n_shard;
-    g.c = dx; g.ldc = d->ldx;
-    g.M = d->m; g.N = d->k_in; g.K = d->n_shard;
-    g.accumulate = q;
-    const sb_status s = gemm_run<true, true, float, float>(g, gated_plan_dx(d), split, split_bytes, st);
-    if (s != SB_OK) return s;
-  }
-  for (int q = 0; q < 2; ++q) {
-    GemmArgs g{};
-    g.a = x; g.lda = d->ldx;
-    g.b = dd + q * mn; g.ldb = d->n_shard;
-    g.c = dw[q]; g.ldc = d->n_shard;
-    g.M = d->k_in; g.N = d->n_shard; g.K = d->m;
-    g.accumulate = accumulate;
-    g.colsum = db[q]; g.colsum_acc = accumulate;
-    const sb_status s = gemm_run<false, false, float, float>(g, gated_plan_dw(d), split, split_bytes, st);
-    if (s != SB_OK) return s;
-  }
-  return SB_OK;
-}
-
-// The weights as lines of 16-byte pieces, np apart.
-static void gated_weights(const sb_gated_desc* d, const void* const* w, const u16** to, bool pack,
+// The weights as lines of whole eights, np apart.
+template <class E>
+static void gated_weights(const sb_gated_desc* d, const void* const* w, const void** to, bool pack,
                           char* ws, const GatedSpace& sp, hipStream_t st) {
   const int np = up8(d->n_shard);
-  to[0] = (const u16*)w[0];
-  to[1] = (const u16*)w[1];
+  to[0] = w[0];
+  to[1] = w[1];
   if (!pack) return;
-  u16* out = (u16*)(ws + sp.w);
-  gated_pack<<<dim3(gated_blocks((size_t)d->k_in * np / 8), 2), 256, 0, st>>>(
-      to[0], to[1], d->k_in, d->n_shard, d->n_shard, np, out);
+  E* out = (E*)(ws + sp.w);
+  gated_pack<E><<<dim3(gated_blocks((size_t)d->k_in * np / 4), 2), 256, 0, st>>>(
+      (const E*)w[0], (const E*)w[1], d->k_in, d->n_shard, d->n_shard, np, out);
   to[0] = out;
   to[1] = out + (size_t)d->k_in * np;
 }
-static const u16* gated_rows(const sb_gated_desc* d, const void* x, bool pack, int* ld, char* ws,
-                             const GatedSpace& sp, hipStream_t st) {
+// x, and its stride and width.
+template <class E>
+static const void* gated_x(const sb_gated_desc* d, const void* x, bool pack, int* ld, int* width,
+                           char* ws, const GatedSpace& sp, hipStream_t st) {
   *ld = d->ldx;
-  if (!pack) return (const u16*)x;
-  const int kp = up8(d->k_in);
-  u16* out = (u16*)(ws + sp.x);
-  gated_pack<<<dim3(gated_blocks((size_t)d->m * kp / 8), 1), 256, 0, st>>>(
-      (const u16*)x, nullptr, d->m, d->k_in, d->ldx, kp, out);
-  *ld = kp;
+  *width = d->k_in;
+  if (!pack) return x;
+  *ld = *width = up8(d->k_in);
+  E* out = (E*)(ws + sp.x);
+  gated_pack<E><<<dim3(gated_blocks((size_t)d->m * *ld / 4), 1), 256, 0, st>>>(
+      (const E*)x, nullptr, d->m, d->k_in, d->ldx, *ld, out);
   return out;
 }
 
-static void gated_fwd_b16(const sb_gated_desc* d, const void* x, const void* const* w,
+template <class E>
+static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* const* w,
                           const float* const* b, void* y, float* pre, const GatedPacks& packs,
                           char* ws, const GatedSpace& sp, hipStream_t st) {
   const int np = up8(d->n_shard);
   DualArgs g{};
-  g.a[0] = gated_rows(d, x, packs.x, &g.lda, ws, sp, st);
-  const u16* wp[2];
-  gated_weights(d, w, wp, packs.w, ws, sp, st);
+  const void* wp[2];
+  g.a[0] = gated_x<E>(d, x, packs.x, &g.lda, &g.K, ws, sp, st);
+  gated_weights<E>(d, w, wp, packs.w, ws, sp, st);
   g.b[0][0] = wp[0]; g.b[1][0] = wp[1];
   g.ldb = np;
-  g.M = d->m; g.N = d->n_shard; g.K = packs.x ? up8(d->k_in) : d->k_in; g.segs = 1;
-  g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + g.K) * 2);
-  g.b_bytes = (uint32_t)((size_t)d->k_in * np * 2);
+  g.M = d->m; g.N = d->n_shard; g.segs = 1;
+  g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + g.K) * sizeof(E));
+  g.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
   g.c[0] = y; g.ldc = d->ldy;
   g.bias[0] = b[0]; g.bias[1] = b[1];
   g.pre = pre;
-  dual_run<kDualFwd>(g, gated_plan(d, kDualFwd), d->act, (float*)(ws + sp.split), st);
+  dual_run<kDualFwd, E>(g, gated_plan(d, kDualFwd), d->act, (float*)(ws + sp.split), st);
 }
 
-static void gated_bwd_b16(const sb_gated_desc* d, const void* x, const void* const* w,
+template <class E>
+static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* const* w,
                           const float* pre, const void* dy, void* dx, float* const* dw,
                           float* const* db, int accumulate, const GatedPacks& packs, char* ws,
                           const GatedSpace& sp, hipStream_t st) {
+  constexpr int NP = sizeof(E) == 2 ? 3 : 1;
   const int np = up8(d->n_shard), chunks = cdiv(d->m, kActRows);
   const size_t plane = (size_t)d->m * np;
-  u16* parts = (u16*)(ws + sp.d);
+  E* parts = (E*)(ws + sp.d);
   float* split = (float*)(ws + sp.split);
   float* sums = db[0] || db[1] ? (float*)(ws + sp.sums) : nullptr;
-  const int vec = d->n_shard % 4 == 0 && at16(pre) && d->ldy % 4 == 0 && ((uintptr_t)dy & 7) == 0;
-  gated_act_bwd_parts<<<dim3(cdiv(np, 256), chunks), 256, 0, st>>>(
-      d->m, d->n_shard, np, d->act, pre, (const u16*)dy, d->ldy, parts, sums, vec);
+  const int vec = d->n_shard % 4 == 0 && at16(pre) && d->ldy % 4 == 0 &&
+                  ((uintptr_t)dy & (4 * sizeof(E) - 1)) == 0;
+  gated_act_bwd<E><<<dim3(cdiv(np, 256), chunks), 256, 0, st>>>(
+      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, sums, vec);
   if (sums)
     gated_bias_sums<<<dim3(cdiv(d->n_shard, 64), 2), 256, 0, st>>>(sums, chunks, d->n_shard, np,
                                                                    db[0], db[1], accumulate);
   if (dx) {
     DualArgs g{};
-    const u16* wp[2];
-    gated_weights(d, w, wp, packs.w, ws, sp, st);
+    const void* wp[2];
+    gated_weights<E>(d, w, wp, packs.w, ws, sp, st);
     for (int q = 0; q < 2; ++q) {
-      g.a[q] = parts + 3 * q * plane;
+      g.a[q] = parts + NP * q * plane;
       g.b[0][q] = wp[q];
     }
     g.lda = g.ldb = np;
     g.M = d->m; g.N = d->k_in; g.K = np; g.segs = 2;
-    g.a_bytes = (uint32_t)(plane * 2);
-    g.b_bytes = (uint32_t)((size_t)d->k_in * np * 2);
+    g.a_bytes = (uint32_t)(plane * sizeof(E));
+    g.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
     g.c[0] = dx; g.ldc = d->ldx;
-    dual_run<kDualDx>(g, gated_plan(d, kDualDx), 0, split, st);
+    dual_run<kDualDx, E>(g, gated_plan(d, kDualDx), 0, split, st);
   }
   DualArgs g{};
-  const u16* xp = gated_rows(d, x, packs.lines, &g.lda, ws, sp, st);
-  for (int p = 0; p < 3; ++p) {                      // the smallest parts first
+  int width;
+  const void* xp = gated_x<E>(d, x, packs.lines, &g.lda, &width, ws, sp, st);
+  for (int p = 0; p < NP; ++p) {                     // the smallest parts first
     g.a[p] = xp;
-    for (int q = 0; q < 2; ++q) g.b[q][p] = parts + (3 * q + 2 - p) * plane;
+    for (int q = 0; q < 2; ++q) g.b[q][p] = parts + (NP * q + NP - 1 - p) * plane;
   }
   g.ldb = np;
-  g.M = d->k_in; g.N = d->n_shard; g.K = d->m; g.segs = 3;
-  g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + (packs.lines ? g.lda : d->k_in)) * 2);
-  g.b_bytes = (uint32_t)(plane * 2);
+  g.M = d->k_in; g.N = d->n_shard; g.K = d->m; g.segs = NP;
+  g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + width) * sizeof(E));
+  g.b_bytes = (uint32_t)(plane * sizeof(E));
   g.c[0] = dw[0]; g.c[1] = dw[1]; g.ldc = d->n_shard;
   g.accumulate = accumulate;
-  dual_run<kDualDw>(g, gated_plan(d, kDualDw), 0, split, st);
+  dual_run<kDualDw, E>(g, gated_plan(d, kDualDw), 0, split, st);
 }
 
 }  // namespace sb
@@ -514,36 +434,34 @@ using namespace sb;
 extern "C" size_t sb_gated_workspace_bytes(const sb_gated_desc* d, int pass) {
   if (gated_check(d) != SB_OK || (pass != SB_FC_FWD && pass != SB_FC_BWD)) return (size_t)-1;
   const bool at = !(d->flags & SB_UNALIGNED);
-  return gated_space(d, pass, gated_packs(d, at, at), false).bytes;
+  return gated_space(d, pass, gated_packs(d, at, at)).bytes;
 }
 
 extern "C" sb_status sb_gated_shard_fwd(const sb_gated_desc* d, const void* x, const void* w_gate,
                                         const void* w_up, const float* b_gate, const float* b_up,
                                         void* y, float* pre, void* ws, size_t ws_bytes,
                                         void* stream) {
-  sb_status s = gated_check(d);
+  const sb_status s = gated_check(d);
   if (s != SB_OK) return s;
   if (!x || !w_gate || !w_up || !y) return SB_ERR_INVALID_ARG;
   const size_t es = sbh::dsize(d->dtype), nb = (size_t)d->n_shard * 4;
   const size_t wb = (size_t)d->k_in * d->n_shard * es;
   const GatedPacks packs = gated_packs(d, at16(x), at16(w_gate) && at16(w_up));
-  const GatedSpace sp = gated_space(d, SB_FC_FWD, packs, pre != nullptr);
-  const size_t need = sp.bytes;
+  const GatedSpace sp = gated_space(d, SB_FC_FWD, packs);
   const Span ins[5] = {{x, ((size_t)(d->m - 1) * d->ldx + d->k_in) * es}, {w_gate, wb},
                        {w_up, wb}, {b_gate, nb}, {b_up, nb}};
   const Span outs[3] = {{y, ((size_t)(d->m - 1) * d->ldy + d->n_shard) * es},
-                        {pre, (size_t)d->m * d->n_shard * 8}, {ws, need}};
+                        {pre, (size_t)d->m * d->n_shard * 8}, {ws, sp.bytes}};
   if (spans_meet(outs, 3, ins, 5) || spans_meet(outs, 1, outs + 1, 2) ||
       spans_meet(outs + 1, 1, outs + 2, 1))
     return SB_ERR_INVALID_ARG;
-  if (need > 0 && (!ws || ws_bytes < need)) return SB_ERR_WORKSPACE;
-  if (need > 0 && !at16(ws)) return SB_ERR_INVALID_ARG;
+  if (sp.bytes > 0 && (!ws || ws_bytes < sp.bytes)) return SB_ERR_WORKSPACE;
+  if (sp.bytes > 0 && !at16(ws)) return SB_ERR_INVALID_ARG;
   const void* w[2] = {w_gate, w_up};
   const float* b[2] = {b_gate, b_up};
-  hipStream_t st = sbh::stream_of(stream);
-  if (d->dtype == SB_BF16) gated_fwd_b16(d, x, w, b, y, pre, packs, (char*)ws, sp, st);
-  else s = gated_fwd_f32(d, x, w, b, y, pre, (char*)ws, sp, st);
-  return s != SB_OK ? s : sbh::launch_status();
+  const auto run = d->dtype == SB_BF16 ? gated_fwd_run<u16> : gated_fwd_run<float>;
+  run(d, x, w, b, y, pre, packs, (char*)ws, sp, sbh::stream_of(stream));
+  return sbh::launch_status();
 }
 
 extern "C" sb_status sb_gated_shard_bwd(const sb_gated_desc* d, const void* x, const void* w_gate,
@@ -551,7 +469,7 @@ extern "C" sb_status sb_gated_shard_bwd(const sb_gated_desc* d, const void* x, c
                                         void* dx, float* dw_gate, float* dw_up, float* db_gate,
                                         float* db_up, int accumulate, void* ws, size_t ws_bytes,
                                         void* stream) {
-  sb_status s = gated_check(d);
+  const sb_status s = gated_check(d);
   if (s != SB_OK) return s;
   if (!x || !w_gate || !w_up || !pre || !dy || !dw_gate || !dw_up) return SB_ERR_INVALID_ARG;
   if (accumulate != 0 && accumulate != 1) return SB_ERR_INVALID_ARG;
@@ -559,25 +477,21 @@ extern "C" sb_status sb_gated_shard_bwd(const sb_gated_desc* d, const void* x, c
   const size_t xb = ((size_t)(d->m - 1) * d->ldx + d->k_in) * es;
   const size_t wn = (size_t)d->k_in * d->n_shard;
   const GatedPacks packs = gated_packs(d, at16(x), at16(w_gate) && at16(w_up));
-  const GatedSpace sp = gated_space(d, SB_FC_BWD, packs, true);
-  const size_t need = sp.bytes;
+  const GatedSpace sp = gated_space(d, SB_FC_BWD, packs);
   const Span ins[5] = {{x, xb}, {w_gate, wn * es}, {w_up, wn * es},
                        {pre, (size_t)d->m * d->n_shard * 8},
                        {dy, ((size_t)(d->m - 1) * d->ldy + d->n_shard) * es}};
   const Span outs[6] = {{dx, xb}, {dw_gate, wn * 4}, {dw_up, wn * 4}, {db_gate, nb}, {db_up, nb},
-                        {ws, need}};
+                        {ws, sp.bytes}};
   if (spans_meet(outs, 6, ins, 5)) return SB_ERR_INVALID_ARG;
   for (int i = 0; i < 5; ++i)
     if (spans_meet(outs + i, 1, outs + i + 1, 5 - i)) return SB_ERR_INVALID_ARG;
-  if (need > 0 && (!ws || ws_bytes < need)) return SB_ERR_WORKSPACE;
-  if (need > 0 && !at16(ws)) return SB_ERR_INVALID_ARG;
+  if (!ws || ws_bytes < sp.bytes) return SB_ERR_WORKSPACE;
+  if (!at16(ws)) return SB_ERR_INVALID_ARG;
   const void* w[2] = {w_gate, w_up};
   float* dw[2] = {dw_gate, dw_up};
   float* db[2] = {db_gate, db_up};
-  hipStream_t st = sbh::stream_of(stream);
-  if (d->dtype == SB_BF16)
-    gated_bwd_b16(d, x, w, pre, dy, dx, dw, db, accumulate, packs, (char*)ws, sp, st);
-  else
-    s = gated_bwd_f32(d, x, w, pre, dy, dx, dw, db, accumulate, (char*)ws, sp, st);
-  return s != SB_OK ? s : sbh::launch_status();
+  const auto run = d->dtype == SB_BF16 ? gated_bwd_run<u16> : gated_bwd_run<float>;
+  run(d, x, w, pre, dy, dx, dw, db, accumulate, packs, (char*)ws, sp, sbh::stream_of(stream));
+  return sbh::launch_status();
 }

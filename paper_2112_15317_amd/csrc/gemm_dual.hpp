@@ -27,85 +27,117 @@
 #pragma once
 
 #include "gate.hpp"
+#include "split_bf16.hpp"
 
 namespace sb {
 
-typedef short s8v __attribute__((ext_vector_type(8)));
 typedef short s4v __attribute__((ext_vector_type(4)));
 typedef float f16v __attribute__((ext_vector_type(16)));
-typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
 enum DualKind { kDualFwd, kDualDx, kDualDw };
 
-template <int F_>
+// E: float (three bf16 parts, F = 2) or bf16 bits.
+template <int F_, class E_>
 struct DualTile {
-  static constexpr int F = F_;
+  typedef E_ E;
+  static constexpr int F = F_, NP = sizeof(E) == 4 ? 3 : 1;
   static constexpr int BM = 64 * F, RC = 32 * F;     // rows; columns of a region
-  static constexpr int OPER = BM * 32;               // elements of an operand's stage
+  static constexpr int PART = BM * 32, OPER = NP * PART;   // elements of an operand's stage
   static constexpr int STAGE = 2 * OPER;
-  static constexpr size_t LDS_BYTES = 3 * (size_t)STAGE * sizeof(u16);
+  static constexpr size_t LDS_STAGES = 3 * (size_t)STAGE * sizeof(u16);
+  static constexpr size_t LDS_BYTES = LDS_STAGES + (NP == 3 ? 16 : 0);   // the redo flag
+  static_assert(LDS_BYTES <= 160 * 1024, "one block per CU");
 };
 
 struct DualArgs {
-  const u16* a[3];                 // per segment
-  const u16* b[2][3];              // per region (DX: region 0) and segment
+  const void* a[3];                // per segment
+  const void* b[2][3];             // per region (DX: region 0) and segment
   uint32_t a_bytes, b_bytes;       // ranges of the operands
   int lda, ldb;
   int M, N, K, segs;               // K: of a segment
   int mt, nt, splits, stages;      // stages per split
   float* part;                     // splits > 1: [split][2][M][N] (DX [split][M][N])
-  void* c[2]; int ldc;             // DX: dx (bf16); DW: fp32 gradients; FWD: y in c[0]
+  void* c[2]; int ldc;             // DX: dx; DW: fp32 gradients; FWD: y in c[0]
   const float* bias[2];            // FWD
   float* pre;                      // FWD, may be null: [2][M][N]
   int accumulate;
 };
 
-__device__ __forceinline__ f16v mfma32(s8v a, s8v b, f16v c) {
+__device__ __forceinline__ f16v mfma32(s8 a, s8 b, f16v c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-__device__ __forceinline__ u4v load16(rsrc_t r, uint32_t off) {
-  return __builtin_bit_cast(u4v, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
+__device__ __forceinline__ u32x4 load16(rsrc_t r, uint32_t off) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0));
 }
+
+// Eight elements on their way to LDS.
+template <class E> struct DualPiece;
+template <> struct DualPiece<u16> {
+  u32x4 v;
+  __device__ __forceinline__ void load(rsrc_t r, uint32_t off) { v = load16(r, off); }
+  __device__ __forceinline__ void store(u16* to, int, uint32_t&) const {
+    *reinterpret_cast<u32x4*>(to) = v;
+  }
+};
+template <> struct DualPiece<float> {
+  u32x4 v[2];
+  __device__ __forceinline__ void load(rsrc_t r, uint32_t off) {
+    v[0] = load16(r, off);
+    v[1] = load16(r, off + 16);
+  }
+  // The three parts, `part` elements apart; lost as in split_pair.
+  __device__ __forceinline__ void store(u16* to, int part, uint32_t& lost) const {
+    f8v f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(v[e / 4][e % 4]);
+    const Split8 t = split8(f, lost);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *reinterpret_cast<s8*>(to + p * part) = t.p[p];
+  }
+};
 
 // A staged operand: KC contiguous along k, otherwise two regions of RC columns.
 template <class T, bool KC>
 struct DualStage {
+  typedef typename T::E E;
   uint32_t off[T::F];              // byte offset of this lane's pieces at k = 0, or kOOB
   int lds[T::F];                   // their place (elements)
   uint32_t step;                   // bytes per k
   int k;                           // KC: the first k of all of them within a stage
   // Rows (KC) or columns from r0 on, `rows` of them; region 1 starts at r1.
   __device__ __forceinline__ void init(int tid, int ld, int rows, int r0, int r1) {
-    step = KC ? 2u : (uint32_t)ld * 2u;
+    step = (KC ? 1u : (uint32_t)ld) * (uint32_t)sizeof(E);
     k = KC ? tid % 4 * 8 : 0;
 #pragma unroll
     for (int i = 0; i < T::F; ++i) {
       if constexpr (KC) {
         const int row = (tid + 256 * i) / 4, p = tid % 4;
         lds[i] = row * 32 + (p ^ (row >> 2 & 3)) * 8;
-        off[i] = r0 + row < rows ? (uint32_t)((r0 + row) * ld + p * 8) * 2u : kOOB;
+        off[i] = r0 + row < rows ? (uint32_t)((r0 + row) * ld + p * 8) * (uint32_t)sizeof(E) : kOOB;
       } else {
         constexpr int PR = T::RC / 8;                // pieces a line
         const int region = i / (T::F / 2);
         const int w = tid + 256 * (i % (T::F / 2)), line = w / PR, p = w % PR;
         const int col = (region ? r1 : r0) + p * 8;
         lds[i] = region * (T::RC * 32) + line * T::RC + ((p / 2 ^ (line & 3)) * 2 + p % 2) * 8;
-        off[i] = col < rows ? (uint32_t)(line * ld + col) * 2u : kOOB;
+        off[i] = col < rows ? (uint32_t)(line * ld + col) * (uint32_t)sizeof(E) : kOOB;
       }
     }
   }
   // Piece i of the stage from k0 on (k0 < K); r: its region's resource.  Lines at
   // and past K lie behind the operand and read 0 by its range, as kOOB does at
   // any k; a row's pieces past K are left out here.
-  __device__ __forceinline__ void load_one(rsrc_t r, int k0, int K, u4v (&v)[T::F], int i) const {
+  __device__ __forceinline__ void load_one(rsrc_t r, int k0, int K, DualPiece<E> (&v)[T::F],
+                                           int i) const {
     uint32_t o = off[i] + (uint32_t)k0 * step;
     if constexpr (KC) o = k0 + k < K ? o : kOOB;
-    v[i] = load16(r, o);
+    v[i].load(r, o);
   }
-  __device__ __forceinline__ void store_one(u16* S, const u4v (&v)[T::F], int i) const {
-    *reinterpret_cast<u4v*>(S + lds[i]) = v[i];
+  __device__ __forceinline__ void store_one(u16* S, const DualPiece<E> (&v)[T::F], int i,
+                                            uint32_t& lost) const {
+    v[i].store(S + lds[i], T::PART, lost);
   }
 };
 
@@ -129,9 +161,9 @@ __device__ __forceinline__ int frag_place(int q, int lane, int row0) {
   }
 }
 template <class T, bool KC>
-__device__ __forceinline__ s8v frag_read(const u16* S, int place, int s) {
+__device__ __forceinline__ s8 frag_read(const u16* S, int place, int s) {
   if constexpr (KC) {
-    return *reinterpret_cast<const s8v*>(S + (place ^ (s * 16)));    // piece + 2 of 4
+    return *reinterpret_cast<const s8*>(S + (place ^ (s * 16)));    // piece + 2 of 4
   } else {
     typedef __attribute__((address_space(3))) s4v* lds4;
     const u16* p = S + place + s * 16 * T::RC;
@@ -143,9 +175,10 @@ __device__ __forceinline__ s8v frag_read(const u16* S, int place, int s) {
 
 // ACT: FWD's activation (its code is unrolled over all the outputs of a lane).
 template <class T, DualKind KIND, int ACT>
-__global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) {
+__global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dual(DualArgs g) {
   extern __shared__ u16 lds[];
-  constexpr int F = T::F;
+  typedef typename T::E E;
+  constexpr int F = T::F, NP = T::NP;
   constexpr bool AKC = KIND != kDualDw, BKC = KIND == kDualDx;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -174,7 +207,8 @@ __global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) 
   sb.init(tid, g.ldb, g.N, n0, n0);
   // The next stage to load.
   int seg = t0 / per_seg, k0 = (t0 - seg * per_seg) * 32;
-  u4v va[2][F], vb[2][F];
+  DualPiece<E> va[2][F], vb[2][F];
+  uint32_t lost = 0;
   // The operands of its segment; its first k.  Stages past the last segment, which
   // nothing multiplies, load the last one again.
   rsrc_t ra, rb, rc;
@@ -194,11 +228,11 @@ __global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) 
       ++seg;
     }
   };
-  auto load_a = [&](u4v (&x)[F], int i) { sa.load_one(ra, ka, g.K, x, i); };
-  auto load_b = [&](u4v (&x)[F], int i) {
+  auto load_a = [&](DualPiece<E> (&x)[F], int i) { sa.load_one(ra, ka, g.K, x, i); };
+  auto load_b = [&](DualPiece<E> (&x)[F], int i) {
     sb.load_one(!BKC && i >= F / 2 ? rc : rb, ka, g.K, x, i);
   };
-  auto load = [&](u4v (&xa)[F], u4v (&xb)[F]) {
+  auto load = [&](DualPiece<E> (&xa)[F], DualPiece<E> (&xb)[F]) {
     next();
 #pragma unroll
     for (int i = 0; i < F; ++i) {
@@ -207,11 +241,11 @@ __global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) 
     }
     if (k0 == 0) segment();
   };
-  auto store = [&](u16* S, const u4v (&xa)[F], const u4v (&xb)[F]) {
+  auto store = [&](u16* S, const DualPiece<E> (&xa)[F], const DualPiece<E> (&xb)[F]) {
 #pragma unroll
     for (int i = 0; i < F; ++i) {
-      sa.store_one(S, xa, i);
-      sb.store_one(S + T::OPER, xb, i);
+      sa.store_one(S, xa, i, lost);
+      sb.store_one(S + T::OPER, xb, i, lost);
     }
   };
 
@@ -223,13 +257,21 @@ __global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) 
     else pb[i] = T::OPER + (i / (F / 2)) * T::RC * 32 +
                  frag_place<T, false>(wn * (F / 2) + i % (F / 2), lane, 0);
   }
-  f16v acc[F][F];                                    // [column block][row block]
+  // [column block][row block]; low: the sums of the five smaller products of the
+  // parts, which are below 2^-8 of the sums they are added to at the end, so their
+  // roundings do not count.
+  f16v acc[F][F], low[NP == 3 ? F : 1][NP == 3 ? F : 1];
+  auto clear = [](f16v& x) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = 0.f;
+  };
 #pragma unroll
   for (int j = 0; j < F; ++j)
 #pragma unroll
-    for (int i = 0; i < F; ++i)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[j][i][v] = 0.f;
+    for (int i = 0; i < F; ++i) {
+      clear(acc[j][i]);
+      if constexpr (NP == 3) clear(low[j][i]);
+    }
 
   load(va[0], vb[0]);
   load(va[1], vb[1]);
@@ -239,59 +281,161 @@ __global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) 
   load(va[1], vb[1]);
   __syncthreads();
 
-  s8v fa[2][F], fb[2][F];
+  s8 fa[2][F][NP], fb[2][F][NP];
+  auto read_a = [&](int c, const u16* S, int i, int p, int s) {
+    fa[c][i][p] = frag_read<T, AKC>(S + p * T::PART, pa[i], s);
+  };
+  auto read_b = [&](int c, const u16* S, int j, int p, int s) {
+    fb[c][j][p] = frag_read<T, BKC>(S + p * T::PART, pb[j], s);
+  };
 #pragma unroll
-  for (int i = 0; i < F; ++i) {
-    fa[0][i] = frag_read<T, AKC>(lds, pa[i], 0);
-    fb[0][i] = frag_read<T, BKC>(lds, pb[i], 0);
-  }
-  // 16 k out of fragment set P: F * F MFMAs, and between them the reads of the next
-  // 16 k from S (one fragment behind each of the first 2 F MFMAs, in the order of their
-  // use), and in a stage's first half, behind the others, the pieces of the stage
-  // after the next one to LDS and the loads that take their registers' place.
-  auto step = [&](auto P, auto W, const u16* S, int s, u16* to) {
-    constexpr int c = decltype(P)::value, r = decltype(W)::value;   // r < 0: nothing to write
+  for (int i = 0; i < F; ++i)
 #pragma unroll
-    for (int n = 0; n < F * F; ++n) {
-      const int j = n / F, i = n % F;
-      acc[j][i] = mfma32(fb[c][j], fa[c][i], acc[j][i]);
-      if (n == 0) fb[c ^ 1][0] = frag_read<T, BKC>(S, pb[0], s);
-      else if (n <= F) fa[c ^ 1][n - 1] = frag_read<T, AKC>(S, pa[n - 1], s);
-      else if (n < 2 * F) fb[c ^ 1][n - F] = frag_read<T, BKC>(S, pb[n - F], s);
-      if constexpr (r >= 0) {
-        // The pieces of A, then of B: 2 F of them over the last MFMAs.
-        constexpr int first = F == 4 ? 8 : 0, each = F == 4 ? 1 : 1;
-        const int x = (n - first) * each;
-        if (x >= 0 && x < F) {
-          sa.store_one(to, va[r], x);
-          load_a(va[r], x);
-        } else if (x >= F && x < 2 * F) {
-          sb.store_one(to + T::OPER, vb[r], x - F);
-          load_b(vb[r], x - F);
+    for (int p = 0; p < NP; ++p) {
+      read_a(0, lds, i, p, 0);
+      read_b(0, lds, i, p, 0);
+    }
+  // 16 k out of fragment set P: the MFMAs, and between them the reads of the next 16 k
+  // from S (one fragment behind each of the first MFMAs, in the order of their use),
+  // and, behind the others, pieces of the stage after the next one to LDS and the loads
+  // that take their registers' place.
+  auto step = [&](auto P, auto H, auto W, const u16* S, int s, u16* to) {
+    constexpr int c = decltype(P)::value, half = decltype(H)::value, r = decltype(W)::value;
+    if constexpr (NP == 1) {
+#pragma unroll
+      for (int n = 0; n < F * F; ++n) {
+        const int j = n / F, i = n % F;
+        acc[j][i] = mfma32(fb[c][j][0], fa[c][i][0], acc[j][i]);
+        if (n == 0) read_b(c ^ 1, S, 0, 0, s);
+        else if (n <= F) read_a(c ^ 1, S, n - 1, 0, s);
+        else if (n < 2 * F) read_b(c ^ 1, S, n - F, 0, s);
+        if (half == 0) {
+          // The pieces of A, then of B: 2 F of them over the last MFMAs.
+          const int x = n - (F == 4 ? 8 : 0);
+          if (x >= 0 && x < F) {
+            sa.store_one(to, va[r], x, lost);
+            load_a(va[r], x);
+          } else if (x >= F && x < 2 * F) {
+            sb.store_one(to + T::OPER, vb[r], x - F, lost);
+            load_b(vb[r], x - F);
+          }
         }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      // Six products of F * F blocks each; A's pieces in a stage's first half, B's in
+      // its second.  The scheduler spreads the splitting over the MFMAs.
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < F; ++x) {
+        if (half == 0) {
+          sa.store_one(to, va[r], x, lost);
+          load_a(va[r], x);
+        } else {
+          sb.store_one(to + T::OPER, vb[r], x, lost);
+          load_b(vb[r], x);
+        }
+      }
+#pragma unroll
+      for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+        for (int i = 0; i < F; ++i) {
+          read_a(c ^ 1, S, i, p, s);
+          read_b(c ^ 1, S, i, p, s);
+        }
+#pragma unroll
+      for (int q = 0; q < 6; ++q)
+#pragma unroll
+        for (int n = 0; n < F * F; ++n) {
+          const int j = n / F, i = n % F;
+          f16v& t = q == 5 ? acc[j][i] : low[j][i];
+          t = mfma32(fb[c][j][kSplitB[q]], fa[c][i][kSplitA[q]], t);
+        }
+#pragma unroll
+      for (int n = 0; n < 6 * F * F; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // an MFMA,
+        __builtin_amdgcn_sched_group_barrier(0x080, 1, 0);   // an LDS access,
+        __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);   // vector ALU
       }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
   // A stage in buffer b0; b2 gets the stage after the next one.
+  typedef std::integral_constant<int, 0> Zero;
+  typedef std::integral_constant<int, 1> One;
   auto stage = [&](auto R, u16* b0, u16* b1, u16* b2) {
     next();
-    step(std::integral_constant<int, 0>{}, R, b0, 1, b2);
-    if (k0 == 0) segment();
-    step(std::integral_constant<int, 1>{}, std::integral_constant<int, -1>{}, b1, 0, nullptr);
+    step(Zero{}, Zero{}, R, b0, 1, b2);
+    if (NP == 1 && k0 == 0) segment();
+    step(One{}, One{}, R, b1, 0, b2);
+    if (NP == 3 && k0 == 0) segment();
     __syncthreads();
   };
   u16 *b0 = lds, *b1 = lds + T::STAGE, *b2 = lds + 2 * T::STAGE;
   int t = 0;
   for (; t + 2 <= nk; t += 2) {
-    stage(std::integral_constant<int, 0>{}, b0, b1, b2);
-    stage(std::integral_constant<int, 1>{}, b1, b2, b0);
+    stage(Zero{}, b0, b1, b2);
+    stage(One{}, b1, b2, b0);
     u16* x = b0;
     b0 = b2;
     b2 = b1;
     b1 = x;
   }
-  if (t < nk) stage(std::integral_constant<int, 0>{}, b0, b1, b2);
+  if (t < nk) stage(Zero{}, b0, b1, b2);
+
+  if constexpr (NP == 3) {
+    // A block with values that the parts do not carry, or sums that are not finite,
+    // does its reduction again on the fp32 MFMA, operands straight from memory.
+    int* redo = reinterpret_cast<int*>(lds + T::LDS_STAGES / sizeof(u16));
+    if (tid == 0) *redo = 0;
+    __syncthreads();
+    float z = 0.f;                                   // stays 0 over finite values
+#pragma unroll
+    for (int j = 0; j < F; ++j)
+#pragma unroll
+      for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          acc[j][i][v] += low[j][i][v];
+          z = fmaf(acc[j][i][v], 0.f, z);
+        }
+    if ((lost & 0xffffu) || !(z == 0.f)) *redo = 1;
+    __syncthreads();
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(*redo), 0)) {
+      int ar[F], bc[F];                              // this lane's rows of A, columns of B
+#pragma unroll
+      for (int q = 0; q < F; ++q) {
+        const int c = lane % 32;
+        ar[q] = m0 + wm * T::RC + (AKC ? q * 32 + c : pair_block<F>(q, c / 16) * 16 + c % 16);
+        bc[q] = n0 + (BKC ? wn * T::RC + q * 32 + c
+                          : pair_block<F>(wn * (F / 2) + q % (F / 2), c / 16) * 16 + c % 16);
+#pragma unroll
+        for (int j = 0; j < F; ++j) clear(acc[j][q]);
+      }
+      for (int u = t0; u < t1; ++u) {
+        const int sg = u / per_seg, kb = (u - sg * per_seg) * 32, ke = min(g.K, kb + 32);
+        const float* A = (const float*)g.a[sg];
+#pragma unroll 1
+        for (int kk = kb; kk < ke; kk += 2) {
+          const int k = kk + lane / 32;
+          float av[F];
+#pragma unroll
+          for (int i = 0; i < F; ++i)
+            av[i] = k < ke && ar[i] < g.M
+                        ? A[AKC ? (size_t)ar[i] * g.lda + k : (size_t)k * g.lda + ar[i]] : 0.f;
+#pragma unroll
+          for (int j = 0; j < F; ++j) {
+            const float* B = (const float*)g.b[BKC ? 0 : j / (F / 2)][sg];
+            const float bv = k < ke && bc[j] < g.N
+                                 ? B[BKC ? (size_t)bc[j] * g.ldb + k : (size_t)k * g.ldb + bc[j]] : 0.f;
+#pragma unroll
+            for (int i = 0; i < F; ++i)
+              acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(bv, av[i], acc[j][i], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
 
   // acc[j][i] element v: output row m of fragment i, column 8 (v / 4) + 4 (lane / 32) + v % 4
   // of fragment j.
@@ -318,12 +462,12 @@ __global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) 
             for (int e = 0; e < 4; ++e)
               if (n + e < g.N) p[e] = s[e];
           } else {
-            u16* p = (u16*)g.c[0] + (size_t)m * g.ldc + n;
-            if (n + 4 <= g.N && ((uintptr_t)p & 7) == 0) Elem<u16>::store4(p, s);
+            E* p = (E*)g.c[0] + (size_t)m * g.ldc + n;
+            if (n + 4 <= g.N && ((uintptr_t)p & (4 * sizeof(E) - 1)) == 0) Elem<E>::store4(p, s);
             else
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (n + e < g.N) p[e] = f32_to_bf16(s[e]);
+                if (n + e < g.N) Elem<E>::store(p, e, s[e]);
           }
         }
       } else {
@@ -338,9 +482,9 @@ __global__ __launch_bounds__(256, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) 
             s[1][e] = acc[j + F / 2][i][v4 * 4 + e];
           }
           if (KIND == kDualFwd && g.splits == 1) {
-            gate_store<u16>(ACT, s[0], s[1], n, g.N, g.bias[0], g.bias[1],
+            gate_store<E>(ACT, s[0], s[1], n, g.N, g.bias[0], g.bias[1],
                             g.pre ? g.pre + (size_t)m * g.N : nullptr, (size_t)g.M * g.N,
-                            (u16*)g.c[0] + (size_t)m * g.ldc);
+                            (E*)g.c[0] + (size_t)m * g.ldc);
           } else {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
