@@ -25,23 +25,28 @@ namespace sb {
 
 // da and du in rows of np (n rounded up to 8, zeros behind n).  fp32: da, then du,
 // m * np elements each.  bf16: three parts of each, part p of da at p * m * np, of du at
-// (3 + p) * m * np.  A block has 256 columns of kActRows rows, a lane four columns of
+// (3 + p) * m * np.  A block has 256 columns of `rows` rows, a lane four columns of
 // every fourth row, and leaves its columns' sums in sums [row block][2][np].
-constexpr int kActRows = 32;
+static int act_rows(int m, int np) {
+  // Down to a row a wave where 32 would leave CUs idle (128 x 256: 10.2 -> 3 us).
+  int rows = 32;
+  while (rows > 4 && (int64_t)((np + 255) / 256) * cdiv(m, rows) < 1024) rows /= 2;
+  return rows;
+}
 
 template <class E>
 __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int act,
                                                      const float* __restrict__ pre,
                                                      const E* __restrict__ dy, int ldy,
                                                      E* __restrict__ d, float* __restrict__ sums,
-                                                     int vec) {
+                                                     int rows, int vec) {
   __shared__ f4 part[2][4][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int c = blockIdx.x * 256 + lane * 4;
   const size_t mn = (size_t)m * n, plane = (size_t)m * np;
-  const int r1 = min(m, (int)(blockIdx.y + 1) * kActRows);
+  const int r1 = min(m, (int)(blockIdx.y + 1) * rows);
   f4 s[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
-  for (int r = blockIdx.y * kActRows + w; r < r1 && c < np; r += 4) {
+  for (int r = blockIdx.y * rows + w; r < r1 && c < np; r += 4) {
     const float* pa = pre + (size_t)r * n + c;
     const E* pd = dy + (size_t)r * ldy + c;
     f4 a = f4{0.f, 0.f, 0.f, 0.f}, u = a, g = a;
@@ -293,7 +298,7 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
   };
   if (pass == SB_FC_BWD) {
     take(s.d, m * np * (d->dtype == SB_BF16 ? 12 : 8));
-    take(s.sums, (size_t)cdiv(d->m, kActRows) * np * 8);
+    take(s.sums, (size_t)cdiv(d->m, act_rows(d->m, (int)np)) * np * 8);
   }
   if (pass == SB_FC_FWD ? k.x : k.lines) take(s.x, m * up8(d->k_in) * es);
   if (k.w) take(s.w, 2 * (size_t)d->k_in * np * es);
@@ -384,7 +389,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
                           float* const* db, int accumulate, const GatedPacks& packs, char* ws,
                           const GatedSpace& sp, hipStream_t st) {
   constexpr int NP = sizeof(E) == 2 ? 3 : 1;
-  const int np = up8(d->n_shard), chunks = cdiv(d->m, kActRows);
+  const int np = up8(d->n_shard), rows = act_rows(d->m, np), chunks = cdiv(d->m, rows);
   const size_t plane = (size_t)d->m * np;
   E* parts = (E*)(ws + sp.d);
   float* split = (float*)(ws + sp.split);
@@ -392,7 +397,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   const int vec = d->n_shard % 4 == 0 && at16(pre) && d->ldy % 4 == 0 &&
                   ((uintptr_t)dy & (4 * sizeof(E) - 1)) == 0;
   gated_act_bwd<E><<<dim3(cdiv(np, 256), chunks), 256, 0, st>>>(
-      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, sums, vec);
+      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, sums, rows, vec);
   if (sums)
     gated_bias_sums<<<dim3(cdiv(d->n_shard, 64), 2), 256, 0, st>>>(sums, chunks, d->n_shard, np,
                                                                    db[0], db[1], accumulate);

@@ -173,6 +173,26 @@ __device__ __forceinline__ s8 frag_read(const u16* S, int place, int s) {
   }
 }
 
+// Four columns n .. n + 3 of a row, those below N.
+template <class E>
+__device__ __forceinline__ void put_quad(E* row, f4 v, int n, int N) {
+  if (n + 4 <= N && ((uintptr_t)(row + n) & (4 * sizeof(E) - 1)) == 0) {
+    Elem<E>::store4(row + n, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < N) Elem<E>::store(row, n + e, v[e]);
+  }
+}
+__device__ __forceinline__ f4 get_quad(const float* row, int n, int N) {
+  if (n + 4 <= N && ((uintptr_t)(row + n) & 15) == 0) return *reinterpret_cast<const f4*>(row + n);
+  f4 v = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < N) v[e] = row[n + e];
+  return v;
+}
+
 // ACT: FWD's activation (its code is unrolled over all the outputs of a lane).
 template <class T, DualKind KIND, int ACT>
 __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dual(DualArgs g) {
@@ -437,73 +457,78 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
     }
   }
 
-  // acc[j][i] element v: output row m of fragment i, column 8 (v / 4) + 4 (lane / 32) + v % 4
-  // of fragment j.
+  // acc[j][i] element v: row lane % 32 of row block i, column 8 (v / 4) + 4 (lane / 32) +
+  // v % 4 of column block j.  Stored from there an access would touch 64 lines, 16 bytes
+  // each, and those of an epilogue with pre took 60 us a tile; so 32 rows at a time go
+  // through the wave's own part of LDS (the last stage's reads are done), and out in
+  // runs of 32 columns or more.
+  constexpr int CW = KIND == kDualDx ? 32 * F : 16 * F;      // columns of an output
+  constexpr int P = 32 * F + 4;                              // pitch (floats)
+  static_assert(4 * 32 * P * sizeof(float) <= T::LDS_STAGES, "the stages' LDS holds the rows");
+  float* W = reinterpret_cast<float*>(lds) + wave * 32 * P;
+  auto rows_out = [&](auto I) {
+    constexpr int i = decltype(I)::value;
+    if constexpr (i < F) {
 #pragma unroll
+      for (int j = 0; j < F; ++j)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4) {
+          f4 t;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[e] = acc[j][i][v4 * 4 + e];
+          *reinterpret_cast<f4*>(W + (lane % 32) * P + j * 32 + 8 * v4 + 4 * (lane / 32)) = t;
+        }
+    }
+  };
+  // One copy of the code that stores (the activations' is long); i is uniform.
+#pragma unroll 1
   for (int i = 0; i < F; ++i) {
-    const int c = lane % 32;
-    const int m = m0 + wm * T::RC +
-                  (AKC ? i * 32 + c : pair_block<F>(i, c / 16) * 16 + c % 16);
-    if (m >= g.M) continue;
+    switch (i) {
+      case 0: rows_out(Zero{}); break;
+      case 1: rows_out(One{}); break;
+      case 2: rows_out(std::integral_constant<int, 2>{}); break;
+      default: rows_out(std::integral_constant<int, 3>{});
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-    for (int v4 = 0; v4 < 4; ++v4) {
-      const int d = 8 * v4 + 4 * (lane / 32);
+    for (int x = 0; x < CW / 8; ++x) {
+      const int row = (x * 64 + lane) / (CW / 4), o = lane % (CW / 4) * 4;
+      const int m = m0 + wm * T::RC + (AKC ? i * 32 + row : pair_block<F>(i, row / 16) * 16 + row % 16);
       if constexpr (KIND == kDualDx) {
-#pragma unroll
-        for (int j = 0; j < F; ++j) {
-          const int n = n0 + wn * T::RC + j * 32 + d;
-          if (n >= g.N) continue;
-          f4 s;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[e] = acc[j][i][v4 * 4 + e];
-          if (g.splits > 1) {
-            float* p = g.part + ((size_t)split * g.M + m) * g.N + n;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (n + e < g.N) p[e] = s[e];
-          } else {
-            E* p = (E*)g.c[0] + (size_t)m * g.ldc + n;
-            if (n + 4 <= g.N && ((uintptr_t)p & (4 * sizeof(E) - 1)) == 0) Elem<E>::store4(p, s);
-            else
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (n + e < g.N) Elem<E>::store(p, e, s[e]);
-          }
+        const int n = n0 + wn * T::RC + o;
+        const f4 v = *reinterpret_cast<const f4*>(W + row * P + o);
+        if (m < g.M && n < g.N) {
+          if (g.splits > 1) put_quad(g.part + ((size_t)split * g.M + m) * g.N, v, n, g.N);
+          else put_quad((E*)g.c[0] + (size_t)m * g.ldc, v, n, g.N);
         }
       } else {
+        // Output columns in order: F = 4 has its blocks' halves 64 columns apart.
+        const int at = F == 4 ? o % 32 / 16 * 32 + o / 32 * 16 + o % 16 : o;
+        const int n = n0 + (F == 4 ? wn * 32 + o / 32 * 64 + o % 32 : wn * 32 + o);
+        f4 v[2];
 #pragma unroll
-        for (int j = 0; j < F / 2; ++j) {
-          const int n = n0 + pair_block<F>(wn * (F / 2) + j, d / 16) * 16 + d % 16;
-          if (n >= g.N) continue;
-          f4 s[2];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            s[0][e] = acc[j][i][v4 * 4 + e];
-            s[1][e] = acc[j + F / 2][i][v4 * 4 + e];
-          }
+        for (int q = 0; q < 2; ++q) v[q] = *reinterpret_cast<const f4*>(W + row * P + q * CW + at);
+        if (m < g.M && n < g.N) {
           if (KIND == kDualFwd && g.splits == 1) {
-            gate_store<E>(ACT, s[0], s[1], n, g.N, g.bias[0], g.bias[1],
-                            g.pre ? g.pre + (size_t)m * g.N : nullptr, (size_t)g.M * g.N,
-                            (E*)g.c[0] + (size_t)m * g.ldc);
+            gate_store<E>(ACT, v[0], v[1], n, g.N, g.bias[0], g.bias[1],
+                          g.pre ? g.pre + (size_t)m * g.N : nullptr, (size_t)g.M * g.N,
+                          (E*)g.c[0] + (size_t)m * g.ldc);
+          } else if (g.splits > 1) {
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+              put_quad(g.part + (((size_t)split * 2 + q) * g.M + m) * g.N, v[q], n, g.N);
           } else {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-              float* p = g.splits > 1 ? g.part + (((size_t)split * 2 + q) * g.M + m) * g.N + n
-                                      : (float*)g.c[q] + (size_t)m * g.ldc + n;
-              const bool add = g.splits == 1 && g.accumulate;
-              if (n + 4 <= g.N && ((uintptr_t)p & 15) == 0) {
-                if (add) s[q] += *reinterpret_cast<const f4*>(p);
-                *reinterpret_cast<f4*>(p) = s[q];
-              } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (n + e < g.N) p[e] = add ? p[e] + s[q][e] : s[q][e];
-              }
+              float* c = (float*)g.c[q] + (size_t)m * g.ldc;
+              if (g.accumulate) v[q] += get_quad(c, n, g.N);
+              put_quad(c, v[q], n, g.N);
             }
           }
         }
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
