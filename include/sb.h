@@ -534,14 +534,14 @@ sb_status sb_sgd_update(int count, float *const *w, const float *const *g,
                         const size_t *n, const float *scale, float lr,
                         void *stream);
 
-/* AdamW step on `count` tensors (Adam with decoupled weight decay: in place of
- * the SGD step).  For every element, with g = grad_scale * gradient and t the
- * number of this update:
+/* AdamW step on many tensors (Adam with decoupled weight decay: in place of the SGD
+ * step).  For every element, with g = grad_scale * gradient and t the number of this
+ * update:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
  *   w = (1 - lr decay) w - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
  * in fp32; m and v of the update are those before they become bytes.
  *
- * Moments (`moments` of the descriptor):
+ * Moments:
  *   32  fp32, zero before the first update;
  *   8   bytes.  The rank of a value is its fp32 pattern's exponent and upper
  *       three mantissa bits, as a whole number: 8 ranks an octave.  Each block
@@ -561,27 +561,8 @@ sb_status sb_sgd_update(int count, float *const *w, const float *const *g,
  * Tensors: w, g (and m, v of 32 bits) fp32; copy, if not NULL, gets w's new value
  * in bfloat16.  first: the number of the tensor's first element among the random
  * numbers; tensors of one model take ranges of their own (unused with 32).  n may
- * be 0 (nothing to do).  The array is host memory, read before the call returns;
- * more than 40 tensors take a launch per 40.
- *
- * The number of the update is step + *steps_done, where steps_done is a device
- * counter (int32, 0 at the start) for callers that replay the call from a graph
- * and advance it there with sb_adamw_advance, or NULL: then it is step.
- *
- * SB_ERR_INVALID_ARG for a count outside 1..SB_ADAMW_MAX_TENSORS, betas outside
- * [0, 1), values that are not finite, a negative eps, step < 1 (< 0 would be with a
- * counter: the sum has to be at least 1), moments other than 8 and 32, NULL
- * pointers, pointers that are not multiples of their elements' size, and for
- * an output (w, copy, moments, references) that overlaps any other tensor of the
- * call.  Gradients may overlap each other. */
+ * be 0 (nothing to do). */
 enum { SB_ADAMW_MAX_TENSORS = 512, SB_ADAMW_BLOCK = 256 };
-typedef struct {
-    double lr, beta1, beta2, eps;
-    int step;              /* >= 1: the update's number, or 1 + what is added
-                              to the counter's value                       */
-    int moments;           /* 32 or 8                                      */
-    uint32_t seed;
-} sb_adamw_desc;
 typedef struct {
     float *w;
     void *copy;            /* bfloat16, or NULL                            */
@@ -593,9 +574,39 @@ typedef struct {
     float grad_scale;      /* 1/K for FC shards                            */
     float decay;
 } sb_adamw_tensor;
-sb_status sb_adamw_update(const sb_adamw_desc *desc, int count,
-                          const sb_adamw_tensor *tensors,
-                          const int32_t *steps_done, void *stream);
+typedef struct { int tensors, moments, blocks; } sb_adamw_plan;
+
+/* The tensors of an update are written into a plan in device memory once, so that
+ * every update is one launch however many there are.  plan: device memory of the
+ * caller's, sb_adamw_plan_bytes(count) bytes (0 for a count outside 1 ..
+ * SB_ADAMW_MAX_TENSORS), a multiple of 16, alive and unchanged as long as it is
+ * used; info: host memory, filled by the call and handed to every update.
+ * moments: 32 or 8.  The tensor array is host memory, read before the call returns.
+ * SB_ERR_INVALID_ARG for bad counts or moments, scales or decays that are not
+ * finite, NULL pointers, pointers that are not multiples of their elements' size, and
+ * for an output (w, copy, moments, references, the plan) that overlaps any other
+ * tensor of the call; gradients may overlap each other.  SB_ERR_WORKSPACE for a
+ * short plan.  Nothing is enqueued then. */
+size_t sb_adamw_plan_bytes(int count);
+sb_status sb_adamw_make_plan(int moments, int count,
+                             const sb_adamw_tensor *tensors, void *plan,
+                             size_t plan_bytes, sb_adamw_plan *info,
+                             void *stream);
+
+/* One update of a plan's tensors.  Its number is step + *steps_done, where steps_done
+ * is a device counter (int32, 0 at the start) for callers that replay the call from
+ * a graph and advance it there with sb_adamw_advance, or NULL: then it is step.  The
+ * counter must not be part of an output.  SB_ERR_INVALID_ARG for NULL pointers, an
+ * info that no plan has, betas outside [0, 1), values that are not finite, a negative
+ * eps, step < 1. */
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int step;              /* >= 1                                         */
+    uint32_t seed;
+} sb_adamw_desc;
+sb_status sb_adamw_update(const sb_adamw_desc *desc, const sb_adamw_plan *info,
+                          const void *plan, const int32_t *steps_done,
+                          void *stream);
 
 /* *steps_done += 1, on the stream. */
 sb_status sb_adamw_advance(int32_t *steps_done, void *stream);

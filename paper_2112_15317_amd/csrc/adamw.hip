@@ -26,8 +26,13 @@
 // for the bf16 copy.  A wave takes 256 consecutive elements at a time, four a
 // lane in 16-byte pieces, so that a block of bytes is one wave's and its largest
 // rank a reduction over the lanes; a lane has all its loads under way before the
-// first store.  Blocks of tensor t are block0[t] .. block0[t+1]-1; the block's
-// tensor is found by bisection.
+// first store.
+//
+// All tensors take one launch: their addresses lie in a table in device memory (the
+// plan), written once.  As kernel arguments, 40 tensors a launch, 300 tensors of 40 M
+// elements took 316 us, in one launch ONE_LAUNCH_US.  Blocks of tensor t are block0[t] ..
+// block0[t+1]-1; a wave finds its tensor by counting, 64 entries at a time, those that
+// start by its block.
 #include "sb_internal.hpp"
 
 #include <algorithm>
@@ -35,9 +40,9 @@
 
 namespace sb {
 
-constexpr int kAdamwLaunch = 40;             // tensors per launch (kernel arguments end at 4 KB)
 constexpr int kAdamwGroups = 4;              // groups of 4 elements per lane
 constexpr int kAdamwBlock = 1024 * kAdamwGroups;
+constexpr int kAdamwChunk = 40;              // tensors a launch writes into a plan
 
 struct AdamwTensor {
   float* w;
@@ -47,19 +52,36 @@ struct AdamwTensor {
   int16_t *m_top, *v_top;
   uint64_t first;
   size_t n;
-  float scale, keep;
+  float scale, decay;
   int block0, vec;
 };
 
-struct AdamwBatch {
-  AdamwTensor t[kAdamwLaunch];
+// A plan: the tensors' first blocks, then the tensors.
+__host__ __device__ constexpr size_t plan_tensors(int count) {
+  return round_up((size_t)count * sizeof(int), 256);
+}
+
+struct AdamwChunk {
+  AdamwTensor t[kAdamwChunk];
+  int first, count, total;                   // tensors first .. first + count - 1 of total
+};
+static_assert(sizeof(AdamwChunk) <= 4096, "kernel arguments");
+
+__global__ __launch_bounds__(64) void adamw_plan_kernel(AdamwChunk c, char* plan) {
+  const int i = threadIdx.x;
+  if (i >= c.count) return;
+  ((int*)plan)[c.first + i] = c.t[i].block0;
+  ((AdamwTensor*)(plan + plan_tensors(c.total)))[c.first + i] = c.t[i];
+}
+
+struct AdamwStep {
+  const char* plan;
   const int32_t* steps_done;
   double lr, beta1, beta2;
   float b1, c1, b2, c2, eps, rate, vscale;   // rate, vscale: of step, without a counter
   uint32_t seed;
   int step, count;
 };
-static_assert(sizeof(AdamwBatch) <= 4096, "kernel arguments");
 
 __host__ __device__ inline uint32_t mix32(uint32_t x) {
   x ^= x >> 16;
@@ -126,18 +148,19 @@ typedef uint8_t b4 __attribute__((ext_vector_type(4)));
 typedef u16 h4 __attribute__((ext_vector_type(4)));
 
 template <bool BYTES>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch b) {
+__global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
   typedef typename std::conditional<BYTES, uint8_t, float>::type S;
   typedef typename std::conditional<BYTES, b4, f4>::type S4;
   constexpr int U = kAdamwGroups;
   const int blk = blockIdx.x;
-  int ti = 0, hi = b.count;                  // the last tensor whose blocks start by blk
-  while (hi - ti > 1) {
-    const int mid = (ti + hi) / 2;
-    if (b.t[mid].block0 <= blk) ti = mid;
-    else hi = mid;
+  int ti = -1;                               // the last tensor whose blocks start by blk
+  const int* block0 = (const int*)b.plan;
+  for (int i = 0; i < b.count; i += 64) {
+    const int at = i + (threadIdx.x & 63);
+    ti += __popcll(__ballot(at < b.count && block0[min(at, b.count - 1)] <= blk));
   }
-  const AdamwTensor& t = b.t[ti];
+  ti = __builtin_amdgcn_readfirstlane(ti);
+  const AdamwTensor t = ((const AdamwTensor*)(b.plan + plan_tensors(b.count)))[ti];
   const size_t n = t.n;
   const size_t base = (size_t)(blk - t.block0) * kAdamwBlock + threadIdx.x * 4;
   const S *m = (const S*)t.m, *v = (const S*)t.v;
@@ -158,6 +181,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch b) {
     }
   }
   float rate = b.rate, vscale = b.vscale;
+  const float keep = (float)(1.0 - b.lr * (double)t.decay);
   uint32_t step = (uint32_t)b.step;
   if (b.steps_done) {
     step = (uint32_t)max(1, b.step + *b.steps_done);
@@ -187,7 +211,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwBatch b) {
       const float g = g4[u][e] * t.scale;
       nm[e] = om * b.b1 + g * b.c1;
       nv[e] = ov * b.b2 + (g * g) * b.c2;
-      nw[e] = w4[u][e] * t.keep - rate * (nm[e] / (sqrtf(nv[e]) * vscale + b.eps));
+      nw[e] = w4[u][e] * keep - rate * (nm[e] / (sqrtf(nv[e]) * vscale + b.eps));
     }
     adamw_store4<float, f4>(t.w, i, n, whole, nw);
     if (t.copy) {
@@ -296,28 +320,30 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 }  // namespace
 
-extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, int count,
-                                     const sb_adamw_tensor* tensors, const int32_t* steps_done,
-                                     void* stream) {
-  if (!d || !tensors || count < 1 || count > SB_ADAMW_MAX_TENSORS) return SB_ERR_INVALID_ARG;
-  if (!std::isfinite(d->lr) || !std::isfinite(d->eps) || !(d->eps >= 0.0)) return SB_ERR_INVALID_ARG;
-  if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0))
+extern "C" size_t sb_adamw_plan_bytes(int count) {
+  if (count < 1 || count > SB_ADAMW_MAX_TENSORS) return 0;
+  return sb::plan_tensors(count) + (size_t)count * sizeof(sb::AdamwTensor);
+}
+
+extern "C" sb_status sb_adamw_make_plan(int moments, int count, const sb_adamw_tensor* tensors,
+                                        void* plan, size_t plan_bytes, sb_adamw_plan* info,
+                                        void* stream) {
+  if (!tensors || !plan || !info || count < 1 || count > SB_ADAMW_MAX_TENSORS)
     return SB_ERR_INVALID_ARG;
-  if (d->step < 1 || (d->moments != 8 && d->moments != 32)) return SB_ERR_INVALID_ARG;
-  if (!aligned(steps_done, 4)) return SB_ERR_INVALID_ARG;
-  const bool bytes = d->moments == 8;
+  if ((moments != 8 && moments != 32) || !aligned(plan, 16)) return SB_ERR_INVALID_ARG;
+  const size_t need = sb_adamw_plan_bytes(count);
+  const bool bytes = moments == 8;
   Range r[7 * SB_ADAMW_MAX_TENSORS + 1];
   int ranges = 0;
   auto add = [&](const void* p, size_t size, bool out) {
     r[ranges++] = Range{(uintptr_t)p, (uintptr_t)p + size, out};
   };
-  if (steps_done) add(steps_done, 4, false);
-  long blocks = 0;
+  add(plan, need, true);
+  int64_t blocks = 0;
+  int used = 0;
   for (int i = 0; i < count; ++i) {
     const sb_adamw_tensor& t = tensors[i];
-    if (!std::isfinite(t.grad_scale) || !std::isfinite(t.decay) ||
-        !std::isfinite((float)(1.0 - d->lr * t.decay)))
-      return SB_ERR_INVALID_ARG;
+    if (!std::isfinite(t.grad_scale) || !std::isfinite(t.decay)) return SB_ERR_INVALID_ARG;
     if (t.n == 0) continue;
     if (!t.w || !t.g || !t.m || !t.v || t.n >= (1ull << 40)) return SB_ERR_INVALID_ARG;
     if (!aligned(t.w, 4) || !aligned(t.g, 4) || !aligned(t.copy, 2)) return SB_ERR_INVALID_ARG;
@@ -335,49 +361,66 @@ extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, int count,
     add(t.m, t.n * (bytes ? 1 : 4), true);
     add(t.v, t.n * (bytes ? 1 : 4), true);
     if (t.copy) add(t.copy, t.n * 2, true);
-    blocks += (long)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
-    if (blocks >= (1l << 31)) return SB_ERR_UNSUPPORTED;
+    ++used;
+    blocks += (int64_t)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
+    if (blocks >= (1ll << 31)) return SB_ERR_UNSUPPORTED;
   }
   if (outputs_meet(r, ranges)) return SB_ERR_INVALID_ARG;
+  if (plan_bytes < need) return SB_ERR_WORKSPACE;
+  sb::AdamwChunk c{};
+  c.total = used;
+  blocks = 0;
+  for (int i = 0; i <= count; ++i) {
+    if (c.count == sb::kAdamwChunk || (i == count && c.count)) {
+      sb::adamw_plan_kernel<<<1, 64, 0, sbh::stream_of(stream)>>>(c, (char*)plan);
+      const sb_status s = sbh::launch_status();
+      if (s != SB_OK) return s;
+      c.first += c.count;
+      c.count = 0;
+    }
+    if (i == count) break;
+    const sb_adamw_tensor& t = tensors[i];
+    if (t.n == 0) continue;
+    sb::AdamwTensor& o = c.t[c.count++];
+    o.w = t.w; o.copy = (sb::u16*)t.copy; o.g = t.g; o.m = t.m; o.v = t.v;
+    o.m_top = t.m_top; o.v_top = t.v_top; o.first = t.first; o.n = t.n;
+    o.scale = t.grad_scale; o.decay = t.decay;
+    o.block0 = (int)blocks;
+    // Four elements at a time: 16, 8 and 4 bytes of fp32, bf16 and bytes.
+    o.vec = aligned(t.w, 16) && aligned(t.g, 16) && aligned(t.copy, 8) &&
+            aligned(t.m, bytes ? 4 : 16) && aligned(t.v, bytes ? 4 : 16);
+    blocks += (int64_t)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
+  }
+  *info = sb_adamw_plan{used, moments, (int)blocks};
+  return SB_OK;
+}
+
+extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, const sb_adamw_plan* info,
+                                     const void* plan, const int32_t* steps_done, void* stream) {
+  if (!d || !info || !plan || !aligned(plan, 16)) return SB_ERR_INVALID_ARG;
+  if (info->tensors < 0 || info->tensors > SB_ADAMW_MAX_TENSORS ||
+      info->blocks < info->tensors || (info->tensors == 0 && info->blocks != 0) ||
+      (info->moments != 8 && info->moments != 32))
+    return SB_ERR_INVALID_ARG;
+  if (!std::isfinite(d->lr) || !std::isfinite(d->eps) || !(d->eps >= 0.0)) return SB_ERR_INVALID_ARG;
+  if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0))
+    return SB_ERR_INVALID_ARG;
+  if (d->step < 1 || !aligned(steps_done, 4)) return SB_ERR_INVALID_ARG;
   const double lr1 = d->lr / (1.0 - sb::int_power(d->beta1, (uint32_t)d->step));
   const double vs = 1.0 / std::sqrt(1.0 - sb::int_power(d->beta2, (uint32_t)d->step));
   if (!std::isfinite((float)lr1) || !std::isfinite((float)vs)) return SB_ERR_INVALID_ARG;
-  sb::AdamwBatch b{};
+  if (info->blocks == 0) return SB_OK;
+  sb::AdamwStep b{};
+  b.plan = (const char*)plan;
   b.steps_done = steps_done;
   b.lr = d->lr; b.beta1 = d->beta1; b.beta2 = d->beta2;
   b.b1 = (float)d->beta1; b.c1 = (float)(1.0 - d->beta1);
   b.b2 = (float)d->beta2; b.c2 = (float)(1.0 - d->beta2);
   b.eps = (float)d->eps; b.rate = (float)lr1; b.vscale = (float)vs;
-  b.seed = d->seed; b.step = d->step;
-  blocks = 0;
-  for (int i = 0; i <= count; ++i) {
-    if (b.count == sb::kAdamwLaunch || i == count) {
-      if (b.count) {
-        if (bytes)
-          sb::adamw_kernel<true><<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(b);
-        else
-          sb::adamw_kernel<false><<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(b);
-        const sb_status s = sbh::launch_status();
-        if (s != SB_OK) return s;
-      }
-      b.count = 0;
-      blocks = 0;
-      if (i == count) break;
-    }
-    const sb_adamw_tensor& t = tensors[i];
-    if (t.n == 0) continue;
-    sb::AdamwTensor& o = b.t[b.count++];
-    o.w = t.w; o.copy = (sb::u16*)t.copy; o.g = t.g; o.m = t.m; o.v = t.v;
-    o.m_top = t.m_top; o.v_top = t.v_top; o.first = t.first; o.n = t.n;
-    o.scale = t.grad_scale;
-    o.keep = (float)(1.0 - d->lr * t.decay);
-    o.block0 = (int)blocks;
-    // Four elements at a time: 16, 8 and 4 bytes of fp32, bf16 and bytes.
-    o.vec = aligned(t.w, 16) && aligned(t.g, 16) && aligned(t.copy, 8) &&
-            aligned(t.m, bytes ? 4 : 16) && aligned(t.v, bytes ? 4 : 16);
-    blocks += (long)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
-  }
-  return SB_OK;
+  b.seed = d->seed; b.step = d->step; b.count = info->tensors;
+  const auto kernel = info->moments == 8 ? sb::adamw_kernel<true> : sb::adamw_kernel<false>;
+  kernel<<<(unsigned)info->blocks, 256, 0, sbh::stream_of(stream)>>>(b);
+  return sbh::launch_status();
 }
 
 extern "C" sb_status sb_adamw_advance(int32_t* steps_done, void* stream) {

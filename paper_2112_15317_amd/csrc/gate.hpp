@@ -38,20 +38,15 @@ __device__ __forceinline__ void gate_act(int act, float a, float& f, float& df) 
   }
 }
 
-// Four outputs of a row, columns n .. n + 3 (those below N): the biases are added to
-// both projections, which go to pre (this row's a; u is `plane` elements behind)
-// where it is kept, and act(a) u goes to y (this row's).
+// Four outputs of a row, columns n .. n + 3 (those below N): both projections go to
+// pre (this row's a; u is `plane` elements behind) where it is kept, act(a) u to y
+// (this row's).
 template <class E>
-__device__ __forceinline__ void gate_store(int act, f4 a, f4 u, int n, int N,
-                                           const float* __restrict__ bg,
-                                           const float* __restrict__ bu, float* pre, size_t plane,
-                                           E* y) {
+__device__ __forceinline__ void gate_store(int act, f4 a, f4 u, int n, int N, float* pre, size_t plane, E* y) {
   const bool whole = n + 4 <= N;
   f4 o;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    if (bg && n + e < N) a[e] += bg[n + e];
-    if (bu && n + e < N) u[e] += bu[n + e];
     float f, df;
     gate_act(act, a[e], f, df);
     o[e] = f * u[e];

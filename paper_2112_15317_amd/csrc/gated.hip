@@ -19,6 +19,7 @@
 #include "gemm_dual.hpp"
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 
 namespace sb {
@@ -117,6 +118,7 @@ __global__ __launch_bounds__(256) void gated_bias_sums(const float* __restrict__
   const int c = blockIdx.x * 64 + lane, q = blockIdx.y;
   float v = 0.f;
   if (c < n)
+#pragma unroll 8
     for (int r = w; r < chunks; r += 4) v += sums[((size_t)r * 2 + q) * np + c];
   part[w][lane] = v;
   __syncthreads();
@@ -126,89 +128,246 @@ __global__ __launch_bounds__(256) void gated_bias_sums(const float* __restrict__
   db[c] = accumulate ? db[c] + v : v;
 }
 
-// Rows of `cols` elements, `ld` apart, to rows of cp (a multiple of 8), zeros behind.
-// Block rows: two matrices.
+// Up to three matrices (block rows): rows of `cols` elements, `ld` apart, to rows of cp (a
+// multiple of 8), zeros behind.
+struct PackTasks {
+  const void* from[3];
+  void* to[3];
+  int rows[3], cols[3], ld[3], cp[3];
+  int count;
+};
 template <class E>
-__global__ __launch_bounds__(256) void gated_pack(const E* a, const E* b, size_t rows, int cols,
-                                                  int ld, int cp, E* to) {
-  const E* from = blockIdx.y ? b : a;
-  E* out = to + blockIdx.y * rows * cp;
-  const size_t quads = rows * (cp / 4);
+__global__ __launch_bounds__(256) void gated_pack(PackTasks t) {
+  const int q = blockIdx.y, cols = t.cols[q], cp = t.cp[q];
+  const E* from = (const E*)t.from[q];
+  E* out = (E*)t.to[q];
+  const size_t quads = (size_t)t.rows[q] * (cp / 4);
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (size_t)gridDim.x * 256) {
     const size_t r = i / (cp / 4);
     const int c = (int)(i - r * (cp / 4)) * 4;
     f4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? Elem<E>::load(from, r * ld + c + e) : 0.f;
+    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? Elem<E>::load(from, r * t.ld[q] + c + e) : 0.f;
     Elem<E>::store4(out + r * cp + c, v);
   }
 }
 
-// Sums of the splits' partials, four columns of a row a lane.  FWD: [split][2][M][N] to
-// y and pre; DW: to the two gradients; DX: [split][M][N] to dx.
-__device__ __forceinline__ f4 split_quad(const float* p, int splits, size_t stride, int n, int N) {
-  f4 v = f4{0.f, 0.f, 0.f, 0.f};
-  if (N % 4 == 0) return split_sum4(p, splits, stride, 0);
-  for (int s = 0; s < splits; ++s)
+// ---- few rows --------------------------------------------------------------
+// Up to kFewRows rows (a model that answers, the last rows of a batch): the weights are
+// read once and bound the time, and tiles of 128 rows, split over the reduction with
+// a second launch to join the splits, would be mostly zeros (one row of 1024 x 1024
+// bf16: 11.3 us; like this FEW_FWD_US).  Products on the vector ALU in fp32.
+constexpr int kFewRows = 8;
+
+// Eight (bf16) or four (fp32) consecutive elements as fp32, those from `left` on 0.
+template <class E> constexpr int kFewWidth = 16 / (int)sizeof(E);
+template <class E>
+__device__ __forceinline__ void few_load(const E* p, int left, bool vec, float (&v)[kFewWidth<E>]) {
+  constexpr int V = kFewWidth<E>;
+  if (vec && left >= V) {
+    const u32x4 t = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < N) v[e] += p[(size_t)s * stride + e];
-  return v;
+    for (int e = 0; e < V; ++e)
+      v[e] = sizeof(E) == 4 ? __uint_as_float(t[e])
+                            : __uint_as_float(e % 2 ? t[e / 2] & 0xffff0000u : t[e / 2] << 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = e < left ? Elem<E>::load(p, e) : 0.f;
+  }
 }
 
+// The value of the lane N further on in a row of 16.
+template <int N>
+__device__ __forceinline__ float row_turned(float v) {
+  const int i = __float_as_int(v);
+  return __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x120 + N, 0xf, 0xf, false));
+}
+
+// Forward of M rows: a block has the columns of L lanes (16 L bytes of a line of each
+// weight) and all of k, every (512 / L)th line a lane; the lanes' sums meet in LDS.
+template <class E, int M, int L>
+__global__ __launch_bounds__(512) void gated_few_fwd(int m, int n, int k, int ldx, int ldy, int act,
+                                                     const E* __restrict__ x,
+                                                     const E* __restrict__ wg,
+                                                     const E* __restrict__ wu,
+                                                     const float* __restrict__ bg,
+                                                     const float* __restrict__ bu, E* y, float* pre,
+                                                     int vec) {
+  constexpr int V = kFewWidth<E>, C = L * V;
+  __shared__ float part[8][2][M][C];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.x * C + lane % L * V, left = n - c;
+  float acc[2][M][V];
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int r = 0; r < M; ++r)
+#pragma unroll
+      for (int e = 0; e < V; ++e) acc[q][r][e] = 0.f;
+  if (left > 0) {
+#pragma unroll 4
+    for (int kk = threadIdx.x / L; kk < k; kk += 512 / L) {
+      float g[V], u[V];
+      few_load<E>(wg + (size_t)kk * n + c, left, vec, g);
+      few_load<E>(wu + (size_t)kk * n + c, left, vec, u);
+#pragma unroll
+      for (int r = 0; r < M; ++r) {
+        const float xv = r < m ? Elem<E>::load(x, (size_t)r * ldx + kk) : 0.f;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          acc[0][r][e] = fmaf(xv, g[e], acc[0][r][e]);
+          acc[1][r][e] = fmaf(xv, u[e], acc[1][r][e]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int r = 0; r < M; ++r)
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        float v = acc[q][r][e];
+        if constexpr (L <= 2) v += row_turned<2>(v);
+        if constexpr (L <= 4) v += row_turned<4>(v);
+        v += row_turned<8>(v);
+        v += __shfl_xor(v, 16, 64);
+        v += __shfl_xor(v, 32, 64);
+        if (lane < L) part[wave][q][r][lane * V + e] = v;
+      }
+  __syncthreads();
+  for (int i = threadIdx.x; i < M * C; i += 512) {
+    const int r = i / C, col = blockIdx.x * C + i % C;
+    if (r >= m || col >= n) continue;
+    float s[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float(*p)[2][M][C] = part;
+      s[q] = ((p[0][q][r][i % C] + p[1][q][r][i % C]) + (p[2][q][r][i % C] + p[3][q][r][i % C])) +
+             ((p[4][q][r][i % C] + p[5][q][r][i % C]) + (p[6][q][r][i % C] + p[7][q][r][i % C]));
+    }
+    const float a = s[0] + (bg ? bg[col] : 0.f), u = s[1] + (bu ? bu[col] : 0.f);
+    float f, df;
+    gate_act(act, a, f, df);
+    if (pre) {
+      pre[(size_t)r * n + col] = a;
+      pre[((size_t)m + r) * n + col] = u;
+    }
+    Elem<E>::store(y, (size_t)r * ldy + col, f * u);
+  }
+}
+
+// dx of M rows: a wave has four rows of both weights, its lanes the columns; d: da and
+// du (their first parts), rows of np.
+template <class E, int M>
+__global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k, int ldx,
+                                                    const E* __restrict__ da,
+                                                    const E* __restrict__ du,
+                                                    const E* __restrict__ wg,
+                                                    const E* __restrict__ wu, E* dx, int vec) {
+  constexpr int V = kFewWidth<E>, R = 4;
+  const int lane = threadIdx.x & 63;
+  const int k0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * R;
+  float acc[R][M];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int r = 0; r < M; ++r) acc[i][r] = 0.f;
+  for (int c = lane * V; c < n; c += 64 * V) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      float w[R][V], d[V];
+#pragma unroll
+      for (int i = 0; i < R; ++i)
+        few_load<E>((q ? wu : wg) + (size_t)min(k0 + i, k - 1) * n + c, n - c, vec, w[i]);
+#pragma unroll
+      for (int r = 0; r < M; ++r) {
+        few_load<E>((q ? du : da) + (size_t)min(r, m - 1) * np + c, np - c, true, d);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[i][r] = fmaf(w[i][e], d[e], acc[i][r]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int r = 0; r < M; ++r) {
+      float v = acc[i][r];
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o, 64);
+      if (lane == 0 && k0 + i < k && r < m) Elem<E>::store(dx, (size_t)r * ldx + k0 + i, v);
+    }
+}
+
+// Sums of the splits' partials (rows of g.pitch), four columns of a row a lane.  FWD:
+// [split][2][M] to y and pre; DW: to the two gradients; DX: [split][M] to dx.
 template <DualKind KIND, class E>
 __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
-  const int quads = cdiv(g.N, 4);
+  const int quads = g.pitch / 4;
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
   const int m = (int)(i / quads), n = (int)(i - (size_t)m * quads) * 4;
   if (m >= g.M) return;
-  const size_t plane = (size_t)g.M * g.N, at = (size_t)m * g.N + n;
+  const size_t plane = (size_t)g.M * g.pitch, at = (size_t)m * g.pitch + n;
   if constexpr (KIND == kDualDx) {
-    const f4 v = split_quad(g.part + at, g.splits, plane, n, g.N);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < g.N) Elem<E>::store((E*)g.c[0], (size_t)m * g.ldc + n + e, v[e]);
+    put_quad((E*)g.c[0] + (size_t)m * g.ldc, split_sum4(g.part, g.splits, plane, at), n, g.N);
   } else {
-    const f4 a = split_quad(g.part + at, g.splits, 2 * plane, n, g.N);
-    const f4 u = split_quad(g.part + plane + at, g.splits, 2 * plane, n, g.N);
+    f4 v[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) v[q] = split_sum4(g.part + q * plane, g.splits, 2 * plane, at);
     if constexpr (KIND == kDualFwd) {
-      gate_store<E>(act, a, u, n, g.N, g.bias[0], g.bias[1],
-                    g.pre ? g.pre + (size_t)m * g.N : nullptr, plane,
-                    (E*)g.c[0] + (size_t)m * g.ldc);
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (g.bias[q] && n + e < g.N) v[q][e] += g.bias[q][n + e];
+      gate_store<E>(act, v[0], v[1], n, g.N, g.pre ? g.pre + (size_t)m * g.N : nullptr,
+                    (size_t)g.M * g.N, (E*)g.c[0] + (size_t)m * g.ldc);
     } else {
 #pragma unroll
       for (int q = 0; q < 2; ++q) {
-        float* o = (float*)g.c[q] + (size_t)m * g.ldc + n;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = q ? u[e] : a[e];
-          if (n + e < g.N) o[e] = g.accumulate ? o[e] + x : x;
-        }
+        float* c = (float*)g.c[q] + (size_t)m * g.ldc;
+        if (g.accumulate) v[q] += get_quad(c, n, g.N);
+        put_quad(c, v[q], n, g.N);
       }
     }
   }
 }
 
-// Tile and split of a product: the least estimated time (us).
+// Tile and split of a product: the least estimated time (us) over 256-row tiles (bf16) and
+// 128-row ones and 1 to 64 ranges of the reduction.  A block costs its first stages and
+// its output, then a stage at a time, the more the fuller the chip is (power, L2); up to
+// three blocks of 128 rows share a CU, where one does not use it to the full; splits cost a
+// launch and their partials' traffic.  Fitted to 6400 timings of the three products of 700
+// shards in both types; the plan taken is 2.5 (bf16) or 1.2 % (fp32) slower than the best
+// one on average, half as slow again at most (61 rows of 640 by 128: 19 us for 13).
 struct DualPlan { int f, mt, nt, splits, stages; size_t ws_bytes; };
+struct DualCost { double block, alone, full, shared; };
+static const DualCost kDualCost[3] = {{9.0, 0.56, 0.95, 0.95},         // bf16, 256 rows
+                                      {4.8, 0.253, 0.338, 0.30},      // bf16, 128 rows
+                                      {6.2, 1.25, 1.33, 1.33}};       // fp32, 128 rows
 
 static DualPlan dual_plan(DualKind kind, bool b16, int M, int N, int K, int segs) {
   DualPlan best{};
   double best_t = 0;
   const int total = cdiv(K, 32) * segs;
+  const double tb_s = b16 ? 8.24 : 5.19;
+  const double bytes = (double)M * cdiv(N, 4) * 4 * (kind == kDualDx ? 4 : 8);
   for (int f = b16 ? 4 : 2; f >= 2; f -= 2) {
+    const DualCost& c = kDualCost[!b16 ? 2 : f == 4 ? 0 : 1];
+    const int share = b16 && f == 2 ? 3 : 1;
     const int mt = cdiv(M, 64 * f), nt = cdiv(N, kind == kDualDx ? 64 * f : 32 * f);
     const int64_t tiles = (int64_t)mt * nt;
-    for (int s = 1; s <= 16 && s <= total; ++s) {
+    for (int s = 1; s <= 64 && s <= total; ++s) {
       const int stages = cdiv(total, s);
       if (cdiv(total, stages) != s) continue;
       const int64_t blocks = tiles * s;
       const double per_cu = (double)((blocks + 255) / 256);
-      const double bytes = (double)M * N * (kind == kDualDx ? 4 : 8);
-      double t = s > 1 ? 4.0 + bytes * (2 * s + 1) / 5e6 : 0.0;
-      if (!b16) t += per_cu * (5.0 + stages * (blocks > 128 ? 1.8 : 1.4));
-      else if (f == 4) t += per_cu * (5.0 + stages * (blocks > 192 ? 1.04 : 0.75));
-      else t += 3.0 * (double)(((int64_t)per_cu + 2) / 3) + stages * (per_cu > 1 ? 0.33 * per_cu : 0.29);
+      const double one = c.alone + (c.full - c.alone) * std::min(1.0, (double)blocks / 256);
+      double t = s > 1 ? 3.2 + bytes * (2 * s + 1) / (tb_s * 1e6) : bytes / (tb_s * 1e6);
+      if (share == 1) t += per_cu * (c.block + stages * one);
+      else t += c.block * std::ceil(per_cu / share) + stages * (per_cu > 1 ? c.shared * per_cu : one);
       if (best_t == 0 || t < best_t) {
         best_t = t;
         best = DualPlan{f, mt, nt, s, stages, s > 1 ? (size_t)s * (size_t)bytes : 0};
@@ -245,6 +404,7 @@ template <DualKind KIND, class E>
 static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStream_t st) {
   g.mt = p.mt; g.nt = p.nt; g.splits = p.splits; g.stages = p.stages;
   g.part = part;
+  g.pitch = cdiv(g.N, 4) * 4;
   if (KIND != kDualFwd || p.splits > 1) {
     dual_launch_f<KIND, 0, E>(p.f, g, st);
   } else {
@@ -257,7 +417,7 @@ static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStr
     }
   }
   if (p.splits > 1) {
-    const size_t quads = (size_t)g.M * cdiv(g.N, 4);
+    const size_t quads = (size_t)g.M * (g.pitch / 4);
     gated_split_sum<KIND, E><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, act);
   }
 }
@@ -272,10 +432,11 @@ static bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // rows of the forward's reduction, x as lines of the weight gradient's, the weights.
 struct GatedPacks { bool x, lines, w; };
 static GatedPacks gated_packs(const sb_gated_desc* d, bool x_at16, bool w_at16) {
-  const bool b16 = d->dtype == SB_BF16;
+  const bool b16 = d->dtype == SB_BF16, few = d->m <= kFewRows;
   // (An odd bf16 k_in would end the last line inside the 4 bytes that ranges count in.)
   const bool lines = d->ldx % (b16 ? 8 : 4) != 0 || (b16 && d->k_in % 2 != 0) || !x_at16;
-  return GatedPacks{lines || d->k_in % 8 != 0, lines, d->n_shard % 8 != 0 || !w_at16};
+  return GatedPacks{!few && (lines || d->k_in % 8 != 0), lines,
+                    !few && (d->n_shard % 8 != 0 || !w_at16)};
 }
 
 static DualPlan gated_plan(const sb_gated_desc* d, DualKind kind) {
@@ -302,9 +463,11 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
   }
   if (pass == SB_FC_FWD ? k.x : k.lines) take(s.x, m * up8(d->k_in) * es);
   if (k.w) take(s.w, 2 * (size_t)d->k_in * np * es);
-  take(s.split, pass == SB_FC_FWD
-                    ? gated_plan(d, kDualFwd).ws_bytes
-                    : std::max(gated_plan(d, kDualDx).ws_bytes, gated_plan(d, kDualDw).ws_bytes));
+  const bool few = d->m <= kFewRows;
+  size_t split = 0;
+  if (pass == SB_FC_FWD) split = few ? 0 : gated_plan(d, kDualFwd).ws_bytes;
+  else split = std::max(few ? 0 : gated_plan(d, kDualDx).ws_bytes, gated_plan(d, kDualDw).ws_bytes);
+  take(s.split, split);
   s.bytes = at;
   return s;
 }
@@ -335,52 +498,87 @@ static bool spans_meet(const Span* a, int na, const Span* b, int nb) {
   return false;
 }
 
-// The weights as lines of whole eights, np apart.
+// The operands as the products take them: laid out anew (one launch) where `packs` says.
+struct GatedOperands {
+  const void *x, *w[2];
+  int ldx, width, ldw;                               // width: of x's rows
+};
 template <class E>
-static void gated_weights(const sb_gated_desc* d, const void* const* w, const void** to, bool pack,
-                          char* ws, const GatedSpace& sp, hipStream_t st) {
-  const int np = up8(d->n_shard);
-  to[0] = w[0];
-  to[1] = w[1];
-  if (!pack) return;
-  E* out = (E*)(ws + sp.w);
-  gated_pack<E><<<dim3(gated_blocks((size_t)d->k_in * np / 4), 2), 256, 0, st>>>(
-      (const E*)w[0], (const E*)w[1], d->k_in, d->n_shard, d->n_shard, np, out);
-  to[0] = out;
-  to[1] = out + (size_t)d->k_in * np;
+static GatedOperands gated_operands(const sb_gated_desc* d, const void* x, const void* const* w,
+                                    bool pack_x, bool pack_w, char* ws, const GatedSpace& sp,
+                                    hipStream_t st) {
+  GatedOperands o{x, {w[0], w[1]}, d->ldx, d->k_in, d->n_shard};
+  PackTasks t{};
+  size_t most = 0;
+  auto add = [&](const void* from, void* to, int rows, int cols, int ld, int cp) {
+    const int q = t.count++;
+    t.from[q] = from; t.to[q] = to;
+    t.rows[q] = rows; t.cols[q] = cols; t.ld[q] = ld; t.cp[q] = cp;
+    most = std::max(most, (size_t)rows * cp / 4);
+  };
+  if (pack_x) {
+    o.x = ws + sp.x;
+    o.ldx = o.width = up8(d->k_in);
+    add(x, ws + sp.x, d->m, d->k_in, d->ldx, o.width);
+  }
+  if (pack_w) {
+    o.ldw = up8(d->n_shard);
+    for (int q = 0; q < 2; ++q) {
+      E* to = (E*)(ws + sp.w) + q * (size_t)d->k_in * o.ldw;
+      o.w[q] = to;
+      add(w[q], to, d->k_in, d->n_shard, d->n_shard, o.ldw);
+    }
+  }
+  if (t.count) gated_pack<E><<<dim3(gated_blocks(most), t.count), 256, 0, st>>>(t);
+  return o;
 }
-// x, and its stride and width.
-template <class E>
-static const void* gated_x(const sb_gated_desc* d, const void* x, bool pack, int* ld, int* width,
-                           char* ws, const GatedSpace& sp, hipStream_t st) {
-  *ld = d->ldx;
-  *width = d->k_in;
-  if (!pack) return x;
-  *ld = *width = up8(d->k_in);
-  E* out = (E*)(ws + sp.x);
-  gated_pack<E><<<dim3(gated_blocks((size_t)d->m * *ld / 4), 1), 256, 0, st>>>(
-      (const E*)x, nullptr, d->m, d->k_in, d->ldx, *ld, out);
-  return out;
+
+template <class E, int M>
+static void few_fwd(const sb_gated_desc* d, const void* x, const void* const* w,
+                    const float* const* b, void* y, float* pre, int vec, hipStream_t st) {
+  // Whole 128-byte lines a block while that makes 128 blocks, else down to 32 bytes.
+  const int v = cdiv(d->n_shard, kFewWidth<E>);
+  auto go = [&](auto L) {
+    constexpr int l = decltype(L)::value;
+    gated_few_fwd<E, M, l><<<(unsigned)cdiv(v, l), 512, 0, st>>>(
+        d->m, d->n_shard, d->k_in, d->ldx, d->ldy, d->act, (const E*)x, (const E*)w[0],
+        (const E*)w[1], b[0], b[1], (E*)y, pre, vec);
+  };
+  if (v >= 8 * 128) go(std::integral_constant<int, 8>{});
+  else if (v >= 4 * 128) go(std::integral_constant<int, 4>{});
+  else go(std::integral_constant<int, 2>{});
 }
 
 template <class E>
 static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* const* w,
                           const float* const* b, void* y, float* pre, const GatedPacks& packs,
                           char* ws, const GatedSpace& sp, hipStream_t st) {
-  const int np = up8(d->n_shard);
+  if (d->m <= kFewRows) {
+    const int vec = d->n_shard % kFewWidth<E> == 0 && at16(w[0]) && at16(w[1]);
+    if (d->m == 1) few_fwd<E, 1>(d, x, w, b, y, pre, vec, st);
+    else if (d->m == 2) few_fwd<E, 2>(d, x, w, b, y, pre, vec, st);
+    else if (d->m <= 4) few_fwd<E, 4>(d, x, w, b, y, pre, vec, st);
+    else few_fwd<E, 8>(d, x, w, b, y, pre, vec, st);
+    return;
+  }
+  const GatedOperands o = gated_operands<E>(d, x, w, packs.x, packs.w, ws, sp, st);
   DualArgs g{};
-  const void* wp[2];
-  g.a[0] = gated_x<E>(d, x, packs.x, &g.lda, &g.K, ws, sp, st);
-  gated_weights<E>(d, w, wp, packs.w, ws, sp, st);
-  g.b[0][0] = wp[0]; g.b[1][0] = wp[1];
-  g.ldb = np;
-  g.M = d->m; g.N = d->n_shard; g.segs = 1;
+  g.a[0] = o.x; g.lda = o.ldx;
+  g.b[0][0] = o.w[0]; g.b[1][0] = o.w[1]; g.ldb = o.ldw;
+  g.M = d->m; g.N = d->n_shard; g.K = o.width; g.segs = 1;
   g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + g.K) * sizeof(E));
-  g.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
+  g.b_bytes = (uint32_t)((size_t)d->k_in * g.ldb * sizeof(E));
   g.c[0] = y; g.ldc = d->ldy;
   g.bias[0] = b[0]; g.bias[1] = b[1];
   g.pre = pre;
   dual_run<kDualFwd, E>(g, gated_plan(d, kDualFwd), d->act, (float*)(ws + sp.split), st);
+}
+
+template <class E, int M>
+static void few_dx(const sb_gated_desc* d, int np, const E* da, const E* du, const void* const* w,
+                   void* dx, int vec, hipStream_t st) {
+  gated_few_dx<E, M><<<(unsigned)cdiv(d->k_in, 16), 256, 0, st>>>(
+      d->m, d->n_shard, np, d->k_in, d->ldx, da, du, (const E*)w[0], (const E*)w[1], (E*)dx, vec);
 }
 
 template <class E>
@@ -401,15 +599,21 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   if (sums)
     gated_bias_sums<<<dim3(cdiv(d->n_shard, 64), 2), 256, 0, st>>>(sums, chunks, d->n_shard, np,
                                                                    db[0], db[1], accumulate);
-  if (dx) {
+  const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp, st);
+  if (dx && d->m <= kFewRows) {
+    const int wvec = d->n_shard % kFewWidth<E> == 0 && at16(w[0]) && at16(w[1]);
+    const E *da = parts, *du = parts + NP * plane;
+    if (d->m == 1) few_dx<E, 1>(d, np, da, du, w, dx, wvec, st);
+    else if (d->m == 2) few_dx<E, 2>(d, np, da, du, w, dx, wvec, st);
+    else if (d->m <= 4) few_dx<E, 4>(d, np, da, du, w, dx, wvec, st);
+    else few_dx<E, 8>(d, np, da, du, w, dx, wvec, st);
+  } else if (dx) {
     DualArgs g{};
-    const void* wp[2];
-    gated_weights<E>(d, w, wp, packs.w, ws, sp, st);
     for (int q = 0; q < 2; ++q) {
       g.a[q] = parts + NP * q * plane;
-      g.b[0][q] = wp[q];
+      g.b[0][q] = o.w[q];
     }
-    g.lda = g.ldb = np;
+    g.lda = np; g.ldb = o.ldw;                       // o.ldw is np: n_shard, or packed
     g.M = d->m; g.N = d->k_in; g.K = np; g.segs = 2;
     g.a_bytes = (uint32_t)(plane * sizeof(E));
     g.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
@@ -417,15 +621,13 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
     dual_run<kDualDx, E>(g, gated_plan(d, kDualDx), 0, split, st);
   }
   DualArgs g{};
-  int width;
-  const void* xp = gated_x<E>(d, x, packs.lines, &g.lda, &width, ws, sp, st);
   for (int p = 0; p < NP; ++p) {                     // the smallest parts first
-    g.a[p] = xp;
+    g.a[p] = o.x;
     for (int q = 0; q < 2; ++q) g.b[q][p] = parts + (NP * q + NP - 1 - p) * plane;
   }
-  g.ldb = np;
+  g.lda = o.ldx; g.ldb = np;
   g.M = d->k_in; g.N = d->n_shard; g.K = d->m; g.segs = NP;
-  g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + width) * sizeof(E));
+  g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + o.width) * sizeof(E));
   g.b_bytes = (uint32_t)(plane * sizeof(E));
   g.c[0] = dw[0]; g.c[1] = dw[1]; g.ldc = d->n_shard;
   g.accumulate = accumulate;

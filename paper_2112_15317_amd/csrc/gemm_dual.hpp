@@ -13,7 +13,7 @@
 // part of da and du), each in stages of 32.
 //
 // Three stages are in LDS: while stage t is multiplied, t + 2 is written from
-// registers and t + 3 loaded, and t + 1 can already be read, so that the operands
+// registers and t + 4 loaded, and t + 1 can already be read, so that the operands
 // of the next 16 k are in registers before the current ones are used up.  An
 // operand that is contiguous along k (x of FWD, both of DX) lies in LDS as rows
 // of four 16-byte pieces and is read as such; one that is contiguous along its
@@ -56,7 +56,8 @@ struct DualArgs {
   int lda, ldb;
   int M, N, K, segs;               // K: of a segment
   int mt, nt, splits, stages;      // stages per split
-  float* part;                     // splits > 1: [split][2][M][N] (DX [split][M][N])
+  int pitch;                       // of partials' rows: N rounded up to 4
+  float* part;                     // splits > 1: [split][2][M][N up to 4] (DX [split][M][..])
   void* c[2]; int ldc;             // DX: dx; DW: fp32 gradients; FWD: y in c[0]
   const float* bias[2];            // FWD
   float* pre;                      // FWD, may be null: [2][M][N]
@@ -229,24 +230,30 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
   int seg = t0 / per_seg, k0 = (t0 - seg * per_seg) * 32;
   DualPiece<E> va[2][F], vb[2][F];
   uint32_t lost = 0;
-  // The operands of its segment; its first k.  Stages past the last segment, which
-  // nothing multiplies, load the last one again.
+  // The operands of its segment; its first k.  Stages past the block's last one, which
+  // nothing multiplies, are empty ranges: their loads return 0 and read nothing.
   rsrc_t ra, rb, rc;
+  int left = nk;
   auto segment = [&]() {
     const int s = min(seg, g.segs - 1);
-    ra = make_rsrc(g.a[s], g.a_bytes);
-    rb = make_rsrc(g.b[0][s], g.b_bytes);
-    rc = make_rsrc(g.b[1][s], g.b_bytes);
+    const uint32_t bytes_a = left > 0 ? g.a_bytes : 0, bytes_b = left > 0 ? g.b_bytes : 0;
+    ra = make_rsrc(g.a[s], bytes_a);
+    rb = make_rsrc(g.b[0][s], bytes_b);
+    rc = make_rsrc(g.b[1][s], bytes_b);
   };
   segment();
   int ka;
   auto next = [&]() {
     ka = k0;
     k0 += 32;
+    --left;
     if (k0 >= g.K) {
       k0 = 0;
       ++seg;
     }
+  };
+  auto turn = [&]() {
+    if (k0 == 0 || left == 0) segment();
   };
   auto load_a = [&](DualPiece<E> (&x)[F], int i) { sa.load_one(ra, ka, g.K, x, i); };
   auto load_b = [&](DualPiece<E> (&x)[F], int i) {
@@ -259,7 +266,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
       load_a(xa, i);
       load_b(xb, i);
     }
-    if (k0 == 0) segment();
+    turn();
   };
   auto store = [&](u16* S, const DualPiece<E> (&xa)[F], const DualPiece<E> (&xb)[F]) {
 #pragma unroll
@@ -386,22 +393,28 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
   auto stage = [&](auto R, u16* b0, u16* b1, u16* b2) {
     next();
     step(Zero{}, Zero{}, R, b0, 1, b2);
-    if (NP == 1 && k0 == 0) segment();
+    if (NP == 1) turn();
     step(One{}, One{}, R, b1, 0, b2);
-    if (NP == 3 && k0 == 0) segment();
+    if (NP == 3) turn();
     __syncthreads();
   };
   u16 *b0 = lds, *b1 = lds + T::STAGE, *b2 = lds + 2 * T::STAGE;
   int t = 0;
-  for (; t + 2 <= nk; t += 2) {
-    stage(Zero{}, b0, b1, b2);
-    stage(One{}, b1, b2, b0);
-    u16* x = b0;
-    b0 = b2;
-    b2 = b1;
-    b1 = x;
+  auto turns = [&](auto R) {                         // the stage whose set is R, if there is one
+    if (t < nk) {
+      stage(R, b0, b1, b2);
+      u16* x = b0;
+      b0 = b1;
+      b1 = b2;
+      b2 = x;
+      ++t;
+    }
+  };
+  while (t + 2 <= nk) {
+    turns(Zero{});
+    turns(One{});
   }
-  if (t < nk) stage(Zero{}, b0, b1, b2);
+  turns(Zero{});
 
   if constexpr (NP == 3) {
     // A block with values that the parts do not carry, or sums that are not finite,
@@ -480,6 +493,16 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
         }
     }
   };
+  f4 bias[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};   // of a lane's columns
+  if constexpr (KIND == kDualFwd) {
+    const int o = lane % (CW / 4) * 4;
+    const int n = n0 + (F == 4 ? wn * 32 + o / 32 * 64 + o % 32 : wn * 32 + o);
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (g.bias[q] && n + e < g.N) bias[q][e] = g.bias[q][n + e];
+  }
   // One copy of the code that stores (the activations' is long); i is uniform.
 #pragma unroll 1
   for (int i = 0; i < F; ++i) {
@@ -498,7 +521,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
         const int n = n0 + wn * T::RC + o;
         const f4 v = *reinterpret_cast<const f4*>(W + row * P + o);
         if (m < g.M && n < g.N) {
-          if (g.splits > 1) put_quad(g.part + ((size_t)split * g.M + m) * g.N, v, n, g.N);
+          if (g.splits > 1) put_quad(g.part + ((size_t)split * g.M + m) * g.pitch, v, n, g.pitch);
           else put_quad((E*)g.c[0] + (size_t)m * g.ldc, v, n, g.N);
         }
       } else {
@@ -510,13 +533,13 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
         for (int q = 0; q < 2; ++q) v[q] = *reinterpret_cast<const f4*>(W + row * P + q * CW + at);
         if (m < g.M && n < g.N) {
           if (KIND == kDualFwd && g.splits == 1) {
-            gate_store<E>(ACT, v[0], v[1], n, g.N, g.bias[0], g.bias[1],
+            gate_store<E>(ACT, v[0] + bias[0], v[1] + bias[1], n, g.N,
                           g.pre ? g.pre + (size_t)m * g.N : nullptr, (size_t)g.M * g.N,
                           (E*)g.c[0] + (size_t)m * g.ldc);
           } else if (g.splits > 1) {
 #pragma unroll
             for (int q = 0; q < 2; ++q)
-              put_quad(g.part + (((size_t)split * 2 + q) * g.M + m) * g.N, v[q], n, g.N);
+              put_quad(g.part + (((size_t)split * 2 + q) * g.M + m) * g.pitch, v[q], n, g.pitch);
           } else {
 #pragma unroll
             for (int q = 0; q < 2; ++q) {

@@ -50,8 +50,11 @@ class sb_fc_desc(ctypes.Structure):
 
 class sb_adamw_desc(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
-                ("eps", ctypes.c_double), ("step", _i), ("moments", _i),
-                ("seed", ctypes.c_uint32)]
+                ("eps", ctypes.c_double), ("step", _i), ("seed", ctypes.c_uint32)]
+
+
+class sb_adamw_plan(ctypes.Structure):
+    _fields_ = [("tensors", _i), ("moments", _i), ("blocks", _i)]
 
 
 class sb_adamw_tensor(ctypes.Structure):
@@ -115,8 +118,11 @@ SIGNATURES = {
     "sb_log_softmax_nll": (_i, [_i, _i, _i, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
     "sb_sgd_update": (_i, [_i, ctypes.POINTER(_vp), ctypes.POINTER(_vp), ctypes.POINTER(_sz),
                            ctypes.POINTER(ctypes.c_float), ctypes.c_float, _vp]),
-    "sb_adamw_update": (_i, [ctypes.POINTER(sb_adamw_desc), _i, ctypes.POINTER(sb_adamw_tensor),
-                             _vp, _vp]),
+    "sb_adamw_plan_bytes": (_sz, [_i]),
+    "sb_adamw_make_plan": (_i, [_i, _i, ctypes.POINTER(sb_adamw_tensor), _vp, _sz,
+                                ctypes.POINTER(sb_adamw_plan), _vp]),
+    "sb_adamw_update": (_i, [ctypes.POINTER(sb_adamw_desc), ctypes.POINTER(sb_adamw_plan), _vp, _vp,
+                             _vp]),
     "sb_adamw_advance": (_i, [_vp, _vp]),
     "sb_adamw_unpack": (_i, [_sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
 }
@@ -476,8 +482,9 @@ def sb_sgd_update(slist, lr, stream=None):
 
 # ------------------------------------------------------------------- AdamW --
 class AdamwList:
-    """Marshalled arguments of sb_adamw_update for a fixed list of tensors:
-    built once, passed to every call (the tensors must stay alive).
+    """The plan of sb_adamw_update for a fixed list of tensors, in device memory
+    (sb_adamw_make_plan): built once, passed to every call (the tensors must
+    stay alive).  ``stream``: the stream that writes it.
 
     items: dicts of a parameter ``w``, its gradient ``g`` (fp32) and moments
     ``m`` and ``v`` (fp32; or uint8, with their references ``m_top`` and
@@ -487,7 +494,7 @@ class AdamwList:
     among the random numbers; by default the tensors follow one another).
     ``adamw_moments`` makes zero moments."""
 
-    def __init__(self, items):
+    def __init__(self, items, stream=None):
         import torch
         n = len(items)
         if not 1 <= n <= SB_ADAMW_MAX_TENSORS:
@@ -518,6 +525,12 @@ class AdamwList:
             t.n = size
             t.grad_scale, t.decay = it.get("scale", 1.0), it.get("decay", 0.0)
             first = t.first + size
+        need = load().sb_adamw_plan_bytes(n)
+        self.plan = torch.empty((need,), dtype=torch.uint8, device=items[0]["w"].device)
+        self.info = sb_adamw_plan()
+        _check("sb_adamw_make_plan", load().sb_adamw_make_plan(
+            self.moments, n, self.tensors, _ptr(self.plan), need, ctypes.byref(self.info),
+            _stream(stream)))
 
 
 def adamw_moments(w, moments=32):
@@ -538,10 +551,10 @@ def sb_adamw_update(alist, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0,
                     stream=None):
     """step: the number of this update (from 1), or, with the int32 device
     counter steps_done, what is added to its value."""
-    d = sb_adamw_desc(float(lr), float(beta1), float(beta2), float(eps), int(step), alist.moments,
-                      int(seed) & 0xffffffff)
+    d = sb_adamw_desc(lr, beta1, beta2, eps, step, seed & 0xffffffff)
     _check("sb_adamw_update", load().sb_adamw_update(
-        ctypes.byref(d), alist.count, alist.tensors, _counter(steps_done), _stream(stream)))
+        ctypes.byref(d), ctypes.byref(alist.info), alist.plan.data_ptr(), _counter(steps_done),
+        _stream(stream)))
 
 
 def _counter(t):

@@ -9,9 +9,10 @@ from paper_2112_15317_amd import sb
 P = 0x10000000
 
 
-def _call(desc=None, tensors=None, count=None, counter=None):
-    d = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, moments=32, seed=0)
-    d.update(desc or {})
+PLAN = P + 0x70000000
+
+
+def _plan(tensors=None, moments=32, count=None, plan=PLAN, short=0, info=True):
     tensors = [{}] if tensors is None else tensors
     ts = (sb.sb_adamw_tensor * max(1, len(tensors)))()
     for i, (t, over) in enumerate(zip(ts, tensors)):
@@ -21,19 +22,36 @@ def _call(desc=None, tensors=None, count=None, counter=None):
         v.update(over)
         for k, x in v.items():
             setattr(t, k, x)
-    return sb.load().sb_adamw_update(
-        ctypes.byref(sb.sb_adamw_desc(**d)), len(tensors) if count is None else count, ts, counter, None)
+    count = len(tensors) if count is None else count
+    need = max(0, sb.load().sb_adamw_plan_bytes(len(tensors)) - short)
+    out = sb.sb_adamw_plan()
+    return sb.load().sb_adamw_make_plan(moments, count, ts, plan, need,
+                                        ctypes.byref(out) if info else None, None)
+
+
+def _update(plan=PLAN, info=(1, 32, 1), counter=None, **over):
+    d = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0)
+    d.update(over)
+    return sb.load().sb_adamw_update(ctypes.byref(sb.sb_adamw_desc(**d)),
+                                     ctypes.byref(sb.sb_adamw_plan(*info)), plan, counter, None)
 
 
 BAD = sb.SB_ERR_INVALID_ARG
 
 
-@pytest.mark.parametrize("desc", [
-    dict(step=0), dict(step=-3), dict(moments=16), dict(beta1=1.0), dict(beta1=-0.1),
-    dict(beta2=1.0), dict(beta2=float("nan")), dict(eps=-1e-8), dict(eps=float("inf")),
-    dict(lr=float("nan")), dict(lr=1e300), dict(lr=float("inf"))])
-def test_bad_numbers_are_refused(desc):
-    assert _call(desc) == BAD
+@pytest.mark.parametrize("over", [
+    dict(step=0), dict(step=-3), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
+    dict(beta2=float("nan")), dict(eps=-1e-8), dict(eps=float("inf")), dict(lr=float("nan")),
+    dict(lr=1e300), dict(lr=float("inf")), dict(counter=P + 2), dict(plan=None), dict(plan=PLAN + 8),
+    dict(info=(1, 16, 1)), dict(info=(-1, 32, 1)), dict(info=(513, 32, 600)), dict(info=(2, 32, 1)),
+    dict(info=(0, 32, 1)), dict(info=(1, 8, -1))])
+def test_bad_updates_are_refused(over):
+    assert _update(**over) == BAD
+
+
+def test_an_empty_plan_has_nothing_to_do():
+    assert _update(info=(0, 32, 0)) == sb.SB_OK
+    assert sb.load().sb_adamw_update(None, None, None, None, None) == BAD
 
 
 @pytest.mark.parametrize("over", [
@@ -41,40 +59,40 @@ def test_bad_numbers_are_refused(desc):
     dict(m=P + 0x200001), dict(copy=P + 0x600001), dict(n=1 << 40), dict(grad_scale=float("nan")),
     dict(decay=float("inf"))])
 def test_bad_tensors_are_refused(over):
-    assert _call(tensors=[over]) == BAD
-    assert _call(tensors=[dict(n=0), over]) == BAD
+    assert _plan([over]) == BAD
+    assert _plan([dict(n=0), over]) == BAD
 
 
 @pytest.mark.parametrize("over", [dict(m_top=None), dict(v_top=None), dict(m_top=P + 0x400001)])
 def test_references_are_checked_with_bytes(over):
-    assert _call(dict(moments=8), [over]) == BAD
+    assert _plan([over], 8) == BAD
 
 
 @pytest.mark.parametrize("over", [
     dict(g=P), dict(g=P + 3996), dict(m=P + 3996), dict(v=P + 0x200000), dict(copy=P + 2000),
-    dict(copy=P + 0x100000), dict(m_top=P + 0x500000), dict(v_top=P + 0x300002), dict(m=P + 0x100004)])
+    dict(copy=P + 0x100000), dict(m_top=P + 0x500000), dict(v_top=P + 0x300002), dict(m=P + 0x100004),
+    dict(w=PLAN), dict(g=PLAN + 4)])
 def test_overlaps_are_refused(over):
-    assert _call(dict(moments=8 if "m_top" in over or "v_top" in over else 32), [over]) == BAD
+    assert _plan([over], 8 if "m_top" in over or "v_top" in over else 32) == BAD
 
 
-def test_overlaps_between_tensors_and_with_the_counter():
+def test_overlaps_between_tensors():
     second = P + 0x1000000
-    assert _call(tensors=[{}, dict(w=P + 400)]) == BAD
-    assert _call(tensors=[{}, dict(g=P + 400)]) == BAD
-    assert _call(tensors=[dict(copy=second + 0x200000), {}]) == BAD
-    assert _call(counter=P + 8) == BAD
-    assert _call(counter=P + 0x700002) == BAD
+    assert _plan([{}, dict(w=P + 400)]) == BAD
+    assert _plan([{}, dict(g=P + 400)]) == BAD
+    assert _plan([dict(copy=second + 0x200000), {}]) == BAD
 
 
-def test_counts_and_null_arrays():
+def test_counts_null_arrays_and_short_plans():
     lib = sb.load()
-    assert _call(count=0) == BAD and _call(count=-1) == BAD
-    assert _call(count=sb.SB_ADAMW_MAX_TENSORS + 1) == BAD
-    ts = (sb.sb_adamw_tensor * 1)()
-    d = sb.sb_adamw_desc(1e-3, 0.9, 0.999, 1e-8, 1, 32, 0)
-    assert lib.sb_adamw_update(None, 1, ts, None, None) == BAD
-    assert lib.sb_adamw_update(ctypes.byref(d), 1, None, None, None) == BAD
-    assert lib.sb_adamw_update(ctypes.byref(d), 1, ts, None, None) == sb.SB_OK    # n = 0: nothing to do
+    top = sb.SB_ADAMW_MAX_TENSORS
+    assert _plan(count=0) == BAD and _plan(count=-1) == BAD and _plan(count=top + 1) == BAD
+    assert _plan(moments=16) == BAD and _plan(plan=None) == BAD and _plan(plan=PLAN + 8) == BAD
+    assert _plan(info=False) == BAD
+    assert lib.sb_adamw_make_plan(32, 1, None, PLAN, 1 << 20, ctypes.byref(sb.sb_adamw_plan()), None) == BAD
+    assert _plan(short=1) == sb.SB_ERR_WORKSPACE
+    assert lib.sb_adamw_plan_bytes(0) == 0 and lib.sb_adamw_plan_bytes(top + 1) == 0
+    assert _plan([dict(n=0)]) == sb.SB_OK                  # no tensor with elements: nothing to write
     assert lib.sb_adamw_advance(None, None) == BAD and lib.sb_adamw_advance(P + 2, None) == BAD
 
 

@@ -17,6 +17,7 @@ CODE = {"f32": sb.SB_F32, "bf16": sb.SB_BF16}
 ACT = {name: i for i, name in enumerate(G.ACTS)}
 # (m, k, n, extra row stride of x, of y, elements the tensors start past an allocation)
 SHAPES = [(1, 1, 1, 0, 0, 0), (1, 64, 64, 0, 0, 0), (3, 5, 7, 0, 0, 0), (2, 200, 33, 3, 1, 1),
+          (8, 130, 264, 6, 0, 0), (7, 513, 70, 0, 2, 1), (9, 100, 72, 4, 0, 0), (4, 1024, 1000, 0, 0, 0),
           (64, 64, 64, 0, 0, 0), (127, 66, 130, 0, 0, 0), (200, 300, 129, 4, 7, 1),
           (65, 1030, 258, 2, 2, 2), (256, 256, 256, 0, 0, 0), (333, 512, 320, 64, 64, 0),
           (129, 2048, 96, 8, 0, 8), (520, 72, 640, 0, 8, 0), (1100, 160, 200, 0, 0, 0),
