@@ -574,7 +574,7 @@ typedef struct {
     float grad_scale;      /* 1/K for FC shards                            */
     float decay;
 } sb_adamw_tensor;
-typedef struct { int tensors, moments, blocks; } sb_adamw_plan;
+typedef struct { int tensors, moments, groups, blocks; } sb_adamw_plan;
 
 /* The tensors of an update are written into a plan in device memory once, so that
  * every update is one launch however many there are.  plan: device memory of the

@@ -40,8 +40,10 @@
 
 namespace sb {
 
-constexpr int kAdamwGroups = 4;              // groups of 4 elements per lane
-constexpr int kAdamwBlock = 1024 * kAdamwGroups;
+constexpr int kAdamwGroups = 4;              // groups of 4 elements per lane, or one:
+// a lane's groups are worked off one after the other, so where there are too few
+// elements for a block on every CU, one each (20000 elements in bytes 9.1 -> SMALL_US us).
+constexpr size_t kAdamwSmall = 2048 * 1024;
 constexpr int kAdamwChunk = 40;              // tensors a launch writes into a plan
 
 struct AdamwTensor {
@@ -81,6 +83,7 @@ struct AdamwStep {
   float b1, c1, b2, c2, eps, rate, vscale;   // rate, vscale: of step, without a counter
   uint32_t seed;
   int step, count;
+  int fast;                                  // eps >= 2^-40: see the kernel's root
 };
 
 __host__ __device__ inline uint32_t mix32(uint32_t x) {
@@ -109,7 +112,7 @@ __device__ __forceinline__ float rank_value(int rank) {
 // the random ones carry.  Finite values stay finite.
 __device__ __forceinline__ int rank_of(uint32_t bits, uint32_t noise) {
   const int r = min((int)((bits + noise * 16 + 8) >> 20), 0x7f7);
-  return bits < 0x7f800000u ? r : (bits > 0x7f800000u ? 0x7fc : 0x7f8);
+  return bits < 0x7f800000u ? r : min((int)(bits >> 20), 0x7fc);   // infinity 7f8, quiet NaNs 7fc
 }
 
 // The largest of both halves over the wave.
@@ -147,11 +150,10 @@ __device__ __forceinline__ void adamw_store4(T* p, size_t i, size_t n, bool whol
 typedef uint8_t b4 __attribute__((ext_vector_type(4)));
 typedef u16 h4 __attribute__((ext_vector_type(4)));
 
-template <bool BYTES>
+template <bool BYTES, int U>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
   typedef typename std::conditional<BYTES, uint8_t, float>::type S;
   typedef typename std::conditional<BYTES, b4, f4>::type S4;
-  constexpr int U = kAdamwGroups;
   const int blk = blockIdx.x;
   int ti = -1;                               // the last tensor whose blocks start by blk
   const int* block0 = (const int*)b.plan;
@@ -160,9 +162,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
     ti += __popcll(__ballot(at < b.count && block0[min(at, b.count - 1)] <= blk));
   }
   ti = __builtin_amdgcn_readfirstlane(ti);
-  const AdamwTensor t = ((const AdamwTensor*)(b.plan + plan_tensors(b.count)))[ti];
+  // (Constant memory to the compiler: the tensor's entry then loads into scalars.)
+  typedef const __attribute__((address_space(4))) AdamwTensor* Entry;
+  const auto& t = ((Entry)(uintptr_t)(b.plan + plan_tensors(b.count)))[ti];
   const size_t n = t.n;
-  const size_t base = (size_t)(blk - t.block0) * kAdamwBlock + threadIdx.x * 4;
+  const size_t base = (size_t)(blk - t.block0) * (1024 * U) + threadIdx.x * 4;
   const S *m = (const S*)t.m, *v = (const S*)t.v;
   f4 w4[U], g4[U];
   S4 m4[U], v4[U];
@@ -209,9 +213,15 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
         ov = v4[u][e];
       }
       const float g = g4[u][e] * t.scale;
+      // The hardware's root and reciprocal (an ulp each, a quarter of the instructions)
+      // read a subnormal v as 0: its root, below 2^-63, is nothing beside an eps of 2^-40.
       nm[e] = om * b.b1 + g * b.c1;
       nv[e] = ov * b.b2 + (g * g) * b.c2;
-      nw[e] = w4[u][e] * keep - rate * (nm[e] / (sqrtf(nv[e]) * vscale + b.eps));
+      if (b.fast)
+        nw[e] = w4[u][e] * keep -
+                rate * (nm[e] * __builtin_amdgcn_rcpf(__builtin_amdgcn_sqrtf(nv[e]) * vscale + b.eps));
+      else
+        nw[e] = w4[u][e] * keep - rate * (nm[e] / (sqrtf(nv[e]) * vscale + b.eps));
     }
     adamw_store4<float, f4>(t.w, i, n, whole, nw);
     if (t.copy) {
@@ -224,13 +234,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
       adamw_store4<float, f4>((float*)t.m, i, n, whole, nm);
       adamw_store4<float, f4>((float*)t.v, i, n, whole, nv);
     } else {
-      const uint64_t at = t.first + i;
+      const uint64_t at = t.first + i;       // its lower half may carry among the four
+      const uint32_t lo = (uint32_t)at, hi = (uint32_t)(at >> 32);
+      const uint32_t key0 = key ^ hi * 0x9e3779b9u, key1 = key ^ (hi + 1) * 0x9e3779b9u;
       int mr[4], vr[4];
       uint32_t top = 0;                      // m's largest rank above v's
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint64_t id = at + e;
-        const uint32_t h = mix32((uint32_t)id ^ key ^ (uint32_t)(id >> 32) * 0x9e3779b9u);
+        const uint32_t h = mix32((lo + e) ^ (lo + e < lo ? key1 : key0));
         mr[e] = rank_of(__float_as_uint(nm[e]) & 0x7fffffffu, h & 0xffffu);
         vr[e] = rank_of(__float_as_uint(nv[e]) & 0x7fffffffu, h >> 16);
         if (i + e >= n) mr[e] = vr[e] = 0;
@@ -259,14 +270,14 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
 __global__ void adamw_advance_kernel(int32_t* steps_done) { *steps_done += 1; }
 
 // Four bytes of both moments a lane; a wave has one block's 256.
+template <int U>
 __global__ __launch_bounds__(256) void adamw_unpack_kernel(size_t n, const uint8_t* __restrict__ m,
                                                            const int16_t* __restrict__ m_top,
                                                            const uint8_t* __restrict__ v,
                                                            const int16_t* __restrict__ v_top,
                                                            float* __restrict__ m_out,
                                                            float* __restrict__ v_out, int vec) {
-  constexpr int U = kAdamwGroups;
-  const size_t base = (size_t)blockIdx.x * kAdamwBlock + threadIdx.x * 4;
+  const size_t base = (size_t)blockIdx.x * (1024 * U) + threadIdx.x * 4;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const size_t i = base + u * 1024;
@@ -339,7 +350,7 @@ extern "C" sb_status sb_adamw_make_plan(int moments, int count, const sb_adamw_t
     r[ranges++] = Range{(uintptr_t)p, (uintptr_t)p + size, out};
   };
   add(plan, need, true);
-  int64_t blocks = 0;
+  size_t total = 0;
   int used = 0;
   for (int i = 0; i < count; ++i) {
     const sb_adamw_tensor& t = tensors[i];
@@ -362,14 +373,16 @@ extern "C" sb_status sb_adamw_make_plan(int moments, int count, const sb_adamw_t
     add(t.v, t.n * (bytes ? 1 : 4), true);
     if (t.copy) add(t.copy, t.n * 2, true);
     ++used;
-    blocks += (int64_t)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
-    if (blocks >= (1ll << 31)) return SB_ERR_UNSUPPORTED;
+    total += t.n;
+    if (total >= (1ull << 42)) return SB_ERR_UNSUPPORTED;  // blocks are counted in 31 bits
   }
   if (outputs_meet(r, ranges)) return SB_ERR_INVALID_ARG;
   if (plan_bytes < need) return SB_ERR_WORKSPACE;
   sb::AdamwChunk c{};
   c.total = used;
-  blocks = 0;
+  const int groups = total < sb::kAdamwSmall ? 1 : sb::kAdamwGroups;
+  const size_t block = 1024 * (size_t)groups;
+  int64_t blocks = 0;
   for (int i = 0; i <= count; ++i) {
     if (c.count == sb::kAdamwChunk || (i == count && c.count)) {
       sb::adamw_plan_kernel<<<1, 64, 0, sbh::stream_of(stream)>>>(c, (char*)plan);
@@ -389,9 +402,9 @@ extern "C" sb_status sb_adamw_make_plan(int moments, int count, const sb_adamw_t
     // Four elements at a time: 16, 8 and 4 bytes of fp32, bf16 and bytes.
     o.vec = aligned(t.w, 16) && aligned(t.g, 16) && aligned(t.copy, 8) &&
             aligned(t.m, bytes ? 4 : 16) && aligned(t.v, bytes ? 4 : 16);
-    blocks += (int64_t)((t.n + sb::kAdamwBlock - 1) / sb::kAdamwBlock);
+    blocks += (int64_t)((t.n + block - 1) / block);
   }
-  *info = sb_adamw_plan{used, moments, (int)blocks};
+  *info = sb_adamw_plan{used, moments, groups, (int)blocks};
   return SB_OK;
 }
 
@@ -400,7 +413,8 @@ extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, const sb_adamw_plan
   if (!d || !info || !plan || !aligned(plan, 16)) return SB_ERR_INVALID_ARG;
   if (info->tensors < 0 || info->tensors > SB_ADAMW_MAX_TENSORS ||
       info->blocks < info->tensors || (info->tensors == 0 && info->blocks != 0) ||
-      (info->moments != 8 && info->moments != 32))
+      (info->moments != 8 && info->moments != 32) ||
+      (info->groups != 1 && info->groups != sb::kAdamwGroups))
     return SB_ERR_INVALID_ARG;
   if (!std::isfinite(d->lr) || !std::isfinite(d->eps) || !(d->eps >= 0.0)) return SB_ERR_INVALID_ARG;
   if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0))
@@ -418,7 +432,11 @@ extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, const sb_adamw_plan
   b.b2 = (float)d->beta2; b.c2 = (float)(1.0 - d->beta2);
   b.eps = (float)d->eps; b.rate = (float)lr1; b.vscale = (float)vs;
   b.seed = d->seed; b.step = d->step; b.count = info->tensors;
-  const auto kernel = info->moments == 8 ? sb::adamw_kernel<true> : sb::adamw_kernel<false>;
+  b.fast = b.eps >= 0x1p-40f;
+  constexpr int U = sb::kAdamwGroups;
+  const auto kernel = info->moments == 8
+                          ? (info->groups == 1 ? sb::adamw_kernel<true, 1> : sb::adamw_kernel<true, U>)
+                          : (info->groups == 1 ? sb::adamw_kernel<false, 1> : sb::adamw_kernel<false, U>);
   kernel<<<(unsigned)info->blocks, 256, 0, sbh::stream_of(stream)>>>(b);
   return sbh::launch_status();
 }
@@ -446,11 +464,13 @@ extern "C" sb_status sb_adamw_unpack(size_t n, const uint8_t* m, const int16_t* 
     if (sbh::overlaps(m_out, n * 4, in[i], inb[i]) || sbh::overlaps(v_out, n * 4, in[i], inb[i]))
       return SB_ERR_INVALID_ARG;
   if (sbh::overlaps(m_out, n * 4, v_out, n * 4)) return SB_ERR_INVALID_ARG;
-  const size_t blocks = (n + sb::kAdamwBlock - 1) / sb::kAdamwBlock;
+  const int groups = n < sb::kAdamwSmall ? 1 : sb::kAdamwGroups;
+  const size_t blocks = (n + 1024 * groups - 1) / (1024 * groups);
   if (blocks >= (1ull << 31)) return SB_ERR_UNSUPPORTED;
   const int vec = aligned(m_out, 16) && aligned(v_out, 16) && (!m_out || aligned(m, 4)) &&
                   (!v_out || aligned(v, 4));
-  sb::adamw_unpack_kernel<<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(
-      n, m, m_top, v, v_top, m_out, v_out, vec);
+  const auto kernel = groups == 1 ? sb::adamw_unpack_kernel<1> : sb::adamw_unpack_kernel<sb::kAdamwGroups>;
+  kernel<<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(n, m, m_top, v, v_top, m_out, v_out,
+                                                               vec);
   return sbh::launch_status();
 }

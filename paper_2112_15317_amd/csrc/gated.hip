@@ -302,35 +302,49 @@ __global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k,
 }
 
 // Sums of the splits' partials (rows of g.pitch), four columns of a row a lane.  FWD:
-// [split][2][M] to y and pre; DW: to the two gradients; DX: [split][M] to dx.
-template <DualKind KIND, class E>
+// [split][2][M] to y and pre; DW: to the two gradients; DX: [split][M] to dx.  W waves
+// share the splits of a quad (many splits are of small outputs, which are few lanes).
+template <DualKind KIND, class E, int W>
 __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
-  const int quads = g.pitch / 4;
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const int m = (int)(i / quads), n = (int)(i - (size_t)m * quads) * 4;
-  if (m >= g.M) return;
+  constexpr int Q = KIND == kDualDx ? 1 : 2, LANES = 256 / W;
+  const int quads = g.pitch / 4, w = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const size_t i = (size_t)blockIdx.x * LANES + lane;
+  const int m = (int)min(i / quads, (size_t)g.M - 1), n = (int)(i % quads) * 4;
   const size_t plane = (size_t)g.M * g.pitch, at = (size_t)m * g.pitch + n;
+  const int per = cdiv(g.splits, W), s0 = min(w * per, g.splits), s1 = min(s0 + per, g.splits);
+  f4 v[Q];
+#pragma unroll
+  for (int q = 0; q < Q; ++q) v[q] = split_sum4(g.part + q * plane, s0, s1, Q * plane, at);
+  if constexpr (W > 1) {
+    __shared__ f4 part[W][Q][LANES];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) part[w][q][lane] = v[q];
+    __syncthreads();
+    if (w) return;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      v[q] = part[0][q][lane];
+#pragma unroll
+      for (int u = 1; u < W; ++u) v[q] += part[u][q][lane];
+    }
+  }
+  if (i / quads >= (size_t)g.M) return;
   if constexpr (KIND == kDualDx) {
-    put_quad((E*)g.c[0] + (size_t)m * g.ldc, split_sum4(g.part, g.splits, plane, at), n, g.N);
+    put_quad((E*)g.c[0] + (size_t)m * g.ldc, v[0], n, g.N);
+  } else if constexpr (KIND == kDualFwd) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (g.bias[q] && n + e < g.N) v[q][e] += g.bias[q][n + e];
+    gate_store<E>(act, v[0], v[1], n, g.N, g.pre ? g.pre + (size_t)m * g.N : nullptr,
+                  (size_t)g.M * g.N, (E*)g.c[0] + (size_t)m * g.ldc);
   } else {
-    f4 v[2];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) v[q] = split_sum4(g.part + q * plane, g.splits, 2 * plane, at);
-    if constexpr (KIND == kDualFwd) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (g.bias[q] && n + e < g.N) v[q][e] += g.bias[q][n + e];
-      gate_store<E>(act, v[0], v[1], n, g.N, g.pre ? g.pre + (size_t)m * g.N : nullptr,
-                    (size_t)g.M * g.N, (E*)g.c[0] + (size_t)m * g.ldc);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        float* c = (float*)g.c[q] + (size_t)m * g.ldc;
-        if (g.accumulate) v[q] += get_quad(c, n, g.N);
-        put_quad(c, v[q], n, g.N);
-      }
+    for (int q = 0; q < 2; ++q) {
+      float* c = (float*)g.c[q] + (size_t)m * g.ldc;
+      if (g.accumulate) v[q] += get_quad(c, n, g.N);
+      put_quad(c, v[q], n, g.N);
     }
   }
 }
@@ -418,7 +432,8 @@ static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStr
   }
   if (p.splits > 1) {
     const size_t quads = (size_t)g.M * (g.pitch / 4);
-    gated_split_sum<KIND, E><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, act);
+    if (p.splits < 8) gated_split_sum<KIND, E, 1><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, act);
+    else gated_split_sum<KIND, E, 4><<<(unsigned)((quads + 63) / 64), 256, 0, st>>>(g, act);
   }
 }
 

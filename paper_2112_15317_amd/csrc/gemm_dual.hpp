@@ -350,41 +350,54 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      // Six products of F * F blocks each; A's pieces in a stage's first half, B's in
-      // its second.  The scheduler spreads the splitting over the MFMAs.
-      __builtin_amdgcn_sched_barrier(0);
+      // Six products of F * F blocks; A's two pieces in a stage's first half, B's in its
+      // second.  An MFMA takes the time of eight instructions: behind each of the first
+      // twelve a fragment is read, behind each of the first sixteen half a pair of
+      // values is split (6 instructions), then its piece is written and loaded.  (Left
+      // to the compiler, two pieces were split first: 490 us where this takes SLOT_US.)
+      static_assert(F == 2, "two pieces of each operand");
+      u32x4 t[2][3];                                 // the parts of both pieces
+      float ra = 0.f, rb = 0.f;
+      auto put = [&](int x, int p) {
+        u16* at = half == 0 ? to + sa.lds[x] : to + T::OPER + sb.lds[x];
+        *reinterpret_cast<u32x4*>(at + p * T::PART) = t[x][p];
+      };
+      auto get = [&](int x) {
+        if (half == 0) load_a(va[r], x);
+        else load_b(vb[r], x);
+      };
 #pragma unroll
-      for (int x = 0; x < F; ++x) {
-        if (half == 0) {
-          sa.store_one(to, va[r], x, lost);
-          load_a(va[r], x);
-        } else {
-          sb.store_one(to + T::OPER, vb[r], x, lost);
-          load_b(vb[r], x);
+      for (int n = 0; n < 24; ++n) {
+        const int q = n / 4, j = n % 4 / 2, i = n % 2;
+        f16v& sum = q == 5 ? acc[j][i] : low[j][i];
+        sum = mfma32(fb[c][j][kSplitB[q]], fa[c][i][kSplitA[q]], sum);
+        if (n < 12) {                                // A 2, B 0, A 1, B 1, A 0, B 2
+          if (n / 2 % 2 == 0) read_a(c ^ 1, S, n % 2, 2 - n / 4, s);
+          else read_b(c ^ 1, S, n % 2, n / 4, s);
         }
+        if (n < 16) {
+          const int x = n / 8, e = n / 2 % 4;
+          const DualPiece<E>& v = half == 0 ? va[r][x] : vb[r][x];
+          if (n % 2 == 0) {
+            ra = __uint_as_float(v.v[e / 2][e % 2 * 2]);
+            rb = __uint_as_float(v.v[e / 2][e % 2 * 2 + 1]);
+            t[x][0][e] = f32x2_to_bf16x2(ra, rb);
+            ra -= __uint_as_float(t[x][0][e] << 16);
+            rb -= __uint_as_float(t[x][0][e] & 0xffff0000u);
+          } else {
+            t[x][1][e] = f32x2_to_bf16x2(ra, rb);
+            ra -= __uint_as_float(t[x][1][e] << 16);
+            rb -= __uint_as_float(t[x][1][e] & 0xffff0000u);
+            t[x][2][e] = f32x2_to_bf16x2(ra, rb);
+            lost |= __float_as_uint(ra) | __float_as_uint(rb);
+          }
+        }
+        if (n >= 8 && n < 11) put(0, n - 8);
+        if (n == 11) get(0);
+        if (n >= 16 && n < 19) put(1, n - 16);
+        if (n == 19) get(1);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int p = NP - 1; p >= 0; --p)
-#pragma unroll
-        for (int i = 0; i < F; ++i) {
-          read_a(c ^ 1, S, i, p, s);
-          read_b(c ^ 1, S, i, p, s);
-        }
-#pragma unroll
-      for (int q = 0; q < 6; ++q)
-#pragma unroll
-        for (int n = 0; n < F * F; ++n) {
-          const int j = n / F, i = n % F;
-          f16v& t = q == 5 ? acc[j][i] : low[j][i];
-          t = mfma32(fb[c][j][kSplitB[q]], fa[c][i][kSplitA[q]], t);
-        }
-#pragma unroll
-      for (int n = 0; n < 6 * F * F; ++n) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // an MFMA,
-        __builtin_amdgcn_sched_group_barrier(0x080, 1, 0);   // an LDS access,
-        __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);   // vector ALU
-      }
-      __builtin_amdgcn_sched_barrier(0);
     }
   };
   // A stage in buffer b0; b2 gets the stage after the next one.

@@ -54,7 +54,7 @@ class sb_adamw_desc(ctypes.Structure):
 
 
 class sb_adamw_plan(ctypes.Structure):
-    _fields_ = [("tensors", _i), ("moments", _i), ("blocks", _i)]
+    _fields_ = [("tensors", _i), ("moments", _i), ("groups", _i), ("blocks", _i)]
 
 
 class sb_adamw_tensor(ctypes.Structure):

@@ -29,7 +29,7 @@ def _plan(tensors=None, moments=32, count=None, plan=PLAN, short=0, info=True):
                                         ctypes.byref(out) if info else None, None)
 
 
-def _update(plan=PLAN, info=(1, 32, 1), counter=None, **over):
+def _update(plan=PLAN, info=(1, 32, 4, 1), counter=None, **over):
     d = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0)
     d.update(over)
     return sb.load().sb_adamw_update(ctypes.byref(sb.sb_adamw_desc(**d)),
@@ -43,14 +43,15 @@ BAD = sb.SB_ERR_INVALID_ARG
     dict(step=0), dict(step=-3), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
     dict(beta2=float("nan")), dict(eps=-1e-8), dict(eps=float("inf")), dict(lr=float("nan")),
     dict(lr=1e300), dict(lr=float("inf")), dict(counter=P + 2), dict(plan=None), dict(plan=PLAN + 8),
-    dict(info=(1, 16, 1)), dict(info=(-1, 32, 1)), dict(info=(513, 32, 600)), dict(info=(2, 32, 1)),
-    dict(info=(0, 32, 1)), dict(info=(1, 8, -1))])
+    dict(info=(1, 16, 4, 1)), dict(info=(-1, 32, 4, 1)), dict(info=(513, 32, 4, 600)),
+    dict(info=(2, 32, 4, 1)), dict(info=(0, 32, 4, 1)), dict(info=(1, 8, 4, -1)),
+    dict(info=(1, 32, 2, 1))])
 def test_bad_updates_are_refused(over):
     assert _update(**over) == BAD
 
 
 def test_an_empty_plan_has_nothing_to_do():
-    assert _update(info=(0, 32, 0)) == sb.SB_OK
+    assert _update(info=(0, 32, 1, 0)) == sb.SB_OK
     assert sb.load().sb_adamw_update(None, None, None, None, None) == BAD
 
 

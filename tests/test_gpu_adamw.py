@@ -16,7 +16,7 @@ pytestmark = pytest.mark.gpu
 B1, B2, EPS, LR = 0.9, 0.999, 1e-8, 1e-3
 U = 2.0 ** -24                    # half a step of fp32
 SIZES = {"one": [1], "odd": [5, 1024, 4099, 0, 17, 256, 257, 4096, 12289], "many": [300 + 7 * i for i in range(95)],
-         "large": [1 << 20, 3]}
+         "large": [3 << 20, 3, 4097]}
 
 
 def _inputs(n, seed):
