@@ -37,6 +37,9 @@ from typing import List, Optional
 # Layer kinds of the paper's sequential CNNs, plus the two it inserts.
 SEQ, RESHAPE, PAD, CONV, POOLING, DROPOUT, RELU, LINEAR, LOG_SOFTMAX = (
     "SEQ", "RESHAPE", "PAD", "CONV", "POOLING", "DROPOUT", "RELU", "LINEAR", "LOG_SOFTMAX")
+# A dense layer with a gate in place of the ReLU, act(x Wg + bg) * (x Wu + bu):
+# split like LINEAR, both projections along their outputs.
+GATED = "GATED"
 MODULO, SHARD = "MODULO", "SHARD"
 _UNSPLIT = (RESHAPE, PAD, CONV, POOLING)
 _ELEMENTWISE = (DROPOUT, RELU)
@@ -55,8 +58,9 @@ class Layer:
     in_dim: int = 0
     out_dim: int = 0
     children: List["Layer"] = field(default_factory=list)
-    shards: int = 1                  # LINEAR: 1 / shards of the outputs live here
-    full_out: Optional[int] = None   # LINEAR: outputs of the unsplit layer
+    shards: int = 1                  # LINEAR, GATED: 1 / shards of the outputs live here
+    full_out: Optional[int] = None   # LINEAR, GATED: outputs of the unsplit layer
+    act: Optional[str] = None        # GATED: the gate's activation
 
     def resize(self, dim: int) -> int:
         """Output width for an input of width ``dim``."""
@@ -75,10 +79,20 @@ def linear(i: int, o: int) -> Layer:
     return Layer(LINEAR, i, o, full_out=o)
 
 
+def gated(i: int, o: int, act: str = "silu") -> Layer:
+    """act: one of GATE_ACTS."""
+    if act not in GATE_ACTS:
+        raise ValueError("a gate's activation is one of %s, not %r" % (", ".join(GATE_ACTS), act))
+    return Layer(GATED, i, o, full_out=o, act=act)
+
+
+GATE_ACTS = ("sigmoid", "silu", "gelu", "gelu_tanh", "relu")
+
+
 def ccr(layer: Layer) -> float:
     """FLOP of forward + backward per byte exchanged, per example."""
     i, o = layer.in_dim, layer.full_out or layer.out_dim
-    return 6.0 * i * o / (4.0 * (i + o))
+    return (12.0 if layer.kind == GATED else 6.0) * i * o / (4.0 * (i + o))
 
 
 # How each layer kind treats the width of its input (sec. 3.1, Layer
@@ -86,7 +100,8 @@ def ccr(layer: Layer) -> float:
 # examples only; element-wise layers keep whatever width they are given; a
 # dense layer may be split over its outputs; the loss needs the whole output.
 _ROLE = {RESHAPE: "whole", PAD: "whole", CONV: "whole", POOLING: "whole",
-         DROPOUT: "pointwise", RELU: "pointwise", LINEAR: "dense", LOG_SOFTMAX: "loss"}
+         DROPOUT: "pointwise", RELU: "pointwise", LINEAR: "dense", GATED: "dense",
+         LOG_SOFTMAX: "loss"}
 
 
 def flatten(net: Layer) -> List[Layer]:
@@ -143,8 +158,8 @@ def partition(net: Layer, workers: int, threshold: float = 1.0) -> List[Layer]:
                 if full_out % workers:
                     raise ValueError("%d outputs cannot be split evenly over %d workers"
                                      % (full_out, workers))
-                layer = Layer(LINEAR, layer.in_dim, full_out // workers, shards=workers,
-                              full_out=full_out)
+                layer = Layer(layer.kind, layer.in_dim, full_out // workers, shards=workers,
+                              full_out=full_out, act=layer.act)
             out.append(layer)
             local, whole = layer.out_dim, full_out
         else:                                   # the loss
@@ -159,8 +174,8 @@ def fc_plan(layers: List[Layer]):
     """The model-parallel tail of a partitioned layer list as the training
     step runs it: from the MODULO layer on, a list of
     ``("modulo", features)``, ``("linear", in, shard_out, full_out, relu)``
-    (relu: a ReLU follows the layer), ``("shard", part, full)`` and
-    ``("loss", classes)`` entries.  Dropout is not part of any workload and
+    (relu: a ReLU follows the layer), ``("gated", in, shard_out, full_out,
+    act)``, ``("shard", part, full)`` and ``("loss", classes)`` entries.  Dropout is not part of any workload and
     is refused, as is a tail that does not start with a MODULO layer."""
     kinds = [l.kind for l in layers]
     if MODULO not in kinds:
@@ -173,12 +188,16 @@ def fc_plan(layers: List[Layer]):
         elif l.kind == LINEAR:
             relu = i + 1 < len(tail) and tail[i + 1].kind == RELU
             plan.append(("linear", l.in_dim, l.out_dim, l.full_out or l.out_dim, relu))
+        elif l.kind == GATED:
+            plan.append(("gated", l.in_dim, l.out_dim, l.full_out or l.out_dim, l.act))
         elif l.kind == SHARD:
             plan.append(("shard", l.in_dim, l.out_dim))
         elif l.kind == LOG_SOFTMAX:
             width = plan[-1][2] if plan[-1][0] == "shard" else plan[-1][3]
             plan.append(("loss", width))
         elif l.kind == RELU:
+            if plan[-1][0] == "gated":
+                raise ValueError("a gated layer has no ReLU behind it")
             continue                              # fused into the layer before
         else:
             raise ValueError("%s in the model-parallel part is not supported" % l.kind)
@@ -186,22 +205,24 @@ def fc_plan(layers: List[Layer]):
 
 
 def fc_shards(layers: List[Layer]):
-    """(input width, shard outputs, full outputs) of every split LINEAR layer."""
+    """(input width, shard outputs, full outputs) of every split LINEAR or GATED layer."""
     return [(l.in_dim, l.out_dim, l.full_out) for l in layers
-            if l.kind == LINEAR and l.shards > 1]
+            if l.kind in (LINEAR, GATED) and l.shards > 1]
 
 
 def parameters(layers: List[Layer], conv_params: int = 0) -> int:
     """Parameters one worker holds: the given conv parameters plus its FC
-    weight (and bias) columns."""
-    return conv_params + sum(l.in_dim * l.out_dim + l.out_dim for l in layers
-                             if l.kind == LINEAR)
+    weight (and bias) columns (two of each for a gated layer)."""
+    return conv_params + sum((2 if l.kind == GATED else 1) * (l.in_dim * l.out_dim + l.out_dim)
+                             for l in layers if l.kind in (LINEAR, GATED))
 
 
-def vgg_net(schedule, in_ch: int, hw: int, fc) -> Layer:
+def vgg_net(schedule, in_ch: int, hw: int, fc, gate: Optional[str] = None) -> Layer:
     """A sequential VGG-style CNN as a layer list: 3x3 convs (each followed
     by a ReLU) and 2x2 pools per the channel schedule, a flatten, the dense
-    layers ``fc`` [(in, out)] with a ReLU between them, then LOG_SOFTMAX."""
+    layers ``fc`` [(in, out)] with a ReLU between them, then LOG_SOFTMAX.
+    With ``gate`` (an activation's name) every dense layer but the last is a
+    gated one."""
     from .configs import POOL
     layers, c = [], in_ch
     for v in schedule:
@@ -213,6 +234,9 @@ def vgg_net(schedule, in_ch: int, hw: int, fc) -> Layer:
             c = v
     layers.append(Layer(RESHAPE, c * hw * hw, c * hw * hw))
     for j, (i, o) in enumerate(fc):
+        if gate and j < len(fc) - 1:
+            layers.append(gated(i, o, gate))
+            continue
         layers.append(linear(i, o))
         if j < len(fc) - 1:
             layers.append(Layer(RELU))

@@ -10,6 +10,8 @@ by a libsb kernel.  torch only allocates device memory and orders streams.
 
 ``ConvStack``   13-layer VGG conv stack fwd + bwd (ReLU, fused ReLU + pool)
 ``FCShard``     one FC column shard fwd + bwd
+``GatedShard``  one gated FC column shard fwd + bwd
+``AdamW``       the settings of an AdamW update, in place of SGD
 ``HybridStep``  conv stack, then FC0 -> ReLU -> FC1 shards on the gathered
                 batch, then backward through both
 ``GroupTrainStep``  a training step of an MP group: conv stack, K modulo
@@ -33,6 +35,10 @@ def _dev_dtype(dtype: str):
 
 def _code(dtype: str):
     return {"f32": sb.SB_F32, "bf16": sb.SB_BF16}[dtype]
+
+
+def _gate_code(act: str):
+    return getattr(sb, "SB_ACT_" + act.upper())
 
 
 def _plain(key, fn, *args):
@@ -406,6 +412,70 @@ class FCShard:
         fn(*args)
 
 
+class GatedShard:
+    """One gated FC column shard: X [m, k_in] (row stride ldx), W [2, k_in, ns]
+    (the gate's weight, then the other projection's), ``pre`` what the forward
+    keeps for the backward."""
+
+    def __init__(self, m, k_in, ns, act="silu", dtype="f32", ldx=None, ldy=None, device="cuda"):
+        self.m, self.k_in, self.ns, self.act = m, k_in, ns, act
+        self.ldx, self.ldy = ldx or k_in, ldy or ns
+        dev = torch.device(device)
+        f32 = dict(dtype=torch.float32, device=dev)
+        self.W = torch.empty((2, k_in, ns), dtype=_dev_dtype(dtype), device=dev)
+        self.desc = sb.gated_desc(m, k_in, ns, _code(dtype), _gate_code(act), self.ldx, self.ldy,
+                                  unaligned=self.W[1].data_ptr() % 16 != 0)
+        self.b = torch.zeros((2, ns), **f32)
+        self.dW = torch.empty((2, k_in, ns), **f32)
+        self.db = torch.empty((2, ns), **f32)
+        self.pre = torch.empty((2, m, ns), **f32)
+        need = max(sb.sb_gated_workspace_bytes(self.desc, p) for p in (sb.SB_FC_FWD, sb.SB_FC_BWD))
+        # Scratch; needs no initialisation.
+        self.ws = torch.empty((max(need, 256) + 255) // 256 * 256, dtype=torch.uint8, device=dev)
+
+    def forward(self, x, y, keep=True, stream=None):
+        sb.sb_gated_shard_fwd(self.desc, x, self.W[0], self.W[1], self.b[0], self.b[1], y,
+                              self.pre if keep else None, self.ws, stream)
+
+    def backward(self, x, dy, dx, accumulate=False, stream=None):
+        sb.sb_gated_shard_bwd(self.desc, x, self.W[0], self.W[1], self.pre, dy, dx, self.dW[0],
+                              self.dW[1], self.db[0], self.db[1], accumulate, self.ws, stream)
+
+
+class AdamW:
+    """Settings of an AdamW update: biases do not decay; ``moments`` 32 or 8 bits."""
+
+    def __init__(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, decay=0.0, moments=32, seed=0):
+        self.lr, self.beta1, self.beta2, self.eps = lr, beta1, beta2, eps
+        self.decay, self.moments, self.seed = decay, moments, seed
+
+
+class _Updates:
+    """The updates of one set of (parameter, gradient, scale, decays): SGD at a
+    rate, or AdamW with the moments and a counter of its updates on the
+    device, so that a captured step counts on when it is replayed."""
+
+    def __init__(self, items, lr, adamw):
+        self.lr, self.adamw = lr, adamw
+        if adamw is None:
+            self.list = sb.SgdList([(w, g, scale) for w, g, scale, _ in items])
+            return
+        self.moments = [sb.adamw_moments(w, adamw.moments) for w, _, _, _ in items]
+        self.list = sb.AdamwList([dict(w=w, g=g, scale=scale, decay=adamw.decay if decays else 0.0,
+                                       **m)
+                                  for (w, g, scale, decays), m in zip(items, self.moments)])
+        self.done = torch.zeros(1, dtype=torch.int32, device=items[0][0].device)
+
+    def calls(self, name, k, stream):
+        """The (key, libsb function, args) calls of one update."""
+        a = self.adamw
+        if a is None:
+            return [(("sgd_" + name, k), sb.sb_sgd_update, (self.list, self.lr, stream))]
+        return [(("adamw_" + name, k), sb.sb_adamw_update,
+                 (self.list, a.lr, a.beta1, a.beta2, a.eps, 1, a.seed, self.done, stream)),
+                (("adamw_count_" + name, k), sb.sb_adamw_advance, (self.done, stream))]
+
+
 class HybridStep:
     """Conv stack on the local batch, then L FC shards on the gathered batch.
 
@@ -535,6 +605,14 @@ class GroupTrainStep:
     0's conv output over its whole local batch: the conv stack runs backward
     and takes one SGD step at rate lr.
 
+    With ``adamw`` (an ``AdamW``) the updates are ``sb_adamw_update`` ones, on
+    the same gradients and scales, lr unused; FC shards and conv layers count
+    their updates apart.  A ("gated", in, shard, full, act) entry of the plan in
+    place of a linear one is a gated layer (``sb_gated_shard_fwd``/``_bwd``):
+    its ``W[j]`` is [K][2][in_j][ns_j], ``b[j]`` [K][2][ns_j] (the gate's, then
+    the other projection's), and ``pre[j]`` [K][2][B][ns_j] what its forward
+    keeps.
+
     Buffers (j: dense layer, r: worker): ``W[j]``/``b[j]`` [K][in_j][ns_j] /
     [K][ns_j] (worker r's shard, fp32), ``dW[j]``/``db[j]`` their gradients,
     ``X[j]`` [B][in_j] the full input of layer j (``X[0]`` the gathered
@@ -544,14 +622,15 @@ class GroupTrainStep:
     the labels of iteration k's gathered rows), ``loss`` [K][B].
     """
 
-    def __init__(self, schedule, n, in_ch, hw, plan, lr=0.01, device="cuda"):
+    def __init__(self, schedule, n, in_ch, hw, plan, lr=0.01, device="cuda", adamw=None):
         dev = torch.device(device)
         if not plan or plan[0][0] != "modulo" or plan[-1][0] != "loss":
             raise ValueError("the plan must run from a modulo layer to the loss")
-        lin = [e for e in plan[1:-1] if e[0] == "linear"]
+        dense = ("linear", "gated")
+        lin = [e for e in plan[1:-1] if e[0] in dense]
         shards = [e for e in plan[1:-1] if e[0] == "shard"]
-        body = [e[0] for e in plan[1:-1]]
-        if body != ["linear", "shard"] * len(lin):
+        body = ["linear" if e[0] in dense else e[0] for e in plan[1:-1]]
+        if not lin or body != ["linear", "shard"] * len(lin):
             raise ValueError("every dense layer must be split and followed by a shard layer")
         K = lin[0][3] // lin[0][2]
         for (_, i, ns, full, _), (_, part, whole) in zip(lin, shards):
@@ -563,7 +642,8 @@ class GroupTrainStep:
         self.ins = [e[1] for e in lin]
         self.ns = [e[2] for e in lin]
         self.full = [e[3] for e in lin]
-        self.relu = [e[4] for e in lin]
+        self.act = [e[4] if e[0] == "gated" else None for e in lin]
+        self.relu = [e[0] == "linear" and e[4] for e in lin]
         self.F = plan[0][1]
         self.classes = plan[-1][1]
         if self.ins[0] != self.F or self.full[-1] != self.classes:
@@ -580,8 +660,11 @@ class GroupTrainStep:
         if int(np.prod(self.conv.A[-1].shape[1:])) != F:
             raise ValueError("the conv stack's output does not have the plan's width")
         L = self.L
-        self.W = [torch.empty((K, self.ins[j], self.ns[j]), **f32) for j in range(L)]
-        self.b = [torch.empty((K, self.ns[j]), **f32) for j in range(L)]
+        both = [(2,) if a else () for a in self.act]
+        self.W = [torch.empty((K,) + both[j] + (self.ins[j], self.ns[j]), **f32) for j in range(L)]
+        self.b = [torch.empty((K,) + both[j] + (self.ns[j],), **f32) for j in range(L)]
+        self.pre = [torch.empty((K, 2, B, self.ns[j]), **f32) if a else None
+                    for j, a in enumerate(self.act)]
         self.dW = [torch.empty_like(w) for w in self.W]
         self.db = [torch.empty_like(b) for b in self.b]
         self.X = [torch.empty((B, self.ins[j]), **f32) for j in range(L)]
@@ -602,38 +685,57 @@ class GroupTrainStep:
                       for j in range(L)]
         need = 0
         for j in range(L):
+            if self.act[j]:
+                # Odd shapes put a worker's weights at any multiple of 4 bytes.
+                self.fdesc[j], self.bdesc[j] = (
+                    sb.gated_desc(B, self.ins[j], self.ns[j], sb.SB_F32, _gate_code(self.act[j]),
+                                  ldy=d.ldy, unaligned=self.ins[j] * self.ns[j] % 4 != 0)
+                    for d in (self.fdesc[j], self.bdesc[j]))
+                need = max(need, sb.sb_gated_workspace_bytes(self.fdesc[j], sb.SB_FC_FWD),
+                           sb.sb_gated_workspace_bytes(self.bdesc[j], sb.SB_FC_BWD))
+                continue
             need = max(need, sb.sb_fc_workspace_bytes(self.fdesc[j], sb.SB_FC_FWD),
                        sb.sb_fc_workspace_bytes(self.bdesc[j], sb.SB_FC_BWD))
         self.ws = torch.empty((max(need, 256) + 255) // 256 * 256, dtype=torch.uint8, device=dev)
-        self.sgd_fc = sb.SgdList([(self.W[j], self.dW[j], 1.0 / K) for j in range(L)] +
-                                 [(self.b[j], self.db[j], 1.0 / K) for j in range(L)])
+        self.update_fc = _Updates([(self.W[j], self.dW[j], 1.0 / K, True) for j in range(L)] +
+                                  [(self.b[j], self.db[j], 1.0 / K, False) for j in range(L)],
+                                  lr, adamw)
         c = self.conv
-        self.sgd_conv = sb.SgdList([(c.W[i], c.dW[i], 1.0) for i in range(len(c.layers))] +
-                                   [(c.b[i], c.db[i], 1.0) for i in range(len(c.layers))])
+        n_conv = len(c.layers)
+        self.update_conv = _Updates([(c.W[i], c.dW[i], 1.0, True) for i in range(n_conv)] +
+                                    [(c.b[i], c.db[i], 1.0, False) for i in range(n_conv)],
+                                    lr, adamw)
         self.call = _plain      # hook: every libsb call of the step goes through it
 
     def load_inputs(self, x, conv_w, conv_b, fc_w, fc_b, local_remote, labels):
-        """fc_w / fc_b: the full dense layers ([in][out], [out]); worker r's
+        """fc_w / fc_b: the full dense layers ([in][out], [out]; for a gated
+        layer pairs of them, the gate's first); worker r's
         shard is columns r*ns .. (r+1)*ns - 1.  local_remote [K-1][B][F]:
         the other workers' conv outputs; labels [K][B]."""
         t = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32))
         self.conv.load_inputs(x, conv_w, conv_b)
         K = self.K
         for j in range(self.L):
-            w = np.asarray(fc_w[j], np.float32).reshape(self.ins[j], K, self.ns[j])
-            self.W[j].copy_(t(w.transpose(1, 0, 2)))
-            self.b[j].copy_(t(np.asarray(fc_b[j], np.float32).reshape(K, self.ns[j])))
+            # [K][in][ns] and [K][ns]; of a gated layer's pairs [K][2][..].
+            w = np.asarray(fc_w[j], np.float32).reshape(-1, self.ins[j], K, self.ns[j])
+            b = np.asarray(fc_b[j], np.float32).reshape(-1, K, self.ns[j])
+            self.W[j].copy_(t(w.transpose(2, 0, 1, 3)).view(self.W[j].shape))
+            self.b[j].copy_(t(b.transpose(1, 0, 2)).view(self.b[j].shape))
         if K > 1:
             self.local[1:].copy_(t(local_remote))
         self.labels.copy_(torch.from_numpy(np.ascontiguousarray(labels, dtype=np.int32)))
 
     def full_weights(self, j):
-        """Layer j's full weight [in][out] on the host (the shards side by side)."""
+        """Layer j's full weight [in][out] on the host (the shards side by side);
+        both of a gated layer, [2][in][out]."""
         w = self.W[j].detach().cpu().numpy()
+        if self.act[j]:
+            return np.ascontiguousarray(w.transpose(1, 2, 0, 3).reshape(2, self.ins[j], -1))
         return np.ascontiguousarray(w.transpose(1, 0, 2).reshape(self.ins[j], -1))
 
     def full_bias(self, j):
-        return self.b[j].detach().cpu().numpy().reshape(-1)
+        b = self.b[j].detach().cpu().numpy()
+        return b.transpose(1, 0, 2).reshape(2, -1) if self.act[j] else b.reshape(-1)
 
     # -- the step ---------------------------------------------------------------
     def iteration(self, k, stream=None):
@@ -643,6 +745,11 @@ class GroupTrainStep:
         c(("mfwd", k), sb.sb_modulo_fwd, self.mdesc, 0, k, self.local, self.X[0], None, stream)
         for j in range(L):
             for r in range(K):
+                if self.act[j]:
+                    w, b = self.W[j][r], self.b[j][r]
+                    c(("gated_fwd", j), sb.sb_gated_shard_fwd, self.fdesc[j], self.X[j], w[0], w[1],
+                      b[0], b[1], self.P[j][r], self.pre[j][r], self.ws, stream)
+                    continue
                 c(("fc_fwd", j), sb.sb_fc_shard_fwd, self.fdesc[j], self.X[j], self.W[j][r],
                   self.b[j][r], self.P[j][r], self.ws, stream)
             c(("sfwd", j), sb.sb_shard_fwd, self.sdesc[j], 0, self.P[j], self.X[j + 1], None,
@@ -655,6 +762,12 @@ class GroupTrainStep:
                     dy = self.dZl.data_ptr() + 4 * r * self.ns[j]     # its columns of dZl
                 else:
                     dy = self.dP[j][r]
+                if self.act[j]:
+                    w, dw, db = self.W[j][r], self.dW[j][r], self.db[j][r]
+                    c(("gated_bwd", j), sb.sb_gated_shard_bwd, self.bdesc[j], self.X[j], w[0], w[1],
+                      self.pre[j][r], dy, self.dF[j][r], dw[0], dw[1], db[0], db[1], False, self.ws,
+                      stream)
+                    continue
                 mask = self.P[j][r] if self.relu[j] else None
                 c(("fc_bwd", j), sb.sb_fc_shard_bwd, self.bdesc[j], self.X[j], self.W[j][r], dy,
                   mask, self.dF[j][r], self.dW[j][r], self.db[j][r], False, self.ws, stream)
@@ -664,12 +777,14 @@ class GroupTrainStep:
             else:
                 c(("mbwd", k), sb.sb_modulo_bwd, self.mdesc, 0, k, self.dF[0], self.dlocal,
                   None, None, stream)
-        c(("sgd_fc", k), sb.sb_sgd_update, self.sgd_fc, self.lr, stream)
+        for key, fn, args in self.update_fc.calls("fc", k, stream):
+            c(key, fn, *args)
 
     def finish(self, stream=None):
         """Conv backward from the gathered local-row gradients, conv update."""
         self.conv.backward(stream)
-        self.call(("sgd_conv", 0), sb.sb_sgd_update, self.sgd_conv, self.lr, stream)
+        for key, fn, args in self.update_conv.calls("conv", 0, stream):
+            self.call(key, fn, *args)
 
     def step(self, stream=None):
         self.conv.forward(stream)
@@ -702,15 +817,17 @@ class AveragedGroups:
     [K][ns] biases, shard r of group g beside shard r of every other group)
     is one ``sb_model_average_replicas`` call over the G buffers.  ``step``
     runs every group's training step, then, after steps period, 2 period,
-    ..., the averages.
+    ..., the averages.  With ``adamw`` the parameters are averaged, each
+    group's moments stay its own.
     """
 
-    def __init__(self, schedule, n, in_ch, hw, plan, groups, period, lr=0.01, device="cuda"):
+    def __init__(self, schedule, n, in_ch, hw, plan, groups, period, lr=0.01, device="cuda",
+                 adamw=None):
         if groups < 1 or groups > sb.SB_MAX_REPLICAS:
             raise ValueError("1 .. %d groups" % sb.SB_MAX_REPLICAS)
         if period < 1:
             raise ValueError("the averaging period is a positive number of steps")
-        self.groups = [GroupTrainStep(schedule, n, in_ch, hw, plan, lr, device)
+        self.groups = [GroupTrainStep(schedule, n, in_ch, hw, plan, lr, device, adamw)
                        for _ in range(groups)]
         self.period = period
         self.steps_done = 0
