@@ -399,7 +399,8 @@ static void dual_launch(const DualArgs& g, hipStream_t st) {
     (void)hipFuncSetAttribute((const void*)gemm_dual<T, KIND, ACT>,
                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)T::LDS_BYTES);
   });
-  gemm_dual<T, KIND, ACT><<<(unsigned)(g.mt * g.nt * g.splits), 256, T::LDS_BYTES, st>>>(g);
+  gemm_dual<T, KIND, ACT>
+      <<<(unsigned)(g.mt * g.nt * g.splits), T::THREADS, T::LDS_BYTES, st>>>(g);
 }
 template <DualKind KIND, int ACT, class E>
 static void dual_launch_f(int f, const DualArgs& g, hipStream_t st) {

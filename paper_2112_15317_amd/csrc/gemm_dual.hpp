@@ -7,8 +7,8 @@
 //
 // A block has 64 F rows (M) by 64 F columns: of FWD and DW 32 F columns of each
 // of the two outputs (N), so the operand they share is staged once and the gate's
-// value and the other projection's for one output element end in one lane.  Four
-// waves, 2 x 2, each F x F blocks of 32 x 32 in registers.  The reduction is a
+// value and the other projection's for one output element end in one wave.  Four
+// waves, 2 x 2 (fp32: eight, 4 x 2), each with FA x F blocks of 32 x 32 in registers.  The reduction is a
 // list of segments of equal length (DX: one per weight matrix; DW: one per bf16
 // part of da and du), each in stages of 32.
 //
@@ -41,6 +41,12 @@ template <int F_, class E_>
 struct DualTile {
   typedef E_ E;
   static constexpr int F = F_, NP = sizeof(E) == 4 ? 3 : 1;
+  // Waves by rows and columns, a wave's blocks of rows (of columns F), its threads'
+  // pieces of an operand's stage.  fp32 takes eight waves of 32 rows: one wave issues
+  // an instruction every five or six cycles, and splitting the operands is as many as
+  // the MFMAs leave room for; two waves a SIMD issue twice as many (FP32_WAVES).
+  static constexpr int WM = NP == 3 ? 4 : 2, WN = 2, THREADS = 64 * WM * WN;
+  static constexpr int FA = 2 * F / WM, PCS = 256 * F / THREADS;
   static constexpr int BM = 64 * F, RC = 32 * F;     // rows; columns of a region
   static constexpr int PART = BM * 32, OPER = NP * PART;   // elements of an operand's stage
   static constexpr int STAGE = 2 * OPER;
@@ -103,8 +109,8 @@ template <> struct DualPiece<float> {
 template <class T, bool KC>
 struct DualStage {
   typedef typename T::E E;
-  uint32_t off[T::F];              // byte offset of this lane's pieces at k = 0, or kOOB
-  int lds[T::F];                   // their place (elements)
+  uint32_t off[T::PCS];            // byte offset of this lane's pieces at k = 0, or kOOB
+  int lds[T::PCS];                 // their place (elements)
   uint32_t step;                   // bytes per k
   int k;                           // KC: the first k of all of them within a stage
   // Rows (KC) or columns from r0 on, `rows` of them; region 1 starts at r1.
@@ -112,31 +118,35 @@ struct DualStage {
     step = (KC ? 1u : (uint32_t)ld) * (uint32_t)sizeof(E);
     k = KC ? tid % 4 * 8 : 0;
 #pragma unroll
-    for (int i = 0; i < T::F; ++i) {
+    for (int i = 0; i < T::PCS; ++i) {
+      const int u = tid + T::THREADS * i;
       if constexpr (KC) {
-        const int row = (tid + 256 * i) / 4, p = tid % 4;
+        const int row = u / 4, p = u % 4;
         lds[i] = row * 32 + (p ^ (row >> 2 & 3)) * 8;
         off[i] = r0 + row < rows ? (uint32_t)((r0 + row) * ld + p * 8) * (uint32_t)sizeof(E) : kOOB;
       } else {
         constexpr int PR = T::RC / 8;                // pieces a line
-        const int region = i / (T::F / 2);
-        const int w = tid + 256 * (i % (T::F / 2)), line = w / PR, p = w % PR;
+        const int region = u / (128 * T::F), w = u % (128 * T::F), line = w / PR, p = w % PR;
         const int col = (region ? r1 : r0) + p * 8;
         lds[i] = region * (T::RC * 32) + line * T::RC + ((p / 2 ^ (line & 3)) * 2 + p % 2) * 8;
         off[i] = col < rows ? (uint32_t)(line * ld + col) * (uint32_t)sizeof(E) : kOOB;
       }
     }
   }
+  // The region of a wave's piece i.
+  __device__ static __forceinline__ int region(int wave, int i) {
+    return (64 * wave + T::THREADS * i) / (128 * T::F);
+  }
   // Piece i of the stage from k0 on (k0 < K); r: its region's resource.  Lines at
   // and past K lie behind the operand and read 0 by its range, as kOOB does at
   // any k; a row's pieces past K are left out here.
-  __device__ __forceinline__ void load_one(rsrc_t r, int k0, int K, DualPiece<E> (&v)[T::F],
+  __device__ __forceinline__ void load_one(rsrc_t r, int k0, int K, DualPiece<E> (&v)[T::PCS],
                                            int i) const {
     uint32_t o = off[i] + (uint32_t)k0 * step;
     if constexpr (KC) o = k0 + k < K ? o : kOOB;
     v[i].load(r, o);
   }
-  __device__ __forceinline__ void store_one(u16* S, const DualPiece<E> (&v)[T::F], int i,
+  __device__ __forceinline__ void store_one(u16* S, const DualPiece<E> (&v)[T::PCS], int i,
                                             uint32_t& lost) const {
     v[i].store(S + lds[i], T::PART, lost);
   }
@@ -196,14 +206,14 @@ __device__ __forceinline__ f4 get_quad(const float* row, int n, int N) {
 
 // ACT: FWD's activation (its code is unrolled over all the outputs of a lane).
 template <class T, DualKind KIND, int ACT>
-__global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dual(DualArgs g) {
+__global__ __launch_bounds__(T::THREADS, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) {
   extern __shared__ u16 lds[];
   typedef typename T::E E;
-  constexpr int F = T::F, NP = T::NP;
+  constexpr int F = T::F, NP = T::NP, FA = T::FA, PCS = T::PCS;
   constexpr bool AKC = KIND != kDualDw, BKC = KIND == kDualDx;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave & 1, wn = wave >> 1;
+  const int wm = wave % T::WM, wn = wave / T::WM;
 
   // Blocks are dealt to the 8 XCDs in contiguous ranges of an order in which 8 row
   // tiles take turns under one column tile, so what an XCD runs at a time is a
@@ -228,7 +238,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
   sb.init(tid, g.ldb, g.N, n0, n0);
   // The next stage to load.
   int seg = t0 / per_seg, k0 = (t0 - seg * per_seg) * 32;
-  DualPiece<E> va[2][F], vb[2][F];
+  DualPiece<E> va[2][PCS], vb[2][PCS];
   uint32_t lost = 0;
   // The operands of its segment; its first k.  Stages past the block's last one, which
   // nothing multiplies, are empty ranges: their loads return 0 and read nothing.
@@ -255,39 +265,49 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
   auto turn = [&]() {
     if (k0 == 0 || left == 0) segment();
   };
-  auto load_a = [&](DualPiece<E> (&x)[F], int i) { sa.load_one(ra, ka, g.K, x, i); };
-  auto load_b = [&](DualPiece<E> (&x)[F], int i) {
-    sb.load_one(!BKC && i >= F / 2 ? rc : rb, ka, g.K, x, i);
+  auto load_a = [&](DualPiece<E> (&x)[PCS], int i) { sa.load_one(ra, ka, g.K, x, i); };
+  auto load_b = [&](DualPiece<E> (&x)[PCS], int i) {
+    sb.load_one(!BKC && sb.region(wave, i) ? rc : rb, ka, g.K, x, i);
   };
-  auto load = [&](DualPiece<E> (&xa)[F], DualPiece<E> (&xb)[F]) {
+  auto load = [&](DualPiece<E> (&xa)[PCS], DualPiece<E> (&xb)[PCS]) {
     next();
 #pragma unroll
-    for (int i = 0; i < F; ++i) {
+    for (int i = 0; i < PCS; ++i) {
       load_a(xa, i);
       load_b(xb, i);
     }
     turn();
   };
-  auto store = [&](u16* S, const DualPiece<E> (&xa)[F], const DualPiece<E> (&xb)[F]) {
+  auto store = [&](u16* S, const DualPiece<E> (&xa)[PCS], const DualPiece<E> (&xb)[PCS]) {
 #pragma unroll
-    for (int i = 0; i < F; ++i) {
+    for (int i = 0; i < PCS; ++i) {
       sa.store_one(S, xa, i, lost);
       sb.store_one(S + T::OPER, xb, i, lost);
     }
   };
 
-  int pa[F], pb[F];
+  // Row block i of the wave: block gf + i of the tile's, F of them a region.
+  const int gf = wm * FA;
+  int pa[FA], pb[F];
+#pragma unroll
+  for (int i = 0; i < FA; ++i)
+    pa[i] = AKC ? frag_place<T, true>(gf + i, lane, 0)
+                : frag_place<T, false>((gf + i) % F, lane, 0) + (gf + i) / F * T::RC * 32;
 #pragma unroll
   for (int i = 0; i < F; ++i) {
-    pa[i] = frag_place<T, AKC>(i, lane, wm * T::RC) + (AKC ? 0 : wm * T::RC * 32);
     if constexpr (BKC) pb[i] = T::OPER + frag_place<T, true>(i, lane, wn * T::RC);
     else pb[i] = T::OPER + (i / (F / 2)) * T::RC * 32 +
                  frag_place<T, false>(wn * (F / 2) + i % (F / 2), lane, 0);
   }
+  // Output row of row c (0 .. 31) of the wave's block i.
+  auto out_row = [&](int i, int c) {
+    const int f = gf + i;
+    return m0 + (AKC ? f * 32 + c : f / F * T::RC + pair_block<F>(f % F, c / 16) * 16 + c % 16);
+  };
   // [column block][row block]; low: the sums of the five smaller products of the
   // parts, which are below 2^-8 of the sums they are added to at the end, so their
   // roundings do not count.
-  f16v acc[F][F], low[NP == 3 ? F : 1][NP == 3 ? F : 1];
+  f16v acc[F][FA], low[NP == 3 ? F : 1][NP == 3 ? FA : 1];
   auto clear = [](f16v& x) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) x[v] = 0.f;
@@ -295,7 +315,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
 #pragma unroll
   for (int j = 0; j < F; ++j)
 #pragma unroll
-    for (int i = 0; i < F; ++i) {
+    for (int i = 0; i < FA; ++i) {
       clear(acc[j][i]);
       if constexpr (NP == 3) clear(low[j][i]);
     }
@@ -308,7 +328,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
   load(va[1], vb[1]);
   __syncthreads();
 
-  s8 fa[2][F][NP], fb[2][F][NP];
+  s8 fa[2][FA][NP], fb[2][F][NP];
   auto read_a = [&](int c, const u16* S, int i, int p, int s) {
     fa[c][i][p] = frag_read<T, AKC>(S + p * T::PART, pa[i], s);
   };
@@ -316,12 +336,12 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
     fb[c][j][p] = frag_read<T, BKC>(S + p * T::PART, pb[j], s);
   };
 #pragma unroll
-  for (int i = 0; i < F; ++i)
+  for (int p = 0; p < NP; ++p) {
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
-      read_a(0, lds, i, p, 0);
-      read_b(0, lds, i, p, 0);
-    }
+    for (int i = 0; i < FA; ++i) read_a(0, lds, i, p, 0);
+#pragma unroll
+    for (int j = 0; j < F; ++j) read_b(0, lds, j, p, 0);
+  }
   // 16 k out of fragment set P: the MFMAs, and between them the reads of the next 16 k
   // from S (one fragment behind each of the first MFMAs, in the order of their use),
   // and, behind the others, pieces of the stage after the next one to LDS and the loads
@@ -350,52 +370,48 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
-      // Six products of F * F blocks; A's two pieces in a stage's first half, B's in its
-      // second.  An MFMA takes the time of eight instructions: behind each of the first
-      // twelve a fragment is read, behind each of the first sixteen half a pair of
-      // values is split (6 instructions), then its piece is written and loaded.  (Left
-      // to the compiler, two pieces were split first: 490 us where this takes SLOT_US.)
-      static_assert(F == 2, "two pieces of each operand");
-      u32x4 t[2][3];                                 // the parts of both pieces
+      // Six products of two blocks; A's piece in a stage's first half, B's in its second.
+      // An MFMA takes the time of eight instructions: behind each of the first nine a
+      // fragment is read, behind each of the first eight half a pair of values is split
+      // (six instructions), behind the others the piece is written, then loaded.  (Left
+      // to the compiler the splitting came first, the MFMAs after it: 490 us for 2048 x
+      // 4096 x 2048, 447 like this.)
+      static_assert(NP == 1 || (F == 2 && FA == 1 && PCS == 1), "one piece of each operand");
+      u32x4 t[3];                                    // the piece's parts
       float ra = 0.f, rb = 0.f;
-      auto put = [&](int x, int p) {
-        u16* at = half == 0 ? to + sa.lds[x] : to + T::OPER + sb.lds[x];
-        *reinterpret_cast<u32x4*>(at + p * T::PART) = t[x][p];
-      };
-      auto get = [&](int x) {
-        if (half == 0) load_a(va[r], x);
-        else load_b(vb[r], x);
-      };
+      const DualPiece<E>& v = half == 0 ? va[r][0] : vb[r][0];
 #pragma unroll
-      for (int n = 0; n < 24; ++n) {
-        const int q = n / 4, j = n % 4 / 2, i = n % 2;
-        f16v& sum = q == 5 ? acc[j][i] : low[j][i];
-        sum = mfma32(fb[c][j][kSplitB[q]], fa[c][i][kSplitA[q]], sum);
-        if (n < 12) {                                // A 2, B 0, A 1, B 1, A 0, B 2
-          if (n / 2 % 2 == 0) read_a(c ^ 1, S, n % 2, 2 - n / 4, s);
-          else read_b(c ^ 1, S, n % 2, n / 4, s);
+      for (int n = 0; n < 12; ++n) {
+        const int q = n / 2, j = n % 2;
+        f16v& sum = q == 5 ? acc[j][0] : low[j][0];
+        sum = mfma32(fb[c][j][kSplitB[q]], fa[c][0][kSplitA[q]], sum);
+        if (n < 9) {                                 // A 2, B 0, A 1, B 1, A 0, B 2
+          if (n % 3 == 0) read_a(c ^ 1, S, 0, 2 - n / 3, s);
+          else read_b(c ^ 1, S, n % 3 - 1, n / 3, s);
         }
-        if (n < 16) {
-          const int x = n / 8, e = n / 2 % 4;
-          const DualPiece<E>& v = half == 0 ? va[r][x] : vb[r][x];
+        if (n < 8) {
+          const int e = n / 2;
           if (n % 2 == 0) {
             ra = __uint_as_float(v.v[e / 2][e % 2 * 2]);
             rb = __uint_as_float(v.v[e / 2][e % 2 * 2 + 1]);
-            t[x][0][e] = f32x2_to_bf16x2(ra, rb);
-            ra -= __uint_as_float(t[x][0][e] << 16);
-            rb -= __uint_as_float(t[x][0][e] & 0xffff0000u);
+            t[0][e] = f32x2_to_bf16x2(ra, rb);
+            ra -= __uint_as_float(t[0][e] << 16);
+            rb -= __uint_as_float(t[0][e] & 0xffff0000u);
           } else {
-            t[x][1][e] = f32x2_to_bf16x2(ra, rb);
-            ra -= __uint_as_float(t[x][1][e] << 16);
-            rb -= __uint_as_float(t[x][1][e] & 0xffff0000u);
-            t[x][2][e] = f32x2_to_bf16x2(ra, rb);
+            t[1][e] = f32x2_to_bf16x2(ra, rb);
+            ra -= __uint_as_float(t[1][e] << 16);
+            rb -= __uint_as_float(t[1][e] & 0xffff0000u);
+            t[2][e] = f32x2_to_bf16x2(ra, rb);
             lost |= __float_as_uint(ra) | __float_as_uint(rb);
           }
+        } else if (n < 11) {
+          u16* at = half == 0 ? to + sa.lds[0] : to + T::OPER + sb.lds[0];
+          *reinterpret_cast<u32x4*>(at + (n - 8) * T::PART) = t[n - 8];
+        } else if (half == 0) {
+          load_a(va[r], 0);
+        } else {
+          load_b(vb[r], 0);
         }
-        if (n >= 8 && n < 11) put(0, n - 8);
-        if (n == 11) get(0);
-        if (n >= 16 && n < 19) put(1, n - 16);
-        if (n == 19) get(1);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -439,7 +455,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
 #pragma unroll
     for (int j = 0; j < F; ++j)
 #pragma unroll
-      for (int i = 0; i < F; ++i)
+      for (int i = 0; i < FA; ++i)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           acc[j][i][v] += low[j][i][v];
@@ -448,15 +464,16 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
     if ((lost & 0xffffu) || !(z == 0.f)) *redo = 1;
     __syncthreads();
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(*redo), 0)) {
-      int ar[F], bc[F];                              // this lane's rows of A, columns of B
+      int ar[FA], bc[F];                             // this lane's rows of A, columns of B
+      const int c = lane % 32;
 #pragma unroll
-      for (int q = 0; q < F; ++q) {
-        const int c = lane % 32;
-        ar[q] = m0 + wm * T::RC + (AKC ? q * 32 + c : pair_block<F>(q, c / 16) * 16 + c % 16);
-        bc[q] = n0 + (BKC ? wn * T::RC + q * 32 + c
-                          : pair_block<F>(wn * (F / 2) + q % (F / 2), c / 16) * 16 + c % 16);
+      for (int i = 0; i < FA; ++i) ar[i] = out_row(i, c);
 #pragma unroll
-        for (int j = 0; j < F; ++j) clear(acc[j][q]);
+      for (int j = 0; j < F; ++j) {
+        bc[j] = n0 + (BKC ? wn * T::RC + j * 32 + c
+                          : pair_block<F>(wn * (F / 2) + j % (F / 2), c / 16) * 16 + c % 16);
+#pragma unroll
+        for (int i = 0; i < FA; ++i) clear(acc[j][i]);
       }
       for (int u = t0; u < t1; ++u) {
         const int sg = u / per_seg, kb = (u - sg * per_seg) * 32, ke = min(g.K, kb + 32);
@@ -464,9 +481,9 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
 #pragma unroll 1
         for (int kk = kb; kk < ke; kk += 2) {
           const int k = kk + lane / 32;
-          float av[F];
+          float av[FA];
 #pragma unroll
-          for (int i = 0; i < F; ++i)
+          for (int i = 0; i < FA; ++i)
             av[i] = k < ke && ar[i] < g.M
                         ? A[AKC ? (size_t)ar[i] * g.lda + k : (size_t)k * g.lda + ar[i]] : 0.f;
 #pragma unroll
@@ -475,7 +492,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
             const float bv = k < ke && bc[j] < g.N
                                  ? B[BKC ? (size_t)bc[j] * g.ldb + k : (size_t)k * g.ldb + bc[j]] : 0.f;
 #pragma unroll
-            for (int i = 0; i < F; ++i)
+            for (int i = 0; i < FA; ++i)
               acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(bv, av[i], acc[j][i], 0, 0, 0);
           }
         }
@@ -490,11 +507,11 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
   // runs of 32 columns or more.
   constexpr int CW = KIND == kDualDx ? 32 * F : 16 * F;      // columns of an output
   constexpr int P = 32 * F + 4;                              // pitch (floats)
-  static_assert(4 * 32 * P * sizeof(float) <= T::LDS_STAGES, "the stages' LDS holds the rows");
+  static_assert(T::THREADS / 64 * 32 * P * sizeof(float) <= T::LDS_STAGES, "the stages' LDS holds the rows");
   float* W = reinterpret_cast<float*>(lds) + wave * 32 * P;
   auto rows_out = [&](auto I) {
     constexpr int i = decltype(I)::value;
-    if constexpr (i < F) {
+    if constexpr (i < FA) {
 #pragma unroll
       for (int j = 0; j < F; ++j)
 #pragma unroll
@@ -518,7 +535,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
   }
   // One copy of the code that stores (the activations' is long); i is uniform.
 #pragma unroll 1
-  for (int i = 0; i < F; ++i) {
+  for (int i = 0; i < FA; ++i) {
     switch (i) {
       case 0: rows_out(Zero{}); break;
       case 1: rows_out(One{}); break;
@@ -529,7 +546,7 @@ __global__ __launch_bounds__(256, T::F == 4 || T::NP == 3 ? 1 : 2) void gemm_dua
 #pragma unroll
     for (int x = 0; x < CW / 8; ++x) {
       const int row = (x * 64 + lane) / (CW / 4), o = lane % (CW / 4) * 4;
-      const int m = m0 + wm * T::RC + (AKC ? i * 32 + row : pair_block<F>(i, row / 16) * 16 + row % 16);
+      const int m = out_row(i, row);
       if constexpr (KIND == kDualDx) {
         const int n = n0 + wn * T::RC + o;
         const f4 v = *reinterpret_cast<const f4*>(W + row * P + o);
