@@ -24,30 +24,75 @@
 
 namespace sb {
 
+// Up to three matrices: rows of `cols` elements, `ld` apart, to rows of cp (a multiple
+// of 8), zeros behind.  Matrix q has blocks block0[q] .. block0[q + 1] - 1.
+struct PackTasks {
+  const void* from[3];
+  void* to[3];
+  int rows[3], cols[3], ld[3], cp[3], block0[4];
+  int count;
+};
+template <class E>
+__device__ __forceinline__ void pack_rows(const PackTasks& t, int block) {
+  const int q = block >= t.block0[2] ? 2 : block >= t.block0[1] ? 1 : 0;
+  const int cols = t.cols[q], cp = t.cp[q];
+  const E* from = (const E*)t.from[q];
+  E* out = (E*)t.to[q];
+  const size_t quads = (size_t)t.rows[q] * (cp / 4);
+  const size_t step = (size_t)(t.block0[q + 1] - t.block0[q]) * 256;
+  for (size_t i = (size_t)(block - t.block0[q]) * 256 + threadIdx.x; i < quads; i += step) {
+    const size_t r = i / (cp / 4);
+    const int c = (int)(i - r * (cp / 4)) * 4;
+    f4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      v[e] = c + e < cols ? Elem<E>::load(from, r * t.ld[q] + c + e) : 0.f;
+    Elem<E>::store4(out + r * cp + c, v);
+  }
+}
+template <class E>
+__global__ __launch_bounds__(256) void gated_pack(PackTasks t) {
+  pack_rows<E>(t, blockIdx.x);
+}
+
 // da and du in rows of np (n rounded up to 8, zeros behind n).  fp32: da, then du,
 // m * np elements each.  bf16: three parts of each, part p of da at p * m * np, of du at
 // (3 + p) * m * np.  A block has 256 columns of `rows` rows, a lane four columns of
-// every fourth row, and leaves its columns' sums in sums [row block][2][np].
+// every fourth row.  Its columns' sums are db where it has all rows, else they go to
+// sums [row block][2][np].  The blocks behind pack the operands of the products to come
+// (each launch less is 4 us to a caller that does not capture its calls).
 static int act_rows(int m, int np) {
-  // Down to a row a wave where 32 would leave CUs idle (128 x 256: 10.2 -> 3 us).
+  // 32 rows, fewer where that would leave CUs idle (128 x 256: 10.2 -> 3.7 us), but all
+  // of them up to 32, which saves the launch that joins the sums.
   int rows = 32;
-  while (rows > 4 && (int64_t)((np + 255) / 256) * cdiv(m, rows) < 1024) rows /= 2;
+  if (m > rows)
+    while (rows > 4 && (int64_t)((np + 255) / 256) * cdiv(m, rows) < 1024) rows /= 2;
   return rows;
 }
+
+struct BiasSums {
+  float *sums, *db[2];                               // sums null: no db asked for, or db itself
+  int accumulate;
+};
 
 template <class E>
 __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int act,
                                                      const float* __restrict__ pre,
                                                      const E* __restrict__ dy, int ldy,
-                                                     E* __restrict__ d, float* __restrict__ sums,
-                                                     int rows, int vec) {
+                                                     E* __restrict__ d, BiasSums bias, int rows,
+                                                     int chunks, int vec, PackTasks packs) {
   __shared__ f4 part[2][4][64];
+  const int by = blockIdx.x % chunks, bx = blockIdx.x / chunks;
+  if (bx * 256 >= np) {
+    pack_rows<E>(packs, blockIdx.x - cdiv(np, 256) * chunks);
+    return;
+  }
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int c = blockIdx.x * 256 + lane * 4;
+  const int c = bx * 256 + lane * 4;
   const size_t mn = (size_t)m * n, plane = (size_t)m * np;
-  const int r1 = min(m, (int)(blockIdx.y + 1) * rows);
+  const int r1 = min(m, (by + 1) * rows);
   f4 s[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
-  for (int r = blockIdx.y * rows + w; r < r1 && c < np; r += 4) {
+  for (int r = by * rows + w; r < r1 && c < np; r += 4) {
     const float* pa = pre + (size_t)r * n + c;
     const E* pd = dy + (size_t)r * ldy + c;
     f4 a = f4{0.f, 0.f, 0.f, 0.f}, u = a, g = a;
@@ -98,13 +143,18 @@ __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int a
       }
     }
   }
-  if (!sums) return;
+  if (!bias.sums && !bias.db[0] && !bias.db[1]) return;
   part[0][w][lane] = s[0];
   part[1][w][lane] = s[1];
   __syncthreads();
-  if (w < 2 && c < np) {
-    const f4 t = (part[w][0][lane] + part[w][1][lane]) + (part[w][2][lane] + part[w][3][lane]);
-    *reinterpret_cast<f4*>(sums + ((size_t)blockIdx.y * 2 + w) * np + c) = t;
+  if (w >= 2 || c >= np) return;
+  const f4 t = (part[w][0][lane] + part[w][1][lane]) + (part[w][2][lane] + part[w][3][lane]);
+  if (bias.sums) {
+    *reinterpret_cast<f4*>(bias.sums + ((size_t)by * 2 + w) * np + c) = t;
+  } else if (float* db = w ? bias.db[1] : bias.db[0]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (c + e < n) db[c + e] = bias.accumulate ? db[c + e] + t[e] : t[e];
   }
 }
 
@@ -126,30 +176,6 @@ __global__ __launch_bounds__(256) void gated_bias_sums(const float* __restrict__
   if (w || c >= n || !db) return;
   v = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
   db[c] = accumulate ? db[c] + v : v;
-}
-
-// Up to three matrices (block rows): rows of `cols` elements, `ld` apart, to rows of cp (a
-// multiple of 8), zeros behind.
-struct PackTasks {
-  const void* from[3];
-  void* to[3];
-  int rows[3], cols[3], ld[3], cp[3];
-  int count;
-};
-template <class E>
-__global__ __launch_bounds__(256) void gated_pack(PackTasks t) {
-  const int q = blockIdx.y, cols = t.cols[q], cp = t.cp[q];
-  const E* from = (const E*)t.from[q];
-  E* out = (E*)t.to[q];
-  const size_t quads = (size_t)t.rows[q] * (cp / 4);
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < quads; i += (size_t)gridDim.x * 256) {
-    const size_t r = i / (cp / 4);
-    const int c = (int)(i - r * (cp / 4)) * 4;
-    f4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = c + e < cols ? Elem<E>::load(from, r * t.ld[q] + c + e) : 0.f;
-    Elem<E>::store4(out + r * cp + c, v);
-  }
 }
 
 // ---- few rows --------------------------------------------------------------
@@ -353,20 +379,20 @@ __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
 // 128-row ones and 1 to 64 ranges of the reduction.  A block costs its first stages and
 // its output, then a stage at a time, the more the fuller the chip is (power, L2); up to
 // three blocks of 128 rows share a CU, where one does not use it to the full; splits cost a
-// launch and their partials' traffic.  Fitted to 6400 timings of the three products of 700
-// shards in both types; the plan taken is 2.5 (bf16) or 1.2 % (fp32) slower than the best
-// one on average, half as slow again at most (61 rows of 640 by 128: 19 us for 13).
+// launch and their partials' traffic.  Fitted to 8000 timings of the three products of 900
+// shards in both types; the plan taken is 1.8 (bf16) or 1.2 % (fp32) slower than the best
+// one on average, at most half as slow again (80 rows of 1280 by 128: 21 us for 13).
 struct DualPlan { int f, mt, nt, splits, stages; size_t ws_bytes; };
 struct DualCost { double block, alone, full, shared; };
-static const DualCost kDualCost[3] = {{9.0, 0.56, 0.95, 0.95},         // bf16, 256 rows
+static const DualCost kDualCost[3] = {{9.0, 0.56, 0.92, 0.92},         // bf16, 256 rows
                                       {4.8, 0.253, 0.338, 0.30},      // bf16, 128 rows
-                                      {6.2, 1.25, 1.33, 1.33}};       // fp32, 128 rows
+                                      {4.1, 0.92, 1.09, 1.09}};       // fp32, 128 rows
 
 static DualPlan dual_plan(DualKind kind, bool b16, int M, int N, int K, int segs) {
   DualPlan best{};
   double best_t = 0;
   const int total = cdiv(K, 32) * segs;
-  const double tb_s = b16 ? 8.24 : 5.19;
+  const double tb_s = b16 ? 8.24 : 5.72;
   const double bytes = (double)M * cdiv(N, 4) * 4 * (kind == kDualDx ? 4 : 8);
   for (int f = b16 ? 4 : 2; f >= 2; f -= 2) {
     const DualCost& c = kDualCost[!b16 ? 2 : f == 4 ? 0 : 1];
@@ -438,9 +464,6 @@ static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStr
   }
 }
 
-static unsigned gated_blocks(size_t count) {
-  return (unsigned)std::min<size_t>((count + 255) / 256, 65536);
-}
 static int up8(int n) { return (n + 7) / 8 * 8; }
 static bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
@@ -514,23 +537,23 @@ static bool spans_meet(const Span* a, int na, const Span* b, int nb) {
   return false;
 }
 
-// The operands as the products take them: laid out anew (one launch) where `packs` says.
+// The operands as the products take them, and what has to be laid out anew for that.
 struct GatedOperands {
   const void *x, *w[2];
   int ldx, width, ldw;                               // width: of x's rows
+  PackTasks packs;
 };
 template <class E>
 static GatedOperands gated_operands(const sb_gated_desc* d, const void* x, const void* const* w,
-                                    bool pack_x, bool pack_w, char* ws, const GatedSpace& sp,
-                                    hipStream_t st) {
-  GatedOperands o{x, {w[0], w[1]}, d->ldx, d->k_in, d->n_shard};
-  PackTasks t{};
-  size_t most = 0;
+                                    bool pack_x, bool pack_w, char* ws, const GatedSpace& sp) {
+  GatedOperands o{x, {w[0], w[1]}, d->ldx, d->k_in, d->n_shard, {}};
+  PackTasks& t = o.packs;
   auto add = [&](const void* from, void* to, int rows, int cols, int ld, int cp) {
     const int q = t.count++;
     t.from[q] = from; t.to[q] = to;
     t.rows[q] = rows; t.cols[q] = cols; t.ld[q] = ld; t.cp[q] = cp;
-    most = std::max(most, (size_t)rows * cp / 4);
+    const int blocks = (int)std::min<size_t>(((size_t)rows * cp / 4 + 255) / 256, 4096);
+    for (int i = q + 1; i < 4; ++i) t.block0[i] = t.block0[q] + blocks;
   };
   if (pack_x) {
     o.x = ws + sp.x;
@@ -545,7 +568,6 @@ static GatedOperands gated_operands(const sb_gated_desc* d, const void* x, const
       add(w[q], to, d->k_in, d->n_shard, d->n_shard, o.ldw);
     }
   }
-  if (t.count) gated_pack<E><<<dim3(gated_blocks(most), t.count), 256, 0, st>>>(t);
   return o;
 }
 
@@ -577,7 +599,8 @@ static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* con
     else few_fwd<E, 8>(d, x, w, b, y, pre, vec, st);
     return;
   }
-  const GatedOperands o = gated_operands<E>(d, x, w, packs.x, packs.w, ws, sp, st);
+  const GatedOperands o = gated_operands<E>(d, x, w, packs.x, packs.w, ws, sp);
+  if (o.packs.count) gated_pack<E><<<o.packs.block0[3], 256, 0, st>>>(o.packs);
   DualArgs g{};
   g.a[0] = o.x; g.lda = o.ldx;
   g.b[0][0] = o.w[0]; g.b[1][0] = o.w[1]; g.ldb = o.ldw;
@@ -607,15 +630,17 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   const size_t plane = (size_t)d->m * np;
   E* parts = (E*)(ws + sp.d);
   float* split = (float*)(ws + sp.split);
-  float* sums = db[0] || db[1] ? (float*)(ws + sp.sums) : nullptr;
+  const BiasSums bias{(db[0] || db[1]) && chunks > 1 ? (float*)(ws + sp.sums) : nullptr,
+                      {db[0], db[1]}, accumulate};
   const int vec = d->n_shard % 4 == 0 && at16(pre) && d->ldy % 4 == 0 &&
                   ((uintptr_t)dy & (4 * sizeof(E) - 1)) == 0;
-  gated_act_bwd<E><<<dim3(cdiv(np, 256), chunks), 256, 0, st>>>(
-      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, sums, rows, vec);
-  if (sums)
-    gated_bias_sums<<<dim3(cdiv(d->n_shard, 64), 2), 256, 0, st>>>(sums, chunks, d->n_shard, np,
-                                                                   db[0], db[1], accumulate);
-  const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp, st);
+  const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp);
+  gated_act_bwd<E><<<(unsigned)(cdiv(np, 256) * chunks + o.packs.block0[3]), 256, 0, st>>>(
+      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, bias, rows, chunks, vec,
+      o.packs);
+  if (bias.sums)
+    gated_bias_sums<<<dim3(cdiv(d->n_shard, 64), 2), 256, 0, st>>>(bias.sums, chunks, d->n_shard,
+                                                                   np, db[0], db[1], accumulate);
   if (dx && d->m <= kFewRows) {
     const int wvec = d->n_shard % kFewWidth<E> == 0 && at16(w[0]) && at16(w[1]);
     const E *da = parts, *du = parts + NP * plane;

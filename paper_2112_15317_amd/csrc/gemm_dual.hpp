@@ -8,7 +8,7 @@
 // A block has 64 F rows (M) by 64 F columns: of FWD and DW 32 F columns of each
 // of the two outputs (N), so the operand they share is staged once and the gate's
 // value and the other projection's for one output element end in one wave.  Four
-// waves, 2 x 2 (fp32: eight, 4 x 2), each with FA x F blocks of 32 x 32 in registers.  The reduction is a
+// waves, 2 x 2, or eight, 4 x 2, each with FA x F blocks of 32 x 32 in registers.  The reduction is a
 // list of segments of equal length (DX: one per weight matrix; DW: one per bf16
 // part of da and du), each in stages of 32.
 //
@@ -42,15 +42,22 @@ struct DualTile {
   typedef E_ E;
   static constexpr int F = F_, NP = sizeof(E) == 4 ? 3 : 1;
   // Waves by rows and columns, a wave's blocks of rows (of columns F), its threads'
-  // pieces of an operand's stage.  fp32 takes eight waves of 32 rows: one wave issues
-  // an instruction every five or six cycles, and splitting the operands is as many as
-  // the MFMAs leave room for; two waves a SIMD issue twice as many (FP32_WAVES).
-  static constexpr int WM = NP == 3 ? 4 : 2, WN = 2, THREADS = 64 * WM * WN;
+  // pieces of an operand's stage.  Eight waves where two of them leave a SIMD room:
+  // one wave issues an instruction every five or six cycles, and what an MFMA has
+  // beside it (fp32: the splitting; bf16: reads, writes and their waits) is about as
+  // many as fit then.  fp32, 512 x 1024 outputs of 4096 k: 62 -> 55 us; bf16 256-row
+  // tiles: 8192 x 8192 of 4096 k 1123 -> 1085 us, 2048 x 2048 of 2048 k 61 -> 55 us.
+  // Tiles of 128 rows in bf16, two or three blocks a CU, keep four: LDS bounds them,
+  // and eight would read a half more.
+  static constexpr int WM = NP == 3 || F == 4 ? 4 : 2, WN = 2, THREADS = 64 * WM * WN;
   static constexpr int FA = 2 * F / WM, PCS = 256 * F / THREADS;
   static constexpr int BM = 64 * F, RC = 32 * F;     // rows; columns of a region
   static constexpr int PART = BM * 32, OPER = NP * PART;   // elements of an operand's stage
   static constexpr int STAGE = 2 * OPER;
-  static constexpr size_t LDS_STAGES = 3 * (size_t)STAGE * sizeof(u16);
+  static constexpr int PITCH = 32 * F + 4;           // floats a row of the output on its way
+  static constexpr size_t LDS_OUT = (size_t)THREADS / 64 * 32 * PITCH * sizeof(float);
+  static constexpr size_t LDS_IN = 3 * (size_t)STAGE * sizeof(u16);
+  static constexpr size_t LDS_STAGES = LDS_IN > LDS_OUT ? LDS_IN : LDS_OUT;
   static constexpr size_t LDS_BYTES = LDS_STAGES + (NP == 3 ? 16 : 0);   // the redo flag
   static_assert(LDS_BYTES <= 160 * 1024, "one block per CU");
 };
@@ -206,7 +213,7 @@ __device__ __forceinline__ f4 get_quad(const float* row, int n, int N) {
 
 // ACT: FWD's activation (its code is unrolled over all the outputs of a lane).
 template <class T, DualKind KIND, int ACT>
-__global__ __launch_bounds__(T::THREADS, T::F == 4 ? 1 : 2) void gemm_dual(DualArgs g) {
+__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual(DualArgs g) {
   extern __shared__ u16 lds[];
   typedef typename T::E E;
   constexpr int F = T::F, NP = T::NP, FA = T::FA, PCS = T::PCS;
@@ -350,21 +357,20 @@ __global__ __launch_bounds__(T::THREADS, T::F == 4 ? 1 : 2) void gemm_dual(DualA
     constexpr int c = decltype(P)::value, half = decltype(H)::value, r = decltype(W)::value;
     if constexpr (NP == 1) {
 #pragma unroll
-      for (int n = 0; n < F * F; ++n) {
-        const int j = n / F, i = n % F;
+      for (int n = 0; n < F * FA; ++n) {
+        const int j = n / FA, i = n % FA;
         acc[j][i] = mfma32(fb[c][j][0], fa[c][i][0], acc[j][i]);
         if (n == 0) read_b(c ^ 1, S, 0, 0, s);
-        else if (n <= F) read_a(c ^ 1, S, n - 1, 0, s);
-        else if (n < 2 * F) read_b(c ^ 1, S, n - F, 0, s);
+        else if (n <= FA) read_a(c ^ 1, S, n - 1, 0, s);
+        else if (n < FA + F) read_b(c ^ 1, S, n - FA, 0, s);
         if (half == 0) {
-          // The pieces of A, then of B: 2 F of them over the last MFMAs.
-          const int x = n - (F == 4 ? 8 : 0);
-          if (x >= 0 && x < F) {
+          const int x = n - (F * FA - 2 * PCS);
+          if (x >= 0 && x < PCS) {
             sa.store_one(to, va[r], x, lost);
             load_a(va[r], x);
-          } else if (x >= F && x < 2 * F) {
-            sb.store_one(to + T::OPER, vb[r], x - F, lost);
-            load_b(vb[r], x - F);
+          } else if (x >= PCS && x < 2 * PCS) {
+            sb.store_one(to + T::OPER, vb[r], x - PCS, lost);
+            load_b(vb[r], x - PCS);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -506,8 +512,7 @@ __global__ __launch_bounds__(T::THREADS, T::F == 4 ? 1 : 2) void gemm_dual(DualA
   // through the wave's own part of LDS (the last stage's reads are done), and out in
   // runs of 32 columns or more.
   constexpr int CW = KIND == kDualDx ? 32 * F : 16 * F;      // columns of an output
-  constexpr int P = 32 * F + 4;                              // pitch (floats)
-  static_assert(T::THREADS / 64 * 32 * P * sizeof(float) <= T::LDS_STAGES, "the stages' LDS holds the rows");
+  constexpr int P = T::PITCH;
   float* W = reinterpret_cast<float*>(lds) + wave * 32 * P;
   auto rows_out = [&](auto I) {
     constexpr int i = decltype(I)::value;

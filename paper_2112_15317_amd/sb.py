@@ -195,6 +195,13 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _on_current_device(t):
+    """The kernels of a call run on the current device's stream."""
+    import torch
+    if not isinstance(t, int) and t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError("tensors on %s, current device %d" % (t.device, torch.cuda.current_device()))
+
+
 def _ws(ws):
     if ws is None:
         return None, 0
@@ -360,6 +367,7 @@ def sb_gated_workspace_bytes(desc, pass_):
 def sb_gated_shard_fwd(desc, x, w_gate, w_up, b_gate, b_up, y, pre=None, ws=None, stream=None):
     """pre: fp32 [2][m][n_shard], kept for the backward, or None."""
     p, nb = _ws(ws)
+    _on_current_device(x)
     _check("sb_gated_shard_fwd", load().sb_gated_shard_fwd(
         ctypes.byref(desc), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(b_gate), _ptr(b_up), _ptr(y),
         _ptr(pre), p, nb, _stream(stream)))
@@ -368,6 +376,7 @@ def sb_gated_shard_fwd(desc, x, w_gate, w_up, b_gate, b_up, y, pre=None, ws=None
 def sb_gated_shard_bwd(desc, x, w_gate, w_up, pre, dy, dx_partial, dw_gate, dw_up, db_gate, db_up,
                        accumulate=False, ws=None, stream=None):
     p, nb = _ws(ws)
+    _on_current_device(x)
     _check("sb_gated_shard_bwd", load().sb_gated_shard_bwd(
         ctypes.byref(desc), _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(pre), _ptr(dy),
         _ptr(dx_partial), _ptr(dw_gate), _ptr(dw_up), _ptr(db_gate), _ptr(db_up),
@@ -525,6 +534,7 @@ class AdamwList:
             t.n = size
             t.grad_scale, t.decay = it.get("scale", 1.0), it.get("decay", 0.0)
             first = t.first + size
+        _on_current_device(items[0]["w"])
         need = load().sb_adamw_plan_bytes(n)
         self.plan = torch.empty((need,), dtype=torch.uint8, device=items[0]["w"].device)
         self.info = sb_adamw_plan()
@@ -551,6 +561,7 @@ def sb_adamw_update(alist, lr, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0,
                     stream=None):
     """step: the number of this update (from 1), or, with the int32 device
     counter steps_done, what is added to its value."""
+    _on_current_device(alist.plan)
     d = sb_adamw_desc(lr, beta1, beta2, eps, step, seed & 0xffffffff)
     _check("sb_adamw_update", load().sb_adamw_update(
         ctypes.byref(d), ctypes.byref(alist.info), alist.plan.data_ptr(), _counter(steps_done),
