@@ -331,10 +331,10 @@ __global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k,
 // [split][2][M] to y and pre; DW: to the two gradients; DX: [split][M] to dx.  W waves
 // share the splits of a quad (many splits are of small outputs, which are few lanes).
 template <DualKind KIND, class E, int W>
-__global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
+__device__ __forceinline__ void split_sum_block(const DualArgs& g, int act, int block, f4* lds) {
   constexpr int Q = KIND == kDualDx ? 1 : 2, LANES = 256 / W;
   const int quads = g.pitch / 4, w = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-  const size_t i = (size_t)blockIdx.x * LANES + lane;
+  const size_t i = (size_t)block * LANES + lane;
   const int m = (int)min(i / quads, (size_t)g.M - 1), n = (int)(i % quads) * 4;
   const size_t plane = (size_t)g.M * g.pitch, at = (size_t)m * g.pitch + n;
   const int per = cdiv(g.splits, W), s0 = min(w * per, g.splits), s1 = min(s0 + per, g.splits);
@@ -342,17 +342,14 @@ __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
 #pragma unroll
   for (int q = 0; q < Q; ++q) v[q] = split_sum4(g.part + q * plane, s0, s1, Q * plane, at);
   if constexpr (W > 1) {
-    __shared__ f4 part[W][Q][LANES];
 #pragma unroll
-    for (int q = 0; q < Q; ++q) part[w][q][lane] = v[q];
+    for (int q = 0; q < Q; ++q) lds[(w * Q + q) * LANES + lane] = v[q];
     __syncthreads();
     if (w) return;
 #pragma unroll
-    for (int q = 0; q < Q; ++q) {
-      v[q] = part[0][q][lane];
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
-      for (int u = 1; u < W; ++u) v[q] += part[u][q][lane];
-    }
+      for (int u = 1; u < W; ++u) v[q] += lds[(u * Q + q) * LANES + lane];
   }
   if (i / quads >= (size_t)g.M) return;
   if constexpr (KIND == kDualDx) {
@@ -373,6 +370,21 @@ __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
       put_quad(c, v[q], n, g.N);
     }
   }
+}
+template <DualKind KIND, class E, int W>
+__global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
+  __shared__ f4 lds[W > 1 ? 512 : 1];
+  split_sum_block<KIND, E, W>(g, act, blockIdx.x, lds);
+}
+// Of dx in the first blocks, of the weight gradients behind them.
+template <class E, int W>
+__global__ __launch_bounds__(256) void gated_split_sums(DualArgs dx, DualArgs dw, int first) {
+  __shared__ f4 lds[W > 1 ? 512 : 1];
+  if ((int)blockIdx.x < first) split_sum_block<kDualDx, E, W>(dx, 0, blockIdx.x, lds);
+  else split_sum_block<kDualDw, E, W>(dw, 0, (int)blockIdx.x - first, lds);
+}
+static int split_sum_blocks(const DualArgs& g, int w) {
+  return g.splits > 1 ? (int)(((size_t)g.M * (g.pitch / 4) + 256 / w - 1) / (256 / w)) : 0;
 }
 
 // Tile and split of a product: the least estimated time (us) over 256-row tiles (bf16) and
@@ -417,6 +429,59 @@ static DualPlan dual_plan(DualKind kind, bool b16, int M, int N, int K, int segs
   return best;
 }
 
+// The plan of dx and the weight gradients in one launch: one tile, splits of each.  The
+// time is the longest block's, or all blocks' over the chip where that is more (a
+// fifth more where a CU takes one block after the other).  One launch instead of two,
+// and one for both sums, saves a third of the time over 120 shards in both types (from
+// 2 % at 593 x 2752 x 1984 fp32 to 43 % at 248 x 1024 x 384 bf16); the plan taken is
+// 2 (fp32) or 7 % (bf16) slower than the best on average over 270, mostly where all
+// take 10 to 20 us.
+struct GradPlan { DualPlan dx, dw; };
+
+static GradPlan grad_plan(bool b16, int m, int k, int n) {
+  static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+  GradPlan best{};
+  double best_t = 0;
+  const int total[2] = {cdiv(n, 32) * 2, cdiv(m, 32) * (b16 ? 3 : 1)};
+  const double bytes[2] = {(double)m * cdiv(k, 4) * 16, (double)k * cdiv(n, 4) * 32};
+  const double tb_s = (b16 ? 8.24 : 5.72) * 1e6;
+  for (int f = b16 ? 4 : 2; f >= 2; f -= 2) {
+    const DualCost& c = kDualCost[!b16 ? 2 : f == 4 ? 0 : 1];
+    const int share = b16 && f == 2 ? 3 : 1;
+    const int mt[2] = {cdiv(m, 64 * f), cdiv(k, 64 * f)}, nt[2] = {cdiv(k, 64 * f), cdiv(n, 32 * f)};
+    for (int s0 : kSplits) {
+      for (int s1 : kSplits) {
+        const int s[2] = {s0, s1};
+        int stages[2];
+        double blocks[2], t = 0.0;
+        bool ok = true;
+        for (int q = 0; q < 2; ++q) {
+          stages[q] = cdiv(total[q], s[q]);
+          ok = ok && cdiv(total[q], stages[q]) == s[q];
+          blocks[q] = (double)mt[q] * nt[q] * s[q];
+          t += s[q] > 1 ? 4.5 + bytes[q] * (2 * s[q] + 1) / tb_s : bytes[q] / tb_s;
+        }
+        if (!ok) continue;
+        const double all = blocks[0] + blocks[1];
+        const double one = c.alone + (c.full - c.alone) * std::min(1.0, all / 256);
+        const double longest = c.block + std::max(stages[0], stages[1]) * one;
+        double sat = 0.0;
+        for (int q = 0; q < 2; ++q) sat += blocks[q] * (c.block / share + stages[q] * c.shared) / 256;
+        if (share == 1) sat *= 1.2;
+        t += all > 256 ? std::max(longest, sat) : longest;
+        if (best_t == 0 || t < best_t) {
+          best_t = t;
+          DualPlan* p[2] = {&best.dx, &best.dw};
+          for (int q = 0; q < 2; ++q)
+            *p[q] = DualPlan{f, mt[q], nt[q], s[q], stages[q],
+                             s[q] > 1 ? (size_t)s[q] * (size_t)bytes[q] : 0};
+        }
+      }
+    }
+  }
+  return best;
+}
+
 template <int F, DualKind KIND, int ACT, class E>
 static void dual_launch(const DualArgs& g, hipStream_t st) {
   typedef DualTile<F, E> T;
@@ -439,13 +504,18 @@ static void dual_launch_f(int f, const DualArgs& g, hipStream_t st) {
   dual_launch<2, KIND, ACT, E>(g, st);
 }
 
+static DualArgs dual_planned(DualArgs g, const DualPlan& p, float* part) {
+  g.mt = p.mt; g.nt = p.nt; g.splits = p.splits; g.stages = p.stages;
+  g.part = part;
+  g.pitch = cdiv(g.N, 4) * 4;
+  return g;
+}
+
 // One product under its plan: unsplit it ends in its outputs, split in the workspace,
 // from where gated_split_sum takes it.
 template <DualKind KIND, class E>
 static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStream_t st) {
-  g.mt = p.mt; g.nt = p.nt; g.splits = p.splits; g.stages = p.stages;
-  g.part = part;
-  g.pitch = cdiv(g.N, 4) * 4;
+  g = dual_planned(g, p, part);
   if (KIND != kDualFwd || p.splits > 1) {
     dual_launch_f<KIND, 0, E>(p.f, g, st);
   } else {
@@ -458,10 +528,39 @@ static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStr
     }
   }
   if (p.splits > 1) {
-    const size_t quads = (size_t)g.M * (g.pitch / 4);
-    if (p.splits < 8) gated_split_sum<KIND, E, 1><<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(g, act);
-    else gated_split_sum<KIND, E, 4><<<(unsigned)((quads + 63) / 64), 256, 0, st>>>(g, act);
+    if (p.splits < 8) gated_split_sum<KIND, E, 1><<<split_sum_blocks(g, 1), 256, 0, st>>>(g, act);
+    else gated_split_sum<KIND, E, 4><<<split_sum_blocks(g, 4), 256, 0, st>>>(g, act);
   }
+}
+
+template <int F, class E>
+static void grads_launch(const DualArgs& dx, const DualArgs& dw, hipStream_t st) {
+  typedef DualTile<F, E> T;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    (void)hipFuncSetAttribute((const void*)gemm_dual_grads<T>,
+                              hipFuncAttributeMaxDynamicSharedMemorySize, (int)T::LDS_BYTES);
+  });
+  const int first = dx.mt * dx.nt * dx.splits;
+  gemm_dual_grads<T><<<(unsigned)(first + dw.mt * dw.nt * dw.splits), T::THREADS, T::LDS_BYTES, st>>>(
+      dx, dw, first);
+}
+// dx and the weight gradients.  part: dx's partials, then the others'.
+template <class E>
+static void grads_run(DualArgs dx, DualArgs dw, const GradPlan& p, char* part, hipStream_t st) {
+  dx = dual_planned(dx, p.dx, (float*)part);
+  dw = dual_planned(dw, p.dw, (float*)(part + round_up(p.dx.ws_bytes, 256)));
+  bool wide = false;
+  if constexpr (sizeof(E) == 2) wide = p.dx.f == 4;
+  if constexpr (sizeof(E) == 2) {
+    if (wide) grads_launch<4, E>(dx, dw, st);
+  }
+  if (!wide) grads_launch<2, E>(dx, dw, st);
+  const int w = std::max(dx.splits, dw.splits) < 8 ? 1 : 4;
+  const int first = split_sum_blocks(dx, w), all = first + split_sum_blocks(dw, w);
+  if (all == 0) return;
+  if (w == 1) gated_split_sums<E, 1><<<all, 256, 0, st>>>(dx, dw, first);
+  else gated_split_sums<E, 4><<<all, 256, 0, st>>>(dx, dw, first);
 }
 
 static int up8(int n) { return (n + 7) / 8 * 8; }
@@ -478,11 +577,15 @@ static GatedPacks gated_packs(const sb_gated_desc* d, bool x_at16, bool w_at16) 
                     !few && (d->n_shard % 8 != 0 || !w_at16)};
 }
 
-static DualPlan gated_plan(const sb_gated_desc* d, DualKind kind) {
+static DualPlan gated_plan_fwd(const sb_gated_desc* d) {
+  return dual_plan(kDualFwd, d->dtype == SB_BF16, d->m, d->n_shard, d->k_in, 1);
+}
+static DualPlan gated_plan_dw(const sb_gated_desc* d) {   // without dx beside it
   const bool b16 = d->dtype == SB_BF16;
-  if (kind == kDualFwd) return dual_plan(kind, b16, d->m, d->n_shard, d->k_in, 1);
-  if (kind == kDualDx) return dual_plan(kind, b16, d->m, d->k_in, up8(d->n_shard), 2);
-  return dual_plan(kind, b16, d->k_in, d->n_shard, d->m, b16 ? 3 : 1);
+  return dual_plan(kDualDw, b16, d->k_in, d->n_shard, d->m, b16 ? 3 : 1);
+}
+static GradPlan gated_plan_grads(const sb_gated_desc* d) {
+  return grad_plan(d->dtype == SB_BF16, d->m, d->k_in, up8(d->n_shard));
 }
 
 // A workspace's parts, each from a multiple of 256 bytes on (offsets).
@@ -504,8 +607,15 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
   if (k.w) take(s.w, 2 * (size_t)d->k_in * np * es);
   const bool few = d->m <= kFewRows;
   size_t split = 0;
-  if (pass == SB_FC_FWD) split = few ? 0 : gated_plan(d, kDualFwd).ws_bytes;
-  else split = std::max(few ? 0 : gated_plan(d, kDualDx).ws_bytes, gated_plan(d, kDualDw).ws_bytes);
+  if (pass == SB_FC_FWD) {
+    split = few ? 0 : gated_plan_fwd(d).ws_bytes;
+  } else {
+    split = gated_plan_dw(d).ws_bytes;
+    if (!few) {
+      const GradPlan p = gated_plan_grads(d);
+      split = std::max(split, round_up(p.dx.ws_bytes, 256) + p.dw.ws_bytes);
+    }
+  }
   take(s.split, split);
   s.bytes = at;
   return s;
@@ -610,7 +720,7 @@ static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* con
   g.c[0] = y; g.ldc = d->ldy;
   g.bias[0] = b[0]; g.bias[1] = b[1];
   g.pre = pre;
-  dual_run<kDualFwd, E>(g, gated_plan(d, kDualFwd), d->act, (float*)(ws + sp.split), st);
+  dual_run<kDualFwd, E>(g, gated_plan_fwd(d), d->act, (float*)(ws + sp.split), st);
 }
 
 template <class E, int M>
@@ -629,7 +739,6 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   const int np = up8(d->n_shard), rows = act_rows(d->m, np), chunks = cdiv(d->m, rows);
   const size_t plane = (size_t)d->m * np;
   E* parts = (E*)(ws + sp.d);
-  float* split = (float*)(ws + sp.split);
   const BiasSums bias{(db[0] || db[1]) && chunks > 1 ? (float*)(ws + sp.sums) : nullptr,
                       {db[0], db[1]}, accumulate};
   const int vec = d->n_shard % 4 == 0 && at16(pre) && d->ldy % 4 == 0 &&
@@ -641,38 +750,40 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   if (bias.sums)
     gated_bias_sums<<<dim3(cdiv(d->n_shard, 64), 2), 256, 0, st>>>(bias.sums, chunks, d->n_shard,
                                                                    np, db[0], db[1], accumulate);
-  if (dx && d->m <= kFewRows) {
+  DualArgs gw{};
+  for (int p = 0; p < NP; ++p) {                     // the smallest parts first
+    gw.a[p] = o.x;
+    for (int q = 0; q < 2; ++q) gw.b[q][p] = parts + (NP * q + NP - 1 - p) * plane;
+  }
+  gw.lda = o.ldx; gw.ldb = np;
+  gw.M = d->k_in; gw.N = d->n_shard; gw.K = d->m; gw.segs = NP;
+  gw.a_bytes = (uint32_t)(((size_t)(d->m - 1) * gw.lda + o.width) * sizeof(E));
+  gw.b_bytes = (uint32_t)(plane * sizeof(E));
+  gw.c[0] = dw[0]; gw.c[1] = dw[1]; gw.ldc = d->n_shard;
+  gw.accumulate = accumulate;
+  if (dx && d->m > kFewRows) {
+    DualArgs gx{};
+    for (int q = 0; q < 2; ++q) {
+      gx.a[q] = parts + NP * q * plane;
+      gx.b[0][q] = gx.b[1][q] = o.w[q];
+    }
+    gx.lda = np; gx.ldb = o.ldw;                     // o.ldw is np: n_shard, or packed
+    gx.M = d->m; gx.N = d->k_in; gx.K = np; gx.segs = 2;
+    gx.a_bytes = (uint32_t)(plane * sizeof(E));
+    gx.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
+    gx.c[0] = dx; gx.ldc = d->ldx;
+    grads_run<E>(gx, gw, gated_plan_grads(d), ws + sp.split, st);
+    return;
+  }
+  if (dx) {
     const int wvec = d->n_shard % kFewWidth<E> == 0 && at16(w[0]) && at16(w[1]);
     const E *da = parts, *du = parts + NP * plane;
     if (d->m == 1) few_dx<E, 1>(d, np, da, du, w, dx, wvec, st);
     else if (d->m == 2) few_dx<E, 2>(d, np, da, du, w, dx, wvec, st);
     else if (d->m <= 4) few_dx<E, 4>(d, np, da, du, w, dx, wvec, st);
     else few_dx<E, 8>(d, np, da, du, w, dx, wvec, st);
-  } else if (dx) {
-    DualArgs g{};
-    for (int q = 0; q < 2; ++q) {
-      g.a[q] = parts + NP * q * plane;
-      g.b[0][q] = o.w[q];
-    }
-    g.lda = np; g.ldb = o.ldw;                       // o.ldw is np: n_shard, or packed
-    g.M = d->m; g.N = d->k_in; g.K = np; g.segs = 2;
-    g.a_bytes = (uint32_t)(plane * sizeof(E));
-    g.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
-    g.c[0] = dx; g.ldc = d->ldx;
-    dual_run<kDualDx, E>(g, gated_plan(d, kDualDx), 0, split, st);
   }
-  DualArgs g{};
-  for (int p = 0; p < NP; ++p) {                     // the smallest parts first
-    g.a[p] = o.x;
-    for (int q = 0; q < 2; ++q) g.b[q][p] = parts + (NP * q + NP - 1 - p) * plane;
-  }
-  g.lda = o.ldx; g.ldb = np;
-  g.M = d->k_in; g.N = d->n_shard; g.K = d->m; g.segs = NP;
-  g.a_bytes = (uint32_t)(((size_t)(d->m - 1) * g.lda + o.width) * sizeof(E));
-  g.b_bytes = (uint32_t)(plane * sizeof(E));
-  g.c[0] = dw[0]; g.c[1] = dw[1]; g.ldc = d->n_shard;
-  g.accumulate = accumulate;
-  dual_run<kDualDw, E>(g, gated_plan(d, kDualDw), 0, split, st);
+  dual_run<kDualDw, E>(gw, gated_plan_dw(d), 0, (float*)(ws + sp.split), st);
 }
 
 }  // namespace sb

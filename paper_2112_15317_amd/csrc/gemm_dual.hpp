@@ -212,9 +212,9 @@ __device__ __forceinline__ f4 get_quad(const float* row, int n, int N) {
 }
 
 // ACT: FWD's activation (its code is unrolled over all the outputs of a lane).
+// Block `block` of a product.
 template <class T, DualKind KIND, int ACT>
-__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual(DualArgs g) {
-  extern __shared__ u16 lds[];
+__device__ __forceinline__ void dual_block(const DualArgs& g, int block, u16* lds) {
   typedef typename T::E E;
   constexpr int F = T::F, NP = T::NP, FA = T::FA, PCS = T::PCS;
   constexpr bool AKC = KIND != kDualDw, BKC = KIND == kDualDx;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(T::THREADS, 2) void gemm_dual(DualArgs g) {
   // tiles take turns under one column tile, so what an XCD runs at a time is a
   // patch of the output that shares rows and columns in its L2.
   const int tiles = g.mt * g.nt, nb = tiles * g.splits;
-  int h = blockIdx.x;
+  int h = block;
   if (nb % 8 == 0) h = (h % 8) * (nb / 8) + h / 8;
   const int split = h / tiles;
   h -= split * tiles;
@@ -588,6 +588,21 @@ __global__ __launch_bounds__(T::THREADS, 2) void gemm_dual(DualArgs g) {
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
+}
+
+template <class T, DualKind KIND, int ACT>
+__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual(DualArgs g) {
+  extern __shared__ u16 lds[];
+  dual_block<T, KIND, ACT>(g, blockIdx.x, lds);
+}
+
+// Both products of the backward in one launch, the weight gradients' blocks behind dx's:
+// neither reads what the other writes, and small shards leave CUs idle in either.
+template <class T>
+__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual_grads(DualArgs dx, DualArgs dw, int first) {
+  extern __shared__ u16 lds[];
+  if ((int)blockIdx.x < first) dual_block<T, kDualDx, 0>(dx, blockIdx.x, lds);
+  else dual_block<T, kDualDw, 0>(dw, (int)blockIdx.x - first, lds);
 }
 
 }  // namespace sb
