@@ -364,8 +364,9 @@ typedef struct {
 } sb_gated_desc;
 
 /* Workspace bytes for `pass` (SB_FC_FWD, SB_FC_BWD); (size_t)-1 for an invalid
- * descriptor, and for one whose x, y or weights reach 2^31 bytes.  (size_t)-1 too where
- * 32 rows of x or of a weight do.  The workspace starts at a multiple of 16.
+ * descriptor, and for one whose x, y or weights, or 32 rows of x or of a weight, reach
+ * 2^31 bytes (the calls return SB_ERR_UNSUPPORTED).  The workspace starts at a multiple
+ * of 16.
  * Operands that no 16-byte access fits are laid out anew in it: those of odd sizes
  * or strides always have their room; for x or weights whose addresses are not
  * multiples of 16 the query is asked with SB_UNALIGNED (a call with less returns
@@ -388,7 +389,8 @@ sb_status sb_gated_shard_fwd(const sb_gated_desc *desc, const void *x,
  * and dw_up, db_up likewise with du (db_gate, db_up may each be NULL).  The
  * parameters' gradients are fp32 and carry da and du in full; SB_BF16's
  * dx_partial, itself rounded to bf16, is summed from da and du rounded to
- * bf16.  As for the FC shard the division by K is the optimiser's.
+ * bf16.  (da and du enter SB_BF16's weight gradients as sums of three bf16 parts, the
+ * last ones often 0, so an infinity in x makes its row of them NaN.)  As for the FC shard the division by K is the optimiser's.
  * The summation order is fixed: repeated calls give bit-identical results. */
 sb_status sb_gated_shard_bwd(const sb_gated_desc *desc, const void *x,
                              const void *w_gate, const void *w_up,
@@ -580,13 +582,15 @@ typedef struct { int tensors, moments, groups, blocks; } sb_adamw_plan;
  * every update is one launch however many there are.  plan: device memory of the
  * caller's, sb_adamw_plan_bytes(count) bytes (0 for a count outside 1 ..
  * SB_ADAMW_MAX_TENSORS), a multiple of 16, alive and unchanged as long as it is
- * used; info: host memory, filled by the call and handed to every update.
+ * used (a kernel on the stream writes it: an update on another stream has to be
+ * ordered behind that); info: host memory, filled by the call and handed to every update.
  * moments: 32 or 8.  The tensor array is host memory, read before the call returns.
  * SB_ERR_INVALID_ARG for bad counts or moments, scales or decays that are not
  * finite, NULL pointers, pointers that are not multiples of their elements' size, and
  * for an output (w, copy, moments, references, the plan) that overlaps any other
  * tensor of the call; gradients may overlap each other.  SB_ERR_WORKSPACE for a
- * short plan.  Nothing is enqueued then. */
+ * short plan, SB_ERR_UNSUPPORTED for 2^35 elements and more.  Nothing is enqueued
+ * then. */
 size_t sb_adamw_plan_bytes(int count);
 sb_status sb_adamw_make_plan(int moments, int count,
                              const sb_adamw_tensor *tensors, void *plan,
@@ -595,8 +599,8 @@ sb_status sb_adamw_make_plan(int moments, int count,
 
 /* One update of a plan's tensors.  Its number is step + *steps_done, where steps_done
  * is a device counter (int32, 0 at the start) for callers that replay the call from
- * a graph and advance it there with sb_adamw_advance, or NULL: then it is step.  The
- * counter must not be part of an output.  SB_ERR_INVALID_ARG for NULL pointers, an
+ * a graph and advance it there with sb_adamw_advance, or NULL: then it is step (sums
+ * below 1 count as 1).  The counter must not be part of an output.  SB_ERR_INVALID_ARG for NULL pointers, an
  * info that no plan has, betas outside [0, 1), values that are not finite, a negative
  * eps, step < 1. */
 typedef struct {

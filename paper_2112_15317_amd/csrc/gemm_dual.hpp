@@ -1,5 +1,6 @@
-// gemm_dual.hpp -- bf16 products of the gated FC shard (gated.hip) on the
-// 32x32x16 MFMA, two weight matrices (or their gradients) at a time.
+// gemm_dual.hpp -- products of the gated FC shard (gated.hip) on the 32x32x16 bf16
+// MFMA, two weight matrices (or their gradients) at a time; fp32 operands as three
+// bf16 parts each, six products of them (split_bf16.hpp).
 //
 //   FWD   gate and up = x * Wg, x * Wu          x [m][k], W [k][n]
 //   DX    sum over q of d_q * W_q^T             d_q [m][n], W_q [kin][n]
@@ -8,9 +9,9 @@
 // A block has 64 F rows (M) by 64 F columns: of FWD and DW 32 F columns of each
 // of the two outputs (N), so the operand they share is staged once and the gate's
 // value and the other projection's for one output element end in one wave.  Four
-// waves, 2 x 2, or eight, 4 x 2, each with FA x F blocks of 32 x 32 in registers.  The reduction is a
-// list of segments of equal length (DX: one per weight matrix; DW: one per bf16
-// part of da and du), each in stages of 32.
+// waves, 2 x 2, or eight, 4 x 2, each with FA x F blocks of 32 x 32 in registers.
+// The reduction is a list of segments of equal length (DX: one per weight matrix;
+// DW: one per bf16 part of da and du), each in stages of 32.
 //
 // Three stages are in LDS: while stage t is multiplied, t + 2 is written from
 // registers and t + 4 loaded, and t + 1 can already be read, so that the operands

@@ -199,9 +199,12 @@ def _stream_for(t, stream):
     """The stream of a call on t's device, which has to be the current one.  (Where torch
     has it, by its number alone: a Stream object takes 2.5 of the 9 us of a small call.)"""
     import torch
+    on = getattr(t, "device", None)          # of a tensor; None and addresses have none
+    if stream is not None and on is None:
+        return _stream(stream)
     dev = torch.cuda.current_device()
-    if not isinstance(t, int) and t.is_cuda and t.device.index != dev:
-        raise ValueError("tensors on %s, current device %d" % (t.device, dev))
+    if on is not None and on.index != dev:
+        raise ValueError("tensors on %s, current device %d" % (on, dev))
     if stream is None:
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         return raw(dev) if raw else torch.cuda.current_stream().cuda_stream
@@ -496,8 +499,10 @@ def sb_sgd_update(slist, lr, stream=None):
 # ------------------------------------------------------------------- AdamW --
 class AdamwList:
     """The plan of sb_adamw_update for a fixed list of tensors, in device memory
-    (sb_adamw_make_plan): built once, passed to every call (the tensors must
-    stay alive).  ``stream``: the stream that writes it.
+    (sb_adamw_make_plan): built once, passed to every call (the list and its
+    tensors must stay alive until the calls' kernels have run).  The plan is
+    written before this returns, so that any stream may use it; a list built
+    while its stream is captured is the graph's alone.
 
     items: dicts of a parameter ``w``, its gradient ``g`` (fp32) and moments
     ``m`` and ``v`` (fp32; or uint8, with their references ``m_top`` and
@@ -548,6 +553,8 @@ class AdamwList:
         _check("sb_adamw_make_plan", load().sb_adamw_make_plan(
             self.moments, n, self.tensors, _ptr(self.plan), need, ctypes.byref(self.info),
             _stream_for(self.plan, stream)))
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.synchronize()
 
 
 def adamw_moments(w, moments=32):

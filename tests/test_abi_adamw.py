@@ -110,6 +110,16 @@ def test_unpack_refusals(args):
     assert sb.load().sb_adamw_unpack(1000, *args, None) == BAD
 
 
+def test_more_elements_than_a_launch_has_lanes_for():
+    assert _plan([dict(n=1 << 35)]) == sb.SB_ERR_UNSUPPORTED
+    assert sb.load().sb_adamw_unpack(1 << 36, P, P, P, P, P, P, None) == sb.SB_ERR_UNSUPPORTED
+
+
+def test_none_is_refused_by_the_library():
+    with pytest.raises(RuntimeError):
+        sb.sb_adamw_advance(None, stream=0)
+
+
 def test_unpack_of_nothing():
     assert sb.load().sb_adamw_unpack(0, None, None, None, None, None, None, None) == sb.SB_OK
     assert sb.load().sb_adamw_unpack(1 << 40, P, P, P, P, P, P, None) == BAD

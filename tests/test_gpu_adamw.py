@@ -211,7 +211,78 @@ def test_on_another_stream():
     t = [torch.from_numpy(x).cuda() for x in (w, g, m, v)]
     torch.cuda.synchronize()
     s = torch.cuda.Stream()
-    sb.sb_adamw_update(sb.AdamwList([dict(w=t[0], g=t[1], m=t[2], v=t[3])]), LR, B1, B2, EPS, step=2,
-                       stream=s)
+    lst = sb.AdamwList([dict(w=t[0], g=t[1], m=t[2], v=t[3])])
+    sb.sb_adamw_update(lst, LR, B1, B2, EPS, step=2, stream=s)
     s.synchronize()
     _check_w(t[0].cpu().numpy(), w, g, m, v, 2, 1.0, 0.0)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_as_many_tensors_as_a_plan_takes(bits):
+    """512 tensors, some of no elements, in one update: as 512 updates of one."""
+    print_case("adamw_512", bits=bits)
+    sizes = [(37 * i) % 700 if i % 50 else 0 for i in range(sb.SB_ADAMW_MAX_TENSORS)]
+    first = np.concatenate([[0], np.cumsum(sizes)])
+    w, g, _, _ = (torch.from_numpy(a).cuda() for a in _inputs(int(first[-1]), 3))
+    out = []
+    for one in (False, True):
+        ws = [w[a:b].clone() for a, b in zip(first, first[1:])]
+        items = [dict(w=x, g=g[a:a + x.numel()], first=int(a), decay=0.1, **sb.adamw_moments(x, bits))
+                 for x, a in zip(ws, first)]
+        lists = [sb.AdamwList([it]) for it in items] if one else [sb.AdamwList(items)]
+        for t in (1, 2):
+            for lst in lists:
+                sb.sb_adamw_update(lst, LR, B1, B2, EPS, step=t, seed=7)
+        torch.cuda.synchronize()
+        out.append(items)
+    for a, b in zip(*out):
+        for key in ("w", "m", "v"):
+            assert torch.equal(a[key], b[key]), key
+    assert not torch.equal(torch.cat([it["w"] for it in out[0]]), w)
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-8])
+def test_small_second_moments(eps):
+    """Roots of values down to fp32's subnormal ones, with an eps that hides them and
+    without: a move of lr m' / (root + eps), roundings as in _check_w, and in v' half
+    a step of the smallest subnormal value for each of its three products and sums."""
+    print_case("adamw_small_v", eps=eps)
+    n = 1000
+    rng = np.random.default_rng(17)
+    f = np.float32
+    v = (2.0 ** rng.uniform(-140, -20, n)).astype(f)
+    m = (np.sqrt(v.astype(np.float64)) * rng.normal(size=n)).astype(f)
+    w, g = np.zeros(n, f), np.zeros(n, f)
+    t = [torch.from_numpy(x).cuda() for x in (w, g, m, v)]
+    lst = sb.AdamwList([dict(w=t[0], g=t[1], m=t[2], v=t[3])])
+    sb.sb_adamw_update(lst, LR, B1, B2, eps, step=5)
+    rw, _, rv = A.update(w, g, m, v, 5, LR, B1, B2, eps)
+    got = t[0].cpu().numpy()
+    assert np.isfinite(got).all()
+    # An error d of v' moves its root by d / (2 root), so the quotient by d / (2 v').
+    far = np.abs(got - rw) / np.abs(rw)
+    assert np.all(far <= 17 * U + 3 * 2.0 ** -150 / (2 * rv))
+
+
+def test_lists_of_a_plan_used_on_several_streams():
+    """A list is ready for any stream when it is made; two lists, a stream each."""
+    print_case("adamw_streams")
+    n = 40000
+    made = []
+    for i in range(2):
+        w, g, m, v = _inputs(n, 60 + i)
+        t = [torch.from_numpy(x).cuda() for x in (w, g, m, v)]
+        made.append((t, [x.clone() for x in t]))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    lists = [sb.AdamwList([dict(zip("wgmv", t))]) for t, _ in made]
+    for step in (1, 2, 3):
+        for lst, s in zip(lists, streams):
+            sb.sb_adamw_update(lst, LR, B1, B2, EPS, step=step, stream=s)
+    torch.cuda.synchronize()
+    for t, u in made:
+        lst = sb.AdamwList([dict(zip("wgmv", u))])
+        for step in (1, 2, 3):
+            sb.sb_adamw_update(lst, LR, B1, B2, EPS, step=step)
+        torch.cuda.synchronize()
+        for a, b in zip(t, u):
+            assert torch.equal(a, b)

@@ -262,3 +262,114 @@ def test_captured_and_concurrent_calls(dtype):
     for case in (c, e):
         for t in ALL:
             assert torch.equal(case.d[t], want[t]), t
+
+
+# Shapes whose products take the 256-row tiles, unsplit and split over the reduction,
+# with tails in all three dimensions: (m, k, n), whether dx is asked for.
+WIDE = [(2829, 205, 2139, True), (410, 1830, 4144, True), (314, 1173, 3339, False),
+        (604, 414, 4212, False), (539, 5700, 854, True), (4010, 907, 968, True),
+        (431, 1922, 2534, True), (3771, 203, 5514, True)]
+
+
+@pytest.mark.parametrize("shape", WIDE, ids=lambda s: "x".join(map(str, s[:3])))
+def test_wide_tiles(shape):
+    print_case("gated_wide", shape=shape)
+    c = Case("silu", "bf16", *shape[:3], xs=2, ys=1)
+    c.fwd()
+    c.bwd(dx=shape[3])
+    names = ALL if shape[3] else tuple(t for t in ALL if t != "dx")
+    c.check(names)
+    c.untouched(names + ("pre",))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(9, 4000, 30), (300, 2000, 70), (520, 300, 40), (64, 64, 4000),
+                                   (3000, 72, 72)], ids=lambda s: "x".join(map(str, s)))
+def test_many_splits(shape, dtype):
+    """Small outputs of long reductions: up to 63 splits, joined by four waves."""
+    print_case("gated_splits", shape=shape, dtype=dtype)
+    c = Case("gelu", dtype, *shape)
+    c.fwd()
+    c.bwd()
+    c.check(ALL)
+    c.bwd(dx=False)
+    c.check(tuple(t for t in ALL if t != "dx"))
+    c.untouched(ALL + ("pre",))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m", [1, 3, 8, 9, 100, 520])
+@pytest.mark.parametrize("stride", [8, 5])
+def test_what_lies_between_the_rows_is_not_read(m, stride, dtype):
+    """NaN between the rows of x and dy, at strides that are taken as they are and
+    at such that are laid out anew."""
+    print_case("gated_between", m=m, stride=stride, dtype=dtype)
+    c = Case("gelu_tanh", dtype, m, 136, 72, xs=stride, ys=stride)
+    c.d["x"][:, c.k:] = float("nan")
+    c.d["dy"][:, c.n:] = float("nan")
+    c.fwd()
+    c.bwd()
+    c.check(ALL)
+    c.bwd(dx=False, db=False)
+    c.check(("dwg", "dwu"))
+    c.untouched(ALL + ("pre",))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_special_values_of_few_rows(dtype):
+    print_case("gated_special_few", dtype=dtype)
+    c = Case("sigmoid", dtype, 5, 264, 100, bias=False)
+    c.x[1, 7], c.x[3, 100] = np.inf, np.nan
+    c.d["x"].copy_(torch.from_numpy(c.x))
+    c.fwd()
+    c.dy[4, 9] = np.nan
+    c.d["dy"].copy_(torch.from_numpy(c.dy))
+    torch.cuda.synchronize()
+    got = c.get("y")
+    assert np.isnan(got[3]).all() and not np.isfinite(got[1]).any()
+    c.x[[1, 3]] = 0
+    rest = [0, 2, 4]
+    c.dy[4, 9] = 0
+    assert np.all(np.abs(got[rest] - c.ref()["y"][rest]) <= c.bound()["y"][rest])
+    c.d["x"].copy_(torch.from_numpy(c.x))
+    c.fwd()                                                # a finite pre
+    c.bwd()
+    torch.cuda.synchronize()
+    dx = c.get("dx")
+    assert np.isnan(dx[4]).all()
+    ok = slice(0, 4)
+    assert np.all(np.abs(dx[ok] - c.ref()["dx"][ok]) <= c.bound()["dx"][ok])
+    for t in ("dwg", "dwu", "dbg", "dbu"):
+        bad = np.isnan(c.get(t))
+        assert bad[..., 9].all() and not np.delete(bad, 9, axis=-1).any(), t
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_two_graphs_with_one_workspace(dtype):
+    """Two captured steps that share a workspace, replayed in turn on one stream."""
+    print_case("gated_two_graphs", dtype=dtype)
+    cases = [Case("silu", dtype, 200, 160, 120, seed=s) for s in (1, 2)]
+    cases[1].ws = cases[0].ws
+    want, graphs = [], []
+    for c in cases:
+        c.fwd()
+        c.bwd()
+        torch.cuda.synchronize()
+        want.append({t: c.d[t].clone() for t in ALL})
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.fwd()
+            c.bwd()
+        graphs.append(g)
+    for _ in range(3):
+        for c in cases:
+            for t in ALL:
+                c.d[t].fill_(5)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            for t, width in (("y", c.n), ("dx", c.k), ("dwg", c.n), ("dwu", c.n)):
+                assert torch.equal(c.d[t][:, :width], w[t][:, :width]), t
+            for t in ("dbg", "dbu"):
+                assert torch.equal(c.d[t], w[t]), t
