@@ -41,13 +41,13 @@ __device__ __forceinline__ void pack_rows(const PackTasks& t, int block) {
   const size_t quads = (size_t)t.rows[q] * (cp / 4);
   const size_t step = (size_t)(t.block0[q + 1] - t.block0[q]) * 256;
   for (size_t i = (size_t)(block - t.block0[q]) * 256 + threadIdx.x; i < quads; i += step) {
-    const size_t r = i / (cp / 4);
-    const int c = (int)(i - r * (cp / 4)) * 4;
+    const uint32_t r = (uint32_t)i / (uint32_t)(cp / 4);     // (quads are below 2^29)
+    const int c = (int)((uint32_t)i - r * (cp / 4)) * 4;
     f4 v;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      v[e] = c + e < cols ? Elem<E>::load(from, r * t.ld[q] + c + e) : 0.f;
-    Elem<E>::store4(out + r * cp + c, v);
+      v[e] = c + e < cols ? Elem<E>::load(from, (size_t)r * t.ld[q] + c + e) : 0.f;
+    Elem<E>::store4(out + (size_t)r * cp + c, v);
   }
 }
 template <class E>
@@ -69,11 +69,6 @@ static int act_rows(int m, int np) {
     while (rows > 4 && (int64_t)((np + 255) / 256) * cdiv(m, rows) < 1024) rows /= 2;
   return rows;
 }
-
-struct BiasSums {
-  float *sums, *db[2];                               // sums null: no db asked for, or db itself
-  int accumulate;
-};
 
 template <class E>
 __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int act,
@@ -156,26 +151,6 @@ __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int a
     for (int e = 0; e < 4; ++e)
       if (c + e < n) db[c + e] = bias.accumulate ? db[c + e] + t[e] : t[e];
   }
-}
-
-// db of the gate (block row 0) and the other projection: a wave has 64 columns and
-// every fourth of the row blocks' sums.
-__global__ __launch_bounds__(256) void gated_bias_sums(const float* __restrict__ sums, int chunks,
-                                                       int n, int np, float* db_gate, float* db_up,
-                                                       int accumulate) {
-  __shared__ float part[4][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int c = blockIdx.x * 64 + lane, q = blockIdx.y;
-  float v = 0.f;
-  if (c < n)
-#pragma unroll 8
-    for (int r = w; r < chunks; r += 4) v += sums[((size_t)r * 2 + q) * np + c];
-  part[w][lane] = v;
-  __syncthreads();
-  float* db = q ? db_up : db_gate;
-  if (w || c >= n || !db) return;
-  v = (part[0][lane] + part[1][lane]) + (part[2][lane] + part[3][lane]);
-  db[c] = accumulate ? db[c] + v : v;
 }
 
 // ---- few rows --------------------------------------------------------------
@@ -333,9 +308,10 @@ __global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k,
 template <DualKind KIND, class E, int W>
 __device__ __forceinline__ void split_sum_block(const DualArgs& g, int act, int block, f4* lds) {
   constexpr int Q = KIND == kDualDx ? 1 : 2, LANES = 256 / W;
-  const int quads = g.pitch / 4, w = threadIdx.x / LANES, lane = threadIdx.x % LANES;
-  const size_t i = (size_t)block * LANES + lane;
-  const int m = (int)min(i / quads, (size_t)g.M - 1), n = (int)(i % quads) * 4;
+  const uint32_t quads = g.pitch / 4;
+  const int w = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const uint32_t i = (uint32_t)block * LANES + lane, row = i / quads;   // (below 2^30)
+  const int m = (int)min(row, (uint32_t)g.M - 1), n = (int)(i - row * quads) * 4;
   const size_t plane = (size_t)g.M * g.pitch, at = (size_t)m * g.pitch + n;
   const int per = cdiv(g.splits, W), s0 = min(w * per, g.splits), s1 = min(s0 + per, g.splits);
   f4 v[Q];
@@ -351,7 +327,7 @@ __device__ __forceinline__ void split_sum_block(const DualArgs& g, int act, int 
 #pragma unroll
       for (int u = 1; u < W; ++u) v[q] += lds[(u * Q + q) * LANES + lane];
   }
-  if (i / quads >= (size_t)g.M) return;
+  if (row >= (uint32_t)g.M) return;
   if constexpr (KIND == kDualDx) {
     put_quad((E*)g.c[0] + (size_t)m * g.ldc, v[0], n, g.N);
   } else if constexpr (KIND == kDualFwd) {
@@ -371,10 +347,10 @@ __device__ __forceinline__ void split_sum_block(const DualArgs& g, int act, int 
     }
   }
 }
-template <DualKind KIND, class E, int W>
+template <class E, int W>
 __global__ __launch_bounds__(256) void gated_split_sum(DualArgs g, int act) {
   __shared__ f4 lds[W > 1 ? 512 : 1];
-  split_sum_block<KIND, E, W>(g, act, blockIdx.x, lds);
+  split_sum_block<kDualFwd, E, W>(g, act, blockIdx.x, lds);
 }
 // Of dx in the first blocks, of the weight gradients behind them.
 template <class E, int W>
@@ -482,26 +458,20 @@ static GradPlan grad_plan(bool b16, int m, int k, int n) {
   return best;
 }
 
-template <int F, DualKind KIND, int ACT, class E>
-static void dual_launch(const DualArgs& g, hipStream_t st) {
+template <int F, int ACT, class E>
+static void fwd_launch(const DualArgs& g, hipStream_t st) {
   typedef DualTile<F, E> T;
   static std::once_flag once;
   std::call_once(once, [] {
-    (void)hipFuncSetAttribute((const void*)gemm_dual<T, KIND, ACT>,
+    (void)hipFuncSetAttribute((const void*)gemm_dual_fwd<T, ACT>,
                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)T::LDS_BYTES);
   });
-  gemm_dual<T, KIND, ACT>
-      <<<(unsigned)(g.mt * g.nt * g.splits), T::THREADS, T::LDS_BYTES, st>>>(g);
+  gemm_dual_fwd<T, ACT><<<(unsigned)(g.mt * g.nt * g.splits), T::THREADS, T::LDS_BYTES, st>>>(g);
 }
-template <DualKind KIND, int ACT, class E>
-static void dual_launch_f(int f, const DualArgs& g, hipStream_t st) {
-  if constexpr (sizeof(E) == 2) {
-    if (f == 4) {
-      dual_launch<4, KIND, ACT, E>(g, st);
-      return;
-    }
-  }
-  dual_launch<2, KIND, ACT, E>(g, st);
+template <int ACT, class E>
+static void fwd_launch_f(int f, const DualArgs& g, hipStream_t st) {
+  if (sizeof(E) == 2 && f == 4) fwd_launch<sizeof(E) == 2 ? 4 : 2, ACT, E>(g, st);
+  else fwd_launch<2, ACT, E>(g, st);
 }
 
 static DualArgs dual_planned(DualArgs g, const DualPlan& p, float* part) {
@@ -511,30 +481,26 @@ static DualArgs dual_planned(DualArgs g, const DualPlan& p, float* part) {
   return g;
 }
 
-// One product under its plan: unsplit it ends in its outputs, split in the workspace,
-// from where gated_split_sum takes it.
-template <DualKind KIND, class E>
-static void dual_run(DualArgs g, const DualPlan& p, int act, float* part, hipStream_t st) {
+// The forward under its plan: unsplit it ends in its outputs, split in the workspace,
+// from where gated_split_sum takes it (whichever activation the product was built for).
+template <class E>
+static void fwd_run(DualArgs g, const DualPlan& p, int act, float* part, hipStream_t st) {
   g = dual_planned(g, p, part);
-  if (KIND != kDualFwd || p.splits > 1) {
-    dual_launch_f<KIND, 0, E>(p.f, g, st);
-  } else {
-    switch (act) {
-      case SB_ACT_SIGMOID: dual_launch_f<kDualFwd, SB_ACT_SIGMOID, E>(p.f, g, st); break;
-      case SB_ACT_SILU: dual_launch_f<kDualFwd, SB_ACT_SILU, E>(p.f, g, st); break;
-      case SB_ACT_GELU: dual_launch_f<kDualFwd, SB_ACT_GELU, E>(p.f, g, st); break;
-      case SB_ACT_GELU_TANH: dual_launch_f<kDualFwd, SB_ACT_GELU_TANH, E>(p.f, g, st); break;
-      default: dual_launch_f<kDualFwd, SB_ACT_RELU, E>(p.f, g, st);
-    }
+  switch (p.splits > 1 ? SB_ACT_RELU : act) {
+    case SB_ACT_SIGMOID: fwd_launch_f<SB_ACT_SIGMOID, E>(p.f, g, st); break;
+    case SB_ACT_SILU: fwd_launch_f<SB_ACT_SILU, E>(p.f, g, st); break;
+    case SB_ACT_GELU: fwd_launch_f<SB_ACT_GELU, E>(p.f, g, st); break;
+    case SB_ACT_GELU_TANH: fwd_launch_f<SB_ACT_GELU_TANH, E>(p.f, g, st); break;
+    default: fwd_launch_f<SB_ACT_RELU, E>(p.f, g, st);
   }
   if (p.splits > 1) {
-    if (p.splits < 8) gated_split_sum<KIND, E, 1><<<split_sum_blocks(g, 1), 256, 0, st>>>(g, act);
-    else gated_split_sum<KIND, E, 4><<<split_sum_blocks(g, 4), 256, 0, st>>>(g, act);
+    if (p.splits < 8) gated_split_sum<E, 1><<<split_sum_blocks(g, 1), 256, 0, st>>>(g, act);
+    else gated_split_sum<E, 4><<<split_sum_blocks(g, 4), 256, 0, st>>>(g, act);
   }
 }
 
 template <int F, class E>
-static void grads_launch(const DualArgs& dx, const DualArgs& dw, hipStream_t st) {
+static void grads_launch(const DualArgs& dx, const DualArgs& dw, const BiasSums& bias, hipStream_t st) {
   typedef DualTile<F, E> T;
   static std::once_flag once;
   std::call_once(once, [] {
@@ -542,16 +508,18 @@ static void grads_launch(const DualArgs& dx, const DualArgs& dw, hipStream_t st)
                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)T::LDS_BYTES);
   });
   const int first = dx.mt * dx.nt * dx.splits;
-  gemm_dual_grads<T><<<(unsigned)(first + dw.mt * dw.nt * dw.splits), T::THREADS, T::LDS_BYTES, st>>>(
-      dx, dw, first);
+  const int last = first + dw.mt * dw.nt * dw.splits, sums = bias.sums ? cdiv(bias.n, 64) : 0;
+  gemm_dual_grads<T><<<(unsigned)(last + sums), T::THREADS, T::LDS_BYTES, st>>>(dx, dw, first, bias);
 }
-// dx and the weight gradients.  part: dx's partials, then the others'.
+// dx (not with an empty plan) and the weight gradients, and the bias gradients where there
+// are sums of them to join.  part: dx's partials, then the others'.
 template <class E>
-static void grads_run(DualArgs dx, DualArgs dw, const GradPlan& p, char* part, hipStream_t st) {
+static void grads_run(DualArgs dx, DualArgs dw, const BiasSums& bias, const GradPlan& p, char* part,
+                      hipStream_t st) {
   dx = dual_planned(dx, p.dx, (float*)part);
   dw = dual_planned(dw, p.dw, (float*)(part + round_up(p.dx.ws_bytes, 256)));
-  if (sizeof(E) == 2 && p.dx.f == 4) grads_launch<sizeof(E) == 2 ? 4 : 2, E>(dx, dw, st);
-  else grads_launch<2, E>(dx, dw, st);
+  if (sizeof(E) == 2 && p.dw.f == 4) grads_launch<sizeof(E) == 2 ? 4 : 2, E>(dx, dw, bias, st);
+  else grads_launch<2, E>(dx, dw, bias, st);
   const int w = std::max(dx.splits, dw.splits) < 8 ? 1 : 4;
   const int first = split_sum_blocks(dx, w), all = first + split_sum_blocks(dw, w);
   if (all == 0) return;
@@ -716,7 +684,7 @@ static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* con
   g.c[0] = y; g.ldc = d->ldy;
   g.bias[0] = b[0]; g.bias[1] = b[1];
   g.pre = pre;
-  dual_run<kDualFwd, E>(g, gated_plan_fwd(d), d->act, (float*)(ws + sp.split), st);
+  fwd_run<E>(g, gated_plan_fwd(d), d->act, (float*)(ws + sp.split), st);
 }
 
 template <class E, int M>
@@ -736,16 +704,13 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   const size_t plane = (size_t)d->m * np;
   E* parts = (E*)(ws + sp.d);
   const BiasSums bias{(db[0] || db[1]) && chunks > 1 ? (float*)(ws + sp.sums) : nullptr,
-                      {db[0], db[1]}, accumulate};
+                      {db[0], db[1]}, d->n_shard, np, chunks, accumulate};
   const int vec = d->n_shard % 4 == 0 && at16(pre) && d->ldy % 4 == 0 &&
                   ((uintptr_t)dy & (4 * sizeof(E) - 1)) == 0;
   const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp);
   gated_act_bwd<E><<<(unsigned)(cdiv(np, 256) * chunks + o.packs.block0[3]), 256, 0, st>>>(
       d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, bias, rows, chunks, vec,
       o.packs);
-  if (bias.sums)
-    gated_bias_sums<<<dim3(cdiv(d->n_shard, 64), 2), 256, 0, st>>>(bias.sums, chunks, d->n_shard,
-                                                                   np, db[0], db[1], accumulate);
   DualArgs gw{};
   for (int p = 0; p < NP; ++p) {                     // the smallest parts first
     gw.a[p] = o.x;
@@ -768,7 +733,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
     gx.a_bytes = (uint32_t)(plane * sizeof(E));
     gx.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
     gx.c[0] = dx; gx.ldc = d->ldx;
-    grads_run<E>(gx, gw, gated_plan_grads(d), ws + sp.split, st);
+    grads_run<E>(gx, gw, bias, gated_plan_grads(d), ws + sp.split, st);
     return;
   }
   if (dx) {
@@ -779,7 +744,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
     else if (d->m <= 4) few_dx<E, 4>(d, np, da, du, w, dx, wvec, st);
     else few_dx<E, 8>(d, np, da, du, w, dx, wvec, st);
   }
-  dual_run<kDualDw, E>(gw, gated_plan_dw(d), 0, (float*)(ws + sp.split), st);
+  grads_run<E>(DualArgs{}, gw, bias, GradPlan{{}, gated_plan_dw(d)}, ws + sp.split, st);
 }
 
 }  // namespace sb

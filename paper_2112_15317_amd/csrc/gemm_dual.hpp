@@ -591,19 +591,47 @@ __device__ __forceinline__ void dual_block(const DualArgs& g, int block, u16* ld
   }
 }
 
-template <class T, DualKind KIND, int ACT>
-__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual(DualArgs g) {
+template <class T, int ACT>
+__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual_fwd(DualArgs g) {
   extern __shared__ u16 lds[];
-  dual_block<T, KIND, ACT>(g, blockIdx.x, lds);
+  dual_block<T, kDualFwd, ACT>(g, blockIdx.x, lds);
 }
 
-// Both products of the backward in one launch, the weight gradients' blocks behind dx's:
-// neither reads what the other writes, and small shards leave CUs idle in either.
+// The bias gradients from `chunks` row blocks' sums ([chunk][2][np]): 64 columns of both
+// a block, every second or fourth row block a wave (of four or eight).
+struct BiasSums {
+  float *sums, *db[2];                               // sums null: nothing to join
+  int n, np, chunks, accumulate;
+};
+template <int THREADS>
+__device__ __forceinline__ void bias_sum_block(const BiasSums& b, int block, float* part) {
+  constexpr int W = THREADS / 128;                   // waves a gradient
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, q = w / W;
+  const int c = block * 64 + lane;
+  float v = 0.f;
+  if (c < b.n)
+#pragma unroll 8
+    for (int r = w % W; r < b.chunks; r += W) v += b.sums[((size_t)r * 2 + q) * b.np + c];
+  part[w * 64 + lane] = v;
+  __syncthreads();
+  float* db = q ? b.db[1] : b.db[0];
+  if (w % W || c >= b.n || !db) return;
+#pragma unroll
+  for (int u = 1; u < W; ++u) v += part[(w + u) * 64 + lane];
+  db[c] = b.accumulate ? db[c] + v : v;
+}
+
+// The products of the backward in one launch, the weight gradients' blocks behind dx's
+// (none: first = 0), behind them the bias gradients': none reads what another writes, and
+// small shards leave CUs idle in each.
 template <class T>
-__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual_grads(DualArgs dx, DualArgs dw, int first) {
+__global__ __launch_bounds__(T::THREADS, 2) void gemm_dual_grads(DualArgs dx, DualArgs dw, int first,
+                                                                 BiasSums bias) {
   extern __shared__ u16 lds[];
-  if ((int)blockIdx.x < first) dual_block<T, kDualDx, 0>(dx, blockIdx.x, lds);
-  else dual_block<T, kDualDw, 0>(dw, (int)blockIdx.x - first, lds);
+  const int block = blockIdx.x, last = first + dw.mt * dw.nt * dw.splits;
+  if (block < first) dual_block<T, kDualDx, 0>(dx, block, lds);
+  else if (block < last) dual_block<T, kDualDw, 0>(dw, block - first, lds);
+  else bias_sum_block<T::THREADS>(bias, block - last, reinterpret_cast<float*>(lds));
 }
 
 }  // namespace sb
