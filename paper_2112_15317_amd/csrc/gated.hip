@@ -155,28 +155,44 @@ __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int a
 
 // ---- few rows --------------------------------------------------------------
 // Up to kFewRows rows (a model that answers, the last rows of a batch): the weights are
-// read once and bound the time, and tiles of 128 rows, split over the reduction with
-// a second launch to join the splits, would be mostly zeros (one row of 1024 x 1024
-// bf16: 11.3 us; like this 8.9).  Products on the vector ALU in fp32.
+// read once and bound the time, and tiles of 128 rows would be mostly zeros.  Products
+// on the vector ALU, whole pieces of a weight's line a lane, sums in fp32.
 constexpr int kFewRows = 8;
 
-// Eight (bf16) or four (fp32) consecutive elements as fp32, those from `left` on 0.
+// A piece: eight (bf16) or four (fp32) consecutive elements, at any address (a 16-byte
+// access need not lie on 16 bytes).  Where fewer are left the piece that ends with the
+// last one is taken and its first elements, which another piece has, are set to 0 (bounds
+// for each element took 8 us of the 12 of 164 x 287): so a row has a piece's elements.
 template <class E> constexpr int kFewWidth = 16 / (int)sizeof(E);
-template <class E>
-__device__ __forceinline__ void few_load(const E* p, int left, bool vec, float (&v)[kFewWidth<E>]) {
-  constexpr int V = kFewWidth<E>;
-  if (vec && left >= V) {
-    const u32x4 t = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-    for (int e = 0; e < V; ++e)
-      v[e] = sizeof(E) == 4 ? __uint_as_float(t[e])
-                            : __uint_as_float(e % 2 ? t[e / 2] & 0xffff0000u : t[e / 2] << 16);
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+template <class E, int N = kFewWidth<E>>
+__device__ __forceinline__ u32x4 few_piece(const E* p) {
+  if constexpr (N * sizeof(E) == 16) {
+    return *reinterpret_cast<const u32x4_any*>(p);
   } else {
-#pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = e < left ? Elem<E>::load(p, e) : 0.f;
+    static_assert(N * sizeof(E) == 8, "half a piece");
+    const u32x2_any t = *reinterpret_cast<const u32x2_any*>(p);
+    return u32x4{t[0], t[1], 0, 0};
   }
 }
-
+// Two bf16 products and s.  (Rounded once or twice: within 2^-23 of the three terms.  A
+// product of a subnormal factor, below 2^-126 of the other, keeps 16 bits or more.)
+__device__ __forceinline__ float few_dot(uint32_t a, uint32_t b, float s) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), s,
+                                         false);
+}
+// Its first `skip` elements 0.
+template <class E>
+__device__ __forceinline__ u32x4 few_without(u32x4 t, int skip) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(E) == 4) t[i] = i < skip ? 0 : t[i];
+    else t[i] &= 2 * i + 1 < skip ? 0 : 2 * i < skip ? 0xffff0000u : 0xffffffffu;
+  }
+  return t;
+}
 // The value of the lane N further on in a row of 16.
 template <int N>
 __device__ __forceinline__ float row_turned(float v) {
@@ -184,77 +200,129 @@ __device__ __forceinline__ float row_turned(float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x120 + N, 0xf, 0xf, false));
 }
 
+// Sums over a wave's four rows of 16 lanes, of four values at once: row 0 of the result
+// has the first, row 1 the third, row 2 the second, row 3 the fourth.  (Swapping halves
+// of two registers adds up two values in the instructions of one.)
+__device__ __forceinline__ float halves_sum(float a, float b) {
+  const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+__device__ __forceinline__ float rows_sum(float a, float b, float c, float d) {
+  const float p = halves_sum(a, b), q = halves_sum(c, d);
+  const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(p), __float_as_uint(q), false, false);
+  return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+struct FewArgs {
+  const void *x, *w[2];
+  const float* bias[2];
+  void* y;
+  float *pre, *part;                                 // part: splits > 1, as DualArgs'
+  int m, n, k, ldx, ldy, pitch, act;
+  int strips, splits, lines;                         // lines of k a split
+};
+
 // Forward of M rows: a block has the columns of L lanes (16 L bytes of a line of each
-// weight) and all of k, every (512 / L)th line a lane; the lanes' sums meet in LDS.
+// weight) and a split's lines, J at a time for each L lanes: 2 J loads of 16 bytes are
+// under way in a lane, and x is a piece for J lines.  L = 8 takes whole lines of the
+// caches.  L = 4 takes half of them and so does half the work a block one after the other,
+// but what the caches read twice bounds it from a few MB on.  One row of bf16 weights:
+// 1024 x 1024 4.3 us (one line of k at a time a lane, reduced by shuffles: 5.5), 4096 x
+// 1024 7.1 (24.1), 4096 x 4096 16.4 (4.1 TB/s); eight rows of 4096 x 4096 20.0.
+template <class E, int M> constexpr int kFewLines = sizeof(E) == 2 && M == 8 ? 4 : kFewWidth<E>;
 template <class E, int M, int L>
-__global__ __launch_bounds__(512) void gated_few_fwd(int m, int n, int k, int ldx, int ldy, int act,
-                                                     const E* __restrict__ x,
-                                                     const E* __restrict__ wg,
-                                                     const E* __restrict__ wu,
-                                                     const float* __restrict__ bg,
-                                                     const float* __restrict__ bu, E* y, float* pre,
-                                                     int vec) {
-  constexpr int V = kFewWidth<E>, C = L * V;
-  __shared__ float part[8][2][M][C];
+__global__ __launch_bounds__(512) void gated_few_fwd(FewArgs g) {
+  constexpr int V = kFewWidth<E>, J = kFewLines<E, M>, C = L * V, NV = 2 * M * V, TH = 512, W = TH / 64;
+  __shared__ float part[W][NV][L];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int c = blockIdx.x * C + lane % L * V, left = n - c;
-  float acc[2][M][V];
+  const int strip = blockIdx.x % g.strips, split = blockIdx.x / g.strips;
+  const int c0 = strip * C + lane % L * V, c = min(c0, g.n - V);
+  const int k1 = min(g.k, (split + 1) * g.lines);
+  const E* x = (const E*)g.x;
+  float acc[NV];
 #pragma unroll
-  for (int q = 0; q < 2; ++q)
+  for (int i = 0; i < NV; ++i) acc[i] = 0.f;
+  if (c0 < g.n) {
+    for (int kk = split * g.lines + threadIdx.x / L * J; kk < k1; kk += TH / L * J) {
+      const int skip = max(kk + J - k1, 0), k0 = kk - skip;
+      u32x4 w[2][J];
 #pragma unroll
-    for (int r = 0; r < M; ++r)
+      for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int e = 0; e < V; ++e) acc[q][r][e] = 0.f;
-  if (left > 0) {
-#pragma unroll 4
-    for (int kk = threadIdx.x / L; kk < k; kk += 512 / L) {
-      float g[V], u[V];
-      few_load<E>(wg + (size_t)kk * n + c, left, vec, g);
-      few_load<E>(wu + (size_t)kk * n + c, left, vec, u);
+        for (int q = 0; q < 2; ++q) w[q][j] = few_piece<E>((const E*)g.w[q] + (size_t)(k0 + j) * g.n + c);
+      u32x4 xs[M];                                   // J elements
 #pragma unroll
-      for (int r = 0; r < M; ++r) {
-        const float xv = r < m ? Elem<E>::load(x, (size_t)r * ldx + kk) : 0.f;
+      for (int r = 0; r < M; ++r)
+        xs[r] = few_piece<E, J>(x + (size_t)min(r, g.m - 1) * g.ldx + k0);
+      if (skip) {                                    // of both: each may be infinite
+#pragma unroll
+        for (int r = 0; r < M; ++r) xs[r] = few_without<E>(xs[r], skip);
+#pragma unroll
+        for (int j = 0; j < J - 1; ++j)
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (j < skip) w[q][j] = u32x4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          acc[0][r][e] = fmaf(xv, g[e], acc[0][r][e]);
-          acc[1][r][e] = fmaf(xv, u[e], acc[1][r][e]);
+          if constexpr (sizeof(E) == 2) {
+            // Two lines at a time, as x has them.
+#pragma unroll
+            for (int j = 0; j < J; j += 2) {
+              const uint32_t v = __builtin_amdgcn_perm(w[q][j + 1][e / 2], w[q][j][e / 2],
+                                                       e % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+              for (int r = 0; r < M; ++r) {
+                float& s = acc[(q * M + r) * V + e];
+                s = few_dot(v, xs[r][j / 2], s);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+              for (int r = 0; r < M; ++r) {
+                float& s = acc[(q * M + r) * V + e];
+                s = fmaf(__uint_as_float(xs[r][j]), __uint_as_float(w[q][j][e]), s);
+              }
+          }
         }
-      }
     }
   }
+  const int row = lane / 16;
 #pragma unroll
-  for (int q = 0; q < 2; ++q)
-#pragma unroll
-    for (int r = 0; r < M; ++r)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        float v = acc[q][r][e];
-        if constexpr (L <= 2) v += row_turned<2>(v);
-        if constexpr (L <= 4) v += row_turned<4>(v);
-        v += row_turned<8>(v);
-        v += __shfl_xor(v, 16, 64);
-        v += __shfl_xor(v, 32, 64);
-        if (lane < L) part[wave][q][r][lane * V + e] = v;
-      }
+  for (int i = 0; i < NV; i += 4) {
+    float v = rows_sum(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+    if constexpr (L <= 8) v += row_turned<8>(v);
+    if constexpr (L <= 4) v += row_turned<4>(v);
+    if constexpr (L <= 2) v += row_turned<2>(v);
+    if (lane % 16 < L) part[wave][i + row / 2 + row % 2 * 2][lane % 16] = v;
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < M * C; i += 512) {
-    const int r = i / C, col = blockIdx.x * C + i % C;
-    if (r >= m || col >= n) continue;
-    float s[2];
+  for (int i = threadIdx.x; i < g.m * C; i += TH) {
+    const int r = i / C, at = i % C, own = strip * C + at / V * V, col = min(own, g.n - V) + at % V;
+    if (own >= g.n || col < own) continue;
+    float s[2] = {0.f, 0.f};
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const float(*p)[2][M][C] = part;
-      s[q] = ((p[0][q][r][i % C] + p[1][q][r][i % C]) + (p[2][q][r][i % C] + p[3][q][r][i % C])) +
-             ((p[4][q][r][i % C] + p[5][q][r][i % C]) + (p[6][q][r][i % C] + p[7][q][r][i % C]));
+    for (int q = 0; q < 2; ++q)
+#pragma unroll
+      for (int w = 0; w < W; ++w) s[q] += part[w][(q * M + r) * V + at % V][at / V];
+    if (g.splits > 1) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) g.part[(((size_t)split * 2 + q) * g.m + r) * g.pitch + col] = s[q];
+      continue;
     }
-    const float a = s[0] + (bg ? bg[col] : 0.f), u = s[1] + (bu ? bu[col] : 0.f);
+    const float a = s[0] + (g.bias[0] ? g.bias[0][col] : 0.f);
+    const float u = s[1] + (g.bias[1] ? g.bias[1][col] : 0.f);
     float f, df;
-    gate_act(act, a, f, df);
-    if (pre) {
-      pre[(size_t)r * n + col] = a;
-      pre[((size_t)m + r) * n + col] = u;
+    gate_act(g.act, a, f, df);
+    if (g.pre) {
+      g.pre[(size_t)r * g.n + col] = a;
+      g.pre[((size_t)g.m + r) * g.n + col] = u;
     }
-    Elem<E>::store(y, (size_t)r * ldy + col, f * u);
+    Elem<E>::store((E*)g.y, (size_t)r * g.ldy + col, f * u);
   }
 }
 
@@ -265,7 +333,7 @@ __global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k,
                                                     const E* __restrict__ da,
                                                     const E* __restrict__ du,
                                                     const E* __restrict__ wg,
-                                                    const E* __restrict__ wu, E* dx, int vec) {
+                                                    const E* __restrict__ wu, E* dx) {
   constexpr int V = kFewWidth<E>, R = 4;
   const int lane = threadIdx.x & 63;
   const int k0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * R;
@@ -274,32 +342,48 @@ __global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k,
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int r = 0; r < M; ++r) acc[i][r] = 0.f;
-  for (int c = lane * V; c < n; c += 64 * V) {
+  for (int c0 = lane * V; c0 < n; c0 += 64 * V) {
+    const int skip = max(c0 + V - n, 0), c = c0 - skip;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      float w[R][V], d[V];
+      u32x4 w[R], d[M];
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        few_load<E>((q ? wu : wg) + (size_t)min(k0 + i, k - 1) * n + c, n - c, vec, w[i]);
+        w[i] = few_piece<E>((q ? wu : wg) + (size_t)min(k0 + i, k - 1) * n + c);
 #pragma unroll
-      for (int r = 0; r < M; ++r) {
-        few_load<E>((q ? du : da) + (size_t)min(r, m - 1) * np + c, np - c, true, d);
+      for (int r = 0; r < M; ++r) d[r] = few_piece<E>((q ? du : da) + (size_t)min(r, m - 1) * np + c);
+      if (skip) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) w[i] = few_without<E>(w[i], skip);
+#pragma unroll
+        for (int r = 0; r < M; ++r) d[r] = few_without<E>(d[r], skip);
+      }
+#pragma unroll
+      for (int r = 0; r < M; ++r)
 #pragma unroll
         for (int i = 0; i < R; ++i)
+          if constexpr (sizeof(E) == 2) {
 #pragma unroll
-          for (int e = 0; e < V; ++e) acc[i][r] = fmaf(w[i][e], d[e], acc[i][r]);
-      }
+            for (int e = 0; e < 4; ++e)
+              acc[i][r] = few_dot(w[i][e], d[r][e], acc[i][r]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[i][r] = fmaf(__uint_as_float(w[i][e]), __uint_as_float(d[r][e]), acc[i][r]);
+          }
     }
   }
+  // The four rows' sums of a row of dx at once, in the four rows of lanes.
+  const int row = lane / 16, at = k0 + row / 2 + row % 2 * 2;
 #pragma unroll
-  for (int i = 0; i < R; ++i)
-#pragma unroll
-    for (int r = 0; r < M; ++r) {
-      float v = acc[i][r];
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o, 64);
-      if (lane == 0 && k0 + i < k && r < m) Elem<E>::store(dx, (size_t)r * ldx + k0 + i, v);
-    }
+  for (int r = 0; r < M; ++r) {
+    float v = rows_sum(acc[0][r], acc[1][r], acc[2][r], acc[3][r]);
+    v += row_turned<8>(v);
+    v += row_turned<4>(v);
+    v += row_turned<2>(v);
+    v += row_turned<1>(v);
+    if (lane % 16 == 0 && at < k && r < m) Elem<E>::store(dx, (size_t)r * ldx + at, v);
+  }
 }
 
 // Sums of the splits' partials (rows of g.pitch), four columns of a row a lane.  FWD:
@@ -481,6 +565,12 @@ static DualArgs dual_planned(DualArgs g, const DualPlan& p, float* part) {
   return g;
 }
 
+template <class E>
+static void split_sum_fwd(const DualArgs& g, int act, hipStream_t st) {
+  if (g.splits < 8) gated_split_sum<E, 1><<<split_sum_blocks(g, 1), 256, 0, st>>>(g, act);
+  else gated_split_sum<E, 4><<<split_sum_blocks(g, 4), 256, 0, st>>>(g, act);
+}
+
 // The forward under its plan: unsplit it ends in its outputs, split in the workspace,
 // from where gated_split_sum takes it (whichever activation the product was built for).
 template <class E>
@@ -493,10 +583,7 @@ static void fwd_run(DualArgs g, const DualPlan& p, int act, float* part, hipStre
     case SB_ACT_GELU_TANH: fwd_launch_f<SB_ACT_GELU_TANH, E>(p.f, g, st); break;
     default: fwd_launch_f<SB_ACT_RELU, E>(p.f, g, st);
   }
-  if (p.splits > 1) {
-    if (p.splits < 8) gated_split_sum<E, 1><<<split_sum_blocks(g, 1), 256, 0, st>>>(g, act);
-    else gated_split_sum<E, 4><<<split_sum_blocks(g, 4), 256, 0, st>>>(g, act);
-  }
+  if (p.splits > 1) split_sum_fwd<E>(g, act, st);
 }
 
 template <int F, class E>
@@ -530,11 +617,52 @@ static void grads_run(DualArgs dx, DualArgs dw, const BiasSums& bias, const Grad
 static int up8(int n) { return (n + 7) / 8 * 8; }
 static bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
+// Whether the kernels for few rows take a call: lines and rows of a piece at least.
+static bool few_rows(const sb_gated_desc* d) {
+  return d->m <= kFewRows && d->n_shard >= 8 && d->k_in >= 8;
+}
+
+// Lanes a line and splits of their forward: the least estimated time (us).  Without
+// splits: the start, M rows' ends, a block's rounds of J lines for each of its groups of
+// lanes, M times as much work in them, and the weights' MB; splits cost a launch and the
+// partials.  Fitted to 3800 timings of 360 shapes of 64 to 8192 (1 to 8 rows, both
+// types); the plan taken is 3 (bf16) or 2 % (fp32) slower than the best on average.
+struct FewPlan { int lanes, strips, splits, lines; size_t ws_bytes; };
+static FewPlan few_plan(const sb_gated_desc* d) {
+  static const double kCost[2][3][6] = {
+      // start, of it a row, round, of it a row, MB, MB of partials
+      {{1.95, 0.15, 0.37, 0.085, 0.251, 0}, {2.01, 0.205, 0.49, 0.049, 0.100, 0},
+       {5.76, 0.091, 0.068, 0.12, 0.132, 1.17}},                      // fp32: 4 lanes, 8, 8 split
+      {{1.46, 0.33, 1.35, 0.194, 0.240, 0}, {1.94, 0.34, 1.14, 0.188, 0.094, 0},
+       {5.87, 0.16, 0.27, 0.344, 0.137, 1.29}}};                      // bf16
+  const bool b16 = d->dtype == SB_BF16;
+  const int es = b16 ? 2 : 4, v = 16 / es, M = d->m <= 2 ? d->m : d->m <= 4 ? 4 : 8;
+  const int J = b16 && M == 8 ? 4 : v;                                // kFewLines
+  const double mb = 2e-6 * d->k_in * d->n_shard * es;
+  FewPlan best{};
+  double best_t = 0;
+  for (int lanes = 4; lanes <= 8; lanes *= 2) {
+    for (int s = 1; s <= (lanes == 8 ? 32 : 1) && (s == 1 || d->k_in / s >= 16); s *= 2) {
+      const double* c = kCost[b16][s > 1 ? 2 : lanes / 8];
+      const int strips = cdiv(cdiv(d->n_shard, v), lanes), lines = cdiv(cdiv(d->k_in, s), J) * J;
+      const int splits = cdiv(d->k_in, lines), group = 512 / lanes * J;
+      const double rounds = cdiv(lines, group) * (double)J / v * std::max(1.0, strips * (double)splits / 256);
+      const size_t part = splits > 1 ? (size_t)splits * 8 * d->m * cdiv(d->n_shard, 4) * 4 : 0;
+      const double t = c[0] + c[1] * M + rounds * (c[2] + c[3] * M) + c[4] * mb + c[5] * 1e-6 * part;
+      if (best_t == 0 || t < best_t) {
+        best_t = t;
+        best = FewPlan{lanes, strips, splits, lines, part};
+      }
+    }
+  }
+  return best;
+}
+
 // Which operands have to be laid out anew for 16-byte pieces of whole eights: x as
 // rows of the forward's reduction, x as lines of the weight gradient's, the weights.
 struct GatedPacks { bool x, lines, w; };
 static GatedPacks gated_packs(const sb_gated_desc* d, bool x_at16, bool w_at16) {
-  const bool b16 = d->dtype == SB_BF16, few = d->m <= kFewRows;
+  const bool b16 = d->dtype == SB_BF16, few = few_rows(d);
   // (An odd bf16 k_in would end the last line inside the 4 bytes that ranges count in.)
   const bool lines = d->ldx % (b16 ? 8 : 4) != 0 || (b16 && d->k_in % 2 != 0) || !x_at16;
   return GatedPacks{!few && (lines || d->k_in % 8 != 0), lines,
@@ -569,10 +697,10 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
   }
   if (pass == SB_FC_FWD ? k.x : k.lines) take(s.x, m * up8(d->k_in) * es);
   if (k.w) take(s.w, 2 * (size_t)d->k_in * np * es);
-  const bool few = d->m <= kFewRows;
+  const bool few = few_rows(d);
   size_t split = 0;
   if (pass == SB_FC_FWD) {
-    split = few ? 0 : gated_plan_fwd(d).ws_bytes;
+    split = few ? few_plan(d).ws_bytes : gated_plan_fwd(d).ws_bytes;
   } else {
     split = gated_plan_dw(d).ws_bytes;
     if (!few) {
@@ -646,31 +774,30 @@ static GatedOperands gated_operands(const sb_gated_desc* d, const void* x, const
 }
 
 template <class E, int M>
-static void few_fwd(const sb_gated_desc* d, const void* x, const void* const* w,
-                    const float* const* b, void* y, float* pre, int vec, hipStream_t st) {
-  // Whole 128-byte lines a block while that makes 128 blocks, else down to 32 bytes.
-  const int v = cdiv(d->n_shard, kFewWidth<E>);
-  auto go = [&](auto L) {
-    constexpr int l = decltype(L)::value;
-    gated_few_fwd<E, M, l><<<(unsigned)cdiv(v, l), 512, 0, st>>>(
-        d->m, d->n_shard, d->k_in, d->ldx, d->ldy, d->act, (const E*)x, (const E*)w[0],
-        (const E*)w[1], b[0], b[1], (E*)y, pre, vec);
-  };
-  if (v >= 8 * 128) go(std::integral_constant<int, 8>{});
-  else if (v >= 4 * 128) go(std::integral_constant<int, 4>{});
-  else go(std::integral_constant<int, 2>{});
+static void few_fwd(FewArgs g, int lanes, hipStream_t st) {
+  const int blocks = g.strips * g.splits;
+  if (lanes == 8) gated_few_fwd<E, M, 8><<<blocks, 512, 0, st>>>(g);
+  else gated_few_fwd<E, M, 4><<<blocks, 512, 0, st>>>(g);
+  if (g.splits == 1) return;
+  DualArgs d{};
+  d.M = g.m; d.N = g.n; d.pitch = g.pitch; d.splits = g.splits; d.part = g.part;
+  d.bias[0] = g.bias[0]; d.bias[1] = g.bias[1];
+  d.pre = g.pre; d.c[0] = g.y; d.ldc = g.ldy;
+  split_sum_fwd<E>(d, g.act, st);
 }
 
 template <class E>
 static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* const* w,
                           const float* const* b, void* y, float* pre, const GatedPacks& packs,
                           char* ws, const GatedSpace& sp, hipStream_t st) {
-  if (d->m <= kFewRows) {
-    const int vec = d->n_shard % kFewWidth<E> == 0 && at16(w[0]) && at16(w[1]);
-    if (d->m == 1) few_fwd<E, 1>(d, x, w, b, y, pre, vec, st);
-    else if (d->m == 2) few_fwd<E, 2>(d, x, w, b, y, pre, vec, st);
-    else if (d->m <= 4) few_fwd<E, 4>(d, x, w, b, y, pre, vec, st);
-    else few_fwd<E, 8>(d, x, w, b, y, pre, vec, st);
+  if (few_rows(d)) {
+    const FewPlan p = few_plan(d);
+    FewArgs g{x, {w[0], w[1]}, {b[0], b[1]}, y, pre, (float*)(ws + sp.split), d->m, d->n_shard,
+              d->k_in, d->ldx, d->ldy, cdiv(d->n_shard, 4) * 4, d->act, p.strips, p.splits, p.lines};
+    if (d->m == 1) few_fwd<E, 1>(g, p.lanes, st);
+    else if (d->m == 2) few_fwd<E, 2>(g, p.lanes, st);
+    else if (d->m <= 4) few_fwd<E, 4>(g, p.lanes, st);
+    else few_fwd<E, 8>(g, p.lanes, st);
     return;
   }
   const GatedOperands o = gated_operands<E>(d, x, w, packs.x, packs.w, ws, sp);
@@ -689,9 +816,9 @@ static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* con
 
 template <class E, int M>
 static void few_dx(const sb_gated_desc* d, int np, const E* da, const E* du, const void* const* w,
-                   void* dx, int vec, hipStream_t st) {
+                   void* dx, hipStream_t st) {
   gated_few_dx<E, M><<<(unsigned)cdiv(d->k_in, 16), 256, 0, st>>>(
-      d->m, d->n_shard, np, d->k_in, d->ldx, da, du, (const E*)w[0], (const E*)w[1], (E*)dx, vec);
+      d->m, d->n_shard, np, d->k_in, d->ldx, da, du, (const E*)w[0], (const E*)w[1], (E*)dx);
 }
 
 template <class E>
@@ -722,7 +849,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   gw.b_bytes = (uint32_t)(plane * sizeof(E));
   gw.c[0] = dw[0]; gw.c[1] = dw[1]; gw.ldc = d->n_shard;
   gw.accumulate = accumulate;
-  if (dx && d->m > kFewRows) {
+  if (dx && !few_rows(d)) {
     DualArgs gx{};
     for (int q = 0; q < 2; ++q) {
       gx.a[q] = parts + NP * q * plane;
@@ -737,12 +864,11 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
     return;
   }
   if (dx) {
-    const int wvec = d->n_shard % kFewWidth<E> == 0 && at16(w[0]) && at16(w[1]);
     const E *da = parts, *du = parts + NP * plane;
-    if (d->m == 1) few_dx<E, 1>(d, np, da, du, w, dx, wvec, st);
-    else if (d->m == 2) few_dx<E, 2>(d, np, da, du, w, dx, wvec, st);
-    else if (d->m <= 4) few_dx<E, 4>(d, np, da, du, w, dx, wvec, st);
-    else few_dx<E, 8>(d, np, da, du, w, dx, wvec, st);
+    if (d->m == 1) few_dx<E, 1>(d, np, da, du, w, dx, st);
+    else if (d->m == 2) few_dx<E, 2>(d, np, da, du, w, dx, st);
+    else if (d->m <= 4) few_dx<E, 4>(d, np, da, du, w, dx, st);
+    else few_dx<E, 8>(d, np, da, du, w, dx, st);
   }
   grads_run<E>(DualArgs{}, gw, bias, GradPlan{{}, gated_plan_dw(d)}, ws + sp.split, st);
 }

@@ -373,3 +373,35 @@ def test_two_graphs_with_one_workspace(dtype):
                 assert torch.equal(c.d[t][:, :width], w[t][:, :width]), t
             for t in ("dbg", "dbu"):
                 assert torch.equal(c.d[t], w[t]), t
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m", [1, 2, 4, 8])
+@pytest.mark.parametrize("k,n", [(8, 8), (13, 19), (15, 9), (1030, 70), (4093, 33), (2600, 260), (9, 1000)])
+def test_ends_of_few_rows(m, k, n, dtype):
+    """Lines and rows that end inside a piece, and infinities in the elements that the
+    last two pieces share: both projections are infinite, by sign, where they are in
+    float64, and NaN nowhere."""
+    print_case("gated_ends", m=m, k=k, n=n, dtype=dtype)
+    c = Case("relu", dtype, m, k, n, shift=1)
+    c.fwd()
+    c.bwd()
+    c.check(ALL)
+    c.untouched(ALL + ("pre",))
+    x, wg = c.x.copy(), c.wg.copy()
+    c.x[0, k - 2] = np.inf
+    c.wg[max(k - 6, 0), n - 3] = np.inf
+    c.d["x"].copy_(torch.from_numpy(c.x))
+    c.d["wg"].copy_(torch.from_numpy(c.wg))
+    c.fwd()
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        _, a, u = G.forward("relu", c.x[:, :k], c.wg, c.wu, c.bg, c.bu)
+    got = c.d["pre"].cpu().numpy().astype(np.float64)
+    for g, r in zip(got, (a, u)):
+        far = ~np.isfinite(r)
+        assert far[0].all() and np.array_equal(g[far], r[far], equal_nan=True)
+        # The rest: k products and sums, each rounded, of values that x and the weights bound.
+        lim = (k + 2) * 2.0 ** -23 * (np.abs(x[:, :k]).astype(np.float64) @ np.maximum(np.abs(wg), np.abs(c.wu)) + 2)
+        ok = np.isfinite(r)
+        assert np.all(np.abs(g[ok] - r[ok]) <= lim[ok])
