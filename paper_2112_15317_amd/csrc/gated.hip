@@ -24,6 +24,30 @@
 
 namespace sb {
 
+// A 16- or 8-byte access need not lie on 16 or 8 bytes.
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+// Elements p[0] .. p[3], those from `left` on 0; at any address.
+template <class E>
+__device__ __forceinline__ f4 load_quad(const E* p, int left) {
+  f4 v = f4{0.f, 0.f, 0.f, 0.f};
+  if (left >= 4) {
+    if constexpr (sizeof(E) == 4) {
+      const u32x4 t = *reinterpret_cast<const u32x4_any*>(p);
+      v = f4{__uint_as_float(t[0]), __uint_as_float(t[1]), __uint_as_float(t[2]), __uint_as_float(t[3])};
+    } else {
+      const u32x2_any t = *reinterpret_cast<const u32x2_any*>(p);
+      v = f4{__uint_as_float(t[0] << 16), __uint_as_float(t[0] & 0xffff0000u),
+             __uint_as_float(t[1] << 16), __uint_as_float(t[1] & 0xffff0000u)};
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+      if (e < left) v[e] = Elem<E>::load(p, e);
+  }
+  return v;
+}
+
 // Up to three matrices: rows of `cols` elements, `ld` apart, to rows of cp (a multiple
 // of 8), zeros behind.  Matrix q has blocks block0[q] .. block0[q + 1] - 1.
 struct PackTasks {
@@ -43,11 +67,7 @@ __device__ __forceinline__ void pack_rows(const PackTasks& t, int block) {
   for (size_t i = (size_t)(block - t.block0[q]) * 256 + threadIdx.x; i < quads; i += step) {
     const uint32_t r = (uint32_t)i / (uint32_t)(cp / 4);     // (quads are below 2^29)
     const int c = (int)((uint32_t)i - r * (cp / 4)) * 4;
-    f4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      v[e] = c + e < cols ? Elem<E>::load(from, (size_t)r * t.ld[q] + c + e) : 0.f;
-    Elem<E>::store4(out + (size_t)r * cp + c, v);
+    Elem<E>::store4(out + (size_t)r * cp + c, load_quad<E>(from + (size_t)r * t.ld[q] + c, cols - c));
   }
 }
 template <class E>
@@ -75,7 +95,7 @@ __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int a
                                                      const float* __restrict__ pre,
                                                      const E* __restrict__ dy, int ldy,
                                                      E* __restrict__ d, BiasSums bias, int rows,
-                                                     int chunks, int vec, PackTasks packs) {
+                                                     int chunks, PackTasks packs) {
   __shared__ f4 part[2][4][64];
   const int by = blockIdx.x % chunks, bx = blockIdx.x / chunks;
   if (bx * 256 >= np) {
@@ -89,21 +109,8 @@ __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int a
   f4 s[2] = {f4{0.f, 0.f, 0.f, 0.f}, f4{0.f, 0.f, 0.f, 0.f}};
   for (int r = by * rows + w; r < r1 && c < np; r += 4) {
     const float* pa = pre + (size_t)r * n + c;
-    const E* pd = dy + (size_t)r * ldy + c;
-    f4 a = f4{0.f, 0.f, 0.f, 0.f}, u = a, g = a;
-    if (vec && c < n) {                              // n a multiple of 4
-      a = *reinterpret_cast<const f4*>(pa);
-      u = *reinterpret_cast<const f4*>(pa + mn);
-      g = Elem<E>::load4(pd);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (c + e < n) {
-          a[e] = pa[e];
-          u[e] = pa[mn + e];
-          g[e] = Elem<E>::load(pd, e);
-        }
-    }
+    const f4 a = load_quad<float>(pa, n - c), u = load_quad<float>(pa + mn, n - c);
+    const f4 g = load_quad<E>(dy + (size_t)r * ldy + c, n - c);
     f4 v[2];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -164,8 +171,6 @@ constexpr int kFewRows = 8;
 // last one is taken and its first elements, which another piece has, are set to 0 (bounds
 // for each element took 8 us of the 12 of 164 x 287): so a row has a piece's elements.
 template <class E> constexpr int kFewWidth = 16 / (int)sizeof(E);
-typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <class E, int N = kFewWidth<E>>
 __device__ __forceinline__ u32x4 few_piece(const E* p) {
@@ -832,11 +837,9 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   E* parts = (E*)(ws + sp.d);
   const BiasSums bias{(db[0] || db[1]) && chunks > 1 ? (float*)(ws + sp.sums) : nullptr,
                       {db[0], db[1]}, d->n_shard, np, chunks, accumulate};
-  const int vec = d->n_shard % 4 == 0 && at16(pre) && d->ldy % 4 == 0 &&
-                  ((uintptr_t)dy & (4 * sizeof(E) - 1)) == 0;
   const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp);
   gated_act_bwd<E><<<(unsigned)(cdiv(np, 256) * chunks + o.packs.block0[3]), 256, 0, st>>>(
-      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, bias, rows, chunks, vec,
+      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, bias, rows, chunks,
       o.packs);
   DualArgs gw{};
   for (int p = 0; p < NP; ++p) {                     // the smallest parts first
