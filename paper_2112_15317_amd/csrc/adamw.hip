@@ -55,7 +55,7 @@ struct AdamwTensor {
   uint64_t first;
   size_t n;
   float scale, decay;
-  int block0, vec;
+  int block0;
 };
 
 // A plan: the tensors' first blocks, then the tensors.
@@ -127,24 +127,32 @@ __device__ __forceinline__ uint32_t wave_max2(uint32_t v) {
   return v;
 }
 
-template <class T, class V>
-__device__ __forceinline__ V adamw_load4(const T* p, size_t i, size_t n, bool whole) {
-  if (whole) return *reinterpret_cast<const V*>(p + i);
-  V v{};
+// Four elements, those below n.  Tensors may be views that start at any element: a 4-, 8-
+// or 16-byte access need not lie on as many bytes.
+template <class T>
+__device__ __forceinline__ auto adamw_load4(const T* p, size_t i, size_t n) {
+  typedef T V __attribute__((ext_vector_type(4)));
+  typedef T Any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  V v = {0, 0, 0, 0};
+  if (i + 4 <= n) {
+    v = *reinterpret_cast<const Any*>(p + i);
+  } else {
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (i + e < n) v[e] = p[i + e];
+    for (int e = 0; e < 3; ++e)
+      if (i + e < n) v[e] = p[i + e];
+  }
   return v;
 }
 template <class T, class V>
-__device__ __forceinline__ void adamw_store4(T* p, size_t i, size_t n, bool whole, V v) {
-  if (whole) {
-    *reinterpret_cast<V*>(p + i) = v;
-    return;
-  }
+__device__ __forceinline__ void adamw_store4(T* p, size_t i, size_t n, V v) {
+  typedef T Any __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  if (i + 4 <= n) {
+    *reinterpret_cast<Any*>(p + i) = v;
+  } else {
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (i + e < n) p[i + e] = v[e];
+    for (int e = 0; e < 3; ++e)
+      if (i + e < n) p[i + e] = v[e];
+  }
 }
 
 typedef uint8_t b4 __attribute__((ext_vector_type(4)));
@@ -174,11 +182,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const size_t i = base + u * 1024;
-    const bool whole = t.vec && i + 4 <= n;
-    g4[u] = adamw_load4<float, f4>(t.g, i, n, whole);
-    m4[u] = adamw_load4<S, S4>(m, i, n, whole);
-    v4[u] = adamw_load4<S, S4>(v, i, n, whole);
-    w4[u] = adamw_load4<float, f4>(t.w, i, n, whole);
+    g4[u] = adamw_load4<float>(t.g, i, n);
+    m4[u] = adamw_load4<S>(m, i, n);
+    v4[u] = adamw_load4<S>(v, i, n);
+    w4[u] = adamw_load4<float>(t.w, i, n);
     if constexpr (BYTES) {
       mtop[u] = i < n ? t.m_top[i / 256] : 0;
       vtop[u] = i < n ? t.v_top[i / 256] : 0;
@@ -197,7 +204,6 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
   for (int u = 0; u < U; ++u) {
     const size_t i = base + u * 1024;
     if (i - threadIdx.x % 64 * 4 >= n) return;   // whole waves leave together
-    const bool whole = t.vec && i + 4 <= n;
     f4 nm, nv, nw;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -223,16 +229,16 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
       else
         nw[e] = w4[u][e] * keep - rate * (nm[e] / (sqrtf(nv[e]) * vscale + b.eps));
     }
-    adamw_store4<float, f4>(t.w, i, n, whole, nw);
+    adamw_store4<float>(t.w, i, n, nw);
     if (t.copy) {
       h4 c;
 #pragma unroll
       for (int e = 0; e < 4; ++e) c[e] = f32_to_bf16(nw[e]);
-      adamw_store4<u16, h4>(t.copy, i, n, whole, c);
+      adamw_store4<u16>(t.copy, i, n, c);
     }
     if constexpr (!BYTES) {
-      adamw_store4<float, f4>((float*)t.m, i, n, whole, nm);
-      adamw_store4<float, f4>((float*)t.v, i, n, whole, nv);
+      adamw_store4<float>((float*)t.m, i, n, nm);
+      adamw_store4<float>((float*)t.v, i, n, nv);
     } else {
       const uint64_t at = t.first + i;       // its lower half may carry among the four
       const uint32_t lo = (uint32_t)at, hi = (uint32_t)(at >> 32);
@@ -257,8 +263,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
         mb[e] = (uint8_t)(mc | (mc > 0 && nm[e] < 0.f ? 128 : 0));
         vb[e] = (uint8_t)(nv[e] == 0.f ? 0 : vc);
       }
-      adamw_store4<uint8_t, b4>((uint8_t*)t.m, i, n, whole, mb);
-      adamw_store4<uint8_t, b4>((uint8_t*)t.v, i, n, whole, vb);
+      adamw_store4<uint8_t>((uint8_t*)t.m, i, n, mb);
+      adamw_store4<uint8_t>((uint8_t*)t.v, i, n, vb);
       if (threadIdx.x % 64 == 0) {
         t.m_top[i / 256] = (int16_t)mt;
         t.v_top[i / 256] = (int16_t)vt;
@@ -276,15 +282,14 @@ __global__ __launch_bounds__(256) void adamw_unpack_kernel(size_t n, const uint8
                                                            const uint8_t* __restrict__ v,
                                                            const int16_t* __restrict__ v_top,
                                                            float* __restrict__ m_out,
-                                                           float* __restrict__ v_out, int vec) {
+                                                           float* __restrict__ v_out) {
   const size_t base = (size_t)blockIdx.x * (1024 * U) + threadIdx.x * 4;
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const size_t i = base + u * 1024;
     if (i >= n) return;
-    const bool whole = vec && i + 4 <= n;
     if (m_out) {
-      const b4 c = adamw_load4<uint8_t, b4>(m, i, n, whole);
+      const b4 c = adamw_load4<uint8_t>(m, i, n);
       const int top = m_top[i / 256];
       f4 o;
 #pragma unroll
@@ -292,15 +297,15 @@ __global__ __launch_bounds__(256) void adamw_unpack_kernel(size_t n, const uint8
         const float x = rank_value((c[e] & 127) ? top + (c[e] & 127) - 127 : 0);
         o[e] = c[e] > 127 ? -x : x;
       }
-      adamw_store4<float, f4>(m_out, i, n, whole, o);
+      adamw_store4<float>(m_out, i, n, o);
     }
     if (v_out) {
-      const b4 c = adamw_load4<uint8_t, b4>(v, i, n, whole);
+      const b4 c = adamw_load4<uint8_t>(v, i, n);
       const int top = v_top[i / 256];
       f4 o;
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = rank_value(c[e] ? top + c[e] - 255 : 0);
-      adamw_store4<float, f4>(v_out, i, n, whole, o);
+      adamw_store4<float>(v_out, i, n, o);
     }
   }
 }
@@ -400,9 +405,6 @@ extern "C" sb_status sb_adamw_make_plan(int moments, int count, const sb_adamw_t
     o.m_top = t.m_top; o.v_top = t.v_top; o.first = t.first; o.n = t.n;
     o.scale = t.grad_scale; o.decay = t.decay;
     o.block0 = (int)blocks;
-    // Four elements at a time: 16, 8 and 4 bytes of fp32, bf16 and bytes.
-    o.vec = aligned(t.w, 16) && aligned(t.g, 16) && aligned(t.copy, 8) &&
-            aligned(t.m, bytes ? 4 : 16) && aligned(t.v, bytes ? 4 : 16);
     blocks += (int64_t)((t.n + block - 1) / block);
   }
   *info = sb_adamw_plan{used, moments, groups, (int)blocks};
@@ -468,10 +470,7 @@ extern "C" sb_status sb_adamw_unpack(size_t n, const uint8_t* m, const int16_t* 
   if (sbh::overlaps(m_out, n * 4, v_out, n * 4)) return SB_ERR_INVALID_ARG;
   const int groups = n < sb::kAdamwSmall ? 1 : sb::kAdamwGroups;
   const size_t blocks = (n + 1024 * groups - 1) / (1024 * groups);
-  const int vec = aligned(m_out, 16) && aligned(v_out, 16) && (!m_out || aligned(m, 4)) &&
-                  (!v_out || aligned(v, 4));
   const auto kernel = groups == 1 ? sb::adamw_unpack_kernel<1> : sb::adamw_unpack_kernel<sb::kAdamwGroups>;
-  kernel<<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(n, m, m_top, v, v_top, m_out, v_out,
-                                                               vec);
+  kernel<<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(n, m, m_top, v, v_top, m_out, v_out);
   return sbh::launch_status();
 }
