@@ -589,7 +589,7 @@ typedef struct { int tensors, moments, groups, blocks; } sb_adamw_plan;
  * finite, NULL pointers, pointers that are not multiples of their elements' size, and
  * for an output (w, copy, moments, references, the plan) that overlaps any other
  * tensor of the call; gradients may overlap each other.  SB_ERR_WORKSPACE for a
- * short plan, SB_ERR_UNSUPPORTED for 2^35 elements and more.  Nothing is enqueued
+ * short plan, SB_ERR_UNSUPPORTED for 2^33 elements and more.  Nothing is enqueued
  * then. */
 size_t sb_adamw_plan_bytes(int count);
 sb_status sb_adamw_make_plan(int moments, int count,

@@ -40,10 +40,12 @@
 
 namespace sb {
 
-constexpr int kAdamwGroups = 4;              // groups of 4 elements per lane, or one:
-// a lane's groups are worked off one after the other, so where there are too few
-// elements for a block on every CU, one each (20000 elements in bytes 9.1 -> 4.8 us).
-constexpr size_t kAdamwSmall = 2048 * 1024;
+// Groups of 4 elements per lane: two where moments are bytes and there are very many
+// elements (134 M of them 406 us with one, 392 with two, 443 with four; 300 tensors of
+// 40 M elements 158, 140, 161), else one (8 M elements 27.4 us, 30.0 with two; fp32 moments
+// as fast with one, two and four).
+constexpr int kAdamwGroups = 2;
+constexpr size_t kAdamwMany = 24u << 20;
 constexpr int kAdamwChunk = 40;              // tensors a launch writes into a plan
 
 struct AdamwTensor {
@@ -276,37 +278,32 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
 __global__ void adamw_advance_kernel(int32_t* steps_done) { *steps_done += 1; }
 
 // Four bytes of both moments a lane; a wave has one block's 256.
-template <int U>
 __global__ __launch_bounds__(256) void adamw_unpack_kernel(size_t n, const uint8_t* __restrict__ m,
                                                            const int16_t* __restrict__ m_top,
                                                            const uint8_t* __restrict__ v,
                                                            const int16_t* __restrict__ v_top,
                                                            float* __restrict__ m_out,
                                                            float* __restrict__ v_out) {
-  const size_t base = (size_t)blockIdx.x * (1024 * U) + threadIdx.x * 4;
+  const size_t i = (size_t)blockIdx.x * 1024 + threadIdx.x * 4;
+  if (i >= n) return;
+  if (m_out) {
+    const b4 c = adamw_load4<uint8_t>(m, i, n);
+    const int top = m_top[i / 256];
+    f4 o;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const size_t i = base + u * 1024;
-    if (i >= n) return;
-    if (m_out) {
-      const b4 c = adamw_load4<uint8_t>(m, i, n);
-      const int top = m_top[i / 256];
-      f4 o;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float x = rank_value((c[e] & 127) ? top + (c[e] & 127) - 127 : 0);
-        o[e] = c[e] > 127 ? -x : x;
-      }
-      adamw_store4<float>(m_out, i, n, o);
+    for (int e = 0; e < 4; ++e) {
+      const float x = rank_value((c[e] & 127) ? top + (c[e] & 127) - 127 : 0);
+      o[e] = c[e] > 127 ? -x : x;
     }
-    if (v_out) {
-      const b4 c = adamw_load4<uint8_t>(v, i, n);
-      const int top = v_top[i / 256];
-      f4 o;
+    adamw_store4<float>(m_out, i, n, o);
+  }
+  if (v_out) {
+    const b4 c = adamw_load4<uint8_t>(v, i, n);
+    const int top = v_top[i / 256];
+    f4 o;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = rank_value(c[e] ? top + c[e] - 255 : 0);
-      adamw_store4<float>(v_out, i, n, o);
-    }
+    for (int e = 0; e < 4; ++e) o[e] = rank_value(c[e] ? top + c[e] - 255 : 0);
+    adamw_store4<float>(v_out, i, n, o);
   }
 }
 
@@ -379,14 +376,14 @@ extern "C" sb_status sb_adamw_make_plan(int moments, int count, const sb_adamw_t
     if (t.copy) add(t.copy, t.n * 2, true);
     ++used;
     total += t.n;
-    // (A launch has fewer than 2^32 lanes, and one has 16 elements of so many.)
-    if (total >= (1ull << 35)) return SB_ERR_UNSUPPORTED;
+    // (A launch has fewer than 2^32 lanes, each of four elements or eight.)
+    if (total >= (1ull << 33)) return SB_ERR_UNSUPPORTED;
   }
   if (outputs_meet(r, ranges)) return SB_ERR_INVALID_ARG;
   if (plan_bytes < need) return SB_ERR_WORKSPACE;
   sb::AdamwChunk c{};
   c.total = used;
-  const int groups = total < sb::kAdamwSmall ? 1 : sb::kAdamwGroups;
+  const int groups = bytes && total >= sb::kAdamwMany ? sb::kAdamwGroups : 1;
   const size_t block = 1024 * (size_t)groups;
   int64_t blocks = 0;
   for (int i = 0; i <= count; ++i) {
@@ -417,7 +414,7 @@ extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, const sb_adamw_plan
   if (info->tensors < 0 || info->tensors > SB_ADAMW_MAX_TENSORS ||
       info->blocks < info->tensors || (info->tensors == 0 && info->blocks != 0) ||
       (info->moments != 8 && info->moments != 32) ||
-      (info->groups != 1 && info->groups != sb::kAdamwGroups))
+      (info->groups != 1 && (info->groups != sb::kAdamwGroups || info->moments != 8)))
     return SB_ERR_INVALID_ARG;
   if (!std::isfinite(d->lr) || !std::isfinite(d->eps) || !(d->eps >= 0.0)) return SB_ERR_INVALID_ARG;
   if (!(d->beta1 >= 0.0 && d->beta1 < 1.0) || !(d->beta2 >= 0.0 && d->beta2 < 1.0))
@@ -436,10 +433,9 @@ extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, const sb_adamw_plan
   b.eps = (float)d->eps; b.rate = (float)lr1; b.vscale = (float)vs;
   b.seed = d->seed; b.step = d->step; b.count = info->tensors;
   b.fast = b.eps >= 0x1p-40f;
-  constexpr int U = sb::kAdamwGroups;
-  const auto kernel = info->moments == 8
-                          ? (info->groups == 1 ? sb::adamw_kernel<true, 1> : sb::adamw_kernel<true, U>)
-                          : (info->groups == 1 ? sb::adamw_kernel<false, 1> : sb::adamw_kernel<false, U>);
+  const auto kernel = info->moments == 32 ? sb::adamw_kernel<false, 1>
+                      : info->groups == 1 ? sb::adamw_kernel<true, 1>
+                                          : sb::adamw_kernel<true, sb::kAdamwGroups>;
   kernel<<<(unsigned)info->blocks, 256, 0, sbh::stream_of(stream)>>>(b);
   return sbh::launch_status();
 }
@@ -455,7 +451,7 @@ extern "C" sb_status sb_adamw_unpack(size_t n, const uint8_t* m, const int16_t* 
                                      float* v_out, void* stream) {
   if (n == 0) return SB_OK;
   if (n >= (1ull << 40)) return SB_ERR_INVALID_ARG;
-  if (n >= (1ull << 36)) return SB_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
+  if (n >= (1ull << 34)) return SB_ERR_UNSUPPORTED;   // a launch has fewer than 2^32 lanes
   if ((m_out && (!m || !m_top)) || (v_out && (!v || !v_top))) return SB_ERR_INVALID_ARG;
   if (!aligned(m_out, 4) || !aligned(v_out, 4) || !aligned(m_top, 2) || !aligned(v_top, 2))
     return SB_ERR_INVALID_ARG;
@@ -468,9 +464,6 @@ extern "C" sb_status sb_adamw_unpack(size_t n, const uint8_t* m, const int16_t* 
     if (sbh::overlaps(m_out, n * 4, in[i], inb[i]) || sbh::overlaps(v_out, n * 4, in[i], inb[i]))
       return SB_ERR_INVALID_ARG;
   if (sbh::overlaps(m_out, n * 4, v_out, n * 4)) return SB_ERR_INVALID_ARG;
-  const int groups = n < sb::kAdamwSmall ? 1 : sb::kAdamwGroups;
-  const size_t blocks = (n + 1024 * groups - 1) / (1024 * groups);
-  const auto kernel = groups == 1 ? sb::adamw_unpack_kernel<1> : sb::adamw_unpack_kernel<sb::kAdamwGroups>;
-  kernel<<<(unsigned)blocks, 256, 0, sbh::stream_of(stream)>>>(n, m, m_top, v, v_top, m_out, v_out);
+  sb::adamw_unpack_kernel<<<(unsigned)((n + 1023) / 1024), 256, 0, sbh::stream_of(stream)>>>(n, m, m_top, v, v_top, m_out, v_out);
   return sbh::launch_status();
 }

@@ -29,7 +29,7 @@ def _plan(tensors=None, moments=32, count=None, plan=PLAN, short=0, info=True):
                                         ctypes.byref(out) if info else None, None)
 
 
-def _update(plan=PLAN, info=(1, 32, 4, 1), counter=None, **over):
+def _update(plan=PLAN, info=(1, 32, 1, 1), counter=None, **over):
     d = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0)
     d.update(over)
     return sb.load().sb_adamw_update(ctypes.byref(sb.sb_adamw_desc(**d)),
@@ -43,9 +43,9 @@ BAD = sb.SB_ERR_INVALID_ARG
     dict(step=0), dict(step=-3), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.0),
     dict(beta2=float("nan")), dict(eps=-1e-8), dict(eps=float("inf")), dict(lr=float("nan")),
     dict(lr=1e300), dict(lr=float("inf")), dict(counter=P + 2), dict(plan=None), dict(plan=PLAN + 8),
-    dict(info=(1, 16, 4, 1)), dict(info=(-1, 32, 4, 1)), dict(info=(513, 32, 4, 600)),
-    dict(info=(2, 32, 4, 1)), dict(info=(0, 32, 4, 1)), dict(info=(1, 8, 4, -1)),
-    dict(info=(1, 32, 2, 1))])
+    dict(info=(1, 16, 1, 1)), dict(info=(-1, 32, 1, 1)), dict(info=(513, 32, 1, 600)),
+    dict(info=(2, 32, 1, 1)), dict(info=(0, 32, 1, 1)), dict(info=(1, 8, 1, -1)),
+    dict(info=(1, 32, 2, 1)), dict(info=(1, 8, 4, 1)), dict(info=(1, 8, 0, 1))])
 def test_bad_updates_are_refused(over):
     assert _update(**over) == BAD
 
@@ -111,8 +111,8 @@ def test_unpack_refusals(args):
 
 
 def test_more_elements_than_a_launch_has_lanes_for():
-    assert _plan([dict(n=1 << 35)]) == sb.SB_ERR_UNSUPPORTED
-    assert sb.load().sb_adamw_unpack(1 << 36, P, P, P, P, P, P, None) == sb.SB_ERR_UNSUPPORTED
+    assert _plan([dict(n=1 << 33)]) == sb.SB_ERR_UNSUPPORTED
+    assert sb.load().sb_adamw_unpack(1 << 34, P, P, P, P, P, P, None) == sb.SB_ERR_UNSUPPORTED
 
 
 def test_none_is_refused_by_the_library():

@@ -286,3 +286,30 @@ def test_lists_of_a_plan_used_on_several_streams():
         torch.cuda.synchronize()
         for a, b in zip(t, u):
             assert torch.equal(a, b)
+
+
+def test_moments_in_bytes_of_very_many_elements():
+    """As many elements as take two groups a lane: the same bits as in pieces that do not."""
+    print_case("adamw_very_many")
+    n = (24 << 20) + 4099
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w, grad = (torch.randn(n, generator=g, device="cuda") * s for s in (0.02, 1e-3))
+    out = []
+    for pieces in (1, 4):
+        x, st = w.clone(), sb.adamw_moments(w, 8)
+        size = -(-n // pieces) // 256 * 256 + 256
+        lists = []
+        for a in range(0, n, size):
+            b = min(n, a + size)
+            tops = slice(a // 256, -(-b // 256))
+            lists.append(sb.AdamwList([dict(w=x[a:b], g=grad[a:b], m=st["m"][a:b], v=st["v"][a:b],
+                                            m_top=st["m_top"][tops], v_top=st["v_top"][tops], first=a)]))
+        for t in (1, 2):
+            for lst in lists:
+                sb.sb_adamw_update(lst, LR, B1, B2, EPS, step=t, seed=7)
+        torch.cuda.synchronize()
+        out.append((x, st, len(lists), lists[0].info.groups))
+    assert (out[0][2:], out[1][2:]) == ((1, 2), (4, 1))
+    assert torch.equal(out[0][0], out[1][0])
+    for key in out[0][1]:
+        assert torch.equal(out[0][1][key], out[1][1][key]), key
