@@ -331,52 +331,91 @@ __global__ __launch_bounds__(512) void gated_few_fwd(FewArgs g) {
   }
 }
 
-// dx of M rows: a wave has four rows of both weights, its lanes the columns; d: da and
-// du (their first parts), rows of np.
+// Backward of M rows, one launch: da and du are so few that every block forms those it
+// needs (as a pass of their own and products on tiles, four launches: 2 x 1024 x 1280 bf16
+// 17.2 us, like this FEW_BWD).
+struct FewBwdArgs {
+  const void *x, *w[2], *dy;
+  const float* pre;
+  void* dx;
+  float *dw[2], *db[2];
+  int m, n, k, ldx, ldy, act, accumulate;
+  int first, strips, lines;                          // first: blocks of dx; lines of k a block behind
+};
+
+// da and du of four columns of a row, those from `left` on 0.
+template <class E>
+__device__ __forceinline__ void few_gates(const FewBwdArgs& g, int r, int c, int left, f4& da, f4& du) {
+  const float* pa = g.pre + (size_t)r * g.n + c;
+  const f4 a = load_quad<float>(pa, left), u = load_quad<float>(pa + (size_t)g.m * g.n, left);
+  const f4 dy = load_quad<E>((const E*)g.dy + (size_t)r * g.ldy + c, left);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float f, df;
+    gate_act(g.act, a[e], f, df);
+    da[e] = e < left ? dy[e] * u[e] * df : 0.f;
+    du[e] = e < left ? dy[e] * f : 0.f;
+  }
+}
+
+// dx: a wave has four rows of both weights, its lanes the columns; the block's waves share
+// out da and du (bf16: rounded) of 64 pieces at a time.
 template <class E, int M>
-__global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k, int ldx,
-                                                    const E* __restrict__ da,
-                                                    const E* __restrict__ du,
-                                                    const E* __restrict__ wg,
-                                                    const E* __restrict__ wu, E* dx) {
+__device__ __forceinline__ void few_dx_block(const FewBwdArgs& g, int block, u32x4* lds) {
   constexpr int V = kFewWidth<E>, R = 4;
-  const int lane = threadIdx.x & 63;
-  const int k0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * R;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int k0 = (block * 4 + wave) * R;
   float acc[R][M];
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int r = 0; r < M; ++r) acc[i][r] = 0.f;
-  for (int c0 = lane * V; c0 < n; c0 += 64 * V) {
-    const int skip = max(c0 + V - n, 0), c = c0 - skip;
+  u32x4* d = lds;                                    // [2][M][64], twice
+  for (int b = 0, odd = 0; b < g.n; b += 64 * V, odd ^= 1) {
+    const int c0 = b + lane * V, c = min(c0, g.n - V), skip = c0 - c;
+    u32x4 w[2][R];
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      u32x4 w[R], d[M];
+    for (int q = 0; q < 2; ++q)
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        w[i] = few_piece<E>((q ? wu : wg) + (size_t)min(k0 + i, k - 1) * n + c);
+        w[q][i] = few_piece<E>((const E*)g.w[q] + (size_t)min(k0 + i, g.k - 1) * g.n + c);
+    d = lds + odd * 2 * M * 64;
+    for (int r = wave; r < g.m; r += 4) {
+      f4 v[2][V / 4];
 #pragma unroll
-      for (int r = 0; r < M; ++r) d[r] = few_piece<E>((q ? du : da) + (size_t)min(r, m - 1) * np + c);
-      if (skip) {
+      for (int i = 0; i < V / 4; ++i) few_gates<E>(g, r, c + 4 * i, 4, v[0][i], v[1][i]);
 #pragma unroll
-        for (int i = 0; i < R; ++i) w[i] = few_without<E>(w[i], skip);
+      for (int q = 0; q < 2; ++q) {
+        u32x4 t;
 #pragma unroll
-        for (int r = 0; r < M; ++r) d[r] = few_without<E>(d[r], skip);
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(E) == 4) t[e] = __float_as_uint(v[q][0][e]);
+          else t[e] = f32x2_to_bf16x2(v[q][e / 2][e % 2 * 2], v[q][e / 2][e % 2 * 2 + 1]);
+        }
+        d[(q * M + r) * 64 + lane] = few_without<E>(t, skip);
       }
-#pragma unroll
-      for (int r = 0; r < M; ++r)
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-          if constexpr (sizeof(E) == 2) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[i][r] = few_dot(w[i][e], d[r][e], acc[i][r]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[i][r] = fmaf(__uint_as_float(w[i][e]), __uint_as_float(d[r][e]), acc[i][r]);
-          }
     }
+    if (skip) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int i = 0; i < R; ++i) w[q][i] = few_without<E>(w[q][i], skip);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < M; ++r)
+      if (r < g.m)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const u32x4 t = d[(q * M + r) * 64 + lane];
+#pragma unroll
+          for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if constexpr (sizeof(E) == 2) acc[i][r] = few_dot(w[q][i][e], t[e], acc[i][r]);
+              else acc[i][r] = fmaf(__uint_as_float(w[q][i][e]), __uint_as_float(t[e]), acc[i][r]);
+            }
+        }
   }
   // The four rows' sums of a row of dx at once, in the four rows of lanes.
   const int row = lane / 16, at = k0 + row / 2 + row % 2 * 2;
@@ -387,8 +426,86 @@ __global__ __launch_bounds__(256) void gated_few_dx(int m, int n, int np, int k,
     v += row_turned<4>(v);
     v += row_turned<2>(v);
     v += row_turned<1>(v);
-    if (lane % 16 == 0 && at < k && r < m) Elem<E>::store(dx, (size_t)r * ldx + at, v);
+    if (lane % 16 == 0 && at < g.k && r < g.m) Elem<E>::store((E*)g.dx, (size_t)r * g.ldx + at, v);
   }
+}
+
+// The weight gradients of 256 columns and g.lines of k, eight lines a wave at a time, and
+// the bias gradients beside the first of them.  What it writes bounds it.
+template <class E, int M>
+__device__ __forceinline__ void few_dw_block(const FewBwdArgs& g, int block, float* lds) {
+  constexpr int V = kFewWidth<E>;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c0 = block % g.strips * 256, c = c0 + lane * 4, k0 = block / g.strips * g.lines;
+  for (int r = wave; r < g.m; r += 4) {
+    f4 da, du;
+    few_gates<E>(g, r, c, g.n - c, da, du);
+    *reinterpret_cast<f4*>(lds + r * 256 + lane * 4) = da;
+    *reinterpret_cast<f4*>(lds + (M + r) * 256 + lane * 4) = du;
+  }
+  __syncthreads();
+  f4 d[2][M];
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int r = 0; r < M; ++r)
+      d[q][r] = r < g.m ? *reinterpret_cast<const f4*>(lds + (q * M + r) * 256 + lane * 4)
+                        : f4{0.f, 0.f, 0.f, 0.f};
+  if (k0 == 0 && wave == 0) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      f4 v = d[q][0];
+#pragma unroll
+      for (int r = 1; r < M; ++r) v += d[q][r];
+      float* db = g.db[q];
+      if (!db) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < g.n) db[c + e] = g.accumulate ? db[c + e] + v[e] : v[e];
+    }
+  }
+  const int k1 = min(g.k, k0 + g.lines);
+  for (int kk = k0 + wave * 8; kk < k1; kk += 32) {
+    const int kx = min(kk, g.k - 8);                 // the last eight may be begun earlier
+    u32x4 x[M][8 / V];
+#pragma unroll
+    for (int r = 0; r < M; ++r)
+#pragma unroll
+      for (int i = 0; i < 8 / V; ++i)
+        x[r][i] = few_piece<E>((const E*)g.x + (size_t)min(r, g.m - 1) * g.ldx + kx + i * V);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (kx + j < kk) continue;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < M; ++r) {
+          if (r >= g.m) continue;
+          const uint32_t t = x[r][j / V][sizeof(E) == 4 ? j % V : j / 2];
+          const float xv = __uint_as_float(sizeof(E) == 4 ? t : j % 2 ? t & 0xffff0000u : t << 16);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(xv, d[q][r][e], v[e]);
+        }
+        float* row = g.dw[q] + (size_t)(kx + j) * g.n + c;
+        if (c + 4 <= g.n) {
+          if (g.accumulate) v += load_quad<float>(row, 4);
+          *reinterpret_cast<u32x4_any*>(row) = __builtin_bit_cast(u32x4, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (c + e < g.n) row[e] = g.accumulate ? row[e] + v[e] : v[e];
+        }
+      }
+    }
+  }
+}
+
+template <class E, int M>
+__global__ __launch_bounds__(256) void gated_few_bwd(FewBwdArgs g) {
+  __shared__ u32x4 lds[2 * 2 * M * 64];
+  if ((int)blockIdx.x < g.first) few_dx_block<E, M>(g, blockIdx.x, lds);
+  else few_dw_block<E, M>(g, (int)blockIdx.x - g.first, reinterpret_cast<float*>(lds));
 }
 
 // Sums of the splits' partials (rows of g.pitch), four columns of a row a lane.  FWD:
@@ -670,7 +787,7 @@ static GatedPacks gated_packs(const sb_gated_desc* d, bool x_at16, bool w_at16) 
   const bool b16 = d->dtype == SB_BF16, few = few_rows(d);
   // (An odd bf16 k_in would end the last line inside the 4 bytes that ranges count in.)
   const bool lines = d->ldx % (b16 ? 8 : 4) != 0 || (b16 && d->k_in % 2 != 0) || !x_at16;
-  return GatedPacks{!few && (lines || d->k_in % 8 != 0), lines,
+  return GatedPacks{!few && (lines || d->k_in % 8 != 0), !few && lines,
                     !few && (d->n_shard % 8 != 0 || !w_at16)};
 }
 
@@ -690,7 +807,9 @@ struct GatedSpace { size_t d, sums, x, w, split, bytes; };
 
 static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks& k) {
   const size_t m = d->m, np = up8(d->n_shard), es = sbh::dsize(d->dtype);
+  const bool few = few_rows(d);
   GatedSpace s{};
+  if (few && pass == SB_FC_BWD) return s;
   size_t at = 0;
   auto take = [&](size_t& part, size_t bytes) {
     part = at;
@@ -702,16 +821,12 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
   }
   if (pass == SB_FC_FWD ? k.x : k.lines) take(s.x, m * up8(d->k_in) * es);
   if (k.w) take(s.w, 2 * (size_t)d->k_in * np * es);
-  const bool few = few_rows(d);
   size_t split = 0;
   if (pass == SB_FC_FWD) {
     split = few ? few_plan(d).ws_bytes : gated_plan_fwd(d).ws_bytes;
   } else {
-    split = gated_plan_dw(d).ws_bytes;
-    if (!few) {
-      const GradPlan p = gated_plan_grads(d);
-      split = std::max(split, round_up(p.dx.ws_bytes, 256) + p.dw.ws_bytes);
-    }
+    const GradPlan p = gated_plan_grads(d);
+    split = std::max(gated_plan_dw(d).ws_bytes, round_up(p.dx.ws_bytes, 256) + p.dw.ws_bytes);
   }
   take(s.split, split);
   s.bytes = at;
@@ -819,18 +934,24 @@ static void gated_fwd_run(const sb_gated_desc* d, const void* x, const void* con
   fwd_run<E>(g, gated_plan_fwd(d), d->act, (float*)(ws + sp.split), st);
 }
 
-template <class E, int M>
-static void few_dx(const sb_gated_desc* d, int np, const E* da, const E* du, const void* const* w,
-                   void* dx, hipStream_t st) {
-  gated_few_dx<E, M><<<(unsigned)cdiv(d->k_in, 16), 256, 0, st>>>(
-      d->m, d->n_shard, np, d->k_in, d->ldx, da, du, (const E*)w[0], (const E*)w[1], (E*)dx);
-}
-
 template <class E>
 static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* const* w,
                           const float* pre, const void* dy, void* dx, float* const* dw,
                           float* const* db, int accumulate, const GatedPacks& packs, char* ws,
                           const GatedSpace& sp, hipStream_t st) {
+  if (few_rows(d)) {
+    const int strips = cdiv(d->n_shard, 256);
+    int lines = 32;                                  // about 512 blocks and more
+    while (lines < d->k_in && strips * (int64_t)cdiv(d->k_in, 2 * lines) >= 512) lines *= 2;
+    const FewBwdArgs g{x, {w[0], w[1]}, dy, pre, dx, {dw[0], dw[1]}, {db[0], db[1]}, d->m,
+                       d->n_shard, d->k_in, d->ldx, d->ldy, d->act, accumulate,
+                       dx ? cdiv(d->k_in, 16) : 0, strips, lines};
+    const int blocks = g.first + strips * cdiv(d->k_in, lines);
+    const auto kernel = d->m == 1 ? gated_few_bwd<E, 1> : d->m == 2 ? gated_few_bwd<E, 2>
+                        : d->m <= 4 ? gated_few_bwd<E, 4> : gated_few_bwd<E, 8>;
+    kernel<<<blocks, 256, 0, st>>>(g);
+    return;
+  }
   constexpr int NP = sizeof(E) == 2 ? 3 : 1;
   const int np = up8(d->n_shard), rows = act_rows(d->m, np), chunks = cdiv(d->m, rows);
   const size_t plane = (size_t)d->m * np;
@@ -852,7 +973,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   gw.b_bytes = (uint32_t)(plane * sizeof(E));
   gw.c[0] = dw[0]; gw.c[1] = dw[1]; gw.ldc = d->n_shard;
   gw.accumulate = accumulate;
-  if (dx && !few_rows(d)) {
+  if (dx) {
     DualArgs gx{};
     for (int q = 0; q < 2; ++q) {
       gx.a[q] = parts + NP * q * plane;
@@ -865,13 +986,6 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
     gx.c[0] = dx; gx.ldc = d->ldx;
     grads_run<E>(gx, gw, bias, gated_plan_grads(d), ws + sp.split, st);
     return;
-  }
-  if (dx) {
-    const E *da = parts, *du = parts + NP * plane;
-    if (d->m == 1) few_dx<E, 1>(d, np, da, du, w, dx, st);
-    else if (d->m == 2) few_dx<E, 2>(d, np, da, du, w, dx, st);
-    else if (d->m <= 4) few_dx<E, 4>(d, np, da, du, w, dx, st);
-    else few_dx<E, 8>(d, np, da, du, w, dx, st);
   }
   grads_run<E>(DualArgs{}, gw, bias, GradPlan{{}, gated_plan_dw(d)}, ws + sp.split, st);
 }
@@ -935,8 +1049,8 @@ extern "C" sb_status sb_gated_shard_bwd(const sb_gated_desc* d, const void* x, c
   if (spans_meet(outs, 6, ins, 5)) return SB_ERR_INVALID_ARG;
   for (int i = 0; i < 5; ++i)
     if (spans_meet(outs + i, 1, outs + i + 1, 5 - i)) return SB_ERR_INVALID_ARG;
-  if (!ws || ws_bytes < sp.bytes) return SB_ERR_WORKSPACE;
-  if (!at16(ws)) return SB_ERR_INVALID_ARG;
+  if (sp.bytes > 0 && (!ws || ws_bytes < sp.bytes)) return SB_ERR_WORKSPACE;
+  if (sp.bytes > 0 && !at16(ws)) return SB_ERR_INVALID_ARG;
   const void* w[2] = {w_gate, w_up};
   float* dw[2] = {dw_gate, dw_up};
   float* db[2] = {db_gate, db_up};

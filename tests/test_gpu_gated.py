@@ -405,3 +405,21 @@ def test_ends_of_few_rows(m, k, n, dtype):
         lim = (k + 2) * 2.0 ** -23 * (np.abs(x[:, :k]).astype(np.float64) @ np.maximum(np.abs(wg), np.abs(c.wu)) + 2)
         ok = np.isfinite(r)
         assert np.all(np.abs(g[ok] - r[ok]) <= lim[ok])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n", [(1, 8, 140000), (3, 300, 70001), (8, 70001, 9), (5, 4100, 600)])
+def test_long_sides_of_few_rows(m, k, n, dtype):
+    """Accumulated gradients of many strips and of many lines a block; without dx."""
+    print_case("gated_long", m=m, k=k, n=n, dtype=dtype)
+    c = Case("silu", dtype, m, k, n)
+    c.fwd()
+    c.bwd()
+    c.check(ALL)
+    for t in ("dwg", "dwu", "dbg", "dbu"):
+        c.d[t].fill_(3.0)
+    c.d["dx"].fill_(77)
+    c.bwd(accumulate=True, dx=False)
+    c.check(("dwg", "dwu", "dbg", "dbu"), base=3.0)
+    assert bool((c.d["dx"] == 77).all())
+    c.untouched(ALL + ("pre",))
