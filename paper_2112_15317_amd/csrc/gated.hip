@@ -331,9 +331,13 @@ __global__ __launch_bounds__(512) void gated_few_fwd(FewArgs g) {
   }
 }
 
-// Backward of M rows, one launch: da and du are so few that every block forms those it
-// needs (as a pass of their own and products on tiles, four launches: 2 x 1024 x 1280 bf16
-// 17.2 us, like this FEW_BWD).
+// Backward of M rows, one launch: da and du of one or two rows are so few that every block
+// forms those it needs (as a pass of their own and products on tiles: 2 x 1024 x 1280 bf16
+// 17.2 us, like this 8.0).  From three rows on dx takes them from the pass over dy (8 x
+// 2048 x 2048 fp32 30.0 us without it, 21.5 with it), the weight gradients' blocks,
+// which need a strip of them, do not.
+constexpr int kFewGates = 2;
+constexpr int kFewDx = 16;                           // lines of k a block of dx
 struct FewBwdArgs {
   const void *x, *w[2], *dy;
   const float* pre;
@@ -341,6 +345,7 @@ struct FewBwdArgs {
   float *dw[2], *db[2];
   int m, n, k, ldx, ldy, act, accumulate;
   int first, strips, lines;                          // first: blocks of dx; lines of k a block behind
+  const void* d[2]; int np;                          // da and du from the pass, M > kFewGates
 };
 
 // da and du of four columns of a row, those from `left` on 0.
@@ -358,66 +363,47 @@ __device__ __forceinline__ void few_gates(const FewBwdArgs& g, int r, int c, int
   }
 }
 
-// dx: a wave has four rows of both weights, its lanes the columns; the block's waves share
-// out da and du (bf16: rounded) of 64 pieces at a time.
+// dx of rows whose da and du the pass has formed: a wave has four lines of both weights,
+// its lanes the columns.
 template <class E, int M>
-__device__ __forceinline__ void few_dx_block(const FewBwdArgs& g, int block, u32x4* lds) {
+__device__ __forceinline__ void few_dx_lines(const FewBwdArgs& g, int block) {
   constexpr int V = kFewWidth<E>, R = 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int k0 = (block * 4 + wave) * R;
+  const int lane = threadIdx.x & 63;
+  const int k0 = (block * 4 + (threadIdx.x >> 6)) * R;
   float acc[R][M];
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int r = 0; r < M; ++r) acc[i][r] = 0.f;
-  u32x4* d = lds;                                    // [2][M][64], twice
-  for (int b = 0, odd = 0; b < g.n; b += 64 * V, odd ^= 1) {
-    const int c0 = b + lane * V, c = min(c0, g.n - V), skip = c0 - c;
-    u32x4 w[2][R];
+  for (int c0 = lane * V; c0 < g.n; c0 += 64 * V) {
+    const int skip = max(c0 + V - g.n, 0), c = c0 - skip;
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+    for (int q = 0; q < 2; ++q) {
+      u32x4 w[R], d[M];
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        w[q][i] = few_piece<E>((const E*)g.w[q] + (size_t)min(k0 + i, g.k - 1) * g.n + c);
-    d = lds + odd * 2 * M * 64;
-    for (int r = wave; r < g.m; r += 4) {
-      f4 v[2][V / 4];
+        w[i] = few_piece<E>((const E*)g.w[q] + (size_t)min(k0 + i, g.k - 1) * g.n + c);
 #pragma unroll
-      for (int i = 0; i < V / 4; ++i) few_gates<E>(g, r, c + 4 * i, 4, v[0][i], v[1][i]);
+      for (int r = 0; r < M; ++r)
+        d[r] = few_piece<E>((const E*)g.d[q] + (size_t)min(r, g.m - 1) * g.np + c);
+      if (skip) {
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32x4 t;
+        for (int i = 0; i < R; ++i) w[i] = few_without<E>(w[i], skip);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (sizeof(E) == 4) t[e] = __float_as_uint(v[q][0][e]);
-          else t[e] = f32x2_to_bf16x2(v[q][e / 2][e % 2 * 2], v[q][e / 2][e % 2 * 2 + 1]);
-        }
-        d[(q * M + r) * 64 + lane] = few_without<E>(t, skip);
+        for (int r = 0; r < M; ++r) d[r] = few_without<E>(d[r], skip);
       }
+#pragma unroll
+      for (int r = 0; r < M; ++r)
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(E) == 2) acc[i][r] = few_dot(w[i][e], d[r][e], acc[i][r]);
+            else acc[i][r] = fmaf(__uint_as_float(w[i][e]), __uint_as_float(d[r][e]), acc[i][r]);
+          }
     }
-    if (skip) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q)
-#pragma unroll
-        for (int i = 0; i < R; ++i) w[q][i] = few_without<E>(w[q][i], skip);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < M; ++r)
-      if (r < g.m)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const u32x4 t = d[(q * M + r) * 64 + lane];
-#pragma unroll
-          for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if constexpr (sizeof(E) == 2) acc[i][r] = few_dot(w[q][i][e], t[e], acc[i][r]);
-              else acc[i][r] = fmaf(__uint_as_float(w[q][i][e]), __uint_as_float(t[e]), acc[i][r]);
-            }
-        }
   }
-  // The four rows' sums of a row of dx at once, in the four rows of lanes.
+  // The sums of four lines at once, in the four rows of lanes.
   const int row = lane / 16, at = k0 + row / 2 + row % 2 * 2;
 #pragma unroll
   for (int r = 0; r < M; ++r) {
@@ -428,6 +414,74 @@ __device__ __forceinline__ void few_dx_block(const FewBwdArgs& g, int block, u32
     v += row_turned<1>(v);
     if (lane % 16 == 0 && at < g.k && r < g.m) Elem<E>::store((E*)g.dx, (size_t)r * g.ldx + at, v);
   }
+}
+
+// dx of up to kFewGates rows: a block has kFewDx lines of both weights, each wave 64 pieces
+// of them at a time, whose da and du (bf16: rounded) it forms.  (With more rows that many
+// activations a wave take longer than all the rest: 8 x 1024 x 1024 bf16 23.8 us for 12.7.)
+template <class E, int M>
+__device__ __forceinline__ void few_dx_block(const FewBwdArgs& g, int block, float* lds) {
+  constexpr int V = kFewWidth<E>, R = kFewDx;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int k0 = block * R;
+  float acc[R][M];
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+#pragma unroll
+    for (int r = 0; r < M; ++r) acc[i][r] = 0.f;
+  for (int b = wave * 64 * V; b < g.n; b += 4 * 64 * V) {
+    const int c0 = b + lane * V, c = min(c0, g.n - V), skip = c0 - c;
+    u32x4 d[2][M];
+#pragma unroll
+    for (int r = 0; r < M; ++r) {
+      f4 v[2][V / 4];
+#pragma unroll
+      for (int i = 0; i < V / 4; ++i)
+        few_gates<E>(g, min(r, g.m - 1), c + 4 * i, 4, v[0][i], v[1][i]);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x4 t;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if constexpr (sizeof(E) == 4) t[e] = __float_as_uint(v[q][0][e]);
+          else t[e] = f32x2_to_bf16x2(v[q][e / 2][e % 2 * 2], v[q][e / 2][e % 2 * 2 + 1]);
+        }
+        d[q][r] = few_without<E>(t, skip);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        u32x4 w = few_piece<E>((const E*)g.w[q] + (size_t)min(k0 + i, g.k - 1) * g.n + c);
+        if (skip) w = few_without<E>(w, skip);
+#pragma unroll
+        for (int r = 0; r < M; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (sizeof(E) == 2) acc[i][r] = few_dot(w[e], d[q][r][e], acc[i][r]);
+            else acc[i][r] = fmaf(__uint_as_float(w[e]), __uint_as_float(d[q][r][e]), acc[i][r]);
+          }
+      }
+  }
+  // The sums of four lines at once, in the four rows of lanes.
+  const int row = lane / 16, at = row / 2 + row % 2 * 2;
+#pragma unroll
+  for (int i = 0; i < R; i += 4)
+#pragma unroll
+    for (int r = 0; r < M; ++r) {
+      float v = rows_sum(acc[i][r], acc[i + 1][r], acc[i + 2][r], acc[i + 3][r]);
+      v += row_turned<8>(v);
+      v += row_turned<4>(v);
+      v += row_turned<2>(v);
+      v += row_turned<1>(v);
+      if (lane % 16 == 0) lds[(wave * M + r) * R + i + at] = v;
+    }
+  __syncthreads();
+  const int r = threadIdx.x / R, i = threadIdx.x % R;
+  if (r < g.m && r < M && k0 + i < g.k)
+    Elem<E>::store((E*)g.dx, (size_t)r * g.ldx + k0 + i,
+                   (lds[r * R + i] + lds[(M + r) * R + i]) + (lds[(2 * M + r) * R + i] + lds[(3 * M + r) * R + i]));
 }
 
 // The weight gradients of 256 columns and g.lines of k, eight lines a wave at a time, and
@@ -503,9 +557,11 @@ __device__ __forceinline__ void few_dw_block(const FewBwdArgs& g, int block, flo
 
 template <class E, int M>
 __global__ __launch_bounds__(256) void gated_few_bwd(FewBwdArgs g) {
-  __shared__ u32x4 lds[2 * 2 * M * 64];
-  if ((int)blockIdx.x < g.first) few_dx_block<E, M>(g, blockIdx.x, lds);
-  else few_dw_block<E, M>(g, (int)blockIdx.x - g.first, reinterpret_cast<float*>(lds));
+  __shared__ __attribute__((aligned(16))) float lds[2 * M * 256];
+  if ((int)blockIdx.x < g.first) {
+    if constexpr (M <= kFewGates) few_dx_block<E, M>(g, blockIdx.x, lds);
+    else few_dx_lines<E, M>(g, blockIdx.x);
+  } else few_dw_block<E, M>(g, (int)blockIdx.x - g.first, lds);
 }
 
 // Sums of the splits' partials (rows of g.pitch), four columns of a row a lane.  FWD:
@@ -809,7 +865,7 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
   const size_t m = d->m, np = up8(d->n_shard), es = sbh::dsize(d->dtype);
   const bool few = few_rows(d);
   GatedSpace s{};
-  if (few && pass == SB_FC_BWD) return s;
+  if (few && pass == SB_FC_BWD && d->m <= kFewGates) return s;
   size_t at = 0;
   auto take = [&](size_t& part, size_t bytes) {
     part = at;
@@ -817,6 +873,10 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
   };
   if (pass == SB_FC_BWD) {
     take(s.d, m * np * (d->dtype == SB_BF16 ? 12 : 8));
+    if (few) {
+      s.bytes = at;
+      return s;
+    }
     take(s.sums, (size_t)cdiv(d->m, act_rows(d->m, (int)np)) * np * 8);
   }
   if (pass == SB_FC_FWD ? k.x : k.lines) take(s.x, m * up8(d->k_in) * es);
@@ -939,29 +999,31 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
                           const float* pre, const void* dy, void* dx, float* const* dw,
                           float* const* db, int accumulate, const GatedPacks& packs, char* ws,
                           const GatedSpace& sp, hipStream_t st) {
-  if (few_rows(d)) {
+  constexpr int NP = sizeof(E) == 2 ? 3 : 1;
+  const int np = up8(d->n_shard), rows = act_rows(d->m, np), chunks = cdiv(d->m, rows);
+  const size_t plane = (size_t)d->m * np;
+  E* parts = (E*)(ws + sp.d);
+  const bool few = few_rows(d), pass = !few || (dx && d->m > kFewGates);
+  const BiasSums bias{!few && (db[0] || db[1]) && chunks > 1 ? (float*)(ws + sp.sums) : nullptr,
+                      {few ? nullptr : db[0], few ? nullptr : db[1]}, d->n_shard, np, chunks, accumulate};
+  const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp);
+  if (pass)
+    gated_act_bwd<E><<<(unsigned)(cdiv(np, 256) * chunks + o.packs.block0[3]), 256, 0, st>>>(
+        d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, bias, rows, chunks, o.packs);
+  if (few) {
     const int strips = cdiv(d->n_shard, 256);
     int lines = 32;                                  // about 512 blocks and more
     while (lines < d->k_in && strips * (int64_t)cdiv(d->k_in, 2 * lines) >= 512) lines *= 2;
     const FewBwdArgs g{x, {w[0], w[1]}, dy, pre, dx, {dw[0], dw[1]}, {db[0], db[1]}, d->m,
                        d->n_shard, d->k_in, d->ldx, d->ldy, d->act, accumulate,
-                       dx ? cdiv(d->k_in, 16) : 0, strips, lines};
+                       dx ? cdiv(d->k_in, kFewDx) : 0, strips, lines,
+                       {parts, parts + NP * plane}, np};
     const int blocks = g.first + strips * cdiv(d->k_in, lines);
     const auto kernel = d->m == 1 ? gated_few_bwd<E, 1> : d->m == 2 ? gated_few_bwd<E, 2>
                         : d->m <= 4 ? gated_few_bwd<E, 4> : gated_few_bwd<E, 8>;
     kernel<<<blocks, 256, 0, st>>>(g);
     return;
   }
-  constexpr int NP = sizeof(E) == 2 ? 3 : 1;
-  const int np = up8(d->n_shard), rows = act_rows(d->m, np), chunks = cdiv(d->m, rows);
-  const size_t plane = (size_t)d->m * np;
-  E* parts = (E*)(ws + sp.d);
-  const BiasSums bias{(db[0] || db[1]) && chunks > 1 ? (float*)(ws + sp.sums) : nullptr,
-                      {db[0], db[1]}, d->n_shard, np, chunks, accumulate};
-  const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp);
-  gated_act_bwd<E><<<(unsigned)(cdiv(np, 256) * chunks + o.packs.block0[3]), 256, 0, st>>>(
-      d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, bias, rows, chunks,
-      o.packs);
   DualArgs gw{};
   for (int p = 0; p < NP; ++p) {                     // the smallest parts first
     gw.a[p] = o.x;
