@@ -366,7 +366,7 @@ typedef struct {
 /* Workspace bytes for `pass` (SB_FC_FWD, SB_FC_BWD); (size_t)-1 for an invalid
  * descriptor, and for one whose x, y or weights, or 32 rows of x or of a weight, reach
  * 2^31 bytes (the calls return SB_ERR_UNSUPPORTED).  The workspace starts at a multiple
- * of 16.
+ * of 16; where its size is 0 it may be NULL.
  * Operands that no 16-byte access fits are laid out anew in it: those of odd sizes
  * or strides always have their room; for x or weights whose addresses are not
  * multiples of 16 the query is asked with SB_UNALIGNED (a call with less returns

@@ -554,7 +554,8 @@ class AdamwList:
             self.moments, n, self.tensors, _ptr(self.plan), need, ctypes.byref(self.info),
             _stream_for(self.plan, stream)))
         if not torch.cuda.is_current_stream_capturing():
-            torch.cuda.synchronize()
+            s = torch.cuda.current_stream() if stream is None else stream
+            s.synchronize() if hasattr(s, "synchronize") else torch.cuda.synchronize()
 
 
 def adamw_moments(w, moments=32):
