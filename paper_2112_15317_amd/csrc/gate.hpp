@@ -42,7 +42,8 @@ __device__ __forceinline__ void gate_act(int act, float a, float& f, float& df) 
 // pre (this row's a; u is `plane` elements behind) where it is kept, act(a) u to y
 // (this row's).
 template <class E>
-__device__ __forceinline__ void gate_store(int act, f4 a, f4 u, int n, int N, float* pre, size_t plane, E* y) {
+__device__ __forceinline__ void gate_store(int act, f4 a, f4 u, int n, int N, float* pre, size_t plane,
+                                           E* y) {
   const bool whole = n + 4 <= N;
   f4 o;
 #pragma unroll
