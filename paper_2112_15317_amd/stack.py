@@ -413,9 +413,9 @@ class FCShard:
 
 
 class GatedShard:
-    """One gated FC column shard: X [m, k_in] (row stride ldx), W [2, k_in, ns]
-    (the gate's weight, then the other projection's), ``pre`` what the forward
-    keeps for the backward."""
+    """One gated FC column shard: X [m, k_in] (row stride ldx, from a multiple of
+    16 bytes on), W [2, k_in, ns] (the gate's weight, then the other
+    projection's), ``pre`` what the forward keeps for the backward."""
 
     def __init__(self, m, k_in, ns, act="silu", dtype="f32", ldx=None, ldy=None, device="cuda"):
         self.m, self.k_in, self.ns, self.act = m, k_in, ns, act
