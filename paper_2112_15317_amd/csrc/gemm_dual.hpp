@@ -495,9 +495,10 @@ __device__ __forceinline__ void dual_block(const DualArgs& g, int block, u16* ld
                         ? A[AKC ? (size_t)ar[i] * g.lda + k : (size_t)k * g.lda + ar[i]] : 0.f;
 #pragma unroll
           for (int j = 0; j < F; ++j) {
+            // (The weights end at b_bytes, before K where FWD's rows of x are padded.)
             const float* B = (const float*)g.b[BKC ? 0 : j / (F / 2)][sg];
-            const float bv = k < ke && bc[j] < g.N
-                                 ? B[BKC ? (size_t)bc[j] * g.ldb + k : (size_t)k * g.ldb + bc[j]] : 0.f;
+            const size_t at = BKC ? (size_t)bc[j] * g.ldb + k : (size_t)k * g.ldb + bc[j];
+            const float bv = k < ke && bc[j] < g.N && at < g.b_bytes / sizeof(float) ? B[at] : 0.f;
 #pragma unroll
             for (int i = 0; i < FA; ++i)
               acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(bv, av[i], acc[j][i], 0, 0, 0);
