@@ -451,12 +451,12 @@ class AdamW:
 
 
 class _Updates:
-    """The updates of one set of (parameter, gradient, scale, decays): SGD at a
-    rate, or AdamW with the moments and a counter of its updates on the
-    device, so that a captured step counts on when it is replayed."""
+    """The updates of one set of (parameter, gradient, scale, decays): SGD, or
+    AdamW with the moments and a counter of its updates on the device, so that
+    a captured step counts on when it is replayed."""
 
-    def __init__(self, items, lr, adamw):
-        self.lr, self.adamw = lr, adamw
+    def __init__(self, items, adamw):
+        self.adamw = adamw
         if adamw is None:
             self.list = sb.SgdList([(w, g, scale) for w, g, scale, _ in items])
             return
@@ -466,11 +466,11 @@ class _Updates:
                                   for (w, g, scale, decays), m in zip(items, self.moments)])
         self.done = torch.zeros(1, dtype=torch.int32, device=items[0][0].device)
 
-    def calls(self, name, k, stream):
-        """The (key, libsb function, args) calls of one update."""
+    def calls(self, name, k, lr, stream):
+        """The (key, libsb function, args) calls of one update; lr: SGD's rate."""
         a = self.adamw
         if a is None:
-            return [(("sgd_" + name, k), sb.sb_sgd_update, (self.list, self.lr, stream))]
+            return [(("sgd_" + name, k), sb.sb_sgd_update, (self.list, lr, stream))]
         return [(("adamw_" + name, k), sb.sb_adamw_update,
                  (self.list, a.lr, a.beta1, a.beta2, a.eps, 1, a.seed, self.done, stream)),
                 (("adamw_count_" + name, k), sb.sb_adamw_advance, (self.done, stream))]
@@ -603,7 +603,8 @@ class GroupTrainStep:
 
     After the K iterations slot 0 of ``dlocal`` holds the gradient of worker
     0's conv output over its whole local batch: the conv stack runs backward
-    and takes one SGD step at rate lr.
+    and takes one SGD step at rate lr.  ``lr`` is read at every update, so it may
+    be set between steps.
 
     With ``adamw`` (an ``AdamW``) the updates are ``sb_adamw_update`` ones, on
     the same gradients and scales, lr unused; FC shards and conv layers count
@@ -699,12 +700,14 @@ class GroupTrainStep:
         self.ws = torch.empty((max(need, 256) + 255) // 256 * 256, dtype=torch.uint8, device=dev)
         self.update_fc = _Updates([(self.W[j], self.dW[j], 1.0 / K, True) for j in range(L)] +
                                   [(self.b[j], self.db[j], 1.0 / K, False) for j in range(L)],
-                                  lr, adamw)
+                                  adamw)
         c = self.conv
         n_conv = len(c.layers)
         self.update_conv = _Updates([(c.W[i], c.dW[i], 1.0, True) for i in range(n_conv)] +
                                     [(c.b[i], c.db[i], 1.0, False) for i in range(n_conv)],
-                                    lr, adamw)
+                                    adamw)
+        self.sgd_fc, self.sgd_conv = ((None, None) if adamw else
+                                      (self.update_fc.list, self.update_conv.list))
         self.call = _plain      # hook: every libsb call of the step goes through it
 
     def load_inputs(self, x, conv_w, conv_b, fc_w, fc_b, local_remote, labels):
@@ -777,13 +780,13 @@ class GroupTrainStep:
             else:
                 c(("mbwd", k), sb.sb_modulo_bwd, self.mdesc, 0, k, self.dF[0], self.dlocal,
                   None, None, stream)
-        for key, fn, args in self.update_fc.calls("fc", k, stream):
+        for key, fn, args in self.update_fc.calls("fc", k, self.lr, stream):
             c(key, fn, *args)
 
     def finish(self, stream=None):
         """Conv backward from the gathered local-row gradients, conv update."""
         self.conv.backward(stream)
-        for key, fn, args in self.update_conv.calls("conv", 0, stream):
+        for key, fn, args in self.update_conv.calls("conv", 0, self.lr, stream):
             self.call(key, fn, *args)
 
     def step(self, stream=None):
