@@ -502,7 +502,9 @@ class AdamwList:
     (sb_adamw_make_plan): built once, passed to every call (the list and its
     tensors must stay alive until the calls' kernels have run).  The plan is
     written before this returns, so that any stream may use it; a list built
-    while its stream is captured is the graph's alone.
+    while its stream is captured is the graph's alone (while another stream is
+    captured, none is built).  stream: where the plan is written, the current one
+    by default.
 
     items: dicts of a parameter ``w``, its gradient ``g`` (fp32) and moments
     ``m`` and ``v`` (fp32; or uint8, with their references ``m_top`` and
@@ -548,14 +550,23 @@ class AdamwList:
             t.grad_scale, t.decay = it.get("scale", 1.0), it.get("decay", 0.0)
             first = t.first + size
         need = load().sb_adamw_plan_bytes(n)
-        self.plan = torch.empty((need,), dtype=torch.uint8, device=items[0]["w"].device)
-        self.info = sb_adamw_plan()
-        _check("sb_adamw_make_plan", load().sb_adamw_make_plan(
-            self.moments, n, self.tensors, _ptr(self.plan), need, ctypes.byref(self.info),
-            _stream_for(self.plan, stream)))
-        if not torch.cuda.is_current_stream_capturing():
-            s = torch.cuda.current_stream() if stream is None else stream
-            s.synchronize() if hasattr(s, "synchronize") else torch.cuda.synchronize()
+        current = torch.cuda.current_stream()
+        s = (current if stream is None else stream if isinstance(stream, torch.cuda.Stream)
+             else torch.cuda.ExternalStream(_stream(stream)))
+        other = torch.cuda.is_current_stream_capturing() and s != current
+        with torch.cuda.stream(s):
+            capturing = torch.cuda.is_current_stream_capturing()
+            if other and not capturing:
+                raise ValueError("the plan's stream is not part of the capture under way")
+            # The stream's own memory: what used it before on another stream, and may
+            # still be at work, could write over the plan.
+            self.plan = torch.empty((need,), dtype=torch.uint8, device=device)
+            self.info = sb_adamw_plan()
+            _check("sb_adamw_make_plan", load().sb_adamw_make_plan(
+                self.moments, n, self.tensors, _ptr(self.plan), need, ctypes.byref(self.info),
+                _stream_for(self.plan, s)))
+        if not capturing:
+            s.synchronize()
 
 
 def adamw_moments(w, moments=32):
