@@ -453,17 +453,23 @@ class AdamW:
 class _Updates:
     """The updates of one set of (parameter, gradient, scale, decays): SGD, or
     AdamW with the moments and a counter of its updates on the device, so that
-    a captured step counts on when it is replayed."""
+    a captured step counts on when it is replayed, and the tensors' elements
+    numbered from ``first`` to ``end`` among the random numbers of the bytes."""
 
-    def __init__(self, items, adamw):
+    def __init__(self, items, adamw, first=0):
         self.adamw = adamw
+        firsts = []
+        for w, _, _, _ in items:
+            firsts.append(first)
+            first += w.numel()
+        self.end = first
         if adamw is None:
             self.list = sb.SgdList([(w, g, scale) for w, g, scale, _ in items])
             return
         self.moments = [sb.adamw_moments(w, adamw.moments) for w, _, _, _ in items]
         self.list = sb.AdamwList([dict(w=w, g=g, scale=scale, decay=adamw.decay if decays else 0.0,
-                                       **m)
-                                  for (w, g, scale, decays), m in zip(items, self.moments)])
+                                       first=at, **m)
+                                  for (w, g, scale, decays), m, at in zip(items, self.moments, firsts)])
         self.done = torch.zeros(1, dtype=torch.int32, device=items[0][0].device)
 
     def calls(self, name, k, lr, stream):
@@ -608,7 +614,9 @@ class GroupTrainStep:
 
     With ``adamw`` (an ``AdamW``) the updates are ``sb_adamw_update`` ones, on
     the same gradients and scales, lr unused; FC shards and conv layers count
-    their updates apart.  A ("gated", in, shard, full, act) entry of the plan in
+    their updates apart.  Their parameters have the numbers ``first`` to ``end``
+    (one past the last) among the random numbers of moments in bytes: groups that
+    share a seed take ranges of their own.  A ("gated", in, shard, full, act) entry of the plan in
     place of a linear one is a gated layer (``sb_gated_shard_fwd``/``_bwd``):
     its ``W[j]`` is [K][2][in_j][ns_j], ``b[j]`` [K][2][ns_j] (the gate's, then
     the other projection's), and ``pre[j]`` [K][2][B][ns_j] what its forward
@@ -623,7 +631,8 @@ class GroupTrainStep:
     the labels of iteration k's gathered rows), ``loss`` [K][B].
     """
 
-    def __init__(self, schedule, n, in_ch, hw, plan, lr=0.01, device="cuda", adamw=None):
+    def __init__(self, schedule, n, in_ch, hw, plan, lr=0.01, device="cuda", adamw=None,
+                 first=0):
         dev = torch.device(device)
         if not plan or plan[0][0] != "modulo" or plan[-1][0] != "loss":
             raise ValueError("the plan must run from a modulo layer to the loss")
@@ -700,12 +709,13 @@ class GroupTrainStep:
         self.ws = torch.empty((max(need, 256) + 255) // 256 * 256, dtype=torch.uint8, device=dev)
         self.update_fc = _Updates([(self.W[j], self.dW[j], 1.0 / K, True) for j in range(L)] +
                                   [(self.b[j], self.db[j], 1.0 / K, False) for j in range(L)],
-                                  adamw)
+                                  adamw, first)
         c = self.conv
         n_conv = len(c.layers)
         self.update_conv = _Updates([(c.W[i], c.dW[i], 1.0, True) for i in range(n_conv)] +
                                     [(c.b[i], c.db[i], 1.0, False) for i in range(n_conv)],
-                                    adamw)
+                                    adamw, self.update_fc.end)
+        self.end = self.update_conv.end
         self.sgd_fc, self.sgd_conv = ((None, None) if adamw else
                                       (self.update_fc.list, self.update_conv.list))
         self.call = _plain      # hook: every libsb call of the step goes through it
@@ -821,7 +831,7 @@ class AveragedGroups:
     is one ``sb_model_average_replicas`` call over the G buffers.  ``step``
     runs every group's training step, then, after steps period, 2 period,
     ..., the averages.  With ``adamw`` the parameters are averaged, each
-    group's moments stay its own.
+    group's moments stay its own, and so do the random numbers that round them.
     """
 
     def __init__(self, schedule, n, in_ch, hw, plan, groups, period, lr=0.01, device="cuda",
@@ -830,8 +840,10 @@ class AveragedGroups:
             raise ValueError("1 .. %d groups" % sb.SB_MAX_REPLICAS)
         if period < 1:
             raise ValueError("the averaging period is a positive number of steps")
-        self.groups = [GroupTrainStep(schedule, n, in_ch, hw, plan, lr, device, adamw)
-                       for _ in range(groups)]
+        self.groups = []
+        for _ in range(groups):
+            first = self.groups[-1].end if self.groups else 0
+            self.groups.append(GroupTrainStep(schedule, n, in_ch, hw, plan, lr, device, adamw, first))
         self.period = period
         self.steps_done = 0
 
