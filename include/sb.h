@@ -541,7 +541,9 @@ sb_status sb_sgd_update(int count, float *const *w, const float *const *g,
  * update:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
  *   w = (1 - lr decay) w - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32; m and v of the update are those before they become bytes.
+ * in fp32, each result of the last line within 17 half steps of its move (the root and
+ * the reciprocal of the sum with eps may be the hardware's, a step off each); m and v of
+ * the update are those before they become bytes.
  *
  * Moments:
  *   32  fp32, zero before the first update;

@@ -85,7 +85,7 @@ struct AdamwStep {
   float b1, c1, b2, c2, eps, rate, vscale;   // rate, vscale: of step, without a counter
   uint32_t seed;
   int step, count;
-  int fast;                                  // eps >= 2^-40: see the kernel's root
+  int fast;                                  // eps hides subnormal v: see fast_root
 };
 
 __host__ __device__ inline uint32_t mix32(uint32_t x) {
@@ -94,6 +94,15 @@ __host__ __device__ inline uint32_t mix32(uint32_t x) {
   x ^= x >> 15;
   x *= 0xb7e15163u;
   return x ^ (x >> 16);
+}
+
+// Whether w's move takes the hardware's root and reciprocal (a step each, a quarter of
+// the instructions).  They read a subnormal v as 0: its root, below 2^-63, times the bias
+// factor, at most 1 / sqrt(1 - beta2), has to be below an eighth of half a step (2^-24)
+// of eps.  A denominator from 2^126 on would have no reciprocal: eps is far below that,
+// and the rest of it, below 2^64 times 2^27.
+inline bool fast_root(double eps, double beta2) {
+  return eps >= 0x1p-36 / std::sqrt(1.0 - beta2) && eps <= 0x1p100;
 }
 
 // beta^t by squaring.
@@ -221,8 +230,6 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamwStep b) {
         ov = v4[u][e];
       }
       const float g = g4[u][e] * t.scale;
-      // The hardware's root and reciprocal (an ulp each, a quarter of the instructions)
-      // read a subnormal v as 0: its root, below 2^-63, is nothing beside an eps of 2^-40.
       nm[e] = om * b.b1 + g * b.c1;
       nv[e] = ov * b.b2 + (g * g) * b.c2;
       if (b.fast)
@@ -432,7 +439,7 @@ extern "C" sb_status sb_adamw_update(const sb_adamw_desc* d, const sb_adamw_plan
   b.b2 = (float)d->beta2; b.c2 = (float)(1.0 - d->beta2);
   b.eps = (float)d->eps; b.rate = (float)lr1; b.vscale = (float)vs;
   b.seed = d->seed; b.step = d->step; b.count = info->tensors;
-  b.fast = b.eps >= 0x1p-40f;
+  b.fast = sb::fast_root(b.eps, d->beta2);
   const auto kernel = info->moments == 32 ? sb::adamw_kernel<false, 1>
                       : info->groups == 1 ? sb::adamw_kernel<true, 1>
                                           : sb::adamw_kernel<true, sb::kAdamwGroups>;
