@@ -389,8 +389,9 @@ sb_status sb_gated_shard_fwd(const sb_gated_desc *desc, const void *x,
  * and dw_up, db_up likewise with du (db_gate, db_up may each be NULL).  The
  * parameters' gradients are fp32 and carry da and du in full; SB_BF16's
  * dx_partial, itself rounded to bf16, is summed from da and du rounded to
- * bf16.  (da and du enter SB_BF16's weight gradients as sums of three bf16 parts, the
- * last ones often 0, so an infinity in x makes its row of them NaN.)  As for the FC shard the division by K is the optimiser's.
+ * bf16.  An infinity in x makes its row of the weights' gradients infinite, by
+ * the signs of da and du.  As for the FC shard the division by K is the
+ * optimiser's.
  * The summation order is fixed: repeated calls give bit-identical results. */
 sb_status sb_gated_shard_bwd(const sb_gated_desc *desc, const void *x,
                              const void *w_gate, const void *w_up,

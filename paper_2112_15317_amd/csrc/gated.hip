@@ -1031,7 +1031,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
     for (int q = 0; q < 2; ++q) gw.b[q][p] = parts + (NP * q + NP - 1 - p) * plane;
   }
   gw.lda = o.ldx; gw.ldb = np;
-  gw.M = d->k_in; gw.N = d->n_shard; gw.K = d->m; gw.segs = NP;
+  gw.M = d->k_in; gw.N = d->n_shard; gw.K = d->m; gw.segs = NP; gw.firsts = 1;
   gw.a_bytes = (uint32_t)(((size_t)(d->m - 1) * gw.lda + o.width) * sizeof(E));
   gw.b_bytes = (uint32_t)(plane * sizeof(E));
   gw.c[0] = dw[0]; gw.c[1] = dw[1]; gw.ldc = d->n_shard;
@@ -1043,7 +1043,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
       gx.b[0][q] = gx.b[1][q] = o.w[q];
     }
     gx.lda = np; gx.ldb = o.ldw;                     // o.ldw is np: n_shard, or packed
-    gx.M = d->m; gx.N = d->k_in; gx.K = np; gx.segs = 2;
+    gx.M = d->m; gx.N = d->k_in; gx.K = np; gx.segs = gx.firsts = 2;
     gx.a_bytes = (uint32_t)(plane * sizeof(E));
     gx.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
     gx.c[0] = dx; gx.ldc = d->ldx;

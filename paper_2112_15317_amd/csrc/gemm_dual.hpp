@@ -69,6 +69,7 @@ struct DualArgs {
   uint32_t a_bytes, b_bytes;       // ranges of the operands
   int lda, ldb;
   int M, N, K, segs;               // K: of a segment
+  int firsts;                      // bf16 DX, DW: the last segments, which have the first parts
   int mt, nt, splits, stages;      // stages per split
   int pitch;                       // of partials' rows: N rounded up to 4
   float* part;                     // splits > 1: [split][2][M][N up to 4] (DX [split][M][..])
@@ -452,12 +453,13 @@ __device__ __forceinline__ void dual_block(const DualArgs& g, int block, u16* ld
   }
   turns(Zero{});
 
-  if constexpr (NP == 3) {
-    // A block with values that the parts do not carry, or sums that are not finite,
-    // does its reduction again on the fp32 MFMA, operands straight from memory.
-    int* redo = reinterpret_cast<int*>(lds + T::LDS_STAGES / sizeof(u16));
-    if (tid == 0) *redo = 0;
-    __syncthreads();
+  // Whether the products are formed again on the fp32 MFMA, operands straight from memory:
+  // those of an fp32 block with values that the parts do not carry, or with sums that are
+  // not finite; those of a bf16 wave whose sums are not, where one operand comes in parts
+  // (an infinity times the lower ones, which are 0 or of either sign, would be NaN).
+  constexpr bool PARTS = NP == 1 && KIND != kDualFwd;
+  bool again = false;
+  if constexpr (NP == 3 || PARTS) {
     float z = 0.f;                                   // stays 0 over finite values
 #pragma unroll
     for (int j = 0; j < F; ++j)
@@ -465,44 +467,61 @@ __device__ __forceinline__ void dual_block(const DualArgs& g, int block, u16* ld
       for (int i = 0; i < FA; ++i)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          acc[j][i][v] += low[j][i][v];
+          if constexpr (NP == 3) acc[j][i][v] += low[j][i][v];
           z = fmaf(acc[j][i][v], 0.f, z);
         }
-    if ((lost & 0xffffu) || !(z == 0.f)) *redo = 1;
-    __syncthreads();
-    if (__builtin_expect(__builtin_amdgcn_readfirstlane(*redo), 0)) {
-      int ar[FA], bc[F];                             // this lane's rows of A, columns of B
-      const int c = lane % 32;
+    if constexpr (NP == 3) {
+      int* redo = reinterpret_cast<int*>(lds + T::LDS_STAGES / sizeof(u16));
+      if (tid == 0) *redo = 0;
+      __syncthreads();
+      if ((lost & 0xffffu) || !(z == 0.f)) *redo = 1;
+      __syncthreads();
+      again = __builtin_amdgcn_readfirstlane(*redo);
+    } else {
+      again = __ballot(!(z == 0.f)) != 0;
+    }
+  }
+  if (__builtin_expect(again, 0)) {
+    int ar[FA], bc[F];                               // this lane's rows of A, columns of B
+    const int c = lane % 32;
 #pragma unroll
-      for (int i = 0; i < FA; ++i) ar[i] = out_row(i, c);
+    for (int i = 0; i < FA; ++i) ar[i] = out_row(i, c);
 #pragma unroll
-      for (int j = 0; j < F; ++j) {
-        bc[j] = n0 + (BKC ? wn * T::RC + j * 32 + c
-                          : pair_block<F>(wn * (F / 2) + j % (F / 2), c / 16) * 16 + c % 16);
+    for (int j = 0; j < F; ++j) {
+      bc[j] = n0 + (BKC ? wn * T::RC + j * 32 + c
+                        : pair_block<F>(wn * (F / 2) + j % (F / 2), c / 16) * 16 + c % 16);
 #pragma unroll
-        for (int i = 0; i < FA; ++i) clear(acc[j][i]);
-      }
-      for (int u = t0; u < t1; ++u) {
-        const int sg = u / per_seg, kb = (u - sg * per_seg) * 32, ke = min(g.K, kb + 32);
-        const float* A = (const float*)g.a[sg];
+      for (int i = 0; i < FA; ++i) clear(acc[j][i]);
+    }
+    for (int u = t0; u < t1; ++u) {
+      const int sg = u / per_seg, kb = (u - sg * per_seg) * 32, ke = min(g.K, kb + 32);
+      const E* A = (const E*)g.a[sg];
+      // Beside a lower part, infinities and NaN of the other operand count as 0: the first
+      // part, an infinite one too, has their terms' signs.
+      const bool lower = PARTS && sg < g.segs - g.firsts;
+      auto whole = [&](float v) {
+        return lower && (__float_as_uint(v) & 0x7f800000u) == 0x7f800000u ? 0.f : v;
+      };
 #pragma unroll 1
-        for (int kk = kb; kk < ke; kk += 2) {
-          const int k = kk + lane / 32;
-          float av[FA];
+      for (int kk = kb; kk < ke; kk += 2) {
+        const int k = kk + lane / 32;
+        float av[FA];
+#pragma unroll
+        for (int i = 0; i < FA; ++i) {
+          const size_t at = AKC ? (size_t)ar[i] * g.lda + k : (size_t)k * g.lda + ar[i];
+          av[i] = k < ke && ar[i] < g.M ? Elem<E>::load(A, at) : 0.f;
+          if constexpr (KIND == kDualDw) av[i] = whole(av[i]);
+        }
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+          // (The weights end at b_bytes, before K where FWD's rows of x are padded.)
+          const E* B = (const E*)g.b[BKC ? 0 : j / (F / 2)][sg];
+          const size_t at = BKC ? (size_t)bc[j] * g.ldb + k : (size_t)k * g.ldb + bc[j];
+          float bv = k < ke && bc[j] < g.N && at < g.b_bytes / sizeof(E) ? Elem<E>::load(B, at) : 0.f;
+          if constexpr (KIND == kDualDx) bv = whole(bv);
 #pragma unroll
           for (int i = 0; i < FA; ++i)
-            av[i] = k < ke && ar[i] < g.M
-                        ? A[AKC ? (size_t)ar[i] * g.lda + k : (size_t)k * g.lda + ar[i]] : 0.f;
-#pragma unroll
-          for (int j = 0; j < F; ++j) {
-            // (The weights end at b_bytes, before K where FWD's rows of x are padded.)
-            const float* B = (const float*)g.b[BKC ? 0 : j / (F / 2)][sg];
-            const size_t at = BKC ? (size_t)bc[j] * g.ldb + k : (size_t)k * g.ldb + bc[j];
-            const float bv = k < ke && bc[j] < g.N && at < g.b_bytes / sizeof(float) ? B[at] : 0.f;
-#pragma unroll
-            for (int i = 0; i < FA; ++i)
-              acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(bv, av[i], acc[j][i], 0, 0, 0);
-          }
+            acc[j][i] = __builtin_amdgcn_mfma_f32_32x32x2f32(bv, av[i], acc[j][i], 0, 0, 0);
         }
       }
     }

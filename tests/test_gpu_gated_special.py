@@ -11,6 +11,8 @@ from tests.test_gpu_gated import Case
 
 pytestmark = pytest.mark.gpu
 
+U = G.U                                # half a step of fp32
+
 
 def _among_nan(t, lines):
     """t's values with `lines` lines of NaN behind them in the same allocation."""
@@ -60,3 +62,55 @@ def test_fp32_sums_end_with_the_weights(m, k, n, what):
         assert np.all(np.abs(got - want)[rows] <= lim[rows])
     assert np.isfinite(y[rows]).all()
     c.untouched(("y", "pre"))
+
+
+# ---- infinite and largest values in bf16 gradients -----------------------------------------
+@pytest.mark.parametrize("m,k,n", [(2, 40, 24), (8, 136, 72), (9, 136, 72), (300, 264, 192), (3000, 72, 72),
+                                   (1100, 300, 4100)])
+def test_infinities_of_x_in_bf16_weight_gradients(m, k, n):
+    """An infinity in x makes its row of the weight gradients infinite by the signs of da
+    and du, NaN only where two of them disagree or x is NaN; the other rows stay what
+    they are."""
+    print_case("gated_inf_x", m=m, k=k, n=n)
+    c = Case("silu", "bf16", m, k, n)
+    c.fwd()                                          # a finite pre
+    x = c.x.copy()
+    places = [(0, 3), (m - 1, 17), (m // 2, k - 1), (0, 20), (m - 1, 20)]
+    for q, (i, j) in enumerate(places):
+        x[i, j] = np.inf if q != 1 else -np.inf
+    x[m // 3, 30] = np.nan
+    c.d["x"].copy_(torch.from_numpy(x))
+    c.bwd()
+    torch.cuda.synchronize()
+    bound = c.bound()
+    _, a, u = G.forward("silu", c.x, c.wg, c.wu, c.bg, c.bu)
+    with np.errstate(all="ignore"):
+        ref = dict(zip(("dwg", "dwu"), G.backward("silu", x, c.wg, c.wu, a, u, c.dy)[1:3]))
+    bad = [3, 17, 20, 30, k - 1]
+    for t in ref:
+        got = c.get(t).astype(np.float64)
+        assert np.array_equal(got[bad], ref[t][bad], equal_nan=True), t
+        far = np.abs(np.delete(got, bad, axis=0) - np.delete(ref[t], bad, axis=0))
+        assert np.all(far <= np.delete(bound[t], bad, axis=0)), t
+
+
+@pytest.mark.parametrize("m,k,n", [(1, 40, 264), (5, 40, 264), (9, 136, 72), (300, 264, 192), (70, 72, 4000)])
+def test_infinities_of_the_weights_in_the_bf16_dx(m, k, n):
+    """An infinity in a weight makes its column of dx infinite by the signs of da and du."""
+    print_case("gated_inf_w", m=m, k=k, n=n)
+    c = Case("silu", "bf16", m, k, n)
+    c.fwd()                                          # a finite pre
+    wg, wu = c.wg.copy(), c.wu.copy()
+    wg[3, 7], wg[20, n - 1], wu[20, 9], wu[k - 1, 0] = np.inf, np.inf, -np.inf, np.inf
+    wu[30, 5] = np.nan
+    c.d["wg"].copy_(torch.from_numpy(wg))
+    c.d["wu"].copy_(torch.from_numpy(wu))
+    c.bwd()
+    torch.cuda.synchronize()
+    _, a, u = G.forward("silu", c.x, c.wg, c.wu, c.bg, c.bu)
+    with np.errstate(all="ignore"):
+        ref = G.backward("silu", c.x, wg, wu, a, u, c.dy)[0]
+    bad, got = [3, 20, 30, k - 1], c.get("dx").astype(np.float64)
+    assert np.array_equal(got[:, bad], ref[:, bad], equal_nan=True)
+    far = np.abs(np.delete(got, bad, axis=1) - np.delete(ref, bad, axis=1))
+    assert np.all(far <= np.delete(c.bound()["dx"], bad, axis=1))
