@@ -388,8 +388,8 @@ sb_status sb_gated_shard_fwd(const sb_gated_desc *desc, const void *x,
  *   db_gate[j]      = (accumulate ? db_gate[j]   : 0) + sum_i da[i,j]
  * and dw_up, db_up likewise with du (db_gate, db_up may each be NULL).  The
  * parameters' gradients are fp32 and carry da and du in full; SB_BF16's
- * dx_partial, itself rounded to bf16, is summed from da and du rounded to
- * bf16.  An infinity in x makes its row of the weights' gradients infinite, by
+ * dx_partial, itself rounded to bf16, is summed from 16 bits of them or
+ * more.  An infinity in x makes its row of the weights' gradients infinite, by
  * the signs of da and du.  As for the FC shard the division by K is the
  * optimiser's.
  * The summation order is fixed: repeated calls give bit-identical results. */

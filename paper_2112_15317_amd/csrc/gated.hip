@@ -13,9 +13,11 @@
 //
 // The weight gradients are fp32 also where x is bf16: da and du go into their
 // products as three bf16 parts, which hold all 24 bits, so a gradient is off by the
-// rounding of its fp32 sums and not by 2^-9 of every term (measured against 64 bits:
-// 3e-7 of the gradient; with two parts 2.6e-6, with one 1.7e-3).  dx of the bf16 path
-// is rounded to bf16 itself and takes their first parts.
+// rounding of its fp32 sums and not by 2^-9 of every term (measured against 64 bits over
+// 2048 rows: 2.5e-7 of the gradient; with two parts 2.6e-6, with one 1.7e-3).  dx of the
+// bf16 path is rounded to bf16 itself and takes their first two parts, 16 bits: with one,
+// it was 2.3e-3 off where the rounding of its result alone is 1.7e-3, for a sixth less of
+// a large step's time (4096 x 4096 x 8192: 2881 us, 2432 with one).
 #include "gemm_dual.hpp"
 
 #include <algorithm>
@@ -75,7 +77,7 @@ __global__ __launch_bounds__(256) void gated_pack(PackTasks t) {
   pack_rows<E>(t, blockIdx.x);
 }
 
-// da and du in rows of np (n rounded up to 8, zeros behind n).  fp32: da, then du,
+// da and du in rows of np (n rounded up to 8, zeros behind n).  D fp32: da, then du,
 // m * np elements each.  bf16: three parts of each, part p of da at p * m * np, of du at
 // (3 + p) * m * np.  A block has 256 columns of `rows` rows, a lane four columns of
 // every fourth row.  Its columns' sums are db where it has all rows, else they go to
@@ -90,11 +92,11 @@ static int act_rows(int m, int np) {
   return rows;
 }
 
-template <class E>
+template <class E, class D>
 __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int act,
                                                      const float* __restrict__ pre,
                                                      const E* __restrict__ dy, int ldy,
-                                                     E* __restrict__ d, BiasSums bias, int rows,
+                                                     D* __restrict__ d, BiasSums bias, int rows,
                                                      int chunks, PackTasks packs) {
   __shared__ f4 part[2][4][64];
   const int by = blockIdx.x % chunks, bx = blockIdx.x / chunks;
@@ -123,7 +125,7 @@ __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int a
     for (int q = 0; q < 2; ++q) {
       s[q] += v[q];
       const size_t at = (size_t)r * np + c;
-      if constexpr (sizeof(E) == 4) {
+      if constexpr (sizeof(D) == 4) {
         *reinterpret_cast<f4*>(d + q * plane + at) = v[q];
       } else {
         f4 rest = v[q];
@@ -333,7 +335,7 @@ __global__ __launch_bounds__(512) void gated_few_fwd(FewArgs g) {
 
 // Backward of M rows, one launch: da and du of one or two rows are so few that every block
 // forms those it needs (as a pass of their own and products on tiles: 2 x 1024 x 1280 bf16
-// 17.2 us, like this 8.0).  From three rows on dx takes them from the pass over dy (8 x
+// 17.2 us, like this 9.1).  From three rows on dx takes them from the pass over dy (8 x
 // 2048 x 2048 fp32 30.0 us without it, 21.5 with it), the weight gradients' blocks,
 // which need a strip of them, do not.
 constexpr int kFewGates = 2;
@@ -345,8 +347,23 @@ struct FewBwdArgs {
   float *dw[2], *db[2];
   int m, n, k, ldx, ldy, act, accumulate;
   int first, strips, lines;                          // first: blocks of dx; lines of k a block behind
-  const void* d[2]; int np;                          // da and du from the pass, M > kFewGates
+  const float* d[2]; int np;                         // da and du from the pass, M > kFewGates
 };
+
+// The dot product of a piece of a weight with as many fp32 values, and s.
+template <class E>
+__device__ __forceinline__ float few_dot_f32(u32x4 w, const f4 (&d)[kFewWidth<E> / 4], float s) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (sizeof(E) == 4) {
+      s = fmaf(__uint_as_float(w[e]), d[0][e], s);
+    } else {
+      s = fmaf(__uint_as_float(w[e] << 16), d[e / 2][e % 2 * 2], s);
+      s = fmaf(__uint_as_float(w[e] & 0xffff0000u), d[e / 2][e % 2 * 2 + 1], s);
+    }
+  }
+  return s;
+}
 
 // da and du of four columns of a row, those from `left` on 0.
 template <class E>
@@ -363,11 +380,12 @@ __device__ __forceinline__ void few_gates(const FewBwdArgs& g, int r, int c, int
   }
 }
 
-// dx of rows whose da and du the pass has formed: a wave has four lines of both weights,
-// its lanes the columns.
+// dx of rows whose da and du the pass has formed, in fp32: a wave has four lines of both
+// weights, its lanes the columns, four at a time (bf16 lines in pieces of eight took 39 us
+// for 8 x 2048 x 2048, 21 in fours: the loads of da and du, not the weights', wait then).
 template <class E, int M>
 __device__ __forceinline__ void few_dx_lines(const FewBwdArgs& g, int block) {
-  constexpr int V = kFewWidth<E>, R = 4;
+  constexpr int R = 4;
   const int lane = threadIdx.x & 63;
   const int k0 = (block * 4 + (threadIdx.x >> 6)) * R;
   float acc[R][M];
@@ -375,32 +393,32 @@ __device__ __forceinline__ void few_dx_lines(const FewBwdArgs& g, int block) {
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int r = 0; r < M; ++r) acc[i][r] = 0.f;
-  for (int c0 = lane * V; c0 < g.n; c0 += 64 * V) {
-    const int skip = max(c0 + V - g.n, 0), c = c0 - skip;
+  for (int c0 = lane * 4; c0 < g.n; c0 += 256) {
+    const int skip = max(c0 + 4 - g.n, 0), c = c0 - skip;
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      u32x4 w[R], d[M];
+      f4 w[R], d[M];
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        w[i] = few_piece<E>((const E*)g.w[q] + (size_t)min(k0 + i, g.k - 1) * g.n + c);
+        w[i] = load_quad<E>((const E*)g.w[q] + (size_t)min(k0 + i, g.k - 1) * g.n + c, 4);
 #pragma unroll
       for (int r = 0; r < M; ++r)
-        d[r] = few_piece<E>((const E*)g.d[q] + (size_t)min(r, g.m - 1) * g.np + c);
+        d[r] = load_quad<float>(g.d[q] + (size_t)min(r, g.m - 1) * g.np + c, 4);
       if (skip) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) w[i] = few_without<E>(w[i], skip);
+        for (int e = 0; e < 3; ++e) {
 #pragma unroll
-        for (int r = 0; r < M; ++r) d[r] = few_without<E>(d[r], skip);
+          for (int i = 0; i < R; ++i) w[i][e] = e < skip ? 0.f : w[i][e];
+#pragma unroll
+          for (int r = 0; r < M; ++r) d[r][e] = e < skip ? 0.f : d[r][e];
+        }
       }
 #pragma unroll
       for (int r = 0; r < M; ++r)
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(E) == 2) acc[i][r] = few_dot(w[i][e], d[r][e], acc[i][r]);
-            else acc[i][r] = fmaf(__uint_as_float(w[i][e]), __uint_as_float(d[r][e]), acc[i][r]);
-          }
+          for (int e = 0; e < 4; ++e) acc[i][r] = fmaf(w[i][e], d[r][e], acc[i][r]);
     }
   }
   // The sums of four lines at once, in the four rows of lanes.
@@ -417,8 +435,8 @@ __device__ __forceinline__ void few_dx_lines(const FewBwdArgs& g, int block) {
 }
 
 // dx of up to kFewGates rows: a block has kFewDx lines of both weights, each wave 64 pieces
-// of them at a time, whose da and du (bf16: rounded) it forms.  (With more rows that many
-// activations a wave take longer than all the rest: 8 x 1024 x 1024 bf16 23.8 us for 12.7.)
+// of them at a time, whose da and du it forms.  (With more rows that many
+// activations a wave take longer than all the rest: 8 x 1024 x 1024 bf16 23.8 us for 12.6.)
 template <class E, int M>
 __device__ __forceinline__ void few_dx_block(const FewBwdArgs& g, int block, float* lds) {
   constexpr int V = kFewWidth<E>, R = kFewDx;
@@ -431,24 +449,19 @@ __device__ __forceinline__ void few_dx_block(const FewBwdArgs& g, int block, flo
     for (int r = 0; r < M; ++r) acc[i][r] = 0.f;
   for (int b = wave * 64 * V; b < g.n; b += 4 * 64 * V) {
     const int c0 = b + lane * V, c = min(c0, g.n - V), skip = c0 - c;
-    u32x4 d[2][M];
+    f4 d[2][M][V / 4];
 #pragma unroll
-    for (int r = 0; r < M; ++r) {
-      f4 v[2][V / 4];
+    for (int r = 0; r < M; ++r)
 #pragma unroll
-      for (int i = 0; i < V / 4; ++i)
-        few_gates<E>(g, min(r, g.m - 1), c + 4 * i, 4, v[0][i], v[1][i]);
+      for (int i = 0; i < V / 4; ++i) {
+        few_gates<E>(g, min(r, g.m - 1), c + 4 * i, 4, d[0][r][i], d[1][r][i]);
+        if (skip) {
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        u32x4 t;
+          for (int q = 0; q < 2; ++q)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          if constexpr (sizeof(E) == 4) t[e] = __float_as_uint(v[q][0][e]);
-          else t[e] = f32x2_to_bf16x2(v[q][e / 2][e % 2 * 2], v[q][e / 2][e % 2 * 2 + 1]);
+            for (int e = 0; e < 4; ++e) d[q][r][i][e] = 4 * i + e < skip ? 0.f : d[q][r][i][e];
         }
-        d[q][r] = few_without<E>(t, skip);
       }
-    }
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
@@ -456,12 +469,7 @@ __device__ __forceinline__ void few_dx_block(const FewBwdArgs& g, int block, flo
         u32x4 w = few_piece<E>((const E*)g.w[q] + (size_t)min(k0 + i, g.k - 1) * g.n + c);
         if (skip) w = few_without<E>(w, skip);
 #pragma unroll
-        for (int r = 0; r < M; ++r)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if constexpr (sizeof(E) == 2) acc[i][r] = few_dot(w[e], d[q][r][e], acc[i][r]);
-            else acc[i][r] = fmaf(__uint_as_float(w[e]), __uint_as_float(d[q][r][e]), acc[i][r]);
-          }
+        for (int r = 0; r < M; ++r) acc[i][r] = few_dot_f32<E>(w, d[q][r], acc[i][r]);
       }
   }
   // The sums of four lines at once, in the four rows of lanes.
@@ -681,7 +689,7 @@ static GradPlan grad_plan(bool b16, int m, int k, int n) {
   static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
   GradPlan best{};
   double best_t = 0;
-  const int total[2] = {cdiv(n, 32) * 2, cdiv(m, 32) * (b16 ? 3 : 1)};
+  const int total[2] = {cdiv(n, 32) * (b16 ? 4 : 2), cdiv(m, 32) * (b16 ? 3 : 1)};
   const double bytes[2] = {(double)m * cdiv(k, 4) * 16, (double)k * cdiv(n, 4) * 32};
   const double tb_s = (b16 ? 8.24 : 5.72) * 1e6;
   for (int f = b16 ? 4 : 2; f >= 2; f -= 2) {
@@ -873,7 +881,7 @@ static GatedSpace gated_space(const sb_gated_desc* d, int pass, const GatedPacks
     at += round_up(bytes, 256);
   };
   if (pass == SB_FC_BWD) {
-    take(s.d, m * np * (d->dtype == SB_BF16 ? 12 : 8));
+    take(s.d, m * np * (d->dtype == SB_BF16 && !few ? 12 : 8));
     if (few) {
       s.bytes = at;
       return s;
@@ -1008,9 +1016,15 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   const BiasSums bias{!few && (db[0] || db[1]) && chunks > 1 ? (float*)(ws + sp.sums) : nullptr,
                       {few ? nullptr : db[0], few ? nullptr : db[1]}, d->n_shard, np, chunks, accumulate};
   const GatedOperands o = gated_operands<E>(d, x, w, packs.lines, dx && packs.w, ws, sp);
-  if (pass)
-    gated_act_bwd<E><<<(unsigned)(cdiv(np, 256) * chunks + o.packs.block0[3]), 256, 0, st>>>(
-        d->m, d->n_shard, np, d->act, pre, (const E*)dy, d->ldy, parts, bias, rows, chunks, o.packs);
+  if (pass) {
+    const unsigned blocks = (unsigned)(cdiv(np, 256) * chunks + o.packs.block0[3]);
+    if (few)
+      gated_act_bwd<E, float><<<blocks, 256, 0, st>>>(d->m, d->n_shard, np, d->act, pre, (const E*)dy,
+                                                      d->ldy, (float*)parts, bias, rows, chunks, o.packs);
+    else
+      gated_act_bwd<E, E><<<blocks, 256, 0, st>>>(d->m, d->n_shard, np, d->act, pre, (const E*)dy,
+                                                  d->ldy, parts, bias, rows, chunks, o.packs);
+  }
   if (few) {
     const int strips = cdiv(d->n_shard, 256);
     int lines = 32;                                  // about 512 blocks and more
@@ -1018,7 +1032,7 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
     const FewBwdArgs g{x, {w[0], w[1]}, dy, pre, dx, {dw[0], dw[1]}, {db[0], db[1]}, d->m,
                        d->n_shard, d->k_in, d->ldx, d->ldy, d->act, accumulate,
                        dx ? cdiv(d->k_in, kFewDx) : 0, strips, lines,
-                       {parts, parts + NP * plane}, np};
+                       {(const float*)parts, (const float*)parts + plane}, np};
     const int blocks = g.first + strips * cdiv(d->k_in, lines);
     const auto kernel = d->m == 1 ? gated_few_bwd<E, 1> : d->m == 2 ? gated_few_bwd<E, 2>
                         : d->m <= 4 ? gated_few_bwd<E, 4> : gated_few_bwd<E, 8>;
@@ -1038,12 +1052,14 @@ static void gated_bwd_run(const sb_gated_desc* d, const void* x, const void* con
   gw.accumulate = accumulate;
   if (dx) {
     DualArgs gx{};
-    for (int q = 0; q < 2; ++q) {
-      gx.a[q] = parts + NP * q * plane;
-      gx.b[0][q] = gx.b[1][q] = o.w[q];
+    constexpr int XP = sizeof(E) == 2 ? 2 : 1;       // parts, the second ones first
+    for (int i = 0; i < 2 * XP; ++i) {
+      const int q = i % 2, p = XP - 1 - i / 2;
+      gx.a[i] = parts + (NP * q + p) * plane;
+      gx.b[0][i] = gx.b[1][i] = o.w[q];
     }
     gx.lda = np; gx.ldb = o.ldw;                     // o.ldw is np: n_shard, or packed
-    gx.M = d->m; gx.N = d->k_in; gx.K = np; gx.segs = gx.firsts = 2;
+    gx.M = d->m; gx.N = d->k_in; gx.K = np; gx.segs = 2 * XP; gx.firsts = 2;
     gx.a_bytes = (uint32_t)(plane * sizeof(E));
     gx.b_bytes = (uint32_t)((size_t)d->k_in * np * sizeof(E));
     gx.c[0] = dx; gx.ldc = d->ldx;

@@ -10,8 +10,8 @@
 // of the two outputs (N), so the operand they share is staged once and the gate's
 // value and the other projection's for one output element end in one wave.  Four
 // waves, 2 x 2, or eight, 4 x 2, each with FA x F blocks of 32 x 32 in registers.
-// The reduction is a list of segments of equal length (DX: one per weight matrix;
-// DW: one per bf16 part of da and du), each in stages of 32.
+// The reduction is a list of segments of equal length (DX: one per weight matrix and bf16
+// part of its d; DW: one per bf16 part of da and du), each in stages of 32.
 //
 // Three stages are in LDS: while stage t is multiplied, t + 2 is written from
 // registers and t + 4 loaded, and t + 1 can already be read, so that the operands
@@ -64,8 +64,8 @@ struct DualTile {
 };
 
 struct DualArgs {
-  const void* a[3];                // per segment
-  const void* b[2][3];             // per region (DX: region 0) and segment
+  const void* a[4];                // per segment
+  const void* b[2][4];             // per region (DX: region 0) and segment
   uint32_t a_bytes, b_bytes;       // ranges of the operands
   int lda, ldb;
   int M, N, K, segs;               // K: of a segment

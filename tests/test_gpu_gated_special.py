@@ -114,3 +114,28 @@ def test_infinities_of_the_weights_in_the_bf16_dx(m, k, n):
     assert np.array_equal(got[:, bad], ref[:, bad], equal_nan=True)
     far = np.abs(np.delete(got, bad, axis=1) - np.delete(ref, bad, axis=1))
     assert np.all(far <= np.delete(c.bound()["dx"], bad, axis=1))
+
+
+# ---- the bf16 dx ---------------------------------------------------------------------
+@pytest.mark.parametrize("m,k,n", [(1, 64, 512), (2, 131, 1000), (3, 200, 260), (8, 1030, 515), (9, 100, 72),
+                                   (70, 264, 130), (333, 512, 741), (520, 72, 640), (64, 64, 4000),
+                                   (410, 1830, 4144)])
+def test_bf16_dx_is_rounded_once(m, k, n):
+    """dx is a sum of da and du with 16 bits or more, rounded to bf16 at its end: beside
+    that half step no term is off by more than 2^-16 of it (two parts of 8 bits) and
+    the roundings of fp32 sums."""
+    print_case("gated_bf16_dx", m=m, k=k, n=n)
+    c = Case("silu", "bf16", m, k, n)
+    c.fwd()
+    c.bwd()
+    torch.cuda.synchronize()
+    args = ("silu", c.x, c.wg, c.wu, c.bg, c.bu)
+    _, a, u = G.forward(*args)
+    ref = G.backward(*args[:4], a, u, c.dy)[0]
+    off = G.bounds(*args, c.dy, False)[1]            # of fp32 da, du and sums
+    f, df = G.act("silu", a)
+    ady = np.abs(c.dy.astype(np.float64))
+    terms = (ady * np.abs(u * df)) @ np.abs(c.wg).T + (ady * np.abs(f)) @ np.abs(c.wu).T
+    off = off + 2.0 ** -16 * terms
+    far = np.abs(c.get("dx").astype(np.float64) - ref)
+    assert np.all(far <= off + G.HALF16 * (np.abs(ref) + off)), float((far / (off + G.HALF16 * np.abs(ref))).max())
