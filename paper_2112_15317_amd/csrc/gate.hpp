@@ -29,7 +29,9 @@ __device__ __forceinline__ void gate_act(int act, float a, float& f, float& df) 
       const float r = 0.79788456080286536f;
       const float t = tanhf(r * (a + 0.044715f * a * a * a));
       f = 0.5f * a * (1.f + t);
-      df = 0.5f * (1.f + t) + 0.5f * a * (1.f - t * t) * r * (1.f + 0.134145f * a * a);
+      // (t is +-1 from |a| = 6 on: within the bound a * a is finite, and 0 times it 0.)
+      const float b = fminf(fmaxf(a, -1e4f), 1e4f);
+      df = 0.5f * (1.f + t) + 0.5f * b * (1.f - t * t) * r * (1.f + 0.134145f * b * b);
       break;
     }
     default:

@@ -139,3 +139,49 @@ def test_bf16_dx_is_rounded_once(m, k, n):
     off = off + 2.0 ** -16 * terms
     far = np.abs(c.get("dx").astype(np.float64) - ref)
     assert np.all(far <= off + G.HALF16 * (np.abs(ref) + off)), float((far / (off + G.HALF16 * np.abs(ref))).max())
+
+
+# ---- values past the middle of fp32's range -----------------------------------------
+HUGE = (1e12, -1e12, 2e19, -2e19, 1e30, -1e30, 8e37, -8e37)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", G.ACTS)
+@pytest.mark.parametrize("m", [2, 5, 96])
+def test_huge_finite_gates(m, act, dtype):
+    """Where the activation has reached a or 0 its derivative is 1 or 0, however large
+    a is: no gradient is NaN, and all are what they are in float64."""
+    print_case("gated_huge", m=m, act=act, dtype=dtype)
+    k, n = 40, 72
+    c = Case(act, dtype, m, k, n)
+    r = np.random.default_rng(3)
+    pre = r.normal(size=(2, m, n)).astype(np.float32)
+    at = [(i % m, 9 * i) for i in range(len(HUGE))]
+    for (i, j), v in zip(at, HUGE):
+        pre[0, i, j] = v
+    c.x, c.dy = c.x * np.float32(0.125), c.dy * np.float32(0.125)
+    c.d["x"].copy_(torch.from_numpy(c.x))
+    c.d["dy"].copy_(torch.from_numpy(c.dy))
+    c.d["pre"].copy_(torch.from_numpy(pre))
+    c.bwd()
+    torch.cuda.synchronize()
+    x, wg, wu, dy, a, u = (t.astype(np.float64) for t in (c.x, c.wg, c.wu, c.dy, pre[0], pre[1]))
+    ref = dict(zip(("dx", "dwg", "dwu", "dbg", "dbu"), G.backward(act, x, wg, wu, a, u, dy)))
+    f, df = G.act(act, a)
+    # da and du: 16 roundings of the activation's pieces (as in oracle.gated.bounds, with
+    # |a|^3 of the tanh form's derivative only where it has not reached 0 or 1), 4 more.
+    small = np.where(np.abs(a) < 20, np.abs(a), 1.0)
+    eda = np.abs(dy * u) * 16 * U * (1 + small ** 3) + 4 * U * np.abs(dy * u * df)
+    edu = np.abs(dy) * 16 * U * np.maximum(1, np.abs(a) * (np.abs(f) > 0)) + 4 * U * np.abs(dy * f)
+    ada, adu = np.abs(dy * u * df) + eda, np.abs(dy * f) + edu
+    ax, awg, awu = np.abs(x), np.abs(wg), np.abs(wu)
+    lim = dict(dwg=ax.T @ eda + (m / 16 + 16) * U * (ax.T @ ada), dwu=ax.T @ edu + (m / 16 + 16) * U * (ax.T @ adu),
+               dbg=eda.sum(0) + (m / 16 + 16) * U * ada.sum(0), dbu=edu.sum(0) + (m / 16 + 16) * U * adu.sum(0))
+    terms = ada @ awg.T + adu @ awu.T
+    lim["dx"] = eda @ awg.T + edu @ awu.T + (2 * n / 16 + 16) * U * terms
+    if dtype == "bf16":                              # two parts of da and du, dx rounded
+        lim["dx"] += 2.0 ** -16 * terms + G.HALF16 * (np.abs(ref["dx"]) + terms * 2.0 ** -12)
+    for t in ref:
+        got = c.get(t).astype(np.float64)
+        assert np.isfinite(got).all(), t
+        assert np.all(np.abs(got - ref[t]) <= lim[t]), t
