@@ -128,21 +128,27 @@ __global__ __launch_bounds__(256) void gated_act_bwd(int m, int n, int np, int a
       if constexpr (sizeof(D) == 4) {
         *reinterpret_cast<f4*>(d + q * plane + at) = v[q];
       } else {
-        f4 rest = v[q];
+        // An infinite or NaN first part is the whole value; a finite value's is not past
+        // bf16's largest, to which those above it would not round.
+        constexpr float most = 0x1.fep127f;
+        f4 rest, part;
+        bool whole[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          rest[e] = v[q][e];
+          whole[e] = (__float_as_uint(rest[e]) & 0x7f800000u) == 0x7f800000u;
+          part[e] = whole[e] ? rest[e] : fminf(fmaxf(rest[e], -most), most);
+        }
 #pragma unroll
         for (int p = 0; p < 3; ++p) {
           uint2 b;
-          b.x = f32x2_to_bf16x2(rest[0], rest[1]);
-          b.y = f32x2_to_bf16x2(rest[2], rest[3]);
+          b.x = f32x2_to_bf16x2(part[0], part[1]);
+          b.y = f32x2_to_bf16x2(part[2], part[3]);
           *reinterpret_cast<uint2*>(d + (3 * q + p) * plane + at) = b;
           const f4 h = f4{__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u),
                           __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xffff0000u)};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            // An infinite or NaN first part is the whole value.
-            const bool whole = (__float_as_uint(h[e]) & 0x7f800000u) == 0x7f800000u;
-            rest[e] = whole ? 0.f : rest[e] - h[e];
-          }
+          for (int e = 0; e < 4; ++e) rest[e] = part[e] = whole[e] ? 0.f : rest[e] - h[e];
         }
       }
     }

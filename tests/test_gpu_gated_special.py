@@ -185,3 +185,35 @@ def test_huge_finite_gates(m, act, dtype):
         got = c.get(t).astype(np.float64)
         assert np.isfinite(got).all(), t
         assert np.all(np.abs(got - ref[t]) <= lim[t]), t
+
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m", [2, 5, 9, 200])
+def test_gradients_next_to_the_largest_value(m, dtype):
+    """da and du that are finite in fp32 and would round to an infinite bf16."""
+    print_case("gated_largest", m=m, dtype=dtype)
+    k, n = 72, 80
+    c = Case("relu", dtype, m, k, n)
+    pre = np.ones((2, m, n), np.float32)
+    pre[0, 1, 5] = pre[1, 1, 7] = np.float32(1.0027)     # du, da: 3.398e38, past bf16's range
+    c.dy[:] = 0.0
+    c.dy[1, 5] = c.dy[1, 7] = np.float32(torch.finfo(torch.bfloat16).max)
+    tiny = np.float32(2.0 ** -30)
+    c.x, c.wg, c.wu = c.x * tiny, c.wg * tiny, c.wu * tiny
+    for t in ("x", "dy", "wg", "wu"):
+        c.d[t].copy_(torch.from_numpy(getattr(c, t)))
+    c.d["pre"].copy_(torch.from_numpy(pre))
+    c.bwd()
+    torch.cuda.synchronize()
+    ref = G.backward("relu", c.x, c.wg, c.wu, pre[0], pre[1], c.dy)
+    da = c.dy.astype(np.float64) * pre[1]
+    du = c.dy.astype(np.float64) * pre[0]
+    terms = np.abs(da) @ np.abs(c.wg).T.astype(np.float64) + np.abs(du) @ np.abs(c.wu).T.astype(np.float64)
+    for t, want in zip(("dx", "dwg", "dwu", "dbg", "dbu"), ref):
+        got = c.get(t).astype(np.float64)
+        # Sums of at most four terms that are not 0; da and du rounded three times.
+        lim = 16 * U * (terms if t == "dx" else np.abs(want))
+        if t == "dx" and dtype == "bf16":
+            lim = lim + 2.0 ** -16 * terms + G.HALF16 * (np.abs(want) + 2.0 ** -15 * terms)
+        assert np.isfinite(got).all() and np.all(np.abs(got - want) <= lim), t
