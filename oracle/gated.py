@@ -59,8 +59,8 @@ def bounds(name, x, wg, wu, bg, bu, dy, bf16):
     epilogues behind it).  The activation and its derivative are off by at most
     16 roundings of their own pieces (of the size of a, and a^3 for the tanh form's
     derivative), their slopes are at most 1.13 and 1.  Next to its corner the ReLU's
-    derivative may be either.  bf16 results add half a step, and so do the first
-    parts of da and du, of which the bf16 dx is made."""
+    derivative may be either.  bf16 results add half a step, and there is room for
+    another one of da and du in the bf16 dx (more than their two parts need)."""
     absx = np.abs(np.asarray(x, np.float64))
     awg, awu = (np.abs(np.asarray(w, np.float64)) for w in (wg, wu))
     y, a, u = forward(name, x, wg, wu, bg, bu)

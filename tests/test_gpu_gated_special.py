@@ -217,3 +217,30 @@ def test_gradients_next_to_the_largest_value(m, dtype):
         if t == "dx" and dtype == "bf16":
             lim = lim + 2.0 ** -16 * terms + G.HALF16 * (np.abs(want) + 2.0 ** -15 * terms)
         assert np.isfinite(got).all() and np.all(np.abs(got - want) <= lim), t
+
+
+# ---- long sums of one sign --------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sums_of_one_sign_do_not_drift(dtype):
+    """8192 positive terms in one unsplit reduction, 16 an instruction.  If each
+    instruction dropped what lies below the last bit of its sum (half a step of 2^-23 on
+    average, of sums that are on average half of the last), the results would be 7e-6 low on
+    average; rounding to nearest leaves a mean of 0 and an error of at most 2^-24 each
+    instruction, random: 512 of them, root 23, of which a third or less remains."""
+    print_case("gated_drift", dtype=dtype)
+    m, k, n = 8192, 4096, 4096
+    g = torch.Generator(device="cuda").manual_seed(1)
+    kind = torch.float32 if dtype == "f32" else torch.bfloat16
+    pos = lambda *s: torch.randn(s, generator=g, device="cuda").abs()
+    x, w, dy = pos(m, k).to(kind), pos(2, k, n).to(kind), pos(m, n).to(kind)
+    pre = pos(2, m, n)
+    d = sb.gated_desc(m, k, n, sb.SB_F32 if dtype == "f32" else sb.SB_BF16, sb.SB_ACT_RELU)
+    ws = torch.empty(sb.sb_gated_workspace_bytes(d, sb.SB_FC_BWD), dtype=torch.uint8, device="cuda")
+    dw = torch.empty(2, k, n, device="cuda")
+    sb.sb_gated_shard_bwd(d, x, w[0], w[1], pre, dy, None, dw[0], dw[1], None, None, False, ws)
+    some = x[:, :32].t().contiguous().double()
+    for q, v in enumerate((dy.float() * pre[1] * (pre[0] > 0), dy.float() * pre[0])):
+        want = some @ v.double()
+        e = (dw[q, :32].double() - want) / want
+        assert abs(float(e.mean())) <= 5e-7, float(e.mean())
+        assert float(e.pow(2).mean().sqrt()) <= 23 * U, float(e.pow(2).mean().sqrt())
