@@ -460,8 +460,10 @@ __device__ __forceinline__ void dual_block(const DualArgs& g, int block, u16* ld
 
   // Whether the products are formed again on the fp32 MFMA, operands straight from memory:
   // those of an fp32 block with values that the parts do not carry, or with sums that are
-  // not finite; those of a bf16 wave whose sums are not, where one operand comes in parts
-  // (an infinity times the lower ones, which are 0 or of either sign, would be NaN).
+  // not finite; those of a bf16 wave with infinities beside lower parts, which are 0 or of
+  // either sign, so that their products would make a NaN of an infinite sum.  Only sums
+  // that are not finite look for infinities: a NaN in dy puts the backward of 4096 x 4096 x
+  // 8192 from 2.7 to 3.2 ms, nothing but NaN to 6.1; an infinity in x, found, to 27.
   constexpr bool PARTS = NP == 1 && KIND != kDualFwd;
   bool again = false;
   if constexpr (NP == 3 || PARTS) {
@@ -486,18 +488,53 @@ __device__ __forceinline__ void dual_block(const DualArgs& g, int block, u16* ld
       again = __ballot(!(z == 0.f)) != 0;
     }
   }
+  int ar[FA], bc[F];                                 // this lane's rows of A, columns of B
   if (__builtin_expect(again, 0)) {
-    int ar[FA], bc[F];                               // this lane's rows of A, columns of B
     const int c = lane % 32;
 #pragma unroll
     for (int i = 0; i < FA; ++i) ar[i] = out_row(i, c);
 #pragma unroll
-    for (int j = 0; j < F; ++j) {
+    for (int j = 0; j < F; ++j)
       bc[j] = n0 + (BKC ? wn * T::RC + j * 32 + c
                         : pair_block<F>(wn * (F / 2) + j % (F / 2), c / 16) * 16 + c % 16);
+    if constexpr (PARTS) {
+      bool found = false;                            // (DW's segments have the same x)
+      for (int u = t0; u < (KIND == kDualDw ? min(t1, t0 + per_seg) : t1); ++u) {
+        const int sg = u / per_seg, kb = (u - sg * per_seg) * 32, ke = min(g.K, kb + 32);
+        if (sg >= g.segs - g.firsts) break;
+        if constexpr (KIND == kDualDw) {
+          const u16* A = (const u16*)g.a[sg];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const int k = kb + 2 * x + lane / 32;
+#pragma unroll
+            for (int i = 0; i < FA; ++i)
+              found |= k < ke && ar[i] < g.M && (A[(size_t)k * g.lda + ar[i]] & 0x7fffu) == 0x7f80u;
+          }
+        } else {                                     // whole pieces: K is a multiple of 8
+          const u16* B = (const u16*)g.b[0][sg];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int k = kb + 16 * x + lane / 32 * 8;
+#pragma unroll
+            for (int j = 0; j < F; ++j) {
+              if (k >= ke || bc[j] >= g.N) continue;
+              const u32x4 v = *reinterpret_cast<const u32x4*>(B + (size_t)bc[j] * g.ldb + k);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                found |= (v[e] & 0x7fffu) == 0x7f80u || (v[e] & 0x7fff0000u) == 0x7f800000u;
+            }
+          }
+        }
+      }
+      again = __ballot(found) != 0;
+    }
+  }
+  if (__builtin_expect(again, 0)) {
+#pragma unroll
+    for (int j = 0; j < F; ++j)
 #pragma unroll
       for (int i = 0; i < FA; ++i) clear(acc[j][i]);
-    }
     for (int u = t0; u < t1; ++u) {
       const int sg = u / per_seg, kb = (u - sg * per_seg) * 32, ke = min(g.K, kb + 32);
       const E* A = (const E*)g.a[sg];
