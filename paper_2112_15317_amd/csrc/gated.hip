@@ -239,9 +239,10 @@ struct FewArgs {
 // weight) and a split's lines, J at a time for each L lanes: 2 J loads of 16 bytes are
 // under way in a lane, and x is a piece for J lines.  L = 8 takes whole lines of the
 // caches.  L = 4 takes half of them and so does half the work a block one after the other,
-// but what the caches read twice bounds it from a few MB on.  One row of bf16 weights:
-// 1024 x 1024 3.8 us (one line of k at a time a lane, reduced by shuffles: 5.5), 4096 x
-// 1024 7.1 (24.1), 4096 x 4096 16.4 (4.1 TB/s); eight rows of 4096 x 4096 20.0.
+// but what the caches read twice bounds it from a few MB on.  One row of bf16 weights
+// (in a captured graph): 1024 x 1024 3.8 us (one line of k at a time a lane, reduced by
+// shuffles: 5.5), 4096 x 1024 7.1 (24.1), 4096 x 4096 16.4 (4.1 TB/s); eight rows of
+// 4096 x 4096 20.0.
 template <class E, int M> constexpr int kFewLines = sizeof(E) == 2 && M == 8 ? 4 : kFewWidth<E>;
 template <class E, int M, int L>
 __global__ __launch_bounds__(512) void gated_few_fwd(FewArgs g) {
@@ -687,8 +688,8 @@ static DualPlan dual_plan(DualKind kind, bool b16, int M, int N, int K, int segs
 // fifth more where a CU takes one block after the other).  One launch instead of two,
 // and one for both sums, saves a third of the time over 120 shards in both types (from
 // 2 % at 593 x 2752 x 1984 fp32 to 43 % at 248 x 1024 x 384 bf16); the plan taken is
-// 2 (fp32) or 7 % (bf16) slower than the best on average over 270, mostly where all
-// take 10 to 20 us.
+// 2 (fp32) or 7 % (bf16, with one part in dx) slower than the best on average over 270,
+// mostly where all take 10 to 20 us.
 struct GradPlan { DualPlan dx, dw; };
 
 static GradPlan grad_plan(bool b16, int m, int k, int n) {
