@@ -390,8 +390,8 @@ sb_status sb_gated_shard_fwd(const sb_gated_desc *desc, const void *x,
  * parameters' gradients are fp32 and carry da and du in full; SB_BF16's
  * dx_partial, itself rounded to bf16, is summed from 16 bits of them or
  * more.  An infinity in x makes its row of the weights' gradients infinite, by
- * the signs of da and du.  As for the FC shard the division by K is the
- * optimiser's.
+ * the signs of da and du (NaN where two of them disagree).  As for the FC shard
+ * the division by K is the optimiser's.
  * The summation order is fixed: repeated calls give bit-identical results. */
 sb_status sb_gated_shard_bwd(const sb_gated_desc *desc, const void *x,
                              const void *w_gate, const void *w_up,
@@ -542,9 +542,8 @@ sb_status sb_sgd_update(int count, float *const *w, const float *const *g,
  * update:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
  *   w = (1 - lr decay) w - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
- * in fp32, each result of the last line within 17 half steps of its move (the root and
- * the reciprocal of the sum with eps may be the hardware's, a step off each); m and v of
- * the update are those before they become bytes.
+ * in fp32 (the root, and the reciprocal of its sum with eps, may be the hardware's, a step
+ * of fp32 off each); m and v of the update are those before they become bytes.
  *
  * Moments:
  *   32  fp32, zero before the first update;
