@@ -370,7 +370,7 @@ def _own_logp(s):
         got.update(logp=s["logp"], entropy=s["entropy"])
     if s["dz"] is not None:
         sb.sb_token_logp_bwd(s["desc"], s["z"], s["stats"], s["targets"], s.get("dlogp"), s["entropy"],
-                             s.get("dentropy"), s["top_ids"], s.get("dtop"), s["dz"])
+                             s.get("dentropy"), s["top_ids"], s["top"], s.get("dtop"), s["dz"])
         got["dz"] = s["dz"]
     return got
 
