@@ -76,6 +76,7 @@ typedef enum { SB_NCHW = 0, SB_NCHW8C = 1 } sb_layout;
 #define SB_PACKED_FILTERS 2u  /* conv fwd / data gradient: `w` holds filters
                                  packed by sb_conv3x3_pack_filters */
 #define SB_UNALIGNED 4u       /* gated FC: x or weights off 16-byte boundaries */
+#define SB_TOP_PROBS 8u       /* token log-probabilities: alternatives' probabilities */
 
 /* Returns a static string naming the status. */
 const char *sb_status_string(sb_status s);
@@ -622,6 +623,167 @@ sb_status sb_adamw_advance(int32_t *steps_done, void *stream);
 sb_status sb_adamw_unpack(size_t n, const uint8_t *m, const int16_t *m_top,
                           const uint8_t *v, const int16_t *v_top, float *m_out,
                           float *v_out, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Embedding: rows of a vocabulary's table for token ids.  The table is split
+ * along the vocabulary as an FC layer is along its outputs: a worker has the
+ * rows of the ids first .. first + vocab - 1, and its outputs are partial, to
+ * be summed over the workers.
+ *
+ *   ids     [tokens]         int32, on the device.  An id outside the shard's
+ *                            range, a negative one (padding) among them, is
+ *                            no row of it: a zero row of y, no gradient.
+ *   table   [vocab][width]   dense
+ *   y, dy   [tokens][width]  row stride ldy
+ * SB_F32, or SB_BF16 (table, y and dy bfloat16, dtable fp32).  tokens may be 0.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+    int tokens, vocab, width;
+    int first;             /* id of the table's first row (>= 0)           */
+    int dtype;             /* sb_dtype                                     */
+    int ldy;               /* row stride of y and dy (>= width)            */
+    float scale;           /* of y; finite                                 */
+} sb_embed_desc;
+
+/* y[i] = scale * table[ids[i] - first], in fp32 and rounded once (with a scale
+ * of 1 the row as it is).  SB_ERR_INVALID_ARG for NULL pointers, pointers that
+ * are not multiples of their elements' size, and a y that overlaps an input. */
+sb_status sb_embed_fwd(const sb_embed_desc *desc, const void *table,
+                       const int32_t *ids, void *y, void *stream);
+
+/* dtable[v] = (accumulate ? dtable[v] : 0) + scale * sum_i dy[i] over the tokens
+ * with ids[i] = first + v.  Sums are fp32 and their order is fixed: repeated
+ * calls give bit-identical results.  With accumulate rows without a token are
+ * not touched.  The workspace starts at a multiple of 16.  Arguments are checked
+ * as above, the workspace must not overlap a tensor; 2^30 tokens and more, or rows
+ * of 2^23 and more, are SB_ERR_UNSUPPORTED (the query: (size_t)-1). */
+size_t sb_embed_workspace_bytes(const sb_embed_desc *desc);
+sb_status sb_embed_bwd(const sb_embed_desc *desc, const int32_t *ids,
+                       const void *dy, float *dtable, int accumulate,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Expert rows: each token goes to `top` experts (dense or gated layers), whose
+ * rows have to lie together, and their outputs come back as one row.  What the
+ * modulo layer does by a fixed rule is done here by the router's choice.  A
+ * worker has the experts first .. first + experts - 1; y and dx are partial,
+ * to be summed over the workers.
+ *
+ *   ids      [tokens][top]   int32: the experts of each token.  One outside the
+ *                            worker's range is not its: no row.
+ *   place    [tokens][top]   int32: the row of each slot among the rows sorted
+ *                            by expert (tokens in their order within one), -1
+ *                            for none.  Made by sb_expert_sort.
+ *   offsets  [experts + 1]   int32: expert e's rows are offsets[e] ..
+ *                            offsets[e + 1] - 1, offsets[experts] their number.
+ *   x, y, dy [tokens][width]         row stride ldx
+ *   xs, ys, dys [tokens * top][width] row stride ldr; rows from
+ *                            offsets[experts] on are neither read nor written
+ *   weights, dweights [tokens][top]  fp32
+ * SB_F32, or SB_BF16 (the rows bfloat16; products and sums fp32, rounded once).
+ * tokens may be 0.  The calls below return SB_ERR_INVALID_ARG for bad
+ * descriptors, NULL pointers, pointers that are not multiples of their elements'
+ * size and outputs that overlap inputs or each other, SB_ERR_UNSUPPORTED for 2^30 slots
+ * and more or rows of 2^24 and more.  Places outside the rows count as none.
+ * ---------------------------------------------------------------------- */
+enum { SB_MAX_EXPERTS = 512 };
+typedef struct {
+    int tokens, top, experts;
+    int first;             /* the worker's first expert (>= 0)             */
+    int width;
+    int dtype;             /* sb_dtype                                     */
+    int ldx;               /* row stride of the tokens' rows (>= width)    */
+    int ldr;               /* row stride of the sorted rows (>= width)     */
+} sb_expert_desc;
+
+/* place and offsets from ids.  The workspace (sb_expert_workspace_bytes, often 0;
+ * (size_t)-1 for a descriptor the calls refuse) starts at a multiple of 16. */
+size_t sb_expert_workspace_bytes(const sb_expert_desc *desc);
+sb_status sb_expert_sort(const sb_expert_desc *desc, const int32_t *ids,
+                         int32_t *place, int32_t *offsets, void *workspace,
+                         size_t workspace_bytes, void *stream);
+
+/* xs[place[t][j]] = x[t]. */
+sb_status sb_expert_gather(const sb_expert_desc *desc, const void *x,
+                           const int32_t *place, void *xs, void *stream);
+
+/* y[t] = sum_j weights[t][j] * ys[place[t][j]], in the order of j; weights may be
+ * NULL (1 each).  A token without a row gets zeros.  Without weights, on the gradient
+ * of xs, this is the gather's backward: dx[t] = sum_j dxs[place[t][j]]. */
+sb_status sb_expert_combine(const sb_expert_desc *desc, const void *ys,
+                            const int32_t *place, const float *weights,
+                            void *y, void *stream);
+
+/* The gradients of sb_expert_combine:
+ *   dys[place[t][j]] = weights[t][j] * dy[t]   (weights NULL: dy[t])
+ *   dweights[t][j]   = sum_c dy[t][c] * ys[place[t][j]][c], 0 where there is no row
+ * dweights may be NULL (ys is then not read and may be NULL). */
+sb_status sb_expert_combine_bwd(const sb_expert_desc *desc, const void *dy,
+                                const void *ys, const int32_t *place,
+                                const float *weights, void *dys,
+                                float *dweights, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Log-probabilities of given tokens on the complete model output (as
+ * sb_log_softmax_nll, for vocabularies: the log-probabilities themselves are
+ * not written), the entropy of each row and its most likely classes, with the
+ * logits' gradient through all of them.  On the rows of a router, with
+ * SB_TOP_PROBS, the alternatives are the experts and their probabilities.
+ *
+ *   z, dz       [m][classes]   row stride ldz; SB_F32, or SB_BF16
+ *   targets     [m]            int32: the token of each row.  Negative: none
+ *                              (padding): logp 0, no gradient.  One >= classes
+ *                              gives logp = NaN and a row of dz of NaN.
+ *   logp        [m]            z[target] - log(sum_c exp(z[c]))
+ *   entropy     [m]            -sum_c p[c] log p[c]
+ *   stats       [m][2]         the largest logit, and the logarithm of
+ *                              sum_c exp(z[c] - largest): for the backward
+ *   top_ids     [m][top]       int32: the `top` most likely classes, most likely
+ *                              first, of equal logits the lower class first
+ *   top_values  [m][top]       their log-probabilities, with SB_TOP_PROBS their
+ *                              probabilities
+ * All but z and dz fp32.  A logit of -inf is ruled out: probability 0, log-
+ * probability -inf.  A row of -inf alone has stats (-inf, -inf), entropy 0,
+ * log-probabilities -inf, and dz 0.  A NaN or +inf in a row makes its
+ * results NaN; NaN ranks above all classes.  m may be 0.
+ * Sums run in a fixed order: repeated calls give bit-identical results.
+ * ---------------------------------------------------------------------- */
+enum { SB_LOGP_MAX_TOP = 32 };
+typedef struct {
+    int m, classes, ldz;
+    int dtype;             /* sb_dtype                                     */
+    int top;               /* 0 .. min(SB_LOGP_MAX_TOP, classes)           */
+    unsigned flags;        /* SB_TOP_PROBS                                 */
+} sb_token_logp_desc;
+
+/* Workspace bytes of the forward (0 for short rows; the backward needs none);
+ * (size_t)-1 for a descriptor that the calls refuse.  It starts at a multiple
+ * of 16. */
+size_t sb_token_logp_workspace_bytes(const sb_token_logp_desc *desc);
+
+/* logp (and targets with it) and entropy may each be NULL; top_ids and top_values
+ * are needed where top > 0.  SB_ERR_INVALID_ARG for bad descriptors, NULL
+ * pointers, pointers that are not multiples of their elements' size and
+ * outputs or a workspace that overlap an input or each other; SB_ERR_UNSUPPORTED for more
+ * than 2^20 classes or 2^30 rows and more. */
+sb_status sb_token_logp_fwd(const sb_token_logp_desc *desc, const void *z,
+                            const int32_t *targets, float *logp, float *entropy,
+                            float *stats, int32_t *top_ids, float *top_values,
+                            void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/* dz = the gradient of sum_i dlogp[i] logp[i] + dentropy[i] entropy[i] +
+ * sum_k dtop[i][k] top_values[i][k], from the forward's stats and, where they are
+ * used, entropy (with dentropy), top_ids (with dtop) and top_values (with dtop and
+ * SB_TOP_PROBS).  dlogp (with targets), dentropy and dtop may each be NULL (0).
+ * The sum is formed in fp32 and rounded once.  dz may be z itself (written in
+ * place); it must not overlap otherwise.  Refusals as above. */
+sb_status sb_token_logp_bwd(const sb_token_logp_desc *desc, const void *z,
+                            const float *stats, const int32_t *targets,
+                            const float *dlogp, const float *entropy,
+                            const float *dentropy, const int32_t *top_ids,
+                            const float *top_values, const float *dtop,
+                            void *dz, void *stream);
 
 #ifdef __cplusplus
 }

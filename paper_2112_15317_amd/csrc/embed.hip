@@ -1,0 +1,294 @@
+// embed.hip -- rows of a vocabulary shard's table for token ids, and the table's
+// gradient.
+//
+// y[i] = scale * table[ids[i] - first], zero for ids of other shards and padding;
+// dtable[v] = scale * sum of dy[i] over ids[i] = first + v.
+//
+// Both move rows and compute next to nothing: HBM bounds them.
+//
+// The gradient sorts the tokens by id (slot_sort.hpp), so that each row of the table
+// is summed by one lane group in the tokens' order: no atomics, the same result in
+// every run.  Words in use are few and some of them are in every sentence, so the
+// work is split by sorted tokens, not by rows of the table: a group takes kRun
+// tokens in a row; an id's tokens that go past a group's end leave partial sums
+// (fp32, at most two a group), which a last launch joins in order.  Rows without a
+// token are zeroed beside the sort.
+#include "rows.hpp"
+#include "slot_sort.hpp"
+
+#include <cmath>
+
+namespace sb {
+
+template <typename T, int U>
+__global__ __launch_bounds__(256) void embed_fwd_kernel(RowPlan rp, int n, int first, int vocab,
+                                                        int width, int ldy, float scale,
+                                                        const T* __restrict__ table,
+                                                        const int32_t* __restrict__ ids,
+                                                        T* __restrict__ y) {
+  constexpr int N = Piece<T>::N;
+  const size_t group = ((size_t)blockIdx.x * 256 + threadIdx.x) >> rp.shift;
+  const int lane = threadIdx.x & ((1 << rp.shift) - 1);
+  const size_t i = group / (unsigned)rp.segs;
+  if (i >= (size_t)n) return;
+  const int c0 = (int)(group - i * rp.segs) * (U << rp.shift) + lane;
+  const int id = ids[i];
+  const bool inside = id >= first && (uint32_t)(id - first) < (uint32_t)vocab;
+  const T* src = table + (size_t)(inside ? id - first : 0) * width;
+  T* dst = y + i * (size_t)ldy;
+  Piece<T> p[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = c0 + (u << rp.shift);
+    p[u].raw = u4{0, 0, 0, 0};
+    if (inside && c < rp.pieces) p[u].load(src + (size_t)c * N, width - c * N);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int c = c0 + (u << rp.shift);
+    if (c >= rp.pieces) continue;
+    if (inside && scale != 1.f) {
+      float v[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = p[u].get(e) * scale;
+      p[u].set(v);
+    }
+    p[u].store(dst + (size_t)c * N, width - c * N);
+  }
+}
+
+struct EmbedBwd {
+  RowPlan rp;
+  const uint2* slots;          // key, token, sorted; key `vocab`: not the shard's
+  int n, vocab, width, ldy;
+  int run, runs;               // sorted tokens of a group; groups along them
+  float scale;
+  int accumulate;
+  float* dtable;
+  float* part;                 // [runs][2][width]: of an id that began before, of one that goes on
+};
+
+// Sums of one group's tokens, N columns a lane.
+template <typename T>
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __restrict__ dy) {
+  constexpr int N = Piece<T>::N, AHEAD = 8;
+  const size_t group = ((size_t)blockIdx.x * 256 + threadIdx.x) >> b.rp.shift;
+  const int lane = threadIdx.x & ((1 << b.rp.shift) - 1);
+  const size_t g = group / (unsigned)b.rp.segs;
+  if (g >= (size_t)b.runs) return;
+  const int c = (int)(group - g * b.rp.segs) * (1 << b.rp.shift) + lane;
+  const int left = b.width - c * N;
+  const int j0 = (int)g * b.run, j1 = min(b.n, j0 + b.run);
+  const uint32_t none = (uint32_t)b.vocab;
+  // The key before the group's first and the one behind its last.
+  uint32_t key = j0 > 0 ? b.slots[j0 - 1].x : ~0u;
+  const uint32_t behind = j1 < b.n ? b.slots[j1].x : ~0u;
+  bool head = j0 > 0 && b.slots[j0].x == key;       // the sum began before this group
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+  key = b.slots[j0].x;
+  for (int j = j0; j < j1; j += AHEAD) {
+    uint2 s[AHEAD];
+    Piece<T> p[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) s[a] = b.slots[min(j + a, j1 - 1)];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      p[a].raw = u4{0, 0, 0, 0};
+      if (j + a < j1 && s[a].x != none && left > 0)
+        p[a].load(dy + (size_t)s[a].y * b.ldy + (size_t)c * N, left);
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      if (j + a >= j1 || key == none) break;
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += p[a].get(e);
+      const bool last = j + a + 1 >= j1;
+      const uint32_t next = last ? behind : a + 1 < AHEAD ? s[(a + 1) % AHEAD].x : b.slots[j + a + 1].x;
+      if (next == key && !last) continue;
+      const bool on = next == key;                  // goes on in the next group
+      const bool whole = !head && !on;
+      float* out = (whole ? b.dtable + (size_t)key * b.width
+                          : b.part + ((size_t)g * 2 + (head ? 0 : 1)) * b.width) + (size_t)c * N;
+#pragma unroll
+      for (int q = 0; q < N; q += 4) {
+        Piece<float> o;
+        if (whole && b.accumulate) o.load(out + q, left - q);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = !whole ? acc[q + e] : b.accumulate ? fmaf(acc[q + e], b.scale, o.get(e)) : acc[q + e] * b.scale;
+        o.set(v);
+        o.store(out + q, left - q);
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] = 0.f;
+      head = false;
+      key = next;
+    }
+  }
+}
+
+// Joins the partial sums of an id whose tokens began in group g and go on behind it.
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd b) {
+  const int g = blockIdx.x;
+  const int c = blockIdx.y * 256 + threadIdx.x;
+  const int j1 = (g + 1) * b.run;                   // a group lies behind
+  const uint32_t key = b.slots[j1 - 1].x;
+  if (key == (uint32_t)b.vocab || b.slots[j1].x != key) return;
+  // Where it began: the head of group g is of another id, or nothing was before.
+  const int j0 = g * b.run;
+  if (b.slots[j0].x == key && g > 0 && b.slots[j0 - 1].x == key) return;
+  int lo = j1, hi = b.n;                            // the first slot behind the id's
+  while (lo < hi) {
+    const int mid = lo + (hi - lo) / 2;
+    if (b.slots[mid].x == key) lo = mid + 1;
+    else hi = mid;
+  }
+  const int end = (lo - 1) / b.run;                 // its last group
+  if (c >= b.width) return;
+  float v = b.part[((size_t)g * 2 + 1) * b.width + c];
+#pragma unroll 8
+  for (int h = g + 1; h <= end; ++h) v += b.part[(size_t)h * 2 * b.width + c];
+  float* o = b.dtable + (size_t)key * b.width + c;
+  *o = b.accumulate ? fmaf(v, b.scale, *o) : v * b.scale;
+}
+
+}  // namespace sb
+
+namespace {
+
+// Sorted tokens of a lane group: long ones leave few partial sums, short ones fill the chip.
+int embed_run(const sb::RowPlan& rp, int n) {
+  int run = 8;
+  while (run < 64 && (int64_t)(n / (2 * run)) * rp.segs << rp.shift >= 256 * 1024) run *= 2;
+  return run;
+}
+
+struct EmbedSpace {
+  size_t a, b, counts, part, bytes;
+};
+
+sb::RowPlan embed_rows(const sb_embed_desc* d) {
+  return sb::row_plan<1>(d->width, 16 / (int)sbh::dsize(d->dtype));
+}
+
+EmbedSpace embed_space(const sb_embed_desc* d) {
+  const sb::SortIn s = sb::sort_plan(nullptr, d->first, d->vocab, d->tokens);
+  const int run = embed_run(embed_rows(d), d->tokens);
+  EmbedSpace e{};
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += sb::round_up(bytes, 256);
+    return here;
+  };
+  e.a = take((size_t)d->tokens * 8);
+  e.b = take(s.passes > 1 ? (size_t)d->tokens * 8 : 0);
+  e.counts = take(sb::sort_count_bytes(s));
+  e.part = take(d->tokens > run ? (size_t)sb::cdiv(d->tokens, run) * 2 * d->width * 4 : 0);
+  e.bytes = at;
+  return e;
+}
+
+sb_status embed_check(const sb_embed_desc* d) {
+  if (!d || d->tokens < 0 || d->vocab < 1 || d->width < 1 || d->first < 0 || d->ldy < d->width)
+    return SB_ERR_INVALID_ARG;
+  if (d->dtype != SB_F32 && d->dtype != SB_BF16) return SB_ERR_INVALID_ARG;
+  if (!std::isfinite(d->scale) || d->first > INT32_MAX - d->vocab) return SB_ERR_INVALID_ARG;
+  if (d->tokens >= 1 << 30 || d->width >= 1 << 23) return SB_ERR_UNSUPPORTED;
+  return SB_OK;
+}
+
+size_t embed_out_bytes(const sb_embed_desc* d) {
+  return d->tokens ? ((size_t)(d->tokens - 1) * d->ldy + d->width) * sbh::dsize(d->dtype) : 0;
+}
+
+template <typename T>
+sb_status embed_fwd(const sb_embed_desc* d, const T* table, const int32_t* ids, T* y,
+                    hipStream_t stream) {
+  constexpr int U = 2;
+  const sb::RowPlan rp = sb::row_plan<U>(d->width, sb::Piece<T>::N);
+  const size_t lanes = (size_t)d->tokens * rp.segs << rp.shift, blocks = (lanes + 255) / 256;
+  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
+  sb::embed_fwd_kernel<T, U><<<(unsigned)blocks, 256, 0, stream>>>(
+      rp, d->tokens, d->first, d->vocab, d->width, d->ldy, d->scale, table, ids, y);
+  return sbh::launch_status();
+}
+
+}  // namespace
+
+extern "C" size_t sb_embed_workspace_bytes(const sb_embed_desc* d) {
+  if (embed_check(d) != SB_OK) return (size_t)-1;
+  return embed_space(d).bytes;
+}
+
+extern "C" sb_status sb_embed_fwd(const sb_embed_desc* d, const void* table, const int32_t* ids,
+                                  void* y, void* stream) {
+  const sb_status s = embed_check(d);
+  if (s != SB_OK) return s;
+  if (d->tokens == 0) return SB_OK;
+  if (!table || !ids || !y) return SB_ERR_INVALID_ARG;
+  const size_t e = sbh::dsize(d->dtype), yb = embed_out_bytes(d);
+  if ((((uintptr_t)table | (uintptr_t)y) & (e - 1)) || ((uintptr_t)ids & 3))
+    return SB_ERR_INVALID_ARG;
+  if (sbh::overlaps(y, yb, table, (size_t)d->vocab * d->width * e) ||
+      sbh::overlaps(y, yb, ids, (size_t)d->tokens * 4))
+    return SB_ERR_INVALID_ARG;
+  if (d->dtype == SB_BF16)
+    return embed_fwd(d, (const sb::u16*)table, ids, (sb::u16*)y, sbh::stream_of(stream));
+  return embed_fwd(d, (const float*)table, ids, (float*)y, sbh::stream_of(stream));
+}
+
+extern "C" sb_status sb_embed_bwd(const sb_embed_desc* d, const int32_t* ids, const void* dy,
+                                  float* dtable, int accumulate, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  sb_status s = embed_check(d);
+  if (s != SB_OK) return s;
+  if (!dtable || (accumulate != 0 && accumulate != 1)) return SB_ERR_INVALID_ARG;
+  if (d->tokens > 0 && (!ids || !dy)) return SB_ERR_INVALID_ARG;
+  const size_t e = sbh::dsize(d->dtype), table = (size_t)d->vocab * d->width;
+  if (((uintptr_t)dy & (e - 1)) || (((uintptr_t)ids | (uintptr_t)dtable) & 3) ||
+      ((uintptr_t)workspace & 15))
+    return SB_ERR_INVALID_ARG;
+  const EmbedSpace at = embed_space(d);
+  const size_t dyb = embed_out_bytes(d), ib = (size_t)d->tokens * 4;
+  if (sbh::overlaps(dtable, table * 4, dy, dyb) || sbh::overlaps(dtable, table * 4, ids, ib) ||
+      sbh::overlaps(workspace, at.bytes, dtable, table * 4) ||
+      sbh::overlaps(workspace, at.bytes, dy, dyb) || sbh::overlaps(workspace, at.bytes, ids, ib))
+    return SB_ERR_INVALID_ARG;
+  if (at.bytes && (!workspace || workspace_bytes < at.bytes)) return SB_ERR_WORKSPACE;
+  if (d->tokens == 0 && accumulate) return SB_OK;
+  char* ws = (char*)workspace;
+  hipStream_t st = sbh::stream_of(stream);
+  const sb::SortIn in = sb::sort_plan(ids, d->first, d->vocab, d->tokens);
+  sb::EmbedBwd b{};
+  b.rp = embed_rows(d);
+  b.n = d->tokens;
+  b.vocab = d->vocab;
+  b.width = d->width;
+  b.ldy = d->ldy;
+  b.run = embed_run(b.rp, d->tokens);
+  b.runs = sb::cdiv(d->tokens, b.run);
+  b.scale = d->scale;
+  b.accumulate = accumulate;
+  b.dtable = dtable;
+  b.part = (float*)(ws + at.part);
+  const size_t blocks = (((size_t)b.runs * b.rp.segs << b.rp.shift) + 255) / 256;
+  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
+  b.slots = sbh::sort_slots(in, nullptr, nullptr, (uint2*)(ws + at.a), (uint2*)(ws + at.b),
+                            (uint32_t*)(ws + at.counts),
+                            sb::Fill{dtable, accumulate ? 0 : table}, st);
+  s = sbh::launch_status();
+  if (s != SB_OK || d->tokens == 0) return s;
+  if (d->dtype == SB_BF16)
+    sb::embed_sum_kernel<sb::u16><<<(unsigned)blocks, 256, 0, st>>>(b, (const sb::u16*)dy);
+  else
+    sb::embed_sum_kernel<float><<<(unsigned)blocks, 256, 0, st>>>(b, (const float*)dy);
+  if (b.runs > 1) {
+    const dim3 grid((unsigned)(b.runs - 1), (unsigned)sb::cdiv(d->width, 256));
+    sb::embed_join_kernel<<<grid, 256, 0, st>>>(b);
+  }
+  return sbh::launch_status();
+}

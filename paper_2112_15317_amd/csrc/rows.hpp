@@ -1,0 +1,99 @@
+// rows.hpp -- rows of a matrix in 16-byte pieces at any address, for kernels
+// that move whole rows (embedding, expert rows).
+//
+// gfx950's vector loads and stores take any address that is a multiple of the
+// element's size, so rows of odd widths and strides are moved 16 bytes at a
+// time too; only the elements behind a row's last whole piece go one by one.
+#pragma once
+
+#include "sb_internal.hpp"
+
+namespace sb {
+
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef u4 u4_at2 __attribute__((aligned(2)));
+typedef u4 u4_at4 __attribute__((aligned(4)));
+
+// 16 bytes of a row: N elements, held as they lie in memory.
+template <typename T> struct Piece;
+
+template <> struct Piece<float> {
+  static constexpr int N = 4;
+  u4 raw;
+  __device__ __forceinline__ void load(const float* p, int left) {
+    if (left >= N) {
+      raw = *reinterpret_cast<const u4_at4*>(p);
+    } else {
+      raw = u4{0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < left) raw[e] = __float_as_uint(p[e]);
+    }
+  }
+  __device__ __forceinline__ void store(float* p, int left) const {
+    if (left >= N) {
+      *reinterpret_cast<u4_at4*>(p) = raw;
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < left) p[e] = __uint_as_float(raw[e]);
+    }
+  }
+  __device__ __forceinline__ float get(int e) const { return __uint_as_float(raw[e]); }
+  __device__ __forceinline__ void set(const float* v) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) raw[e] = __float_as_uint(v[e]);
+  }
+};
+
+template <> struct Piece<u16> {
+  static constexpr int N = 8;
+  u4 raw;
+  __device__ __forceinline__ void load(const u16* p, int left) {
+    if (left >= N) {
+      raw = *reinterpret_cast<const u4_at2*>(p);
+    } else {
+      raw = u4{0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < left) raw[e / 2] |= (uint32_t)p[e] << (e % 2 * 16);
+    }
+  }
+  __device__ __forceinline__ void store(u16* p, int left) const {
+    if (left >= N) {
+      *reinterpret_cast<u4_at2*>(p) = raw;
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e < left) p[e] = (u16)(raw[e / 2] >> (e % 2 * 16));
+    }
+  }
+  __device__ __forceinline__ float get(int e) const {
+    return __uint_as_float(e % 2 ? raw[e / 2] & 0xffff0000u : raw[e / 2] << 16);
+  }
+  __device__ __forceinline__ void set(const float* v) {   // rounds to nearest, ties to even
+#pragma unroll
+    for (int e = 0; e < N; e += 2) raw[e / 2] = f32x2_to_bf16x2(v[e], v[e + 1]);
+  }
+};
+
+// A row's pieces are spread over a group of G = 1 << shift lanes (8 to 64: the
+// smallest that holds the row in one go, so narrow rows share a wave), U pieces a
+// lane; a wider row is `segs` such stretches.
+struct RowPlan {
+  int shift;                   // lanes of a group
+  int pieces;                  // of a row
+  int segs;                    // stretches of a row, each a group's work
+};
+
+template <int U>
+inline RowPlan row_plan(int width, int n_per_piece) {
+  RowPlan p;
+  p.pieces = cdiv(width, n_per_piece);
+  p.shift = 3;
+  while (p.shift < 6 && (1 << p.shift) < p.pieces) ++p.shift;
+  p.segs = cdiv(p.pieces, U << p.shift);
+  return p;
+}
+
+}  // namespace sb

@@ -1,0 +1,682 @@
+// token_logp.hip -- log-probabilities of given tokens, entropy and the most likely
+// alternatives of rows of logits, and the logits' gradient.
+//
+// With M a row's largest logit and S = sum_c exp(z_c - M):
+//   logp_c = (z_c - M) - log S,   H = log S - sum_c exp(z_c - M) (z_c - M) / S
+// The largest term is left out of the sum, O = S - 1, and log S is log1p(O): where a
+// row is sure of its token, logp and H are small and keep their bits.
+//
+// Backward: a gradient g on the log-probabilities of some classes and dH on the entropy give
+//   dz_c = sum of g at c - p_c (sum of all g + dH (logp_c + H)).
+//
+// Rows of up to 1024 classes (a router's): 8 to 64 lanes have a row in registers and do
+// everything in one launch.  Longer rows are cut into stretches, one a wave, held in
+// registers so that z is read once: maximum, sums, and the stretch's best classes; a
+// second launch joins a row's stretches.  Sums run in a fixed order.
+//
+// The best `top` classes of a stretch: every lane's maximum is known, and the
+// top-th largest of those 64 is a bound that at least `top` elements reach and few
+// others.  What reaches it goes to LDS and is ranked there.  Where too much does
+// (many equal logits) or a NaN is about, the slow way takes one after another.
+#include "rows.hpp"
+
+#include <cfloat>
+#include <cmath>
+
+namespace sb {
+
+constexpr int kTopList = 256;          // classes of a stretch that are ranked in LDS
+constexpr int kMaxStretches = 512;     // of a row
+constexpr int kNarrow = 1024;          // classes of a row in one launch
+constexpr int kNarrowElems = 16;       // of a lane there
+constexpr float kLog2e = 1.44269504088896341f;
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Whole numbers in the order of the logits: -0 is 0, any NaN above all.  0 is none.
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t b = __float_as_uint(v + 0.f);
+  const uint32_t o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+  return v != v ? 0xffffffffu : o;
+}
+__device__ __forceinline__ float value_of(uint32_t o) {
+  return o == 0xffffffffu ? NAN : __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o);
+}
+// Larger logits first, then lower classes.
+__device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t cls) {
+  return (uint64_t)order << 32 | (uint32_t)~cls;
+}
+__device__ __forceinline__ uint32_t class_of(uint64_t key) { return ~(uint32_t)key; }
+
+__device__ __forceinline__ float group_max(float v, int lanes) {
+  for (int o = 1; o < lanes; o *= 2) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+__device__ __forceinline__ float group_sum(float v, int lanes) {
+  for (int o = 1; o < lanes; o *= 2) v += __shfl_xor(v, o, 64);
+  return v;
+}
+__device__ __forceinline__ uint64_t group_max(uint64_t v, int lanes) {
+  for (int o = 1; o < lanes; o *= 2) {
+    const uint64_t t = (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, 64) << 32 |
+                       (uint32_t)__shfl_xor((int)v, o, 64);
+    v = t > v ? t : v;
+  }
+  return v;
+}
+
+struct LogpFwd {
+  int m, classes, ldz, top, probs;
+  int stretches;               // of a row
+  const int32_t* targets;
+  float *logp, *entropy, *stats;
+  int32_t* top_ids;
+  float* top_values;
+  float* part;                 // [m][stretches][3]: maximum, sum without it, weighted sum
+  uint64_t* keys;              // [m][stretches][top], in order, 0: none
+};
+
+// Sums of a lane's elements against the maximum mx of its row or stretch: o without
+// the elements that equal it (their number is added to `equal`), s of exp(t) t.
+// Masked elements (-inf) give nothing.  A NaN ends up in o.
+template <int E>
+__device__ __forceinline__ void lane_sums(const float* v, float mx, float& o, float& s,
+                                          int& equal) {
+  o = 0.f;
+  s = 0.f;
+  equal = 0;
+  const float base = mx == -INFINITY ? 0.f : mx;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float t = v[e] - base;
+    const float x = exp2_hw(t * kLog2e);
+    const bool is_max = v[e] == mx;
+    equal += is_max ? 1 : 0;
+    o += is_max ? 0.f : x;
+    s += x > 0.f ? x * t : 0.f;
+  }
+}
+
+// What a row gives once its maximum M, O = S - 1 and the weighted sum are known.
+struct RowSums {
+  float mx, ls, h;
+};
+__device__ __forceinline__ RowSums row_sums(float mx, float o, float s) {
+  RowSums r;
+  r.mx = mx;
+  // Nothing is left of a row of -inf alone: probabilities 0, entropy 0, log S -inf.
+  const bool none = mx == -INFINITY && o == o;
+  r.ls = none ? -INFINITY : mx == INFINITY ? NAN : log1pf(o);
+  r.h = none ? 0.f : r.ls - s / (1.f + o);
+  return r;
+}
+__device__ __forceinline__ float row_logp(const RowSums& r, float z) {
+  return z == -INFINITY && r.ls == r.ls ? -INFINITY : (z - r.mx) - r.ls;
+}
+
+template <typename T>
+__device__ __forceinline__ float target_logp(const RowSums& r, const T* z, int target,
+                                             int classes) {
+  if (target < 0) return 0.f;
+  if (target >= classes) return NAN;
+  return row_logp(r, Elem<T>::load(z, target));
+}
+
+// E elements of a lane: pieces lane, lane + lanes, ... of the row from `first` on.
+// Elements past the row are -inf.
+template <typename T, int E>
+__device__ __forceinline__ void load_row(const T* row, int classes, int first, int lane, int lanes,
+                                         float* v) {
+  constexpr int N = Piece<T>::N;
+  Piece<T> p[E / N];
+#pragma unroll
+  for (int u = 0; u < E / N; ++u) {
+    const int c = first + (lane + u * lanes) * N;
+    p[u].raw = u4{0, 0, 0, 0};
+    if (c < classes) p[u].load(row + c, classes - c);
+  }
+#pragma unroll
+  for (int u = 0; u < E / N; ++u) {
+    const int c = first + (lane + u * lanes) * N;
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[u * N + e] = c + e < classes ? p[u].get(e) : -INFINITY;
+  }
+}
+template <typename T>
+__device__ __forceinline__ int class_at(int first, int lane, int lanes, int e) {
+  constexpr int N = Piece<T>::N;
+  return first + (lane + e / N * lanes) * N + e % N;
+}
+
+// ------------------------------------------------------------- narrow rows --
+template <typename T>
+__global__ __launch_bounds__(256) void logp_narrow_fwd(LogpFwd b, int shift,
+                                                       const T* __restrict__ z) {
+  constexpr int E = kNarrowElems;
+  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
+  const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> shift;
+  if (row >= (size_t)b.m) return;             // whole groups leave together
+  const T* zr = z + row * (size_t)b.ldz;
+  float v[E];
+  load_row<T, E>(zr, b.classes, 0, lane, lanes, v);
+  float mx = v[0];
+#pragma unroll
+  for (int e = 1; e < E; ++e) mx = fmaxf(mx, v[e]);
+  if (mx != mx) mx = -INFINITY;
+  mx = group_max(mx, lanes);
+  float o, s;
+  int equal;
+  lane_sums<E>(v, mx, o, s, equal);
+  o = group_sum(o, lanes);
+  s = group_sum(s, lanes);
+  const float others = group_sum((float)equal, lanes) - 1.f;
+  if (mx != -INFINITY) o += others;           // (else the -inf elements are all that is there)
+  const RowSums r = row_sums(mx, o, s);
+  if (lane == 0) {
+    b.stats[row * 2] = r.mx;
+    b.stats[row * 2 + 1] = r.ls;
+    if (b.entropy) b.entropy[row] = r.h;
+    if (b.logp) b.logp[row] = target_logp(r, zr, b.targets ? b.targets[row] : -1, b.classes);
+  }
+  if (!b.top) return;
+  uint32_t order[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    order[e] = class_at<T>(0, lane, lanes, e) < b.classes ? order_of(v[e]) : 0;
+  for (int k = 0; k < b.top; ++k) {
+    uint32_t best = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) best = max(best, order[e]);
+    int at = 0;                               // the first of them: classes grow with e
+#pragma unroll
+    for (int e = E - 1; e >= 0; --e) at = order[e] == best ? e : at;
+    const uint64_t key = best ? key_of(best, class_at<T>(0, lane, lanes, at)) : 0;
+    const uint64_t most = group_max(key, lanes);
+#pragma unroll
+    for (int e = 0; e < E; ++e) order[e] = key == most && e == at ? 0 : order[e];
+    if (lane == 0) {
+      const float lp = row_logp(r, value_of((uint32_t)(most >> 32)));
+      b.top_ids[row * b.top + k] = (int32_t)class_of(most);
+      b.top_values[row * b.top + k] = b.probs ? expf(lp) : lp;
+    }
+  }
+}
+
+// ---------------------------------------------------------------- long rows --
+// The k-th largest (k >= 1) of the 64 lanes' numbers.
+__device__ __forceinline__ uint32_t wave_kth(uint32_t v, int k) {
+  uint32_t got = 0;
+  for (int b = 31; b >= 0; --b) {
+    const uint32_t t = got | 1u << b;
+    if (__popcll(__ballot(v >= t)) >= k) got = t;
+  }
+  return got;
+}
+
+template <typename T, int E>
+__device__ __forceinline__ void stretch_top(const LogpFwd& b, const float* v, int first, int lane,
+                                            bool odd, uint64_t* list, uint64_t* out) {
+  uint32_t best = 0;
+  int count = kTopList + 1;
+  if (!odd) {
+    float most = v[0];
+#pragma unroll
+    for (int e = 1; e < E; ++e) most = fmaxf(most, v[e]);
+    best = class_at<T>(first, lane, 64, 0) < b.classes ? order_of(most) : 0;
+    const uint32_t bound = wave_kth(best, b.top);
+    const float least = bound ? value_of(bound) : -INFINITY;
+    count = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const bool in = v[e] >= least && class_at<T>(first, lane, 64, e) < b.classes;
+      const uint64_t mask = __ballot(in);
+      if (mask) {
+        const int at = count + __popcll(mask & ((1ull << lane) - 1));
+        if (in && at < kTopList)
+          list[at] = key_of(order_of(v[e]), class_at<T>(first, lane, 64, e));
+        count += __popcll(mask);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (count <= kTopList) {
+    for (int i = lane; i < count; i += 64) {
+      const uint64_t mine = list[i];
+      int rank = 0;
+      for (int j = 0; j < count; ++j) rank += list[j] > mine ? 1 : 0;
+      if (rank < b.top) out[rank] = mine;
+    }
+    for (int k = count + lane; k < b.top; k += 64) out[k] = 0;
+    return;
+  }
+  uint64_t last = ~0ull;
+  for (int k = 0; k < b.top; ++k) {
+    uint64_t most = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int c = class_at<T>(first, lane, 64, e);
+      const uint64_t key = c < b.classes ? key_of(order_of(v[e]), c) : 0;
+      if (key < last && key > most) most = key;
+    }
+    last = group_max(most, 64);
+    if (lane == 0) out[k] = last;
+  }
+}
+
+template <typename T, int P>
+__global__ __launch_bounds__(256) void logp_stretch_fwd(LogpFwd b, const T* __restrict__ z) {
+  constexpr int E = P * Piece<T>::N;
+  __shared__ uint64_t list[4][kTopList];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const size_t unit = (size_t)blockIdx.x * 4 + wave;
+  const size_t row = unit / (unsigned)b.stretches;
+  if (row >= (size_t)b.m) return;
+  const int first = (int)(unit - row * b.stretches) * (E * 64);
+  float v[E];
+  load_row<T, E>(z + row * (size_t)b.ldz, b.classes, first, lane, 64, v);
+  float mx = v[0];
+#pragma unroll
+  for (int e = 1; e < E; ++e) mx = fmaxf(mx, v[e]);
+  if (mx != mx) mx = -INFINITY;
+  mx = group_max(mx, 64);
+  float o, s;
+  int equal;
+  lane_sums<E>(v, mx, o, s, equal);
+  o = group_sum(o, 64);
+  s = group_sum(s, 64);
+  const float others = group_sum((float)equal, 64) - 1.f;
+  if (mx != -INFINITY) o += others;
+  if (lane == 0) {
+    float* p = b.part + unit * 3;
+    p[0] = mx;
+    p[1] = o;
+    p[2] = s;
+  }
+  if (b.top) stretch_top<T, E>(b, v, first, lane, o != o, list[wave], b.keys + unit * b.top);
+}
+
+// One wave joins a row's stretches.
+template <typename T>
+__global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict__ z) {
+  const int lane = threadIdx.x & 63;
+  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= (size_t)b.m) return;
+  const float* part = b.part + row * b.stretches * 3;
+  float mx = -INFINITY;
+  int who = INT32_MAX;                          // the first stretch that has it
+  for (int p = lane; p < b.stretches; p += 64) {
+    if (part[p * 3] > mx || who == INT32_MAX) {
+      mx = part[p * 3];
+      who = p;
+    }
+  }
+  const float all = group_max(mx, 64);
+  who = mx == all ? who : INT32_MAX;
+  for (int q = 1; q < 64; q *= 2) who = min(who, __shfl_xor(who, q, 64));
+  float o = 0.f, s = 0.f;
+  for (int p = lane; p < b.stretches; p += 64) {
+    const float pm = part[p * 3], po = part[p * 3 + 1], ps = part[p * 3 + 2];
+    if (pm == -INFINITY) {                      // nothing, or NaNs
+      o += po != po ? NAN : 0.f;
+      continue;
+    }
+    const float t = pm - all, f = exp2_hw(t * kLog2e);
+    o += p == who ? po : f * (1.f + po);
+    s += f > 0.f ? f * (ps + t * (1.f + po)) : 0.f;
+  }
+  o = group_sum(o, 64);
+  s = group_sum(s, 64);
+  const RowSums r = row_sums(all, o, s);
+  if (lane == 0) {
+    b.stats[row * 2] = r.mx;
+    b.stats[row * 2 + 1] = r.ls;
+    if (b.entropy) b.entropy[row] = r.h;
+    if (b.logp)
+      b.logp[row] = target_logp(r, z + row * (size_t)b.ldz, b.targets ? b.targets[row] : -1,
+                                b.classes);
+  }
+  if (!b.top) return;
+  // The stretches' lists are in order: the best of a lane's heads, again and again.
+  const uint64_t* keys = b.keys + row * b.stretches * b.top;
+  uint64_t heads = 0;                           // 8 bits for each of a lane's (at most 8) lists
+  for (int k = 0; k < b.top; ++k) {
+    uint64_t best = 0;
+    int from = 0;
+    for (int p = lane, i = 0; p < b.stretches; p += 64, ++i) {
+      const int at = (int)(heads >> (8 * i)) & 255;
+      const uint64_t key = at < b.top ? keys[(size_t)p * b.top + at] : 0;
+      if (key > best) {
+        best = key;
+        from = i;
+      }
+    }
+    const uint64_t most = group_max(best, 64);
+    if (best == most && most) heads += 1ull << (8 * from);
+    if (lane == 0) {
+      const float lp = row_logp(r, value_of((uint32_t)(most >> 32)));
+      b.top_ids[row * b.top + k] = (int32_t)class_of(most);
+      b.top_values[row * b.top + k] = b.probs ? expf(lp) : lp;
+    }
+  }
+}
+
+// ----------------------------------------------------------------- backward --
+struct LogpBwd {
+  int m, classes, ldz, top, probs;
+  int stretches;
+  const float *stats, *entropy;
+  const int32_t* targets;
+  const float *dlogp, *dentropy;
+  const int32_t* top_ids;
+  const float *top_values, *dtop;
+};
+
+// What a row's gradient needs: logp = z - mx - ls; all = the sum of g, and dH H.
+struct RowGrad {
+  float mx, ls, dh, all;
+  int target;
+  float g;                     // at the target
+  bool bad;                    // a target past the classes: a row of NaN
+};
+__device__ __forceinline__ RowGrad row_grad(const LogpBwd& b, size_t row) {
+  RowGrad r;
+  r.mx = b.stats[row * 2];
+  r.ls = b.stats[row * 2 + 1];
+  r.dh = b.dentropy ? b.dentropy[row] : 0.f;
+  r.all = b.dentropy ? r.dh * b.entropy[row] : 0.f;
+  r.target = b.dlogp ? b.targets[row] : -1;
+  r.g = r.target >= 0 ? b.dlogp[row] : 0.f;
+  r.bad = r.target >= b.classes;
+  r.all += r.g;
+  return r;
+}
+// Gradient of a row's k-th alternative on its log-probability; its class in id.
+__device__ __forceinline__ float top_grad(const LogpBwd& b, size_t row, int k, int& id) {
+  id = b.top_ids[row * b.top + k];
+  const float d = b.dtop[row * b.top + k];
+  if (id < 0 || id >= b.classes) return 0.f;
+  if (!b.probs) return d;
+  const float p = b.top_values[row * b.top + k];
+  return p == 0.f ? 0.f : d * p;
+}
+// dz of a class that has the gradient g itself (0 for most).
+__device__ __forceinline__ float class_grad(const RowGrad& r, float z, float g) {
+  const float lp = (z - r.mx) - r.ls;
+  const float p = exp2_hw(lp * kLog2e);
+  const float d = p > 0.f ? p * (r.all - g + r.dh * lp) : p == 0.f ? 0.f : p;
+  return (g != 0.f ? -g * expm1f(lp) : 0.f) - d;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void logp_narrow_bwd(LogpBwd b, int shift, const T* z, T* dz) {
+  constexpr int E = kNarrowElems, N = Piece<T>::N;
+  const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
+  const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> shift;
+  if (row >= (size_t)b.m) return;
+  const T* zr = z + row * (size_t)b.ldz;
+  float v[E], g[E];
+  load_row<T, E>(zr, b.classes, 0, lane, lanes, v);
+  RowGrad r = row_grad(b, row);
+#pragma unroll
+  for (int e = 0; e < E; ++e) g[e] = class_at<T>(0, lane, lanes, e) == r.target ? r.g : 0.f;
+  if (b.dtop) {
+    for (int k = 0; k < b.top; ++k) {
+      int id;
+      const float d = top_grad(b, row, k, id);
+      r.all += d;
+#pragma unroll
+      for (int e = 0; e < E; ++e) g[e] += class_at<T>(0, lane, lanes, e) == id ? d : 0.f;
+    }
+  }
+  const bool none = r.ls == -INFINITY;          // nothing is left of the row
+#pragma unroll
+  for (int u = 0; u < E / N; ++u) {
+    const int c = (lane + u * lanes) * N;
+    if (c >= b.classes) continue;
+    float d[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      d[e] = r.bad ? NAN : none ? 0.f : class_grad(r, v[u * N + e], g[u * N + e]);
+    Piece<T> p;
+    p.set(d);
+    p.store(dz + row * (size_t)b.ldz + c, b.classes - c);
+  }
+}
+
+// A stretch of a long row, one a wave.  Lane l < top has alternative l, lane `top` the
+// target: those in the stretch are read before the stretch is written (dz may be z)
+// and written again behind it.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void logp_stretch_bwd(LogpBwd b, const T* z, T* dz) {
+  constexpr int N = Piece<T>::N, E = P * N;
+  const int lane = threadIdx.x & 63;
+  const size_t unit = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const size_t row = unit / (unsigned)b.stretches;
+  if (row >= (size_t)b.m) return;
+  const int first = (int)(unit - row * b.stretches) * (E * 64);
+  const T* zr = z + row * (size_t)b.ldz;
+  T* out = dz + row * (size_t)b.ldz;
+  float v[E];
+  load_row<T, E>(zr, b.classes, first, lane, 64, v);
+  RowGrad r = row_grad(b, row);
+  const int tops = b.dtop ? b.top : 0;
+  int id = -1;
+  float g = 0.f;
+  if (lane < tops) g = top_grad(b, row, lane, id);
+  r.all += group_sum(g, 64);
+  if (lane == tops && !r.bad) {
+    id = r.target;
+    g = r.g;
+  }
+  const bool mine = id >= first && id < min(b.classes, first + E * 64);
+  const bool any = __ballot(mine) != 0;
+  float special = 0.f;
+  if (any) {
+    const float z0 = mine ? Elem<T>::load(zr, id) : 0.f;
+    float sum = 0.f;                            // of all that name this class
+    for (int k = 0; k <= tops; ++k) {
+      const float gk = __shfl(g, k, 64);
+      sum += __shfl(id, k, 64) == id ? gk : 0.f;
+    }
+    special = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum);
+  }
+#pragma unroll
+  for (int u = 0; u < P; ++u) {
+    const int c = first + (lane + u * 64) * N;
+    if (c >= b.classes) continue;
+    float d[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      d[e] = r.bad ? NAN : r.ls == -INFINITY ? 0.f : class_grad(r, v[u * N + e], 0.f);
+    Piece<T> p;
+    p.set(d);
+    p.store(out + c, b.classes - c);
+  }
+  if (any && !r.bad) {
+    __threadfence();                            // behind what this wave has just written there
+    if (mine) Elem<T>::store(out, id, special);
+  }
+}
+
+}  // namespace sb
+
+namespace {
+
+sb_status logp_check(const sb_token_logp_desc* d) {
+  if (!d || d->m < 0 || d->classes < 1 || d->ldz < d->classes || d->top < 0 ||
+      d->top > SB_LOGP_MAX_TOP || d->top > d->classes)
+    return SB_ERR_INVALID_ARG;
+  if ((d->dtype != SB_F32 && d->dtype != SB_BF16) || (d->flags & ~SB_TOP_PROBS))
+    return SB_ERR_INVALID_ARG;
+  if (d->classes > 1 << 20 || d->m >= 1 << 30) return SB_ERR_UNSUPPORTED;
+  return SB_OK;
+}
+
+// 16-byte pieces of a row that a lane holds, and stretches of a row: long stretches
+// where there are rows enough for four waves on each SIMD, short ones else.
+struct LogpPlan {
+  int pieces, stretches;
+};
+LogpPlan logp_plan(const sb_token_logp_desc* d) {
+  const int per = 64 * 16 / (int)sbh::dsize(d->dtype);
+  LogpPlan p{8, 0};
+  auto stretches = [&](int pieces) { return sb::cdiv(d->classes, per * pieces); };
+  while (p.pieces > 1 && (int64_t)d->m * stretches(p.pieces) < 4096 &&
+         stretches(p.pieces / 2) <= sb::kMaxStretches)
+    p.pieces /= 2;
+  p.stretches = stretches(p.pieces);
+  return p;
+}
+
+bool narrow(const sb_token_logp_desc* d) { return d->classes <= sb::kNarrow; }
+int narrow_shift(const sb_token_logp_desc* d) {
+  int s = 3;
+  while (sb::kNarrowElems << s < d->classes) ++s;
+  return s;
+}
+
+size_t logp_part_bytes(const sb_token_logp_desc* d, const LogpPlan& p) {
+  return sb::round_up((size_t)d->m * p.stretches * 3 * 4, 256);
+}
+
+bool off(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+
+template <typename T>
+sb_status logp_fwd(const sb_token_logp_desc* d, const sb::LogpFwd& b, const LogpPlan& p, const T* z,
+                   hipStream_t st) {
+  if (narrow(d)) {
+    const int shift = narrow_shift(d);
+    const size_t blocks = (((size_t)d->m << shift) + 255) / 256;
+    sb::logp_narrow_fwd<T><<<(unsigned)blocks, 256, 0, st>>>(b, shift, z);
+    return sbh::launch_status();
+  }
+  const size_t blocks = ((size_t)d->m * p.stretches + 3) / 4;
+  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
+  switch (p.pieces) {
+    case 8: sb::logp_stretch_fwd<T, 8><<<(unsigned)blocks, 256, 0, st>>>(b, z); break;
+    case 4: sb::logp_stretch_fwd<T, 4><<<(unsigned)blocks, 256, 0, st>>>(b, z); break;
+    case 2: sb::logp_stretch_fwd<T, 2><<<(unsigned)blocks, 256, 0, st>>>(b, z); break;
+    default: sb::logp_stretch_fwd<T, 1><<<(unsigned)blocks, 256, 0, st>>>(b, z); break;
+  }
+  sb::logp_join<T><<<(unsigned)sb::cdiv(d->m, 4), 256, 0, st>>>(b, z);
+  return sbh::launch_status();
+}
+
+template <typename T>
+sb_status logp_bwd(const sb_token_logp_desc* d, const sb::LogpBwd& b, const LogpPlan& p, const T* z,
+                   T* dz, hipStream_t st) {
+  if (narrow(d)) {
+    const int shift = narrow_shift(d);
+    const size_t blocks = (((size_t)d->m << shift) + 255) / 256;
+    sb::logp_narrow_bwd<T><<<(unsigned)blocks, 256, 0, st>>>(b, shift, z, dz);
+    return sbh::launch_status();
+  }
+  const size_t blocks = ((size_t)d->m * p.stretches + 3) / 4;
+  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
+  switch (p.pieces) {
+    case 8: sb::logp_stretch_bwd<T, 8><<<(unsigned)blocks, 256, 0, st>>>(b, z, dz); break;
+    case 4: sb::logp_stretch_bwd<T, 4><<<(unsigned)blocks, 256, 0, st>>>(b, z, dz); break;
+    case 2: sb::logp_stretch_bwd<T, 2><<<(unsigned)blocks, 256, 0, st>>>(b, z, dz); break;
+    default: sb::logp_stretch_bwd<T, 1><<<(unsigned)blocks, 256, 0, st>>>(b, z, dz); break;
+  }
+  return sbh::launch_status();
+}
+
+}  // namespace
+
+extern "C" size_t sb_token_logp_workspace_bytes(const sb_token_logp_desc* d) {
+  if (logp_check(d) != SB_OK) return (size_t)-1;
+  if (narrow(d) || d->m == 0) return 0;
+  const LogpPlan p = logp_plan(d);
+  return logp_part_bytes(d, p) + sb::round_up((size_t)d->m * p.stretches * d->top * 8, 256);
+}
+
+extern "C" sb_status sb_token_logp_fwd(const sb_token_logp_desc* d, const void* z,
+                                       const int32_t* targets, float* logp, float* entropy,
+                                       float* stats, int32_t* top_ids, float* top_values,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  const sb_status s = logp_check(d);
+  if (s != SB_OK) return s;
+  if (d->m == 0) return SB_OK;
+  const size_t e = sbh::dsize(d->dtype), m = (size_t)d->m;
+  if (!z || !stats || (logp && !targets) || (d->top > 0 && (!top_ids || !top_values)))
+    return SB_ERR_INVALID_ARG;
+  if (off(z, e) || off(targets, 4) || off(logp, 4) || off(entropy, 4) || off(stats, 4) ||
+      off(top_ids, 4) || off(top_values, 4) || off(workspace, 16))
+    return SB_ERR_INVALID_ARG;
+  const size_t need = sb_token_logp_workspace_bytes(d);
+  const size_t zb = ((m - 1) * d->ldz + d->classes) * e, tb = m * d->top * 4;
+  const void* outs[6] = {logp, entropy, stats, d->top ? top_ids : nullptr,
+                         d->top ? top_values : nullptr, workspace};
+  const size_t ob[6] = {m * 4, m * 4, m * 8, tb, tb, need};
+  for (int i = 0; i < 6; ++i) {
+    if (sbh::overlaps(outs[i], ob[i], z, zb) || sbh::overlaps(outs[i], ob[i], targets, m * 4))
+      return SB_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (sbh::overlaps(outs[i], ob[i], outs[j], ob[j])) return SB_ERR_INVALID_ARG;
+  }
+  if (need && (!workspace || workspace_bytes < need)) return SB_ERR_WORKSPACE;
+  const LogpPlan p = logp_plan(d);
+  sb::LogpFwd b{};
+  b.m = d->m;
+  b.classes = d->classes;
+  b.ldz = d->ldz;
+  b.top = d->top;
+  b.probs = (d->flags & SB_TOP_PROBS) != 0;
+  b.stretches = p.stretches;
+  b.targets = targets;
+  b.logp = logp;
+  b.entropy = entropy;
+  b.stats = stats;
+  b.top_ids = top_ids;
+  b.top_values = top_values;
+  b.part = (float*)workspace;
+  b.keys = (uint64_t*)((char*)workspace + logp_part_bytes(d, p));
+  if (d->dtype == SB_BF16)
+    return logp_fwd(d, b, p, (const sb::u16*)z, sbh::stream_of(stream));
+  return logp_fwd(d, b, p, (const float*)z, sbh::stream_of(stream));
+}
+
+extern "C" sb_status sb_token_logp_bwd(const sb_token_logp_desc* d, const void* z,
+                                       const float* stats, const int32_t* targets,
+                                       const float* dlogp, const float* entropy,
+                                       const float* dentropy, const int32_t* top_ids,
+                                       const float* top_values, const float* dtop, void* dz,
+                                       void* stream) {
+  const sb_status s = logp_check(d);
+  if (s != SB_OK) return s;
+  if (d->m == 0) return SB_OK;
+  const size_t e = sbh::dsize(d->dtype), m = (size_t)d->m;
+  if (!z || !stats || !dz || (dlogp && !targets) || (dentropy && !entropy) ||
+      (dtop && (d->top == 0 || !top_ids || ((d->flags & SB_TOP_PROBS) && !top_values))))
+    return SB_ERR_INVALID_ARG;
+  if (off(z, e) || off(dz, e) || off(stats, 4) || off(targets, 4) || off(dlogp, 4) ||
+      off(entropy, 4) || off(dentropy, 4) || off(top_ids, 4) || off(top_values, 4) || off(dtop, 4))
+    return SB_ERR_INVALID_ARG;
+  const size_t zb = ((m - 1) * d->ldz + d->classes) * e, tb = m * d->top * 4;
+  const void* ins[8] = {stats, targets, dlogp, entropy, dentropy, top_ids, top_values, dtop};
+  const size_t ib[8] = {m * 8, m * 4, m * 4, m * 4, m * 4, tb, tb, tb};
+  if (dz != z && sbh::overlaps(dz, zb, z, zb)) return SB_ERR_INVALID_ARG;
+  for (int i = 0; i < 8; ++i)
+    if (sbh::overlaps(dz, zb, ins[i], ib[i])) return SB_ERR_INVALID_ARG;
+  const LogpPlan p = logp_plan(d);
+  sb::LogpBwd b{};
+  b.m = d->m;
+  b.classes = d->classes;
+  b.ldz = d->ldz;
+  b.top = d->top;
+  b.probs = (d->flags & SB_TOP_PROBS) != 0;
+  b.stretches = p.stretches;
+  b.stats = stats;
+  b.entropy = entropy;
+  b.targets = targets;
+  b.dlogp = dlogp;
+  b.dentropy = dentropy;
+  b.top_ids = top_ids;
+  b.top_values = top_values;
+  b.dtop = dtop;
+  if (d->dtype == SB_BF16)
+    return logp_bwd(d, b, p, (const sb::u16*)z, (sb::u16*)dz, sbh::stream_of(stream));
+  return logp_bwd(d, b, p, (const float*)z, (float*)dz, sbh::stream_of(stream));
+}

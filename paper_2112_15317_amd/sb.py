@@ -25,12 +25,14 @@ SB_NCHW, SB_NCHW8C = 0, 1
 SB_FUSE_RELU = 1
 SB_PACKED_FILTERS = 2
 SB_UNALIGNED = 4
+SB_TOP_PROBS = 8
 SB_PASS_FWD, SB_PASS_BWD_DATA, SB_PASS_BWD_WEIGHT, SB_PASS_FWD_POOL = 0, 1, 2, 3
 SIZE_MAX = 2 ** 64 - 1          # (size_t)-1: the workspace queries' "not supported"
 SB_FC_FWD, SB_FC_BWD = 0, 1
 SB_ACT_SIGMOID, SB_ACT_SILU, SB_ACT_GELU, SB_ACT_GELU_TANH, SB_ACT_RELU = range(5)
 SB_SGD_MAX_TENSORS = 64
 SB_ADAMW_MAX_TENSORS, SB_ADAMW_BLOCK = 512, 256
+SB_MAX_EXPERTS, SB_LOGP_MAX_TOP = 512, 32
 SB_NOALLOC_SCRATCH_BYTES = 40 << 20
 
 _vp = ctypes.c_void_p
@@ -66,6 +68,21 @@ class sb_adamw_tensor(ctypes.Structure):
 class sb_gated_desc(ctypes.Structure):
     _fields_ = [("m", _i), ("k_in", _i), ("n_shard", _i), ("dtype", _i), ("act", _i),
                 ("ldx", _i), ("ldy", _i), ("flags", ctypes.c_uint)]
+
+
+class sb_embed_desc(ctypes.Structure):
+    _fields_ = [("tokens", _i), ("vocab", _i), ("width", _i), ("first", _i), ("dtype", _i),
+                ("ldy", _i), ("scale", ctypes.c_float)]
+
+
+class sb_expert_desc(ctypes.Structure):
+    _fields_ = [("tokens", _i), ("top", _i), ("experts", _i), ("first", _i), ("width", _i),
+                ("dtype", _i), ("ldx", _i), ("ldr", _i)]
+
+
+class sb_token_logp_desc(ctypes.Structure):
+    _fields_ = [("m", _i), ("classes", _i), ("ldz", _i), ("dtype", _i), ("top", _i),
+                ("flags", ctypes.c_uint)]
 
 
 class sb_modulo_desc(ctypes.Structure):
@@ -125,6 +142,20 @@ SIGNATURES = {
                              _vp]),
     "sb_adamw_advance": (_i, [_vp, _vp]),
     "sb_adamw_unpack": (_i, [_sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "sb_embed_workspace_bytes": (_sz, [ctypes.POINTER(sb_embed_desc)]),
+    "sb_embed_fwd": (_i, [ctypes.POINTER(sb_embed_desc), _vp, _vp, _vp, _vp]),
+    "sb_embed_bwd": (_i, [ctypes.POINTER(sb_embed_desc), _vp, _vp, _vp, _i, _vp, _sz, _vp]),
+    "sb_expert_workspace_bytes": (_sz, [ctypes.POINTER(sb_expert_desc)]),
+    "sb_expert_sort": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp, _sz, _vp]),
+    "sb_expert_gather": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp]),
+    "sb_expert_combine": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp, _vp]),
+    "sb_expert_combine_bwd": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp, _vp, _vp,
+                                   _vp]),
+    "sb_token_logp_workspace_bytes": (_sz, [ctypes.POINTER(sb_token_logp_desc)]),
+    "sb_token_logp_fwd": (_i, [ctypes.POINTER(sb_token_logp_desc), _vp, _vp, _vp, _vp, _vp, _vp,
+                               _vp, _vp, _sz, _vp]),
+    "sb_token_logp_bwd": (_i, [ctypes.POINTER(sb_token_logp_desc), _vp, _vp, _vp, _vp, _vp, _vp,
+                               _vp, _vp, _vp, _vp, _vp]),
 }
 
 _lock = threading.Lock()
@@ -609,3 +640,126 @@ def sb_adamw_unpack(n, m, m_top, v, v_top, m_out, v_out, stream=None):
     _check("sb_adamw_unpack", load().sb_adamw_unpack(
         int(n), _ptr(m), _ptr(m_top), _ptr(v), _ptr(v_top), _ptr(m_out), _ptr(v_out),
         _stream_for(m if m is not None else v if v is not None else 0, stream)))
+
+
+# -------------------------------------------------------------- embedding --
+def _typed(desc, **tensors):
+    """Tensors (not addresses) of a call have the descriptor's type."""
+    for name, t in tensors.items():
+        if t is not None and not isinstance(t, int) and _dtype_code(t) != desc.dtype:
+            raise ValueError("%s has another type than the descriptor" % name)
+
+
+def _kind(kind, **tensors):
+    for name, t in tensors.items():
+        if t is not None and not isinstance(t, int) and str(t.dtype) != "torch." + kind:
+            raise ValueError("%s is %s" % (name, kind))
+
+
+def embed_desc(tokens, vocab, width, dtype=SB_F32, first=0, ldy=None, scale=1.0):
+    """first: the id of the table's first row (a vocabulary shard's)."""
+    return sb_embed_desc(tokens, vocab, width, first, dtype, ldy or width, scale)
+
+
+def sb_embed_workspace_bytes(desc):
+    return load().sb_embed_workspace_bytes(ctypes.byref(desc))
+
+
+def sb_embed_fwd(desc, table, ids, y, stream=None):
+    """ids: int32."""
+    _typed(desc, table=table, y=y)
+    _kind("int32", ids=ids)
+    _check("sb_embed_fwd", load().sb_embed_fwd(
+        ctypes.byref(desc), _ptr(table), _ptr(ids), _ptr(y), _stream_for(table, stream)))
+
+
+def sb_embed_bwd(desc, ids, dy, dtable, accumulate=False, ws=None, stream=None):
+    """dtable: fp32 [vocab][width]."""
+    p, nb = _ws(ws)
+    _typed(desc, dy=dy)
+    _kind("int32", ids=ids)
+    _kind("float32", dtable=dtable)
+    _check("sb_embed_bwd", load().sb_embed_bwd(
+        ctypes.byref(desc), _ptr(ids), _ptr(dy), _ptr(dtable), 1 if accumulate else 0, p, nb,
+        _stream_for(dtable, stream)))
+
+
+# ------------------------------------------------------------ expert rows --
+def expert_desc(tokens, top, experts, width, dtype=SB_F32, first=0, ldx=None, ldr=None):
+    """first: the worker's first expert."""
+    return sb_expert_desc(tokens, top, experts, first, width, dtype, ldx or width, ldr or width)
+
+
+def sb_expert_workspace_bytes(desc):
+    return load().sb_expert_workspace_bytes(ctypes.byref(desc))
+
+
+def sb_expert_sort(desc, ids, place, offsets, ws=None, stream=None):
+    """All int32: ids and place [tokens][top], offsets [experts + 1]."""
+    p, nb = _ws(ws)
+    _kind("int32", ids=ids, place=place, offsets=offsets)
+    _check("sb_expert_sort", load().sb_expert_sort(
+        ctypes.byref(desc), _ptr(ids), _ptr(place), _ptr(offsets), p, nb,
+        _stream_for(offsets, stream)))
+
+
+def sb_expert_gather(desc, x, place, xs, stream=None):
+    _typed(desc, x=x, xs=xs)
+    _kind("int32", place=place)
+    _check("sb_expert_gather", load().sb_expert_gather(
+        ctypes.byref(desc), _ptr(x), _ptr(place), _ptr(xs), _stream_for(x, stream)))
+
+
+def sb_expert_combine(desc, ys, place, weights, y, stream=None):
+    """weights: fp32 [tokens][top], or None (1 each: the gather's backward)."""
+    _typed(desc, ys=ys, y=y)
+    _kind("int32", place=place)
+    _kind("float32", weights=weights)
+    _check("sb_expert_combine", load().sb_expert_combine(
+        ctypes.byref(desc), _ptr(ys), _ptr(place), _ptr(weights), _ptr(y),
+        _stream_for(y, stream)))
+
+
+def sb_expert_combine_bwd(desc, dy, ys, place, weights, dys, dweights=None, stream=None):
+    _typed(desc, dy=dy, ys=ys, dys=dys)
+    _kind("int32", place=place)
+    _kind("float32", weights=weights, dweights=dweights)
+    _check("sb_expert_combine_bwd", load().sb_expert_combine_bwd(
+        ctypes.byref(desc), _ptr(dy), _ptr(ys), _ptr(place), _ptr(weights), _ptr(dys),
+        _ptr(dweights), _stream_for(dy, stream)))
+
+
+# ------------------------------------------------- token log-probabilities --
+def token_logp_desc(m, classes, top=0, dtype=SB_F32, ldz=None, probs=False):
+    """probs: the alternatives' probabilities in place of their logarithms."""
+    return sb_token_logp_desc(m, classes, ldz or classes, dtype, top, SB_TOP_PROBS if probs else 0)
+
+
+def sb_token_logp_workspace_bytes(desc):
+    return load().sb_token_logp_workspace_bytes(ctypes.byref(desc))
+
+
+def sb_token_logp_fwd(desc, z, targets, logp, entropy, stats, top_ids=None, top_values=None,
+                      ws=None, stream=None):
+    """targets, top_ids: int32; logp, entropy, stats [m][2], top_values: fp32.
+    targets, logp and entropy may be None."""
+    p, nb = _ws(ws)
+    _typed(desc, z=z)
+    _kind("int32", targets=targets, top_ids=top_ids)
+    _kind("float32", logp=logp, entropy=entropy, stats=stats, top_values=top_values)
+    _check("sb_token_logp_fwd", load().sb_token_logp_fwd(
+        ctypes.byref(desc), _ptr(z), _ptr(targets), _ptr(logp), _ptr(entropy), _ptr(stats),
+        _ptr(top_ids), _ptr(top_values), p, nb, _stream_for(z, stream)))
+
+
+def sb_token_logp_bwd(desc, z, stats, targets, dlogp, entropy, dentropy, top_ids, top_values, dtop,
+                      dz, stream=None):
+    """dlogp, dentropy and dtop, and what they go with, may be None; dz may be z."""
+    _typed(desc, z=z, dz=dz)
+    _kind("int32", targets=targets, top_ids=top_ids)
+    _kind("float32", stats=stats, dlogp=dlogp, entropy=entropy, dentropy=dentropy,
+          top_values=top_values, dtop=dtop)
+    _check("sb_token_logp_bwd", load().sb_token_logp_bwd(
+        ctypes.byref(desc), _ptr(z), _ptr(stats), _ptr(targets), _ptr(dlogp), _ptr(entropy),
+        _ptr(dentropy), _ptr(top_ids), _ptr(top_values), _ptr(dtop), _ptr(dz),
+        _stream_for(z, stream)))
