@@ -29,7 +29,10 @@ constexpr int kTopList = 256;          // classes of a stretch that are ranked i
 constexpr int kMaxStretches = 512;     // of a row
 constexpr int kNarrow = 1024;          // classes of a row in one launch
 constexpr int kNarrowElems = 16;       // of a lane there
-constexpr float kLog2e = 1.44269504088896341f;
+template <typename T> constexpr int kNarrowPieces = kNarrowElems / Piece<T>::N;
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLeastPower = -1000.f; // of 2, in place of masked elements' -inf: 0 times it is 0
+constexpr float kLeastPlain = -1e30f;  // smaller maxima take the careful sums
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -48,21 +51,61 @@ __device__ __forceinline__ uint64_t key_of(uint32_t order, uint32_t cls) {
 }
 __device__ __forceinline__ uint32_t class_of(uint64_t key) { return ~(uint32_t)key; }
 
-__device__ __forceinline__ float group_max(float v, int lanes) {
-  for (int o = 1; o < lanes; o *= 2) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+// Reductions over a group of 8 to 64 lanes, which all get the result: within 16 lanes by
+// moves inside the vector unit, beyond by swapped halves; no LDS, a fixed order.
+template <int CTRL>
+__device__ __forceinline__ uint32_t lane_move(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
 }
-__device__ __forceinline__ float group_sum(float v, int lanes) {
-  for (int o = 1; o < lanes; o *= 2) v += __shfl_xor(v, o, 64);
-  return v;
+struct Both {
+  uint32_t a, b;
+};
+__device__ __forceinline__ Both swap16(uint32_t v) {
+  const auto t = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return Both{t[0], t[1]};
 }
-__device__ __forceinline__ uint64_t group_max(uint64_t v, int lanes) {
-  for (int o = 1; o < lanes; o *= 2) {
-    const uint64_t t = (uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, 64) << 32 |
-                       (uint32_t)__shfl_xor((int)v, o, 64);
-    v = t > v ? t : v;
+__device__ __forceinline__ Both swap32(uint32_t v) {
+  const auto t = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return Both{t[0], t[1]};
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+
+template <typename F>
+__device__ __forceinline__ uint32_t group_reduce(uint32_t v, int lanes, F f) {
+  v = f(v, lane_move<kXor1>(v));
+  v = f(v, lane_move<kXor2>(v));
+  v = f(v, lane_move<kMirror8>(v));
+  if (lanes > 8) v = f(v, lane_move<kMirror16>(v));
+  if (lanes > 16) {
+    const Both t = swap16(v);
+    v = f(t.a, t.b);
+  }
+  if (lanes > 32) {
+    const Both t = swap32(v);
+    v = f(t.a, t.b);
   }
   return v;
+}
+__device__ __forceinline__ float maximum(float a, float b) {   // NaN if one is
+  return __builtin_elementwise_maximum(a, b);
+}
+__device__ __forceinline__ float group_max(float v, int lanes) {
+  return __uint_as_float(group_reduce(__float_as_uint(v), lanes, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(maximum(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+__device__ __forceinline__ float group_sum(float v, int lanes) {
+  return __uint_as_float(group_reduce(__float_as_uint(v), lanes, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+__device__ __forceinline__ uint32_t group_max(uint32_t v, int lanes) {
+  return group_reduce(v, lanes, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+// The largest of 64-bit numbers: upper halves first, lower ones where those agree.
+__device__ __forceinline__ uint64_t group_max(uint64_t v, int lanes) {
+  const uint32_t hi = (uint32_t)(v >> 32), top = group_max(hi, lanes);
+  return (uint64_t)top << 32 | group_max(hi == top ? (uint32_t)v : 0u, lanes);
 }
 
 struct LogpFwd {
@@ -76,21 +119,23 @@ struct LogpFwd {
   uint64_t* keys;              // [m][stretches][top], in order, 0: none
 };
 
-// Sums of a lane's elements against the maximum mx of its row or stretch: o without
-// the elements that equal it (their number is added to `equal`), s of exp(t) t.
-// Masked elements (-inf) give nothing.  A NaN ends up in o.
-template <int E>
-__device__ __forceinline__ void lane_sums(const float* v, float mx, float& o, float& s,
+// Sums of a lane's elements against the maximum mx of its row or stretch, whatever they
+// are: o without the elements that equal it (their number is `equal`), s of
+// exp(t) t.  Masked elements (-inf) give nothing.  A NaN ends up in o.
+template <typename T, int P>
+__device__ __forceinline__ void lane_sums(const Piece<T>* p, float mx, float& o, float& s,
                                           int& equal) {
+  constexpr int N = Piece<T>::N;
   o = 0.f;
   s = 0.f;
   equal = 0;
   const float base = mx == -INFINITY ? 0.f : mx;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const float t = v[e] - base;
+  for (int e = 0; e < P * N; ++e) {
+    const float v = p[e / N].get(e % N);
+    const float t = v - base;
     const float x = exp2_hw(t * kLog2e);
-    const bool is_max = v[e] == mx;
+    const bool is_max = v == mx;
     equal += is_max ? 1 : 0;
     o += is_max ? 0.f : x;
     s += x > 0.f ? x * t : 0.f;
@@ -122,24 +167,35 @@ __device__ __forceinline__ float target_logp(const RowSums& r, const T* z, int t
   return row_logp(r, Elem<T>::load(z, target));
 }
 
-// E elements of a lane: pieces lane, lane + lanes, ... of the row from `first` on.
+// P pieces of a lane: pieces lane, lane + lanes, ... of the row from `first` on.
 // Elements past the row are -inf.
-template <typename T, int E>
+template <typename T> __device__ __forceinline__ uint32_t minus_inf();
+template <> __device__ __forceinline__ uint32_t minus_inf<float>() { return 0xff800000u; }
+template <> __device__ __forceinline__ uint32_t minus_inf<u16>() { return 0xff80ff80u; }
+
+template <typename T, int P>
 __device__ __forceinline__ void load_row(const T* row, int classes, int first, int lane, int lanes,
-                                         float* v) {
+                                         Piece<T>* p) {
   constexpr int N = Piece<T>::N;
-  Piece<T> p[E / N];
+  if (first + P * N * lanes <= classes) {
 #pragma unroll
-  for (int u = 0; u < E / N; ++u) {
-    const int c = first + (lane + u * lanes) * N;
-    p[u].raw = u4{0, 0, 0, 0};
-    if (c < classes) p[u].load(row + c, classes - c);
+    for (int u = 0; u < P; ++u) p[u].load(row + first + (lane + u * lanes) * N, N);
+    return;
   }
 #pragma unroll
-  for (int u = 0; u < E / N; ++u) {
-    const int c = first + (lane + u * lanes) * N;
+  for (int u = 0; u < P; ++u) {
+    const int left = classes - (first + (lane + u * lanes) * N);
+    const uint32_t none = minus_inf<T>();
+    p[u].raw = u4{none, none, none, none};
+    if (left >= N) {
+      p[u].load(row + classes - left, N);
+    } else if (left > 0) {
+      float v[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[u * N + e] = c + e < classes ? p[u].get(e) : -INFINITY;
+      for (int e = 0; e < N; ++e)
+        v[e] = e < left ? Elem<T>::load(row, classes - left + e) : -INFINITY;
+      p[u].set(v);
+    }
   }
 }
 template <typename T>
@@ -152,21 +208,23 @@ __device__ __forceinline__ int class_at(int first, int lane, int lanes, int e) {
 template <typename T>
 __global__ __launch_bounds__(256) void logp_narrow_fwd(LogpFwd b, int shift,
                                                        const T* __restrict__ z) {
-  constexpr int E = kNarrowElems;
+  constexpr int N = Piece<T>::N, P = kNarrowPieces<T>, E = P * N;
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
   const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> shift;
   if (row >= (size_t)b.m) return;             // whole groups leave together
   const T* zr = z + row * (size_t)b.ldz;
+  Piece<T> p[P];
+  load_row<T, P>(zr, b.classes, 0, lane, lanes, p);
   float v[E];
-  load_row<T, E>(zr, b.classes, 0, lane, lanes, v);
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = p[e / N].get(e % N);
   float mx = v[0];
 #pragma unroll
-  for (int e = 1; e < E; ++e) mx = fmaxf(mx, v[e]);
-  if (mx != mx) mx = -INFINITY;
+  for (int e = 1; e < E; ++e) mx = maximum(mx, v[e]);
   mx = group_max(mx, lanes);
   float o, s;
   int equal;
-  lane_sums<E>(v, mx, o, s, equal);
+  lane_sums<T, P>(p, mx, o, s, equal);
   o = group_sum(o, lanes);
   s = group_sum(s, lanes);
   const float others = group_sum((float)equal, lanes) - 1.f;
@@ -183,80 +241,99 @@ __global__ __launch_bounds__(256) void logp_narrow_fwd(LogpFwd b, int shift,
 #pragma unroll
   for (int e = 0; e < E; ++e)
     order[e] = class_at<T>(0, lane, lanes, e) < b.classes ? order_of(v[e]) : 0;
+  uint64_t kept = 0;                          // by lane j: the best class j of those at hand
   for (int k = 0; k < b.top; ++k) {
-    uint32_t best = 0;
+    uint32_t best = order[0];
 #pragma unroll
-    for (int e = 0; e < E; ++e) best = max(best, order[e]);
+    for (int e = 1; e < E; ++e) best = max(best, order[e]);
     int at = 0;                               // the first of them: classes grow with e
 #pragma unroll
     for (int e = E - 1; e >= 0; --e) at = order[e] == best ? e : at;
     const uint64_t key = best ? key_of(best, class_at<T>(0, lane, lanes, at)) : 0;
     const uint64_t most = group_max(key, lanes);
+    const int gone = key == most ? at : -1;
 #pragma unroll
-    for (int e = 0; e < E; ++e) order[e] = key == most && e == at ? 0 : order[e];
-    if (lane == 0) {
-      const float lp = row_logp(r, value_of((uint32_t)(most >> 32)));
-      b.top_ids[row * b.top + k] = (int32_t)class_of(most);
-      b.top_values[row * b.top + k] = b.probs ? expf(lp) : lp;
+    for (int e = 0; e < E; ++e) order[e] = e == gone ? 0 : order[e];
+    const int j = k & (lanes - 1);
+    if (lane == j) kept = most;
+    if (j != lanes - 1 && k != b.top - 1) continue;
+    if (lane <= j) {
+      const size_t to = row * b.top + k - j + lane;
+      const float lp = row_logp(r, value_of((uint32_t)(kept >> 32)));
+      b.top_ids[to] = (int32_t)class_of(kept);
+      b.top_values[to] = b.probs ? expf(lp) : lp;
     }
   }
 }
 
 // ---------------------------------------------------------------- long rows --
-// The k-th largest (k >= 1) of the 64 lanes' numbers.
+// A bound that at least k (>= 1) of the 64 lanes' numbers reach, and few more: the k-th
+// largest of their upper halves.
 __device__ __forceinline__ uint32_t wave_kth(uint32_t v, int k) {
   uint32_t got = 0;
-  for (int b = 31; b >= 0; --b) {
+#pragma unroll
+  for (int b = 31; b >= 16; --b) {
     const uint32_t t = got | 1u << b;
     if (__popcll(__ballot(v >= t)) >= k) got = t;
   }
   return got;
 }
 
-template <typename T, int E>
-__device__ __forceinline__ void stretch_top(const LogpFwd& b, const float* v, int first, int lane,
-                                            bool odd, uint64_t* list, uint64_t* out) {
-  uint32_t best = 0;
+// The best `top` of `count` <= kTopList different keys in LDS, in order; `give` gets each
+// rank and key.  One wave.
+template <typename F>
+__device__ __forceinline__ void rank_list(const uint64_t* list, int count, int top, int lane,
+                                          F give) {
+  for (int i = lane; i < count; i += 64) {
+    const uint64_t mine = list[i];
+    int rank = 0;
+    for (int j = 0; j < count; ++j) rank += list[j] > mine ? 1 : 0;
+    if (rank < top) give(rank, mine);
+  }
+}
+
+// best: the largest of each of the lane's pieces; lm: of the lane.
+template <typename T, int P>
+__device__ __forceinline__ void stretch_top(const LogpFwd& b, const T* row, const Piece<T>* p,
+                                            const float* best, float lm, bool plain, int first,
+                                            int lane, uint64_t* list, uint64_t* out) {
+  constexpr int N = Piece<T>::N;
   int count = kTopList + 1;
-  if (!odd) {
-    float most = v[0];
+  if (plain) {
+    const uint32_t bound = wave_kth(order_of(lm), b.top);
+    const float least = value_of(bound);      // (upper halves above -inf's are no NaN's)
+    if (least > -INFINITY) {
+      count = 0;
 #pragma unroll
-    for (int e = 1; e < E; ++e) most = fmaxf(most, v[e]);
-    best = class_at<T>(first, lane, 64, 0) < b.classes ? order_of(most) : 0;
-    const uint32_t bound = wave_kth(best, b.top);
-    const float least = bound ? value_of(bound) : -INFINITY;
-    count = 0;
+      for (int u = 0; u < P; ++u) {
+        if (!__ballot(best[u] >= least)) continue;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const bool in = v[e] >= least && class_at<T>(first, lane, 64, e) < b.classes;
-      const uint64_t mask = __ballot(in);
-      if (mask) {
-        const int at = count + __popcll(mask & ((1ull << lane) - 1));
-        if (in && at < kTopList)
-          list[at] = key_of(order_of(v[e]), class_at<T>(first, lane, 64, e));
-        count += __popcll(mask);
+        for (int e = 0; e < N; ++e) {
+          const float v = p[u].get(e);
+          const uint64_t mask = __ballot(v >= least);
+          if (!mask) continue;
+          const int at = count + __popcll(mask & ((1ull << lane) - 1));
+          if (v >= least && at < kTopList)
+            list[at] = key_of(order_of(v), class_at<T>(first, lane, 64, u * N + e));
+          count += __popcll(mask);
+        }
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
   if (count <= kTopList) {
-    for (int i = lane; i < count; i += 64) {
-      const uint64_t mine = list[i];
-      int rank = 0;
-      for (int j = 0; j < count; ++j) rank += list[j] > mine ? 1 : 0;
-      if (rank < b.top) out[rank] = mine;
-    }
-    for (int k = count + lane; k < b.top; k += 64) out[k] = 0;
+    rank_list(list, count, b.top, lane, [&](int rank, uint64_t key) { out[rank] = key; });
     return;
   }
   uint64_t last = ~0ull;
+#pragma unroll 1
   for (int k = 0; k < b.top; ++k) {
     uint64_t most = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int c = class_at<T>(first, lane, 64, e);
-      const uint64_t key = c < b.classes ? key_of(order_of(v[e]), c) : 0;
+    const int end = min(b.classes, first + P * N * 64);
+#pragma unroll 1
+    for (int c = first + lane; c < end; c += 64) {
+      const uint64_t key = key_of(order_of(Elem<T>::load(row, c)), c);
       if (key < last && key > most) most = key;
     }
     last = group_max(most, 64);
@@ -264,65 +341,131 @@ __device__ __forceinline__ void stretch_top(const LogpFwd& b, const float* v, in
   }
 }
 
+// Sums of a stretch without its largest element, for a maximum that is an ordinary
+// number.  Powers of 2: exp(z - M) = 2^(z log2 e - c) * fix, c = M log2 e rounded and
+// fix its error's power, so that an element costs one fused product.  Every lane sums all
+// it has; the first lane that has the maximum does not count, and its elements are summed
+// by all lanes once more, without the maximum.
+template <typename T, int P>
+__device__ __forceinline__ void stretch_sums(const Piece<T>* p, float mx, float lm, int lane,
+                                             u4* share, float& o, float& s) {
+  constexpr int N = Piece<T>::N, E = P * N;
+  const float c = mx * kLog2e, err = fmaf(mx, kLog2e, -c);
+  float sx = 0.f, sy = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float y = fmaxf(fmaf(p[e / N].get(e % N), kLog2e, -c), kLeastPower);
+    const float x = exp2_hw(y);
+    sx += x;
+    sy = fmaf(x, y, sy);
+  }
+  const int leader = __ffsll((unsigned long long)__ballot(lm == mx)) - 1;
+  if (lane == leader) {
+#pragma unroll
+    for (int u = 0; u < P; ++u) share[u] = p[u].raw;
+    sx = sy = 0.f;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const float v = lane < E ? Elem<T>::load(reinterpret_cast<const T*>(share), lane) : -INFINITY;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (lane != __ffsll((unsigned long long)__ballot(v == mx)) - 1) {
+    const float y = fmaxf(fmaf(v, kLog2e, -c), kLeastPower);
+    const float x = exp2_hw(y);
+    sx += x;
+    sy = fmaf(x, y, sy);
+  }
+  sx = group_sum(sx, 64);
+  sy = group_sum(sy, 64);
+  const float fix = exp2_hw(-err);
+  o = sx * fix;
+  s = kLn2 * (fix * fmaf(-err, sx, sy));
+}
+
 template <typename T, int P>
 __global__ __launch_bounds__(256) void logp_stretch_fwd(LogpFwd b, const T* __restrict__ z) {
-  constexpr int E = P * Piece<T>::N;
+  constexpr int N = Piece<T>::N, E = P * N;
   __shared__ uint64_t list[4][kTopList];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const size_t unit = (size_t)blockIdx.x * 4 + wave;
   const size_t row = unit / (unsigned)b.stretches;
   if (row >= (size_t)b.m) return;
   const int first = (int)(unit - row * b.stretches) * (E * 64);
-  float v[E];
-  load_row<T, E>(z + row * (size_t)b.ldz, b.classes, first, lane, 64, v);
-  float mx = v[0];
+  const T* zr = z + row * (size_t)b.ldz;
+  Piece<T> p[P];
+  load_row<T, P>(zr, b.classes, first, lane, 64, p);
+  float best[P], lm = 0.f;
 #pragma unroll
-  for (int e = 1; e < E; ++e) mx = fmaxf(mx, v[e]);
-  if (mx != mx) mx = -INFINITY;
-  mx = group_max(mx, 64);
-  float o, s;
-  int equal;
-  lane_sums<E>(v, mx, o, s, equal);
-  o = group_sum(o, 64);
-  s = group_sum(s, 64);
-  const float others = group_sum((float)equal, 64) - 1.f;
-  if (mx != -INFINITY) o += others;
-  if (lane == 0) {
-    float* p = b.part + unit * 3;
-    p[0] = mx;
-    p[1] = o;
-    p[2] = s;
+  for (int u = 0; u < P; ++u) {
+    best[u] = p[u].get(0);
+#pragma unroll
+    for (int e = 1; e < N; ++e) best[u] = maximum(best[u], p[u].get(e));
+    lm = u ? maximum(lm, best[u]) : best[u];
+    // (Unpacked again for the sums: kept as fp32 they would cost half of the waves.)
+    asm volatile("" : "+v"(p[u].raw));
   }
-  if (b.top) stretch_top<T, E>(b, v, first, lane, o != o, list[wave], b.keys + unit * b.top);
+  const float mx = group_max(lm, 64);
+  const bool plain = mx > kLeastPlain && mx < INFINITY;    // not where a NaN is
+  float o, s;
+  if (plain) {
+    stretch_sums<T, P>(p, mx, lm, lane, reinterpret_cast<u4*>(list[wave]), o, s);
+  } else {
+    int equal;
+    lane_sums<T, P>(p, mx, o, s, equal);
+    o = group_sum(o, 64);
+    s = group_sum(s, 64);
+    const float others = group_sum((float)equal, 64) - 1.f;
+    if (mx != -INFINITY) o += others;
+  }
+  if (lane == 0) {
+    float* q = b.part + unit * 3;
+    q[0] = mx;
+    q[1] = o;
+    q[2] = s;
+  }
+  if (b.top)
+    stretch_top<T, P>(b, zr, p, best, lm, plain, first, lane, list[wave], b.keys + unit * b.top);
 }
 
-// One wave joins a row's stretches.
+// Outputs of one of a row's best classes.
+__device__ __forceinline__ void give_top(const LogpFwd& b, const RowSums& r, size_t row, int rank,
+                                         uint64_t key) {
+  const float lp = row_logp(r, value_of((uint32_t)(key >> 32)));
+  b.top_ids[row * b.top + rank] = (int32_t)class_of(key);
+  b.top_values[row * b.top + rank] = b.probs ? expf(lp) : lp;
+}
+
+// One wave joins a row's stretches.  A stretch's list is in order: with d = `depth` and q
+// lists of which the d-th entry reaches a bound, q d classes do.
 template <typename T>
 __global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict__ z) {
-  const int lane = threadIdx.x & 63;
-  const size_t row = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ uint64_t all_lists[4][kTopList];
+  __shared__ int counts[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const size_t row = (size_t)blockIdx.x * 4 + wave;
   if (row >= (size_t)b.m) return;
   const float* part = b.part + row * b.stretches * 3;
+  const uint64_t* keys = b.keys + row * b.stretches * b.top;
+  const int lists = min(b.stretches, 64);
+  const int depth = min(b.top, max(1, (2 * b.top + lists - 1) / lists));
+  uint64_t deep = 0;                            // the best d-th entry of the lane's lists
+  if (b.top)
+    for (int p = lane; p < b.stretches; p += 64) deep = max(deep, keys[(size_t)p * b.top + depth - 1]);
+  if (lane == 0) counts[wave] = 0;
   float mx = -INFINITY;
-  int who = INT32_MAX;                          // the first stretch that has it
-  for (int p = lane; p < b.stretches; p += 64) {
-    if (part[p * 3] > mx || who == INT32_MAX) {
-      mx = part[p * 3];
-      who = p;
-    }
-  }
+  for (int p = lane; p < b.stretches; p += 64) mx = maximum(mx, part[p * 3]);
   const float all = group_max(mx, 64);
-  who = mx == all ? who : INT32_MAX;
-  for (int q = 1; q < 64; q *= 2) who = min(who, __shfl_xor(who, q, 64));
+  uint32_t who = ~0u;                           // (negated) the first stretch that has it
+  for (int p = lane; p < b.stretches; p += 64)
+    if (part[p * 3] == all && who == ~0u) who = p;
+  who = ~group_max(~who, 64);
   float o = 0.f, s = 0.f;
   for (int p = lane; p < b.stretches; p += 64) {
     const float pm = part[p * 3], po = part[p * 3 + 1], ps = part[p * 3 + 2];
-    if (pm == -INFINITY) {                      // nothing, or NaNs
-      o += po != po ? NAN : 0.f;
-      continue;
-    }
+    if (pm == -INFINITY) continue;              // nothing
     const float t = pm - all, f = exp2_hw(t * kLog2e);
-    o += p == who ? po : f * (1.f + po);
+    o += (uint32_t)p == who ? po : f * (1.f + po);
     s += f > 0.f ? f * (ps + t * (1.f + po)) : 0.f;
   }
   o = group_sum(o, 64);
@@ -337,8 +480,26 @@ __global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict_
                                 b.classes);
   }
   if (!b.top) return;
-  // The stretches' lists are in order: the best of a lane's heads, again and again.
-  const uint64_t* keys = b.keys + row * b.stretches * b.top;
+  uint64_t* list = all_lists[wave];
+  const uint32_t bound = wave_kth((uint32_t)(deep >> 32), (b.top + depth - 1) / depth);
+  for (int p = lane; p < b.stretches; p += 64) {
+    for (int at = 0; at < b.top; ++at) {
+      const uint64_t key = keys[(size_t)p * b.top + at];
+      if (key == 0 || (uint32_t)(key >> 32) < bound) break;
+      // (Their order in the list does not matter: every one is ranked.)
+      const int to = atomicAdd(&counts[wave], 1);
+      if (to < kTopList) list[to] = key;
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int count = counts[wave];
+  if (count <= kTopList) {
+    rank_list(list, count, b.top, lane,
+              [&](int rank, uint64_t key) { give_top(b, r, row, rank, key); });
+    return;
+  }
+  // Many equal ones: the best of a lane's heads, again and again.
   uint64_t heads = 0;                           // 8 bits for each of a lane's (at most 8) lists
   for (int k = 0; k < b.top; ++k) {
     uint64_t best = 0;
@@ -353,11 +514,7 @@ __global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict_
     }
     const uint64_t most = group_max(best, 64);
     if (best == most && most) heads += 1ull << (8 * from);
-    if (lane == 0) {
-      const float lp = row_logp(r, value_of((uint32_t)(most >> 32)));
-      b.top_ids[row * b.top + k] = (int32_t)class_of(most);
-      b.top_values[row * b.top + k] = b.probs ? expf(lp) : lp;
-    }
+    if (lane == 0) give_top(b, r, row, k, most);
   }
 }
 
@@ -408,39 +565,69 @@ __device__ __forceinline__ float class_grad(const RowGrad& r, float z, float g) 
   return (g != 0.f ? -g * expm1f(lp) : 0.f) - d;
 }
 
+// The same for classes without a gradient of their own, in rows of an ordinary M and
+// log S, as one fused product each for log p and what multiplies p: in powers of 2, with
+// c = (M + log S) log2 e rounded and its error in the factors.
+struct PlainGrad {
+  float c, a, b;               // dz = -2^y (a + b y), y = z log2 e - c
+  __device__ __forceinline__ explicit PlainGrad(const RowGrad& r) {
+#pragma clang fp contract(off)
+    const float hi = r.mx * kLog2e, lo = fmaf(r.mx, kLog2e, -hi), l = r.ls * kLog2e;
+    c = hi + l;
+    const float back = c - hi;
+    const float err = ((hi - (c - back)) + (l - back)) + lo;       // what c lacks
+    const float fix = exp2_hw(-err);
+    b = fix * (kLn2 * r.dh);
+    a = fmaf(-err, b, fix * r.all);
+  }
+  __device__ __forceinline__ float operator()(float z) const {
+    const float y = fmaxf(fmaf(z, kLog2e, -c), kLeastPower);
+    return -exp2_hw(y) * fmaf(b, y, a);
+  }
+};
+
 template <typename T>
 __global__ __launch_bounds__(256) void logp_narrow_bwd(LogpBwd b, int shift, const T* z, T* dz) {
-  constexpr int E = kNarrowElems, N = Piece<T>::N;
+  constexpr int N = Piece<T>::N, P = kNarrowPieces<T>, E = P * N, AHEAD = 8;
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
   const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> shift;
   if (row >= (size_t)b.m) return;
   const T* zr = z + row * (size_t)b.ldz;
-  float v[E], g[E];
-  load_row<T, E>(zr, b.classes, 0, lane, lanes, v);
+  Piece<T> p[P];
+  float g[E];
+  load_row<T, P>(zr, b.classes, 0, lane, lanes, p);
   RowGrad r = row_grad(b, row);
 #pragma unroll
   for (int e = 0; e < E; ++e) g[e] = class_at<T>(0, lane, lanes, e) == r.target ? r.g : 0.f;
-  if (b.dtop) {
-    for (int k = 0; k < b.top; ++k) {
-      int id;
-      const float d = top_grad(b, row, k, id);
-      r.all += d;
+  const int tops = b.dtop ? b.top : 0;
+  for (int k0 = 0; k0 < tops; k0 += AHEAD) {
+    int id[AHEAD];
+    float d[AHEAD];
 #pragma unroll
-      for (int e = 0; e < E; ++e) g[e] += class_at<T>(0, lane, lanes, e) == id ? d : 0.f;
+    for (int k = 0; k < AHEAD; ++k) {
+      id[k] = -1;
+      d[k] = k0 + k < tops ? top_grad(b, row, k0 + k, id[k]) : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (k0 + k >= tops) break;
+      r.all += d[k];
+#pragma unroll
+      for (int e = 0; e < E; ++e) g[e] += class_at<T>(0, lane, lanes, e) == id[k] ? d[k] : 0.f;
     }
   }
   const bool none = r.ls == -INFINITY;          // nothing is left of the row
 #pragma unroll
-  for (int u = 0; u < E / N; ++u) {
+  for (int u = 0; u < P; ++u) {
     const int c = (lane + u * lanes) * N;
     if (c >= b.classes) continue;
     float d[N];
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      d[e] = r.bad ? NAN : none ? 0.f : class_grad(r, v[u * N + e], g[u * N + e]);
-    Piece<T> p;
-    p.set(d);
-    p.store(dz + row * (size_t)b.ldz + c, b.classes - c);
+      d[e] = r.bad ? NAN : none ? 0.f : class_grad(r, p[u].get(e), g[u * N + e]);
+    Piece<T> q;
+    q.set(d);
+    q.store(dz + row * (size_t)b.ldz + c, b.classes - c);
   }
 }
 
@@ -457,8 +644,8 @@ __global__ __launch_bounds__(256) void logp_stretch_bwd(LogpBwd b, const T* z, T
   const int first = (int)(unit - row * b.stretches) * (E * 64);
   const T* zr = z + row * (size_t)b.ldz;
   T* out = dz + row * (size_t)b.ldz;
-  float v[E];
-  load_row<T, E>(zr, b.classes, first, lane, 64, v);
+  Piece<T> p[P];
+  load_row<T, P>(zr, b.classes, first, lane, 64, p);
   RowGrad r = row_grad(b, row);
   const int tops = b.dtop ? b.top : 0;
   int id = -1;
@@ -481,20 +668,27 @@ __global__ __launch_bounds__(256) void logp_stretch_bwd(LogpBwd b, const T* z, T
     }
     special = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum);
   }
+  const bool plain = fabsf(r.mx) < -kLeastPlain && r.ls == r.ls && !r.bad;
+  const PlainGrad grad(r);
 #pragma unroll
   for (int u = 0; u < P; ++u) {
     const int c = first + (lane + u * 64) * N;
-    if (c >= b.classes) continue;
     float d[N];
+    if (plain) {
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      d[e] = r.bad ? NAN : r.ls == -INFINITY ? 0.f : class_grad(r, v[u * N + e], 0.f);
-    Piece<T> p;
-    p.set(d);
-    p.store(out + c, b.classes - c);
+      for (int e = 0; e < N; ++e) d[e] = grad(p[u].get(e));
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        d[e] = r.bad ? NAN : r.ls == -INFINITY ? 0.f : class_grad(r, p[u].get(e), 0.f);
+    }
+    Piece<T> q;
+    q.set(d);
+    if (c < b.classes) q.store(out + c, b.classes - c);
   }
   if (any && !r.bad) {
-    __threadfence();                            // behind what this wave has just written there
+    // Behind what this wave has just written there.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (mine) Elem<T>::store(out, id, special);
   }
 }
