@@ -12,7 +12,9 @@
 // work is split by sorted tokens, not by rows of the table: a group takes kRun
 // tokens in a row; an id's tokens that go past a group's end leave partial sums
 // (fp32, at most two a group), which a last launch joins in order.  Rows without a
-// token are zeroed beside the sort.
+// token are zeroed beside the sort where that is one launch (and every row is), beside
+// the sums else: 65536 tokens of a table of 131072 x 2048 name a quarter of its rows, and
+// zeroing these too would be a sixth of all traffic.
 #include "rows.hpp"
 #include "slot_sort.hpp"
 
@@ -62,16 +64,70 @@ struct EmbedBwd {
   const uint2* slots;          // key, token, sorted; key `vocab`: not the shard's
   int n, vocab, width, ldy;
   int run, runs;               // sorted tokens of a group; groups along them
+  int sum_blocks;
   float scale;
   int accumulate;
   float* dtable;
   float* part;                 // [runs][2][width]: of an id that began before, of one that goes on
 };
 
-// Sums of one group's tokens, N columns a lane.
+// Where keys of at least `key` start among the slots from lo on: 64 probes at a time, one
+// wave.
+__device__ __forceinline__ int slot_from(const EmbedBwd& b, uint32_t key, int lo, int lane) {
+  int hi = b.n;                                     // somewhere in lo .. hi
+  while (lo < hi) {
+    const int step = (hi - lo + 63) / 64, j = lo + lane * step;
+    const int below = __popcll(__ballot(j < hi && b.slots[j].x < key));
+    if (below == 0) return lo;
+    const int last = lo + (below - 1) * step;       // below the key
+    hi = min(hi, last + step);
+    lo = last + 1;
+  }
+  return lo;
+}
+
+// Zeros in those of the kAbsent rows from v0 on that have no token; one wave.
+constexpr int kAbsent = 64;
+__device__ __forceinline__ void fill_absent(const EmbedBwd& b, int v0, int lane) {
+  const int v1 = min(b.vocab, v0 + kAbsent);
+  uint32_t lo = 0, hi = 0;                          // a bit for each row with a token
+  for (int j = slot_from(b, v0, 0, lane); j < b.n;) {
+    const uint32_t key = j + lane < b.n ? b.slots[j + lane].x : ~0u;
+    const uint32_t at = key - v0;
+    uint32_t l = at < 32 ? 1u << at : 0, h = at - 32 < 32 ? 1u << (at - 32) : 0;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      l |= __shfl_xor((int)l, o, 64);
+      h |= __shfl_xor((int)h, o, 64);
+    }
+    lo |= l;
+    hi |= h;
+    const uint32_t first = __shfl((int)key, 0, 64), last = __shfl((int)key, 63, 64);
+    if (last >= (uint32_t)v1) break;
+    j = first == last ? slot_from(b, first + 1, j + 64, lane) : j + 64;
+  }
+  const int pieces = cdiv(b.width, 4);
+  const int shift = pieces >= 64 ? 6 : 32 - __clz((pieces - 1) | 1);    // lanes of a row
+  for (int v = v0 + (lane >> shift); v < v1; v += 64 >> shift) {
+    const int at = v - v0;
+    if ((at < 32 ? lo >> at : hi >> (at - 32)) & 1) continue;
+    for (int c = lane & ((1 << shift) - 1); c < pieces; c += 1 << shift) {
+      Piece<float> p;
+      p.raw = u4{0, 0, 0, 0};
+      p.store(b.dtable + (size_t)v * b.width + c * 4, b.width - c * 4);
+    }
+  }
+}
+
+// Sums of one group's tokens, N columns a lane; the blocks behind these zero rows.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __restrict__ dy) {
   constexpr int N = Piece<T>::N, AHEAD = 8;
+  if (blockIdx.x >= (unsigned)b.sum_blocks) {
+    const int64_t v0 = ((int64_t)(blockIdx.x - b.sum_blocks) * 4 + (threadIdx.x >> 6)) * kAbsent;
+    if (v0 < b.vocab) fill_absent(b, (int)v0, threadIdx.x & 63);
+    return;
+  }
   const size_t group = ((size_t)blockIdx.x * 256 + threadIdx.x) >> b.rp.shift;
   const int lane = threadIdx.x & ((1 << b.rp.shift) - 1);
   const size_t g = group / (unsigned)b.rp.segs;
@@ -87,12 +143,16 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __r
   float acc[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
-  key = b.slots[j0].x;
+  uint2 s[AHEAD], ahead[AHEAD];
+#pragma unroll
+  for (int a = 0; a < AHEAD; ++a) ahead[a] = b.slots[min(j0 + a, j1 - 1)];
+  key = ahead[0].x;
   for (int j = j0; j < j1; j += AHEAD) {
-    uint2 s[AHEAD];
     Piece<T> p[AHEAD];
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) s[a] = b.slots[min(j + a, j1 - 1)];
+    for (int a = 0; a < AHEAD; ++a) s[a] = ahead[a];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) ahead[a] = b.slots[min(j + AHEAD + a, j1 - 1)];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       p[a].raw = u4{0, 0, 0, 0};
@@ -105,7 +165,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __r
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] += p[a].get(e);
       const bool last = j + a + 1 >= j1;
-      const uint32_t next = last ? behind : a + 1 < AHEAD ? s[(a + 1) % AHEAD].x : b.slots[j + a + 1].x;
+      const uint32_t next = last ? behind : a + 1 < AHEAD ? s[(a + 1) % AHEAD].x : ahead[0].x;
       if (next == key && !last) continue;
       const bool on = next == key;                  // goes on in the next group
       const bool whole = !head && !on;
@@ -130,29 +190,58 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __r
   }
 }
 
-// Joins the partial sums of an id whose tokens began in group g and go on behind it.
+// Joins the partial sums of an id whose tokens began in group g and go on behind it: a
+// block has 256 columns, each of its waves a quarter of the partial sums.
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd b) {
+  __shared__ f4 quarter[3][64];
   const int g = blockIdx.x;
-  const int c = blockIdx.y * 256 + threadIdx.x;
-  const int j1 = (g + 1) * b.run;                   // a group lies behind
-  const uint32_t key = b.slots[j1 - 1].x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int j0 = g * b.run, j1 = j0 + b.run;        // a group lies behind
+  const uint32_t key = b.slots[j1 - 1].x, first = b.slots[j0].x;
+  const uint32_t before = g > 0 ? b.slots[j0 - 1].x : ~0u;
   if (key == (uint32_t)b.vocab || b.slots[j1].x != key) return;
-  // Where it began: the head of group g is of another id, or nothing was before.
-  const int j0 = g * b.run;
-  if (b.slots[j0].x == key && g > 0 && b.slots[j0 - 1].x == key) return;
-  int lo = j1, hi = b.n;                            // the first slot behind the id's
-  while (lo < hi) {
-    const int mid = lo + (hi - lo) / 2;
-    if (b.slots[mid].x == key) lo = mid + 1;
-    else hi = mid;
+  if (first == key && before == key) return;        // it began in an earlier group
+  int end = g + 1;                                  // behind the last group that begins with it
+  for (;;) {
+    const int64_t j = (int64_t)(end + lane) * b.run;
+    const uint64_t other = ~__ballot(j < b.n && b.slots[j].x == key);
+    if (other) {
+      end += __ffsll((unsigned long long)other) - 1;
+      break;
+    }
+    end += 64;
   }
-  const int end = (lo - 1) / b.run;                 // its last group
-  if (c >= b.width) return;
-  float v = b.part[((size_t)g * 2 + 1) * b.width + c];
+  const int c = (blockIdx.y * 64 + lane) * 4, left = b.width - c;
+  const int each = (end - g - 1 + 3) / 4;
+  const int h0 = g + 1 + wave * each, h1 = min(end, h0 + each);
+  f4 v = f4{0.f, 0.f, 0.f, 0.f};
+  if (left > 0) {
 #pragma unroll 8
-  for (int h = g + 1; h <= end; ++h) v += b.part[(size_t)h * 2 * b.width + c];
+    for (int h = h0; h < h1; ++h) {
+      Piece<float> p;
+      p.load(b.part + (size_t)h * 2 * b.width + c, left);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += p.get(e);
+    }
+  }
+  if (wave) quarter[wave - 1][lane] = v;
+  __syncthreads();
+  if (wave || left <= 0) return;
+  Piece<float> p;
+  p.load(b.part + ((size_t)g * 2 + 1) * b.width + c, left);
   float* o = b.dtable + (size_t)key * b.width + c;
-  *o = b.accumulate ? fmaf(v, b.scale, *o) : v * b.scale;
+  Piece<float> old;
+  if (b.accumulate) old.load(o, left);
+  float sum[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    sum[e] = p.get(e) + v[e];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) sum[e] += quarter[q][lane][e];
+    sum[e] = b.accumulate ? fmaf(sum[e], b.scale, old.get(e)) : sum[e] * b.scale;
+  }
+  p.set(sum);
+  p.store(o, left);
 }
 
 }  // namespace sb
@@ -185,7 +274,7 @@ EmbedSpace embed_space(const sb_embed_desc* d) {
     return here;
   };
   e.a = take((size_t)d->tokens * 8);
-  e.b = take(s.passes > 1 ? (size_t)d->tokens * 8 : 0);
+  e.b = take(s.tiles && s.passes > 1 ? (size_t)d->tokens * 8 : 0);
   e.counts = take(sb::sort_count_bytes(s));
   e.part = take(d->tokens > run ? (size_t)sb::cdiv(d->tokens, run) * 2 * d->width * 4 : 0);
   e.bytes = at;
@@ -275,11 +364,14 @@ extern "C" sb_status sb_embed_bwd(const sb_embed_desc* d, const int32_t* ids, co
   b.accumulate = accumulate;
   b.dtable = dtable;
   b.part = (float*)(ws + at.part);
-  const size_t blocks = (((size_t)b.runs * b.rp.segs << b.rp.shift) + 255) / 256;
+  const size_t sums = (((size_t)b.runs * b.rp.segs << b.rp.shift) + 255) / 256;
+  const size_t fills = in.tiles && !accumulate ? ((size_t)d->vocab + 4 * sb::kAbsent - 1) / (4 * sb::kAbsent) : 0;
+  const size_t blocks = sums + fills;
   if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
+  b.sum_blocks = (int)sums;
   b.slots = sbh::sort_slots(in, nullptr, nullptr, (uint2*)(ws + at.a), (uint2*)(ws + at.b),
                             (uint32_t*)(ws + at.counts),
-                            sb::Fill{dtable, accumulate ? 0 : table}, st);
+                            sb::Fill{dtable, accumulate || in.tiles ? 0 : table}, st);
   s = sbh::launch_status();
   if (s != SB_OK || d->tokens == 0) return s;
   if (d->dtype == SB_BF16)

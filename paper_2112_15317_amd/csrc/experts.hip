@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
                                                              const int32_t* __restrict__ place,
                                                              const float* __restrict__ weights,
                                                              T* __restrict__ y) {
-  constexpr int N = Piece<T>::N;
+  constexpr int N = Piece<T>::N, AHEAD = 4;           // rows on their way at once
   const size_t group = ((size_t)blockIdx.x * 256 + threadIdx.x) >> b.rp.shift;
   const int lane = threadIdx.x & ((1 << b.rp.shift) - 1);
   const size_t t = group / (unsigned)b.rp.segs;
@@ -68,19 +68,32 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[u][e] = 0.f;
-#pragma unroll 4
-  for (int j = 0; j < b.top; ++j) {
-    const uint32_t from = (uint32_t)place[t * b.top + j];
-    if (from >= b.rows) continue;
-    const float w = weights ? weights[t * b.top + j] : 1.f;
+  for (int j0 = 0; j0 < b.top; j0 += AHEAD) {
+    uint32_t from[AHEAD];
+    float w[AHEAD];
+    Piece<T> p[AHEAD][U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int c = c0 + (u << b.rp.shift);
-      if (c >= b.rp.pieces) continue;
-      Piece<T> p;
-      p.load(ys + from * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
+    for (int j = 0; j < AHEAD; ++j) {
+      const bool there = j0 + j < b.top;
+      from[j] = there ? (uint32_t)place[t * b.top + j0 + j] : ~0u;
+      w[j] = there && weights ? weights[t * b.top + j0 + j] : 1.f;
+    }
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[u][e] = fmaf(w, p.get(e), acc[u][e]);
+    for (int j = 0; j < AHEAD; ++j) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = c0 + (u << b.rp.shift);
+        if (from[j] < b.rows && c < b.rp.pieces)
+          p[j][u].load(ys + from[j] * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (from[j] >= b.rows) continue;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[u][e] = fmaf(w[j], p[j][u].get(e), acc[u][e]);
     }
   }
 #pragma unroll

@@ -5,21 +5,22 @@ namespace sb {
 
 constexpr int kFillBlocks = 512;       // two a CU of the size that the sort has
 
-__global__ __launch_bounds__(kSortThreads) void slot_sort_small(SortIn s, uint2* a, uint2* b,
-                                                                SortPass last, Fill fill) {
-  __shared__ SortShared h;
-  if (blockIdx.x == 0) sort_small(s, a, b, last, h);
-  else fill_zero(fill, blockIdx.x - 1, gridDim.x - 1);
+template <int I, int R>
+__global__ __launch_bounds__(kSortThreads) void slot_sort_small(SortIn s, int32_t* place,
+                                                                int32_t* offsets, uint2* out,
+                                                                int blocks, Fill fill) {
+  __shared__ u4 numbers[kSortWaves][16 * R];
+  __shared__ uint32_t share[kSortWaves][2][64];
+  if ((int)blockIdx.x < blocks)
+    sort_by_count<I, R>(s, place, offsets, out, blockIdx.x, numbers, share);
+  else
+    fill_zero(fill, blockIdx.x - blocks, gridDim.x - blocks);
 }
 
 // counts[tile][digit] of one pass.
-__global__ __launch_bounds__(kSortThreads) void slot_sort_count(SortIn s, SortPass p, Fill fill) {
+__global__ __launch_bounds__(kSortThreads) void slot_sort_count(SortIn s, SortPass p) {
   __shared__ SortShared h;
   const int tile = blockIdx.x;
-  if (tile >= s.tiles) {
-    fill_zero(fill, tile - s.tiles, gridDim.x - s.tiles);
-    return;
-  }
   const uint32_t bins = 1u << s.digit;
   if (threadIdx.x < bins) h.base[threadIdx.x] = 0;
   __syncthreads();
@@ -54,25 +55,34 @@ namespace sbh {
 
 const uint2* sort_slots(const sb::SortIn& s, int32_t* place, int32_t* offsets, uint2* a, uint2* b,
                         uint32_t* counts, const sb::Fill& fill, hipStream_t stream) {
-  const size_t quads = fill.n / 4 + 1;
-  const int fills = fill.n == 0 ? 0
-                    : (int)(quads < (size_t)sb::kFillBlocks * sb::kSortThreads
-                                ? (quads + sb::kSortThreads - 1) / sb::kSortThreads
-                                : (size_t)sb::kFillBlocks);
+  constexpr size_t per = 4 * sb::kSortThreads;
+  if (s.tiles == 0) {
+    const size_t want = (fill.n + per - 1) / per;
+    const int queries = s.n + (offsets ? (int)s.keys + 1 : 0);
+    const int fills = want < (size_t)sb::kFillBlocks ? (int)want : sb::kFillBlocks;
+    if (queries + fills == 0) return a;
+    auto launch = [&](auto slots, auto r) {
+      constexpr int I = decltype(slots)::value, R = decltype(r)::value;
+      const int sorts = sb::cdiv(queries, 2 * I);
+      sb::slot_sort_small<I, R><<<sorts + fills, sb::kSortThreads, 0, stream>>>(
+          s, place, offsets, a, sorts, fill);
+    };
+    using std::integral_constant;
+    if (s.n <= 1024) launch(integral_constant<int, 8>(), integral_constant<int, 1>());
+    else if (s.n <= 4096) launch(integral_constant<int, 8>(), integral_constant<int, 4>());
+    else if (s.n <= 8192) launch(integral_constant<int, 16>(), integral_constant<int, 8>());
+    else launch(integral_constant<int, 32>(), integral_constant<int, 16>());
+    return a;
+  }
   sb::SortPass p{};
   p.place = place;
   p.offsets = offsets;
   p.counts = counts;
-  if (s.tiles <= 1) {
-    sb::slot_sort_small<<<1 + fills, sb::kSortThreads, 0, stream>>>(s, a, b, p, fill);
-    return (s.passes - 1) % 2 ? b : a;
-  }
   for (int pass = 0; pass < s.passes; ++pass) {
     p.in = p.out;
     p.out = pass + 1 == s.passes && place ? nullptr : pass % 2 ? b : a;
     p.shift = pass * s.digit;
-    sb::slot_sort_count<<<s.tiles + (pass == 0 ? fills : 0), sb::kSortThreads, 0, stream>>>(s, p,
-                                                                                            fill);
+    sb::slot_sort_count<<<s.tiles, sb::kSortThreads, 0, stream>>>(s, p);
     sb::slot_sort_move<<<s.tiles, sb::kSortThreads, 0, stream>>>(s, p);
   }
   return p.out;
