@@ -46,12 +46,13 @@ __global__ __launch_bounds__(256) void expert_gather_kernel(ExpertRows b, const 
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int c = c0 + (u << b.rp.shift);
-      if (c < b.rp.pieces) p[u].store(xs + to * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
+      if (c < b.rp.pieces)
+        p[u].template store<true>(xs + to * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
     }
   }
 }
 
-template <typename T, int U>
+template <typename T, int U, bool FAR>
 __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
                                                              const T* __restrict__ ys,
                                                              const int32_t* __restrict__ place,
@@ -84,7 +85,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
       for (int u = 0; u < U; ++u) {
         const int c = c0 + (u << b.rp.shift);
         if (from[j] < b.rows && c < b.rp.pieces)
-          p[j][u].load(ys + from[j] * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
+          p[j][u].template load<FAR>(ys + from[j] * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
       }
     }
 #pragma unroll
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
     if (c >= b.rp.pieces) continue;
     Piece<T> p;
     p.set(acc[u]);
-    p.store(y + t * (size_t)b.ldx + (size_t)c * N, b.width - c * N);
+    p.template store<true>(y + t * (size_t)b.ldx + (size_t)c * N, b.width - c * N);
   }
 }
 
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(
 #pragma unroll
           for (int e = 0; e < N; ++e) v[e] = d.get(e) * w;
           o.set(v);
-          o.store(dys + at, left);
+          o.template store<true>(dys + at, left);
         }
       }
     }
@@ -218,6 +219,9 @@ unsigned blocks_of(const sb::RowPlan& rp, size_t groups) {
 }
 
 constexpr int kUnits = 2, kBwdUnits = 4;      // pieces of a row that a lane has at once
+// Rows of more than the last cache holds are read past the caches by the combining kernel:
+// 1 GB in 209 us, 225 as other loads; 67 MB that lie there take 18.1 and 16.9.
+constexpr size_t kFarBytes = (size_t)256 << 20;
 
 }  // namespace
 
@@ -287,12 +291,19 @@ extern "C" sb_status sb_expert_combine(const sb_expert_desc* d, const void* ys,
   const unsigned blocks = blocks_of(b.rp, (size_t)d->tokens * b.rp.segs);
   if (!blocks) return SB_ERR_UNSUPPORTED;
   hipStream_t st = sbh::stream_of(stream);
-  if (d->dtype == SB_BF16)
-    sb::expert_combine_kernel<sb::u16, kUnits><<<blocks, 256, 0, st>>>(
-        b, (const sb::u16*)ys, place, weights, (sb::u16*)y);
-  else
-    sb::expert_combine_kernel<float, kUnits><<<blocks, 256, 0, st>>>(b, (const float*)ys, place,
-                                                                     weights, (float*)y);
+  const bool far = row_bytes(d) >= kFarBytes;
+  auto launch = [&](auto e, auto f) {
+    using T = decltype(e);
+    sb::expert_combine_kernel<T, kUnits, decltype(f)::value><<<blocks, 256, 0, st>>>(
+        b, (const T*)ys, place, weights, (T*)y);
+  };
+  if (d->dtype == SB_BF16) {
+    if (far) launch(sb::u16(), std::true_type());
+    else launch(sb::u16(), std::false_type());
+  } else {
+    if (far) launch(float(), std::true_type());
+    else launch(float(), std::false_type());
+  }
   return sbh::launch_status();
 }
 

@@ -20,9 +20,11 @@ template <typename T> struct Piece;
 template <> struct Piece<float> {
   static constexpr int N = 4;
   u4 raw;
+  template <bool FAR = false>
   __device__ __forceinline__ void load(const float* p, int left) {
     if (left >= N) {
-      raw = *reinterpret_cast<const u4_at4*>(p);
+      if constexpr (FAR) raw = __builtin_nontemporal_load(reinterpret_cast<const u4_at4*>(p));
+      else raw = *reinterpret_cast<const u4_at4*>(p);
     } else {
       raw = u4{0, 0, 0, 0};
 #pragma unroll
@@ -30,9 +32,12 @@ template <> struct Piece<float> {
         if (e < left) raw[e] = __float_as_uint(p[e]);
     }
   }
+  // FAR: read or written once, not to be kept in the caches.
+  template <bool FAR = false>
   __device__ __forceinline__ void store(float* p, int left) const {
     if (left >= N) {
-      *reinterpret_cast<u4_at4*>(p) = raw;
+      if constexpr (FAR) __builtin_nontemporal_store(raw, reinterpret_cast<u4_at4*>(p));
+      else *reinterpret_cast<u4_at4*>(p) = raw;
     } else {
 #pragma unroll
       for (int e = 0; e < N; ++e)
@@ -49,9 +54,11 @@ template <> struct Piece<float> {
 template <> struct Piece<u16> {
   static constexpr int N = 8;
   u4 raw;
+  template <bool FAR = false>
   __device__ __forceinline__ void load(const u16* p, int left) {
     if (left >= N) {
-      raw = *reinterpret_cast<const u4_at2*>(p);
+      if constexpr (FAR) raw = __builtin_nontemporal_load(reinterpret_cast<const u4_at2*>(p));
+      else raw = *reinterpret_cast<const u4_at2*>(p);
     } else {
       raw = u4{0, 0, 0, 0};
 #pragma unroll
@@ -59,9 +66,12 @@ template <> struct Piece<u16> {
         if (e < left) raw[e / 2] |= (uint32_t)p[e] << (e % 2 * 16);
     }
   }
+  // FAR: read or written once, not to be kept in the caches.
+  template <bool FAR = false>
   __device__ __forceinline__ void store(u16* p, int left) const {
     if (left >= N) {
-      *reinterpret_cast<u4_at2*>(p) = raw;
+      if constexpr (FAR) __builtin_nontemporal_store(raw, reinterpret_cast<u4_at2*>(p));
+      else *reinterpret_cast<u4_at2*>(p) = raw;
     } else {
 #pragma unroll
       for (int e = 0; e < N; ++e)

@@ -31,7 +31,7 @@ constexpr int kNarrow = 1024;          // classes of a row in one launch
 constexpr int kNarrowElems = 16;       // of a lane there
 template <typename T> constexpr int kNarrowPieces = kNarrowElems / Piece<T>::N;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
-constexpr float kLeastPower = -1000.f; // of 2, in place of masked elements' -inf: 0 times it is 0
+constexpr float kLeastPower = -1000.f; // in place of masked elements' -inf: 0 times it is 0
 constexpr float kLeastPlain = -1e30f;  // smaller maxima take the careful sums
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -566,68 +566,98 @@ __device__ __forceinline__ float class_grad(const RowGrad& r, float z, float g) 
 }
 
 // The same for classes without a gradient of their own, in rows of an ordinary M and
-// log S, as one fused product each for log p and what multiplies p: in powers of 2, with
-// c = (M + log S) log2 e rounded and its error in the factors.
+// log S: with t = z - M (exact where z is near M: sure rows keep their bits),
+// dz = -2^(t log2 e - l) (a + dH t).
 struct PlainGrad {
-  float c, a, b;               // dz = -2^y (a + b y), y = z log2 e - c
-  __device__ __forceinline__ explicit PlainGrad(const RowGrad& r) {
-#pragma clang fp contract(off)
-    const float hi = r.mx * kLog2e, lo = fmaf(r.mx, kLog2e, -hi), l = r.ls * kLog2e;
-    c = hi + l;
-    const float back = c - hi;
-    const float err = ((hi - (c - back)) + (l - back)) + lo;       // what c lacks
-    const float fix = exp2_hw(-err);
-    b = fix * (kLn2 * r.dh);
-    a = fmaf(-err, b, fix * r.all);
-  }
+  float mx, l, a, dh;
+  __device__ __forceinline__ explicit PlainGrad(const RowGrad& r)
+      : mx(r.mx), l(r.ls * kLog2e), a(fmaf(-r.dh, r.ls, r.all)), dh(r.dh) {}
   __device__ __forceinline__ float operator()(float z) const {
-    const float y = fmaxf(fmaf(z, kLog2e, -c), kLeastPower);
-    return -exp2_hw(y) * fmaf(b, y, a);
+    const float t = fmaxf(z - mx, kLeastPower);
+    return -exp2_hw(fmaf(t, kLog2e, -l)) * fmaf(dh, t, a);
   }
 };
 
+// Whether a row takes PlainGrad: ordinary stats and no target past the classes.
+__device__ __forceinline__ bool is_plain(const RowGrad& r) {
+  return fabsf(r.mx) < -kLeastPlain && r.ls == r.ls && !r.bad;
+}
+// N elements of such a row, or of any other one.
+template <int N, typename T>
+__device__ __forceinline__ Piece<T> grad_piece(const RowGrad& r, const PlainGrad& grad, bool plain,
+                                               const Piece<T>& z) {
+  float d[N];
+  if (plain) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) d[e] = grad(z.get(e));
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      d[e] = r.bad ? NAN : r.ls == -INFINITY ? 0.f : class_grad(r, z.get(e), 0.f);
+  }
+  Piece<T> q;
+  q.set(d);
+  return q;
+}
+
+// The classes with a gradient of their own (alternatives, then the target) are a row's
+// entries; lane l has entries l, l + lanes, ...  Their logits are read before the row is
+// written (dz may be z), and they are written again behind it.
 template <typename T>
 __global__ __launch_bounds__(256) void logp_narrow_bwd(LogpBwd b, int shift, const T* z, T* dz) {
-  constexpr int N = Piece<T>::N, P = kNarrowPieces<T>, E = P * N, AHEAD = 8;
+  constexpr int N = Piece<T>::N, P = kNarrowPieces<T>;
+  constexpr int ENTRIES = SB_LOGP_MAX_TOP + 1, MORE = (ENTRIES + 7) / 8;
+  __shared__ int ids[256 / 8][ENTRIES];
+  __shared__ float gs[256 / 8][ENTRIES];
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
   const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> shift;
   if (row >= (size_t)b.m) return;
+  int* id = ids[threadIdx.x >> shift];
+  float* g = gs[threadIdx.x >> shift];
   const T* zr = z + row * (size_t)b.ldz;
+  T* out = dz + row * (size_t)b.ldz;
   Piece<T> p[P];
-  float g[E];
   load_row<T, P>(zr, b.classes, 0, lane, lanes, p);
   RowGrad r = row_grad(b, row);
-#pragma unroll
-  for (int e = 0; e < E; ++e) g[e] = class_at<T>(0, lane, lanes, e) == r.target ? r.g : 0.f;
-  const int tops = b.dtop ? b.top : 0;
-  for (int k0 = 0; k0 < tops; k0 += AHEAD) {
-    int id[AHEAD];
-    float d[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      id[k] = -1;
-      d[k] = k0 + k < tops ? top_grad(b, row, k0 + k, id[k]) : 0.f;
-    }
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      if (k0 + k >= tops) break;
-      r.all += d[k];
-#pragma unroll
-      for (int e = 0; e < E; ++e) g[e] += class_at<T>(0, lane, lanes, e) == id[k] ? d[k] : 0.f;
-    }
+  const int tops = b.dtop ? b.top : 0, entries = tops + (r.target >= 0 && !r.bad ? 1 : 0);
+  float all = 0.f;
+  for (int k = lane; k < entries; k += lanes) {
+    int c = r.target;
+    const float gk = k < tops ? top_grad(b, row, k, c) : r.g;
+    if (k < tops) all += gk;
+    id[k] = c;
+    g[k] = gk;
   }
-  const bool none = r.ls == -INFINITY;          // nothing is left of the row
+  r.all += group_sum(all, lanes);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  float special[MORE];
+#pragma unroll
+  for (int i = 0; i < MORE; ++i) {
+    const int k = i * lanes + lane;
+    if (k >= entries) break;
+    const int c = id[k];
+    const float z0 = c >= 0 && c < b.classes ? Elem<T>::load(zr, c) : 0.f;
+    float sum = 0.f;                            // of all that name this class
+    for (int j = 0; j < entries; ++j) sum += id[j] == c ? g[j] : 0.f;
+    special[i] = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum);
+  }
+  const bool plain = __all(is_plain(r));
+  const PlainGrad grad(r);
 #pragma unroll
   for (int u = 0; u < P; ++u) {
     const int c = (lane + u * lanes) * N;
-    if (c >= b.classes) continue;
-    float d[N];
+    const Piece<T> q = grad_piece<N>(r, grad, plain, p[u]);
+    if (c < b.classes) q.store(out + c, b.classes - c);
+  }
+  // Behind what this wave has just written there.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int e = 0; e < N; ++e)
-      d[e] = r.bad ? NAN : none ? 0.f : class_grad(r, p[u].get(e), g[u * N + e]);
-    Piece<T> q;
-    q.set(d);
-    q.store(dz + row * (size_t)b.ldz + c, b.classes - c);
+  for (int i = 0; i < MORE; ++i) {
+    const int k = i * lanes + lane;
+    if (k >= entries || r.bad) break;
+    const int c = id[k];
+    if (c >= 0 && c < b.classes) Elem<T>::store(out, c, special[i]);
   }
 }
 
@@ -668,22 +698,12 @@ __global__ __launch_bounds__(256) void logp_stretch_bwd(LogpBwd b, const T* z, T
     }
     special = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum);
   }
-  const bool plain = fabsf(r.mx) < -kLeastPlain && r.ls == r.ls && !r.bad;
+  const bool plain = is_plain(r);
   const PlainGrad grad(r);
 #pragma unroll
   for (int u = 0; u < P; ++u) {
     const int c = first + (lane + u * 64) * N;
-    float d[N];
-    if (plain) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) d[e] = grad(p[u].get(e));
-    } else {
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        d[e] = r.bad ? NAN : r.ls == -INFINITY ? 0.f : class_grad(r, p[u].get(e), 0.f);
-    }
-    Piece<T> q;
-    q.set(d);
+    const Piece<T> q = grad_piece<N>(r, grad, plain, p[u]);
     if (c < b.classes) q.store(out + c, b.classes - c);
   }
   if (any && !r.bad) {

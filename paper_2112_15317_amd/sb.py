@@ -233,7 +233,8 @@ def _stream_for(t, stream):
     on = getattr(t, "device", None)          # of a tensor; None and addresses have none
     if stream is not None and on is None:
         return _stream(stream)
-    dev = torch.cuda.current_device()
+    dev = (torch.cuda.current_device if on is None else
+           getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))()
     if on is not None and on.index != dev:
         raise ValueError("tensors on %s, current device %d" % (on, dev))
     if stream is None:
@@ -643,17 +644,20 @@ def sb_adamw_unpack(n, m, m_top, v, v_top, m_out, v_out, stream=None):
 
 
 # -------------------------------------------------------------- embedding --
-def _typed(desc, **tensors):
-    """Tensors (not addresses) of a call have the descriptor's type."""
-    for name, t in tensors.items():
-        if t is not None and not isinstance(t, int) and _dtype_code(t) != desc.dtype:
-            raise ValueError("%s has another type than the descriptor" % name)
+_types = None                   # torch's types by sb_dtype, then int32
 
 
-def _kind(kind, **tensors):
-    for name, t in tensors.items():
-        if t is not None and not isinstance(t, int) and str(t.dtype) != "torch." + kind:
-            raise ValueError("%s is %s" % (name, kind))
+def _kinds(dtype, rows=(), i32=(), f32=()):
+    """Tensors (not addresses) of a call have the descriptor's type, int32 and float32."""
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.float32, torch.bfloat16, torch.int32)
+    for want, tensors in ((_types[dtype] if dtype in (SB_F32, SB_BF16) else None, rows),
+                          (_types[2], i32), (_types[0], f32)):
+        for t in tensors:
+            if t is not None and t.__class__ is not int and t.dtype is not want:
+                raise ValueError("a tensor of %s, expected %s" % (t.dtype, want))
 
 
 def embed_desc(tokens, vocab, width, dtype=SB_F32, first=0, ldy=None, scale=1.0):
@@ -667,8 +671,7 @@ def sb_embed_workspace_bytes(desc):
 
 def sb_embed_fwd(desc, table, ids, y, stream=None):
     """ids: int32."""
-    _typed(desc, table=table, y=y)
-    _kind("int32", ids=ids)
+    _kinds(desc.dtype, (table, y), (ids,))
     _check("sb_embed_fwd", load().sb_embed_fwd(
         ctypes.byref(desc), _ptr(table), _ptr(ids), _ptr(y), _stream_for(table, stream)))
 
@@ -676,9 +679,7 @@ def sb_embed_fwd(desc, table, ids, y, stream=None):
 def sb_embed_bwd(desc, ids, dy, dtable, accumulate=False, ws=None, stream=None):
     """dtable: fp32 [vocab][width]."""
     p, nb = _ws(ws)
-    _typed(desc, dy=dy)
-    _kind("int32", ids=ids)
-    _kind("float32", dtable=dtable)
+    _kinds(desc.dtype, (dy,), (ids,), (dtable,))
     _check("sb_embed_bwd", load().sb_embed_bwd(
         ctypes.byref(desc), _ptr(ids), _ptr(dy), _ptr(dtable), 1 if accumulate else 0, p, nb,
         _stream_for(dtable, stream)))
@@ -697,33 +698,28 @@ def sb_expert_workspace_bytes(desc):
 def sb_expert_sort(desc, ids, place, offsets, ws=None, stream=None):
     """All int32: ids and place [tokens][top], offsets [experts + 1]."""
     p, nb = _ws(ws)
-    _kind("int32", ids=ids, place=place, offsets=offsets)
+    _kinds(desc.dtype, (), (ids, place, offsets))
     _check("sb_expert_sort", load().sb_expert_sort(
         ctypes.byref(desc), _ptr(ids), _ptr(place), _ptr(offsets), p, nb,
         _stream_for(offsets, stream)))
 
 
 def sb_expert_gather(desc, x, place, xs, stream=None):
-    _typed(desc, x=x, xs=xs)
-    _kind("int32", place=place)
+    _kinds(desc.dtype, (x, xs), (place,))
     _check("sb_expert_gather", load().sb_expert_gather(
         ctypes.byref(desc), _ptr(x), _ptr(place), _ptr(xs), _stream_for(x, stream)))
 
 
 def sb_expert_combine(desc, ys, place, weights, y, stream=None):
     """weights: fp32 [tokens][top], or None (1 each: the gather's backward)."""
-    _typed(desc, ys=ys, y=y)
-    _kind("int32", place=place)
-    _kind("float32", weights=weights)
+    _kinds(desc.dtype, (ys, y), (place,), (weights,))
     _check("sb_expert_combine", load().sb_expert_combine(
         ctypes.byref(desc), _ptr(ys), _ptr(place), _ptr(weights), _ptr(y),
         _stream_for(y, stream)))
 
 
 def sb_expert_combine_bwd(desc, dy, ys, place, weights, dys, dweights=None, stream=None):
-    _typed(desc, dy=dy, ys=ys, dys=dys)
-    _kind("int32", place=place)
-    _kind("float32", weights=weights, dweights=dweights)
+    _kinds(desc.dtype, (dy, ys, dys), (place,), (weights, dweights))
     _check("sb_expert_combine_bwd", load().sb_expert_combine_bwd(
         ctypes.byref(desc), _ptr(dy), _ptr(ys), _ptr(place), _ptr(weights), _ptr(dys),
         _ptr(dweights), _stream_for(dy, stream)))
@@ -744,9 +740,7 @@ def sb_token_logp_fwd(desc, z, targets, logp, entropy, stats, top_ids=None, top_
     """targets, top_ids: int32; logp, entropy, stats [m][2], top_values: fp32.
     targets, logp and entropy may be None."""
     p, nb = _ws(ws)
-    _typed(desc, z=z)
-    _kind("int32", targets=targets, top_ids=top_ids)
-    _kind("float32", logp=logp, entropy=entropy, stats=stats, top_values=top_values)
+    _kinds(desc.dtype, (z,), (targets, top_ids), (logp, entropy, stats, top_values))
     _check("sb_token_logp_fwd", load().sb_token_logp_fwd(
         ctypes.byref(desc), _ptr(z), _ptr(targets), _ptr(logp), _ptr(entropy), _ptr(stats),
         _ptr(top_ids), _ptr(top_values), p, nb, _stream_for(z, stream)))
@@ -755,10 +749,8 @@ def sb_token_logp_fwd(desc, z, targets, logp, entropy, stats, top_ids=None, top_
 def sb_token_logp_bwd(desc, z, stats, targets, dlogp, entropy, dentropy, top_ids, top_values, dtop,
                       dz, stream=None):
     """dlogp, dentropy and dtop, and what they go with, may be None; dz may be z."""
-    _typed(desc, z=z, dz=dz)
-    _kind("int32", targets=targets, top_ids=top_ids)
-    _kind("float32", stats=stats, dlogp=dlogp, entropy=entropy, dentropy=dentropy,
-          top_values=top_values, dtop=dtop)
+    _kinds(desc.dtype, (z, dz), (targets, top_ids),
+           (stats, dlogp, entropy, dentropy, top_values, dtop))
     _check("sb_token_logp_bwd", load().sb_token_logp_bwd(
         ctypes.byref(desc), _ptr(z), _ptr(stats), _ptr(targets), _ptr(dlogp), _ptr(entropy),
         _ptr(dentropy), _ptr(top_ids), _ptr(top_values), _ptr(dtop), _ptr(dz),
