@@ -707,14 +707,15 @@ sb_status sb_expert_sort(const sb_expert_desc *desc, const int32_t *ids,
 sb_status sb_expert_gather(const sb_expert_desc *desc, const void *x,
                            const int32_t *place, void *xs, void *stream);
 
-/* y[t] = sum_j weights[t][j] * ys[place[t][j]], in the order of j; weights may be
- * NULL (1 each).  A token without a row gets zeros.  Without weights, on the gradient
- * of xs, this is the gather's backward: dx[t] = sum_j dxs[place[t][j]]. */
+/* y[t] = add[t] + sum_j weights[t][j] * ys[place[t][j]], in the order of j; weights may
+ * be NULL (1 each), and so may add (0; rows as y's, or y itself: added to in place).  A
+ * token without a row gets add's.  Without weights, on the gradient of xs, this is the
+ * gather's backward: dx[t] = sum_j dxs[place[t][j]]. */
 sb_status sb_expert_combine(const sb_expert_desc *desc, const void *ys,
                             const int32_t *place, const float *weights,
-                            void *y, void *stream);
+                            const void *add, void *y, void *stream);
 
-/* The gradients of sb_expert_combine:
+/* The gradients of sb_expert_combine (that of add is dy):
  *   dys[place[t][j]] = weights[t][j] * dy[t]   (weights NULL: dy[t])
  *   dweights[t][j]   = sum_c dy[t][c] * ys[place[t][j]][c], 0 where there is no row
  * dweights may be NULL (ys is then not read and may be NULL). */

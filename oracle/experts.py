@@ -32,8 +32,8 @@ def gather(x, place, rows):
     return xs
 
 
-def combine(ys, place, weights=None):
-    y = np.zeros((place.shape[0], ys.shape[1]))
+def combine(ys, place, weights=None, add=None):
+    y = np.zeros((place.shape[0], ys.shape[1])) if add is None else np.array(add, np.float64)
     for t, j in np.argwhere(place >= 0):
         y[t] += (1.0 if weights is None else float(weights[t, j])) * np.asarray(ys[place[t, j]], np.float64)
     return y
@@ -47,14 +47,14 @@ def combine_backward(dy, ys, place, weights, rows):
     return dys, dw
 
 
-def bounds(dy, ys, place, weights, rows, bf16):
+def bounds(dy, ys, place, weights, rows, bf16, add=None):
     """Bounds on the errors of (y, dys, dw).  y: `top` fused products, each sum rounded once in fp32; dys: one
     product; dw: at most width / 64 + 8 products a lane and 6 sums of lanes.  bf16 adds half a step of the
     result (not of dw, which is fp32)."""
     w = None if weights is None else np.abs(weights)
     half = HALF16 if bf16 else 0.0
-    y = np.abs(combine(ys, place, weights))
-    ey = place.shape[1] * U * combine(np.abs(ys), place, w)
+    y = np.abs(combine(ys, place, weights, add))
+    ey = place.shape[1] * U * combine(np.abs(ys), place, w, None if add is None else np.abs(add))
     ey = ey + half * (y + ey)
     dys, dw = combine_backward(np.abs(dy), np.abs(ys), place, w, np.zeros_like(rows))
     edys = U * dys

@@ -5,7 +5,7 @@
 // them; -1 where its expert is not one of this worker's.
 //
 //   xs[place[t][j]] = x[t]
-//   y[t]            = sum_j w[t][j] ys[place[t][j]]
+//   y[t]            = add[t] + sum_j w[t][j] ys[place[t][j]]
 //   dys[place]      = w[t][j] dy[t],   dw[t][j] = <dy[t], ys[place]>
 //
 // HBM bounds all of them.  Going by tokens a row of x or dy is read once for all
@@ -57,7 +57,7 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
                                                              const T* __restrict__ ys,
                                                              const int32_t* __restrict__ place,
                                                              const float* __restrict__ weights,
-                                                             T* __restrict__ y) {
+                                                             const T* add, T* y) {
   constexpr int N = Piece<T>::N, AHEAD = 4;           // rows on their way at once
   const size_t group = ((size_t)blockIdx.x * 256 + threadIdx.x) >> b.rp.shift;
   const int lane = threadIdx.x & ((1 << b.rp.shift) - 1);
@@ -66,9 +66,14 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
   const int c0 = (int)(group - t * b.rp.segs) * (U << b.rp.shift) + lane;
   float acc[U][N];
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+  for (int u = 0; u < U; ++u) {
+    const int c = c0 + (u << b.rp.shift);
+    Piece<T> p;
+    p.raw = u4{0, 0, 0, 0};
+    if (add && c < b.rp.pieces) p.load(add + t * (size_t)b.ldx + (size_t)c * N, b.width - c * N);
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[u][e] = 0.f;
+    for (int e = 0; e < N; ++e) acc[u][e] = p.get(e);
+  }
   for (int j0 = 0; j0 < b.top; j0 += AHEAD) {
     uint32_t from[AHEAD];
     float w[AHEAD];
@@ -276,17 +281,19 @@ extern "C" sb_status sb_expert_gather(const sb_expert_desc* d, const void* x, co
 }
 
 extern "C" sb_status sb_expert_combine(const sb_expert_desc* d, const void* ys,
-                                       const int32_t* place, const float* weights, void* y,
-                                       void* stream) {
+                                       const int32_t* place, const float* weights,
+                                       const void* add, void* y, void* stream) {
   const sb_status s = expert_check(d);
   if (s != SB_OK) return s;
   if (d->tokens == 0) return SB_OK;
   const size_t e = sbh::dsize(d->dtype);
-  if (!ys || !place || !y || off(ys, e) || off(y, e) || off(place, 4) || off(weights, 4))
+  if (!ys || !place || !y || off(ys, e) || off(y, e) || off(add, e) || off(place, 4) ||
+      off(weights, 4))
     return SB_ERR_INVALID_ARG;
-  const Span in[3] = {{ys, row_bytes(d)}, {place, slot_bytes(d)}, {weights, slot_bytes(d)}};
+  const Span in[4] = {{ys, row_bytes(d)}, {place, slot_bytes(d)}, {weights, slot_bytes(d)},
+                      {add == y ? nullptr : add, token_bytes(d)}};
   const Span out{y, token_bytes(d)};
-  if (meets(&out, 1, in, 3)) return SB_ERR_INVALID_ARG;
+  if (meets(&out, 1, in, 4)) return SB_ERR_INVALID_ARG;
   const sb::ExpertRows b = expert_rows<kUnits>(d);
   const unsigned blocks = blocks_of(b.rp, (size_t)d->tokens * b.rp.segs);
   if (!blocks) return SB_ERR_UNSUPPORTED;
@@ -295,7 +302,7 @@ extern "C" sb_status sb_expert_combine(const sb_expert_desc* d, const void* ys,
   auto launch = [&](auto e, auto f) {
     using T = decltype(e);
     sb::expert_combine_kernel<T, kUnits, decltype(f)::value><<<blocks, 256, 0, st>>>(
-        b, (const T*)ys, place, weights, (T*)y);
+        b, (const T*)ys, place, weights, (const T*)add, (T*)y);
   };
   if (d->dtype == SB_BF16) {
     if (far) launch(sb::u16(), std::true_type());

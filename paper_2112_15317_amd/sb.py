@@ -148,7 +148,7 @@ SIGNATURES = {
     "sb_expert_workspace_bytes": (_sz, [ctypes.POINTER(sb_expert_desc)]),
     "sb_expert_sort": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp, _sz, _vp]),
     "sb_expert_gather": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp]),
-    "sb_expert_combine": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp, _vp]),
+    "sb_expert_combine": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp, _vp, _vp]),
     "sb_expert_combine_bwd": (_i, [ctypes.POINTER(sb_expert_desc), _vp, _vp, _vp, _vp, _vp, _vp,
                                    _vp]),
     "sb_token_logp_workspace_bytes": (_sz, [ctypes.POINTER(sb_token_logp_desc)]),
@@ -710,11 +710,12 @@ def sb_expert_gather(desc, x, place, xs, stream=None):
         ctypes.byref(desc), _ptr(x), _ptr(place), _ptr(xs), _stream_for(x, stream)))
 
 
-def sb_expert_combine(desc, ys, place, weights, y, stream=None):
-    """weights: fp32 [tokens][top], or None (1 each: the gather's backward)."""
-    _kinds(desc.dtype, (ys, y), (place,), (weights,))
+def sb_expert_combine(desc, ys, place, weights, y, add=None, stream=None):
+    """weights: fp32 [tokens][top], or None (1 each: the gather's backward); add: rows
+    like y's that the sum starts from, or y itself."""
+    _kinds(desc.dtype, (ys, add, y), (place,), (weights,))
     _check("sb_expert_combine", load().sb_expert_combine(
-        ctypes.byref(desc), _ptr(ys), _ptr(place), _ptr(weights), _ptr(y),
+        ctypes.byref(desc), _ptr(ys), _ptr(place), _ptr(weights), _ptr(add), _ptr(y),
         _stream_for(y, stream)))
 
 

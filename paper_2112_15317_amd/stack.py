@@ -17,9 +17,13 @@ by a libsb kernel.  torch only allocates device memory and orders streams.
 ``GroupTrainStep``  a training step of an MP group: conv stack, K modulo
                 iterations of the FC shards with an update after each, conv
                 backward and update
+``ExpertShard`` a worker's gated experts behind a router, fwd + bwd
+``TokenTrainStep``  a training step on token ids: embedding, experts, FC layer
+                over the vocabulary, log-probabilities, backward, AdamW
 """
 from __future__ import annotations
 
+import contextlib
 import re
 
 import numpy as np
@@ -43,6 +47,15 @@ def _gate_code(act: str):
 
 def _plain(key, fn, *args):
     fn(*args)
+
+
+def _on(stream):
+    """A context in which ``stream`` (a torch stream, a hipStream_t's number or None) is
+    torch's current one."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream)
+                             else torch.cuda.ExternalStream(stream))
 
 
 def capture_graph(step_fn, steps=1):
@@ -454,9 +467,10 @@ class _Updates:
     """The updates of one set of (parameter, gradient, scale, decays): SGD, or
     AdamW with the moments and a counter of its updates on the device, so that
     a captured step counts on when it is replayed, and the tensors' elements
-    numbered from ``first`` to ``end`` among the random numbers of the bytes."""
+    numbered from ``first`` to ``end`` among the random numbers of the bytes.
+    copies: with AdamW, bfloat16 tensors (or None) that get the new parameters."""
 
-    def __init__(self, items, adamw, first=0):
+    def __init__(self, items, adamw, first=0, copies=None):
         self.adamw = adamw
         firsts = []
         for w, _, _, _ in items:
@@ -467,9 +481,11 @@ class _Updates:
             self.list = sb.SgdList([(w, g, scale) for w, g, scale, _ in items])
             return
         self.moments = [sb.adamw_moments(w, adamw.moments) for w, _, _, _ in items]
+        copies = copies or [None] * len(items)
         self.list = sb.AdamwList([dict(w=w, g=g, scale=scale, decay=adamw.decay if decays else 0.0,
-                                       first=at, **m)
-                                  for (w, g, scale, decays), m, at in zip(items, self.moments, firsts)])
+                                       first=at, copy=c, **m)
+                                  for (w, g, scale, decays), m, at, c in
+                                  zip(items, self.moments, firsts, copies)])
         self.done = torch.zeros(1, dtype=torch.int32, device=items[0][0].device)
 
     def calls(self, name, k, lr, stream):
@@ -872,3 +888,197 @@ class AveragedGroups:
         self.steps_done += 1
         if self.steps_done % self.period == 0:
             self.average(stream)
+
+
+class _Parameters:
+    """Parameters in fp32 with their gradients, and what the calls read: the same
+    tensors, or bfloat16 copies.  Biases have no copy."""
+
+    def __init__(self, dtype, device):
+        self.dtype, self.device, self.items, self.copies = dtype, torch.device(device), [], []
+
+    def add(self, shape, decays=True, bias=False):
+        """(parameter, gradient, what the calls read)."""
+        f32 = dict(dtype=torch.float32, device=self.device)
+        w, g = torch.zeros(shape, **f32), torch.zeros(shape, **f32)
+        half = self.dtype == "bf16" and not bias
+        c = torch.zeros(shape, dtype=torch.bfloat16, device=self.device) if half else None
+        self.items.append((w, g, 1.0, decays and not bias))
+        self.copies.append(c)
+        return w, g, c if half else w
+
+    def load(self, w, value):
+        """Sets a parameter (and its copy) from a host array."""
+        w.copy_(torch.from_numpy(np.ascontiguousarray(value, np.float32)).view(w.shape))
+        for (p, _, _, _), c in zip(self.items, self.copies):
+            if p is w and c is not None:
+                c.copy_(w)
+
+
+class ExpertShard:
+    """A worker's experts behind a router: gated layers (``sb_gated_shard_*``), each on
+    the rows of the tokens that chose it.
+
+    The router is an FC layer from the tokens' rows to ``whole`` logits, all workers'
+    experts; each token goes to the ``top`` most likely ones with their probabilities as
+    weights (``sb_token_logp_fwd`` with ``SB_TOP_PROBS``).  This worker has the
+    ``experts`` experts from ``first`` on; y and dx are partial, to be summed over the
+    workers (``dx_router`` of one worker with the others').  The tokens' rows are laid
+    out by expert (``sb_expert_sort``, ``sb_expert_gather``), and brought back with
+    their weights (``sb_expert_combine``).
+
+    How many rows an expert has is known on the device alone, and its products are
+    planned on the host: the forward reads the counts, which waits for the stream, so
+    that it can't be captured.  ``rows`` are the counts of the last forward.
+
+    Parameters (``_Parameters``): ``Wr`` [width][whole], ``br``; ``W``
+    [experts][2][width][shard] (the gate's weight, then the other projection's),
+    ``b`` [experts][2][shard]; ``dW...`` their gradients."""
+
+    def __init__(self, params, tokens, width, shard, experts, top, act="silu", first=0, whole=None):
+        whole = whole or first + experts
+        self.tokens, self.width, self.shard, self.experts, self.top = tokens, width, shard, experts, top
+        dev, dtype = params.device, params.dtype
+        tdt, code = _dev_dtype(dtype), _code(dtype)
+        self.act, self.code = _gate_code(act), code
+        self.Wr, self.dWr, self._wr = params.add((width, whole))
+        self.br, self.dbr, _ = params.add((whole,), bias=True)
+        self.W, self.dW, self._w = params.add((experts, 2, width, shard))
+        self.b, self.db, _ = params.add((experts, 2, shard), bias=True)
+        slots = tokens * top
+        rows = lambda n, w: torch.empty((n, w), dtype=tdt, device=dev)
+        f32, i32 = dict(dtype=torch.float32, device=dev), dict(dtype=torch.int32, device=dev)
+        self.logits, self.dlogits = rows(tokens, whole), rows(tokens, whole)
+        self.stats = torch.empty((tokens, 2), **f32)
+        self.ids, self.place = torch.empty((tokens, top), **i32), torch.empty((tokens, top), **i32)
+        self.weights, self.dweights = torch.empty((tokens, top), **f32), torch.empty((tokens, top), **f32)
+        self.offsets = torch.empty((experts + 1,), **i32)
+        self.xs, self.dxs = rows(slots, width), rows(slots, width)
+        self.ys, self.dys = rows(slots, shard), rows(slots, shard)
+        self.pre = torch.empty((2 * slots * shard,), **f32)
+        self.dx_router = rows(tokens, width)
+        self.rdesc = sb.fc_desc(tokens, width, whole, code)
+        self.tdesc = sb.token_logp_desc(tokens, whole, top, code, probs=True)
+        self.xdesc = sb.expert_desc(tokens, top, experts, width, code, first)
+        self.ydesc = sb.expert_desc(tokens, top, experts, shard, code, first)
+        need = max(sb.sb_fc_workspace_bytes(self.rdesc, sb.SB_FC_FWD),
+                   sb.sb_fc_workspace_bytes(self.rdesc, sb.SB_FC_BWD),
+                   sb.sb_token_logp_workspace_bytes(self.tdesc), sb.sb_expert_workspace_bytes(self.xdesc))
+        self.ws = torch.empty((max(need, 256),), dtype=torch.uint8, device=dev)
+        self.rows = [0] * (experts + 1)
+
+    def _space(self, need):
+        """Experts' row counts change from call to call, and their workspace with them."""
+        if need > self.ws.numel():
+            torch.cuda.current_stream().synchronize()      # calls may be at work in the old one
+            self.ws = torch.empty((need + need // 4,), dtype=torch.uint8, device=self.ws.device)
+        return self.ws
+
+    def _expert(self, e):
+        """Of an expert with rows: descriptor, first row, last, and its part of ``pre``."""
+        r0, r1 = self.rows[e], self.rows[e + 1]
+        desc = sb.gated_desc(r1 - r0, self.width, self.shard, self.code, self.act, unaligned=True)
+        return desc, r0, r1, self.pre[2 * r0 * self.shard:2 * r1 * self.shard]
+
+    def forward(self, x, y, add=None, stream=None):
+        """y = add + the experts' weighted outputs."""
+        with _on(stream):
+            sb.sb_fc_shard_fwd(self.rdesc, x, self._wr, self.br, self.logits, self.ws)
+            sb.sb_token_logp_fwd(self.tdesc, self.logits, None, None, None, self.stats, self.ids,
+                                 self.weights, self.ws)
+            sb.sb_expert_sort(self.xdesc, self.ids, self.place, self.offsets, self.ws)
+            sb.sb_expert_gather(self.xdesc, x, self.place, self.xs)
+            self.rows = self.offsets.tolist()
+            for e in range(self.experts):
+                if self.rows[e + 1] == self.rows[e]:
+                    continue
+                desc, r0, r1, pre = self._expert(e)
+                ws = self._space(sb.sb_gated_workspace_bytes(desc, sb.SB_FC_FWD))
+                sb.sb_gated_shard_fwd(desc, self.xs[r0:r1], self._w[e, 0], self._w[e, 1],
+                                      self.b[e, 0], self.b[e, 1], self.ys[r0:r1], pre, ws)
+            sb.sb_expert_combine(self.ydesc, self.ys, self.place, self.weights, y, add)
+
+    def backward(self, x, dy, dx, stream=None):
+        """dx and the parameters' gradients, from the gradient of y (add's is dy)."""
+        with _on(stream):
+            sb.sb_expert_combine_bwd(self.ydesc, dy, self.ys, self.place, self.weights, self.dys,
+                                     self.dweights)
+            for e in range(self.experts):
+                if self.rows[e + 1] == self.rows[e]:
+                    self.dW[e].zero_()
+                    self.db[e].zero_()
+                    continue
+                desc, r0, r1, pre = self._expert(e)
+                ws = self._space(sb.sb_gated_workspace_bytes(desc, sb.SB_FC_BWD))
+                sb.sb_gated_shard_bwd(desc, self.xs[r0:r1], self._w[e, 0], self._w[e, 1], pre,
+                                      self.dys[r0:r1], self.dxs[r0:r1], self.dW[e, 0],
+                                      self.dW[e, 1], self.db[e, 0], self.db[e, 1], False, ws)
+            sb.sb_token_logp_bwd(self.tdesc, self.logits, self.stats, None, None, None, None,
+                                 self.ids, self.weights, self.dweights, self.dlogits)
+            sb.sb_fc_shard_bwd(self.rdesc, x, self._wr, self.dlogits, None, self.dx_router, self.dWr,
+                               self.dbr, False, self.ws)
+            sb.sb_expert_combine(self.xdesc, self.dxs, self.place, None, dx, self.dx_router)
+
+
+class TokenTrainStep:
+    """A training step of a model on token ids, on one worker: the rows of the ids
+    (``sb_embed_fwd``), gated experts behind a router (``ExpertShard``), an FC layer to
+    the vocabulary, and the log-probabilities of the target tokens
+    (``sb_token_logp_fwd``); then backward through all of it and one AdamW update.
+
+    ``ids`` and ``targets`` [tokens] int32 (negative: padding), ``dlogp`` and
+    ``dentropy`` [tokens] fp32 what the step descends along: the gradient of the loss
+    with respect to each log-probability and entropy (-1 / tokens and 0 to start
+    with).  After a step ``logp``, ``entropy`` and ``top_ids``/``top_values`` (the
+    `alternatives` most likely tokens of each row) are those before its update.
+
+    Parameters: ``table`` [vocab][width], those of ``experts``, ``Wo``
+    [shard][vocab] and ``bo``; fp32, with bfloat16 copies that the calls read where
+    dtype is "bf16".  The logits' gradient is written over the logits."""
+
+    def __init__(self, tokens, vocab, width, shard, experts, top, adamw, dtype="f32", act="silu",
+                 scale=1.0, alternatives=0, device="cuda"):
+        p = self.params = _Parameters(dtype, device)
+        dev, tdt, code = p.device, _dev_dtype(dtype), _code(dtype)
+        self.table, self.dtable, self._table = p.add((vocab, width), decays=False)
+        self.experts = ExpertShard(p, tokens, width, shard, experts, top, act)
+        self.Wo, self.dWo, self._wo = p.add((shard, vocab))
+        self.bo, self.dbo, _ = p.add((vocab,), bias=True)
+        f32, i32 = dict(dtype=torch.float32, device=dev), dict(dtype=torch.int32, device=dev)
+        rows = lambda w: torch.empty((tokens, w), dtype=tdt, device=dev)
+        self.ids, self.targets = torch.zeros((tokens,), **i32), torch.zeros((tokens,), **i32)
+        self.dlogp, self.dentropy = torch.full((tokens,), -1.0 / tokens, **f32), torch.zeros((tokens,), **f32)
+        self.x, self.y, self.logits = rows(width), rows(shard), rows(vocab)
+        self.dx, self.dy = rows(width), rows(shard)
+        self.logp, self.entropy = torch.empty((tokens,), **f32), torch.empty((tokens,), **f32)
+        self.stats = torch.empty((tokens, 2), **f32)
+        self.top_ids = torch.empty((tokens, alternatives), **i32) if alternatives else None
+        self.top_values = torch.empty((tokens, alternatives), **f32) if alternatives else None
+        self.edesc = sb.embed_desc(tokens, vocab, width, code, scale=scale)
+        self.odesc = sb.fc_desc(tokens, shard, vocab, code)
+        self.tdesc = sb.token_logp_desc(tokens, vocab, alternatives, code)
+        need = max(sb.sb_embed_workspace_bytes(self.edesc), sb.sb_token_logp_workspace_bytes(self.tdesc),
+                   *(sb.sb_fc_workspace_bytes(self.odesc, q) for q in (sb.SB_FC_FWD, sb.SB_FC_BWD)))
+        self.ws = torch.empty((max(need, 256),), dtype=torch.uint8, device=dev)
+        self.updates = _Updates(p.items, adamw, copies=p.copies)
+
+    def forward(self, stream=None):
+        sb.sb_embed_fwd(self.edesc, self._table, self.ids, self.x, stream)
+        self.experts.forward(self.x, self.y, stream=stream)
+        sb.sb_fc_shard_fwd(self.odesc, self.y, self._wo, self.bo, self.logits, self.ws, stream)
+        sb.sb_token_logp_fwd(self.tdesc, self.logits, self.targets, self.logp, self.entropy,
+                             self.stats, self.top_ids, self.top_values, self.ws, stream)
+
+    def backward(self, stream=None):
+        sb.sb_token_logp_bwd(self.tdesc, self.logits, self.stats, self.targets, self.dlogp,
+                             self.entropy, self.dentropy, None, None, None, self.logits, stream)
+        sb.sb_fc_shard_bwd(self.odesc, self.y, self._wo, self.logits, None, self.dy, self.dWo,
+                           self.dbo, False, self.ws, stream)
+        self.experts.backward(self.x, self.dy, self.dx, stream)
+        sb.sb_embed_bwd(self.edesc, self.ids, self.dx, self.dtable, False, self.ws, stream)
+
+    def step(self, stream=None):
+        self.forward(stream)
+        self.backward(stream)
+        for _, fn, args in self.updates.calls("tokens", 0, None, stream):
+            fn(*args)

@@ -23,7 +23,7 @@ CALLS = {
     "sb_expert_sort": (EXPERT, ("ids", "place", "offsets"), ("place", "offsets"), (), False,
                        sb.sb_expert_workspace_bytes),
     "sb_expert_gather": (EXPERT, ("x", "place", "xs"), ("xs",), (), False, None),
-    "sb_expert_combine": (EXPERT, ("ys", "place", "weights", "y"), ("y",), ("weights",), False, None),
+    "sb_expert_combine": (EXPERT, ("ys", "place", "weights", "add", "y"), ("y",), ("weights", "add"), False, None),
     "sb_expert_combine_bwd": (EXPERT, ("dy", "ys", "place", "weights", "dys", "dweights"), ("dys", "dweights"),
                               ("weights", "dweights"), False, None),
     "sb_token_logp_fwd": (LOGP, ("z", "targets", "logp", "entropy", "stats", "top_ids", "top_values"),
@@ -110,7 +110,7 @@ def test_addresses_off_their_elements(name, t):
 def test_overlaps(name, a, b):
     at = P + CALLS[name][1].index(b) * GAP
     assert _call(name, **{a: at + 16}) == BAD
-    if (name, a, b) != ("sb_token_logp_bwd", "dz", "z"):
+    if (name, a, b) not in (("sb_token_logp_bwd", "dz", "z"), ("sb_expert_combine", "y", "add")):   # in place
         assert _call(name, **{a: at}) == BAD
 
 
@@ -137,7 +137,7 @@ def test_empty_batches_need_no_tensors():
     assert lib.sb_embed_fwd(ctypes.byref(e), None, None, None, None) == sb.SB_OK
     assert lib.sb_embed_bwd(ctypes.byref(e), None, None, P, 1, None, 0, None) == sb.SB_OK
     assert lib.sb_expert_gather(ctypes.byref(x), None, None, None, None) == sb.SB_OK
-    assert lib.sb_expert_combine(ctypes.byref(x), None, None, None, None, None) == sb.SB_OK
+    assert lib.sb_expert_combine(ctypes.byref(x), None, None, None, None, None, None) == sb.SB_OK
     assert lib.sb_expert_combine_bwd(ctypes.byref(x), None, None, None, None, None, None, None) == sb.SB_OK
     assert lib.sb_token_logp_fwd(ctypes.byref(z), *[None] * 7, None, 0, None) == sb.SB_OK
     assert lib.sb_token_logp_bwd(ctypes.byref(z), *[None] * 11) == sb.SB_OK

@@ -75,9 +75,9 @@ class Case:
         w = d["weights"] if weights else None
         sb.sb_expert_sort(self.desc, d["ids"], d["place"], d["offsets"], self.ws, stream)
         sb.sb_expert_gather(self.desc, d["x"], d["place"], d["xs"], stream)
-        sb.sb_expert_combine(self.desc, d["ys"], d["place"], w, d["y"], stream)
+        sb.sb_expert_combine(self.desc, d["ys"], d["place"], w, d["y"], stream=stream)
         sb.sb_expert_combine_bwd(self.desc, d["dy"], d["ys"], d["place"], w, d["dys"], d["dweights"], stream)
-        sb.sb_expert_combine(self.desc, d["dxs"], d["place"], None, d["dx"], stream)
+        sb.sb_expert_combine(self.desc, d["dxs"], d["place"], None, d["dx"], stream=stream)
 
     def get(self, k):
         return self.d[k].double().cpu().numpy()[:, :self.width]
@@ -117,6 +117,23 @@ def test_shapes(shape, dtype):
     c.run()
     c.check()
     c.untouched()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_combining_on_top_of_rows(dtype):
+    c = Case(dtype, *SHAPES[5])
+    c.run()
+    place, _ = X.sort(c.ids, c.first, c.experts)
+    add, ys = c.h["dy"][:, :c.width], c.h["ys"][:, :c.width]
+    ref = X.combine(ys, place, c.weights, add)
+    lim = X.bounds(add, ys, place, c.weights, ys, dtype == "bf16", add)[0]
+    sb.sb_expert_combine(c.desc, c.d["ys"], c.d["place"], c.d["weights"], c.d["y"], c.d["dy"])
+    assert np.all(np.abs(c.get("y") - ref) <= lim)
+    c.untouched()
+    there = c.d["dy"].clone()                       # in place: what lies between the rows stays
+    sb.sb_expert_combine(c.desc, c.d["ys"], c.d["place"], c.d["weights"], there, there)
+    assert torch.equal(there[:, :c.width], c.d["y"][:, :c.width])
+    assert torch.equal(there[:, c.width:], c.d["dy"][:, c.width:])
 
 
 def test_without_weights_and_without_their_gradient():
