@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(
     ExpertRows b, const T* __restrict__ dy, const T* __restrict__ ys,
     const int32_t* __restrict__ place, const float* __restrict__ weights, T* __restrict__ dys,
     float* __restrict__ dweights) {
-  constexpr int N = Piece<T>::N;
+  constexpr int N = Piece<T>::N, AHEAD = 2;           // rows on their way at once
   const size_t t = ((size_t)blockIdx.x * 256 + threadIdx.x) >> b.rp.shift;
   const int lane = threadIdx.x & ((1 << b.rp.shift) - 1);
   if (t >= (size_t)b.n) return;
@@ -130,36 +130,50 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(
     g[u].raw = u4{0, 0, 0, 0};
     if (c < b.rp.pieces) g[u].load(from + (size_t)c * N, b.width - c * N);
   }
-  for (int j = 0; j < b.top; ++j) {
-    const uint32_t row = (uint32_t)place[t * b.top + j];
-    float dot = 0.f;
-    if (row < b.rows) {
-      const float w = weights ? weights[t * b.top + j] : 1.f;
-      for (int s = 0; s < b.rp.segs; ++s) {
+  for (int j0 = 0; j0 < b.top; j0 += AHEAD) {
+    uint32_t row[AHEAD];
+    float w[AHEAD], dot[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const bool there = j0 + j < b.top;
+      row[j] = there ? (uint32_t)place[t * b.top + j0 + j] : ~0u;
+      w[j] = there && weights ? weights[t * b.top + j0 + j] : 1.f;
+      dot[j] = 0.f;
+    }
+    for (int s = 0; s < b.rp.segs; ++s) {
+      Piece<T> o[AHEAD][U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = lane + ((s * U + u) << b.rp.shift), left = b.width - c * N;
+        if (c >= b.rp.pieces) continue;
+        if (b.rp.segs > 1) g[u].load(from + (size_t)c * N, left);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+          if (dweights && row[j] < b.rows) o[j][u].load(ys + row[j] * (size_t)b.ldr + (size_t)c * N, left);
+      }
+#pragma unroll
+      for (int j = 0; j < AHEAD; ++j) {
+        if (row[j] >= b.rows) continue;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int c = lane + ((s * U + u) << b.rp.shift);
           if (c >= b.rp.pieces) continue;
-          const int left = b.width - c * N;
-          const size_t at = row * (size_t)b.ldr + (size_t)c * N;
-          Piece<T> d = g[u], o;
-          if (b.rp.segs > 1) d.load(from + (size_t)c * N, left);
-          if (dweights) {
-            o.load(ys + at, left);
-#pragma unroll
-            for (int e = 0; e < N; ++e) dot = fmaf(d.get(e), o.get(e), dot);
-          }
           float v[N];
 #pragma unroll
-          for (int e = 0; e < N; ++e) v[e] = d.get(e) * w;
-          o.set(v);
-          o.template store<true>(dys + at, left);
+          for (int e = 0; e < N; ++e) {
+            if (dweights) dot[j] = fmaf(g[u].get(e), o[j][u].get(e), dot[j]);
+            v[e] = g[u].get(e) * w[j];
+          }
+          o[j][u].set(v);
+          o[j][u].template store<true>(dys + row[j] * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
         }
       }
     }
-    if (dweights) {
-      for (int o = 1; o < 1 << b.rp.shift; o *= 2) dot += __shfl_xor(dot, o, 64);
-      if (lane == 0) dweights[t * b.top + j] = dot;
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      if (!dweights || j0 + j >= b.top) continue;
+      for (int o = 1; o < 1 << b.rp.shift; o *= 2) dot[j] += __shfl_xor(dot[j], o, 64);
+      if (lane == 0) dweights[t * b.top + j0 + j] = dot[j];
     }
   }
 }

@@ -10,9 +10,10 @@
 //   dz_c = sum of g at c - p_c (sum of all g + dH (logp_c + H)).
 //
 // Rows of up to 1024 classes (a router's): 8 to 64 lanes have a row in registers and do
-// everything in one launch.  Longer rows are cut into stretches, one a wave, held in
-// registers so that z is read once: maximum, sums, and the stretch's best classes; a
-// second launch joins a row's stretches.  Sums run in a fixed order.
+// everything in one launch.  Longer rows are cut into stretches, each held in a wave's
+// registers so that z is read once: maximum, sums, and the stretch's best classes.  A
+// block's waves have a row's stretches and join them in LDS; few very long rows have theirs
+// over the whole chip, joined by a second launch.  Sums run in a fixed order.
 //
 // The best `top` classes of a stretch: every lane's maximum is known, and the
 // top-th largest of those 64 is a bound that at least `top` elements reach and few
@@ -383,16 +384,11 @@ __device__ __forceinline__ void stretch_sums(const Piece<T>* p, float mx, float 
   s = kLn2 * (fix * fmaf(-err, sx, sy));
 }
 
+// A stretch by one wave: its maximum and sums to part[3], its best classes to keys[top].
 template <typename T, int P>
-__global__ __launch_bounds__(256) void logp_stretch_fwd(LogpFwd b, const T* __restrict__ z) {
-  constexpr int N = Piece<T>::N, E = P * N;
-  __shared__ uint64_t list[4][kTopList];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const size_t unit = (size_t)blockIdx.x * 4 + wave;
-  const size_t row = unit / (unsigned)b.stretches;
-  if (row >= (size_t)b.m) return;
-  const int first = (int)(unit - row * b.stretches) * (E * 64);
-  const T* zr = z + row * (size_t)b.ldz;
+__device__ __forceinline__ void stretch(const LogpFwd& b, const T* zr, int first, int lane,
+                                        uint64_t* list, float* part, uint64_t* keys) {
+  constexpr int N = Piece<T>::N;
   Piece<T> p[P];
   load_row<T, P>(zr, b.classes, first, lane, 64, p);
   float best[P], lm = 0.f;
@@ -409,7 +405,7 @@ __global__ __launch_bounds__(256) void logp_stretch_fwd(LogpFwd b, const T* __re
   const bool plain = mx > kLeastPlain && mx < INFINITY;    // not where a NaN is
   float o, s;
   if (plain) {
-    stretch_sums<T, P>(p, mx, lm, lane, reinterpret_cast<u4*>(list[wave]), o, s);
+    stretch_sums<T, P>(p, mx, lm, lane, reinterpret_cast<u4*>(list), o, s);
   } else {
     int equal;
     lane_sums<T, P>(p, mx, o, s, equal);
@@ -419,13 +415,11 @@ __global__ __launch_bounds__(256) void logp_stretch_fwd(LogpFwd b, const T* __re
     if (mx != -INFINITY) o += others;
   }
   if (lane == 0) {
-    float* q = b.part + unit * 3;
-    q[0] = mx;
-    q[1] = o;
-    q[2] = s;
+    part[0] = mx;
+    part[1] = o;
+    part[2] = s;
   }
-  if (b.top)
-    stretch_top<T, P>(b, zr, p, best, lm, plain, first, lane, list[wave], b.keys + unit * b.top);
+  if (b.top) stretch_top<T, P>(b, zr, p, best, lm, plain, first, lane, list, keys);
 }
 
 // Outputs of one of a row's best classes.
@@ -437,22 +431,20 @@ __device__ __forceinline__ void give_top(const LogpFwd& b, const RowSums& r, siz
 }
 
 // One wave joins a row's stretches.  A stretch's list is in order: with d = `depth` and q
-// lists of which the d-th entry reaches a bound, q d classes do.
+// lists of which the d-th entry reaches a bound, q d classes do.  counter: LDS.
 template <typename T>
-__global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict__ z) {
-  __shared__ uint64_t all_lists[4][kTopList];
-  __shared__ int counts[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const size_t row = (size_t)blockIdx.x * 4 + wave;
-  if (row >= (size_t)b.m) return;
-  const float* part = b.part + row * b.stretches * 3;
-  const uint64_t* keys = b.keys + row * b.stretches * b.top;
+__device__ __forceinline__ void join_row(const LogpFwd& b, const T* zr, size_t row,
+                                         const float* part, const uint64_t* keys, int lane,
+                                         uint64_t* list, int* counter) {
+  const int target = b.logp ? b.targets[row] : -1;
+  // (Read ahead of the sums; a class past the row is told by its number later.)
+  const float zt = target >= 0 && target < b.classes ? Elem<T>::load(zr, target) : 0.f;
   const int lists = min(b.stretches, 64);
   const int depth = min(b.top, max(1, (2 * b.top + lists - 1) / lists));
   uint64_t deep = 0;                            // the best d-th entry of the lane's lists
   if (b.top)
     for (int p = lane; p < b.stretches; p += 64) deep = max(deep, keys[(size_t)p * b.top + depth - 1]);
-  if (lane == 0) counts[wave] = 0;
+  if (lane == 0) *counter = 0;
   float mx = -INFINITY;
   for (int p = lane; p < b.stretches; p += 64) mx = maximum(mx, part[p * 3]);
   const float all = group_max(mx, 64);
@@ -475,25 +467,22 @@ __global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict_
     b.stats[row * 2] = r.mx;
     b.stats[row * 2 + 1] = r.ls;
     if (b.entropy) b.entropy[row] = r.h;
-    if (b.logp)
-      b.logp[row] = target_logp(r, z + row * (size_t)b.ldz, b.targets ? b.targets[row] : -1,
-                                b.classes);
+    if (b.logp) b.logp[row] = target < 0 ? 0.f : target >= b.classes ? NAN : row_logp(r, zt);
   }
   if (!b.top) return;
-  uint64_t* list = all_lists[wave];
   const uint32_t bound = wave_kth((uint32_t)(deep >> 32), (b.top + depth - 1) / depth);
   for (int p = lane; p < b.stretches; p += 64) {
     for (int at = 0; at < b.top; ++at) {
       const uint64_t key = keys[(size_t)p * b.top + at];
       if (key == 0 || (uint32_t)(key >> 32) < bound) break;
       // (Their order in the list does not matter: every one is ranked.)
-      const int to = atomicAdd(&counts[wave], 1);
+      const int to = atomicAdd(counter, 1);
       if (to < kTopList) list[to] = key;
     }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  const int count = counts[wave];
+  const int count = *counter;
   if (count <= kTopList) {
     rank_list(list, count, b.top, lane,
               [&](int rank, uint64_t key) { give_top(b, r, row, rank, key); });
@@ -516,6 +505,61 @@ __global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict_
     if (best == most && most) heads += 1ull << (8 * from);
     if (lane == 0) give_top(b, r, row, k, most);
   }
+}
+
+// A row by one block, a stretch a wave; the first wave joins them in LDS.
+struct RowShare {
+  size_t part, keys, bytes;    // offsets in LDS, behind a list for each wave
+};
+__host__ __device__ inline RowShare row_share(int waves, int stretches, int top) {
+  RowShare s;
+  s.keys = (size_t)waves * kTopList * 8;
+  s.part = s.keys + (size_t)stretches * top * 8;
+  s.bytes = s.part + ((size_t)stretches * 3 + 1) * 4;
+  return s;
+}
+
+template <typename T, int P>
+__global__ __launch_bounds__(1024) void logp_row_fwd(LogpFwd b, const T* __restrict__ z) {
+  constexpr int E = P * Piece<T>::N;
+  extern __shared__ uint64_t lists[];
+  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const RowShare at = row_share(waves, b.stretches, b.top);
+  uint64_t* keys = lists + at.keys / 8;
+  float* part = reinterpret_cast<float*>(lists) + at.part / 4;
+  const size_t row = blockIdx.x;
+  const T* zr = z + row * (size_t)b.ldz;
+  stretch<T, P>(b, zr, wave * (E * 64), lane, lists + wave * kTopList, part + wave * 3,
+                keys + wave * b.top);
+  __syncthreads();
+  if (wave) return;
+  join_row(b, zr, row, part, keys, lane, lists,
+           reinterpret_cast<int*>(part + b.stretches * 3));
+}
+
+// Few rows, long ones: a stretch a wave anywhere on the chip, joined by a second launch.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void logp_stretch_fwd(LogpFwd b, const T* __restrict__ z) {
+  constexpr int E = P * Piece<T>::N;
+  __shared__ uint64_t list[4][kTopList];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const size_t unit = (size_t)blockIdx.x * 4 + wave;
+  const size_t row = unit / (unsigned)b.stretches;
+  if (row >= (size_t)b.m) return;
+  const int first = (int)(unit - row * b.stretches) * (E * 64);
+  stretch<T, P>(b, z + row * (size_t)b.ldz, first, lane, list[wave], b.part + unit * 3,
+                b.keys + unit * b.top);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void logp_join(LogpFwd b, const T* __restrict__ z) {
+  __shared__ uint64_t list[4][kTopList];
+  __shared__ int counts[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const size_t row = (size_t)blockIdx.x * 4 + wave;
+  if (row >= (size_t)b.m) return;
+  join_row(b, z + row * (size_t)b.ldz, row, b.part + row * b.stretches * 3,
+           b.keys + row * b.stretches * b.top, lane, list[wave], &counts[wave]);
 }
 
 // ----------------------------------------------------------------- backward --
@@ -727,19 +771,34 @@ sb_status logp_check(const sb_token_logp_desc* d) {
   return SB_OK;
 }
 
-// 16-byte pieces of a row that a lane holds, and stretches of a row: long stretches
-// where there are rows enough for four waves on each SIMD, short ones else.
+// 16-byte pieces of a row that a lane holds, stretches of a row, and in the forward the
+// waves of a row's block (0: stretches anywhere, joined by a second launch).
 struct LogpPlan {
-  int pieces, stretches;
+  int pieces, stretches, waves;
 };
-LogpPlan logp_plan(const sb_token_logp_desc* d) {
+constexpr int kEnough = 4096;          // stretches: four waves for each SIMD
+
+LogpPlan logp_plan(const sb_token_logp_desc* d, bool fwd) {
   const int per = 64 * 16 / (int)sbh::dsize(d->dtype);
-  LogpPlan p{8, 0};
   auto stretches = [&](int pieces) { return sb::cdiv(d->classes, per * pieces); };
-  while (p.pieces > 1 && (int64_t)d->m * stretches(p.pieces) < 4096 &&
-         stretches(p.pieces / 2) <= sb::kMaxStretches)
+  LogpPlan p{8, stretches(8), 0};
+  const bool few = (int64_t)d->m * p.stretches < kEnough;
+  // A block a row saves the second launch: one row of 32000 bf16 8.4 us and not 4.2 + 4.4
+  // and the time between, 2048 rows 40.5 and not 38.0 + 4.9.  More than 8 waves a block
+  // hold up one another where there are many rows: 333 rows of 50001 fp32 in blocks of 13
+  // waves took 31 us, apart 17.5 + 6.1.
+  if (fwd && p.stretches <= (few ? 16 : 8)) {
+    while (few && p.pieces > 1 && stretches(p.pieces / 2) <= 16) p.pieces /= 2;
+    p.waves = p.stretches = stretches(p.pieces);
+    return p;
+  }
+  // Long stretches where there are enough of them (these 333 rows with 1, 2 and 8 pieces a
+  // lane: 35, 24 and 17.5 us), short ones else.
+  while (p.pieces > 1 && (int64_t)d->m * p.stretches < kEnough &&
+         stretches(p.pieces / 2) <= sb::kMaxStretches) {
     p.pieces /= 2;
-  p.stretches = stretches(p.pieces);
+    p.stretches = stretches(p.pieces);
+  }
   return p;
 }
 
@@ -763,6 +822,17 @@ sb_status logp_fwd(const sb_token_logp_desc* d, const sb::LogpFwd& b, const Logp
     const int shift = narrow_shift(d);
     const size_t blocks = (((size_t)d->m << shift) + 255) / 256;
     sb::logp_narrow_fwd<T><<<(unsigned)blocks, 256, 0, st>>>(b, shift, z);
+    return sbh::launch_status();
+  }
+  if (p.waves) {
+    const unsigned threads = 64 * p.waves;
+    const size_t lds = sb::row_share(p.waves, p.stretches, d->top).bytes;
+    switch (p.pieces) {
+      case 8: sb::logp_row_fwd<T, 8><<<d->m, threads, lds, st>>>(b, z); break;
+      case 4: sb::logp_row_fwd<T, 4><<<d->m, threads, lds, st>>>(b, z); break;
+      case 2: sb::logp_row_fwd<T, 2><<<d->m, threads, lds, st>>>(b, z); break;
+      default: sb::logp_row_fwd<T, 1><<<d->m, threads, lds, st>>>(b, z); break;
+    }
     return sbh::launch_status();
   }
   const size_t blocks = ((size_t)d->m * p.stretches + 3) / 4;
@@ -802,7 +872,8 @@ sb_status logp_bwd(const sb_token_logp_desc* d, const sb::LogpBwd& b, const Logp
 extern "C" size_t sb_token_logp_workspace_bytes(const sb_token_logp_desc* d) {
   if (logp_check(d) != SB_OK) return (size_t)-1;
   if (narrow(d) || d->m == 0) return 0;
-  const LogpPlan p = logp_plan(d);
+  const LogpPlan p = logp_plan(d, true);
+  if (p.waves) return 0;
   return logp_part_bytes(d, p) + sb::round_up((size_t)d->m * p.stretches * d->top * 8, 256);
 }
 
@@ -831,7 +902,7 @@ extern "C" sb_status sb_token_logp_fwd(const sb_token_logp_desc* d, const void* 
       if (sbh::overlaps(outs[i], ob[i], outs[j], ob[j])) return SB_ERR_INVALID_ARG;
   }
   if (need && (!workspace || workspace_bytes < need)) return SB_ERR_WORKSPACE;
-  const LogpPlan p = logp_plan(d);
+  const LogpPlan p = logp_plan(d, true);
   sb::LogpFwd b{};
   b.m = d->m;
   b.classes = d->classes;
@@ -874,7 +945,7 @@ extern "C" sb_status sb_token_logp_bwd(const sb_token_logp_desc* d, const void* 
   if (dz != z && sbh::overlaps(dz, zb, z, zb)) return SB_ERR_INVALID_ARG;
   for (int i = 0; i < 8; ++i)
     if (sbh::overlaps(dz, zb, ins[i], ib[i])) return SB_ERR_INVALID_ARG;
-  const LogpPlan p = logp_plan(d);
+  const LogpPlan p = logp_plan(d, false);
   sb::LogpBwd b{};
   b.m = d->m;
   b.classes = d->classes;

@@ -647,17 +647,26 @@ def sb_adamw_unpack(n, m, m_top, v, v_top, m_out, v_out, stream=None):
 _types = None                   # torch's types by sb_dtype, then int32
 
 
-def _kinds(dtype, rows=(), i32=(), f32=()):
-    """Tensors (not addresses) of a call have the descriptor's type, int32 and float32."""
+def _kinds(desc):
+    """The types of a call: the descriptor's, int32, float32."""
     global _types
     if _types is None:
         import torch
         _types = (torch.float32, torch.bfloat16, torch.int32)
-    for want, tensors in ((_types[dtype] if dtype in (SB_F32, SB_BF16) else None, rows),
-                          (_types[2], i32), (_types[0], f32)):
-        for t in tensors:
-            if t is not None and t.__class__ is not int and t.dtype is not want:
-                raise ValueError("a tensor of %s, expected %s" % (t.dtype, want))
+    return _types[desc.dtype if desc.dtype in (SB_F32, SB_BF16) else 0], _types[2], _types[0]
+
+
+def _at(t, kind):
+    """The address of a device tensor of that type, of None and of an address itself."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.dtype is not kind:
+        raise ValueError("a tensor of %s, expected %s" % (t.dtype, kind))
+    if not t.is_cuda:
+        raise ValueError("libsb takes device tensors")
+    if not t.is_contiguous():
+        raise ValueError("libsb takes contiguous tensors (strides go in the descriptor)")
+    return t.data_ptr()
 
 
 def embed_desc(tokens, vocab, width, dtype=SB_F32, first=0, ldy=None, scale=1.0):
@@ -671,18 +680,18 @@ def sb_embed_workspace_bytes(desc):
 
 def sb_embed_fwd(desc, table, ids, y, stream=None):
     """ids: int32."""
-    _kinds(desc.dtype, (table, y), (ids,))
+    row, i32, _ = _kinds(desc)
     _check("sb_embed_fwd", load().sb_embed_fwd(
-        ctypes.byref(desc), _ptr(table), _ptr(ids), _ptr(y), _stream_for(table, stream)))
+        ctypes.byref(desc), _at(table, row), _at(ids, i32), _at(y, row), _stream_for(table, stream)))
 
 
 def sb_embed_bwd(desc, ids, dy, dtable, accumulate=False, ws=None, stream=None):
     """dtable: fp32 [vocab][width]."""
     p, nb = _ws(ws)
-    _kinds(desc.dtype, (dy,), (ids,), (dtable,))
+    row, i32, f32 = _kinds(desc)
     _check("sb_embed_bwd", load().sb_embed_bwd(
-        ctypes.byref(desc), _ptr(ids), _ptr(dy), _ptr(dtable), 1 if accumulate else 0, p, nb,
-        _stream_for(dtable, stream)))
+        ctypes.byref(desc), _at(ids, i32), _at(dy, row), _at(dtable, f32), 1 if accumulate else 0,
+        p, nb, _stream_for(dtable, stream)))
 
 
 # ------------------------------------------------------------ expert rows --
@@ -698,32 +707,32 @@ def sb_expert_workspace_bytes(desc):
 def sb_expert_sort(desc, ids, place, offsets, ws=None, stream=None):
     """All int32: ids and place [tokens][top], offsets [experts + 1]."""
     p, nb = _ws(ws)
-    _kinds(desc.dtype, (), (ids, place, offsets))
+    i32 = _kinds(desc)[1]
     _check("sb_expert_sort", load().sb_expert_sort(
-        ctypes.byref(desc), _ptr(ids), _ptr(place), _ptr(offsets), p, nb,
+        ctypes.byref(desc), _at(ids, i32), _at(place, i32), _at(offsets, i32), p, nb,
         _stream_for(offsets, stream)))
 
 
 def sb_expert_gather(desc, x, place, xs, stream=None):
-    _kinds(desc.dtype, (x, xs), (place,))
+    row, i32, _ = _kinds(desc)
     _check("sb_expert_gather", load().sb_expert_gather(
-        ctypes.byref(desc), _ptr(x), _ptr(place), _ptr(xs), _stream_for(x, stream)))
+        ctypes.byref(desc), _at(x, row), _at(place, i32), _at(xs, row), _stream_for(x, stream)))
 
 
 def sb_expert_combine(desc, ys, place, weights, y, add=None, stream=None):
     """weights: fp32 [tokens][top], or None (1 each: the gather's backward); add: rows
     like y's that the sum starts from, or y itself."""
-    _kinds(desc.dtype, (ys, add, y), (place,), (weights,))
+    row, i32, f32 = _kinds(desc)
     _check("sb_expert_combine", load().sb_expert_combine(
-        ctypes.byref(desc), _ptr(ys), _ptr(place), _ptr(weights), _ptr(add), _ptr(y),
-        _stream_for(y, stream)))
+        ctypes.byref(desc), _at(ys, row), _at(place, i32), _at(weights, f32), _at(add, row),
+        _at(y, row), _stream_for(y, stream)))
 
 
 def sb_expert_combine_bwd(desc, dy, ys, place, weights, dys, dweights=None, stream=None):
-    _kinds(desc.dtype, (dy, ys, dys), (place,), (weights, dweights))
+    row, i32, f32 = _kinds(desc)
     _check("sb_expert_combine_bwd", load().sb_expert_combine_bwd(
-        ctypes.byref(desc), _ptr(dy), _ptr(ys), _ptr(place), _ptr(weights), _ptr(dys),
-        _ptr(dweights), _stream_for(dy, stream)))
+        ctypes.byref(desc), _at(dy, row), _at(ys, row), _at(place, i32), _at(weights, f32),
+        _at(dys, row), _at(dweights, f32), _stream_for(dy, stream)))
 
 
 # ------------------------------------------------- token log-probabilities --
@@ -741,18 +750,17 @@ def sb_token_logp_fwd(desc, z, targets, logp, entropy, stats, top_ids=None, top_
     """targets, top_ids: int32; logp, entropy, stats [m][2], top_values: fp32.
     targets, logp and entropy may be None."""
     p, nb = _ws(ws)
-    _kinds(desc.dtype, (z,), (targets, top_ids), (logp, entropy, stats, top_values))
+    row, i32, f32 = _kinds(desc)
     _check("sb_token_logp_fwd", load().sb_token_logp_fwd(
-        ctypes.byref(desc), _ptr(z), _ptr(targets), _ptr(logp), _ptr(entropy), _ptr(stats),
-        _ptr(top_ids), _ptr(top_values), p, nb, _stream_for(z, stream)))
+        ctypes.byref(desc), _at(z, row), _at(targets, i32), _at(logp, f32), _at(entropy, f32),
+        _at(stats, f32), _at(top_ids, i32), _at(top_values, f32), p, nb, _stream_for(z, stream)))
 
 
 def sb_token_logp_bwd(desc, z, stats, targets, dlogp, entropy, dentropy, top_ids, top_values, dtop,
                       dz, stream=None):
     """dlogp, dentropy and dtop, and what they go with, may be None; dz may be z."""
-    _kinds(desc.dtype, (z, dz), (targets, top_ids),
-           (stats, dlogp, entropy, dentropy, top_values, dtop))
+    row, i32, f32 = _kinds(desc)
     _check("sb_token_logp_bwd", load().sb_token_logp_bwd(
-        ctypes.byref(desc), _ptr(z), _ptr(stats), _ptr(targets), _ptr(dlogp), _ptr(entropy),
-        _ptr(dentropy), _ptr(top_ids), _ptr(top_values), _ptr(dtop), _ptr(dz),
-        _stream_for(z, stream)))
+        ctypes.byref(desc), _at(z, row), _at(stats, f32), _at(targets, i32), _at(dlogp, f32),
+        _at(entropy, f32), _at(dentropy, f32), _at(top_ids, i32), _at(top_values, f32),
+        _at(dtop, f32), _at(dz, row), _stream_for(z, stream)))

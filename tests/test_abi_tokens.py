@@ -16,7 +16,7 @@ WS = P + 30 * GAP
 #        tensors that may be NULL, whether `accumulate` follows, the workspace's size or None)
 EMBED = (sb.embed_desc, dict(tokens=9000, vocab=50, width=24, first=10, ldy=32))
 EXPERT = (sb.expert_desc, dict(tokens=9000, top=2, experts=6, width=24, first=3, ldx=32, ldr=40))
-LOGP = (sb.token_logp_desc, dict(m=50, classes=2000, top=4, ldz=2048, probs=True))
+LOGP = (sb.token_logp_desc, dict(m=5, classes=300000, top=4, ldz=300032, probs=True))
 CALLS = {
     "sb_embed_fwd": (EMBED, ("table", "ids", "y"), ("y",), (), False, None),
     "sb_embed_bwd": (EMBED, ("ids", "dy", "dtable"), ("dtable",), (), True, sb.sb_embed_workspace_bytes),
@@ -65,7 +65,7 @@ BAD_DESCS = (
         dict(tokens=-1), dict(top=0), dict(experts=0), dict(experts=513), dict(width=0), dict(first=-1),
         dict(dtype=-1), dict(ldx=23), dict(ldr=23), dict(first=2 ** 31 - 6))] +
     [(n, o) for n in NAMES if "logp" in n for o in (
-        dict(m=-1), dict(classes=0), dict(ldz=1999), dict(top=-1), dict(top=33), dict(classes=3), dict(dtype=2),
+        dict(m=-1), dict(classes=0), dict(ldz=299999), dict(top=-1), dict(top=33), dict(classes=3), dict(dtype=2),
         dict(flags=1))])
 
 
