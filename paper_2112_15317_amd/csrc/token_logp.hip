@@ -30,6 +30,7 @@ constexpr int kTopList = 256;          // classes of a stretch that are ranked i
 constexpr int kMaxStretches = 512;     // of a row
 constexpr int kNarrow = 1024;          // classes of a row in one launch
 constexpr int kNarrowElems = 16;       // of a lane there
+constexpr int kMoreTop = 2;            // fp32 classes there that are ranked beside the best
 template <typename T> constexpr int kNarrowPieces = kNarrowElems / Piece<T>::N;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLeastPower = -1000.f; // in place of masked elements' -inf: 0 times it is 0
@@ -205,11 +206,48 @@ __device__ __forceinline__ int class_at(int first, int lane, int lanes, int e) {
   return first + (lane + e / N * lanes) * N + e % N;
 }
 
+// Outputs of one of a row's best classes.
+__device__ __forceinline__ void give_top(const LogpFwd& b, const RowSums& r, size_t row, int rank,
+                                         uint64_t key) {
+  const float lp = row_logp(r, value_of((uint32_t)(key >> 32)));
+  b.top_ids[row * b.top + rank] = (int32_t)class_of(key);
+  b.top_values[row * b.top + rank] = b.probs ? expf(lp) : lp;
+}
+
 // ------------------------------------------------------------- narrow rows --
+// The best classes one after another, whatever the logits.
+template <typename T>
+__device__ __forceinline__ void narrow_top_exact(const LogpFwd& b, const RowSums& r, const T* zr,
+                                                 size_t row, int lane, int lanes) {
+  constexpr int N = Piece<T>::N, E = kNarrowElems;
+  Piece<T> p[E / N];
+  load_row<T, E / N>(zr, b.classes, 0, lane, lanes, p);
+  uint32_t order[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e)
+    order[e] = class_at<T>(0, lane, lanes, e) < b.classes ? order_of(p[e / N].get(e % N)) : 0;
+#pragma unroll 1
+  for (int k = 0; k < b.top; ++k) {
+    uint32_t best = order[0];
+#pragma unroll
+    for (int e = 1; e < E; ++e) best = max(best, order[e]);
+    int at = 0;                               // the first of them: classes grow with e
+#pragma unroll
+    for (int e = E - 1; e >= 0; --e) at = order[e] == best ? e : at;
+    const uint64_t key = best ? key_of(best, class_at<T>(0, lane, lanes, at)) : 0;
+    const uint64_t most = group_max(key, lanes);
+    const int gone = key == most ? at : -1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) order[e] = e == gone ? 0 : order[e];
+    if (lane == (k & (lanes - 1))) give_top(b, r, row, k, most);
+  }
+}
+
 template <typename T>
 __global__ __launch_bounds__(256) void logp_narrow_fwd(LogpFwd b, int shift,
                                                        const T* __restrict__ z) {
   constexpr int N = Piece<T>::N, P = kNarrowPieces<T>, E = P * N;
+  __shared__ uint64_t lists[256 / 8][SB_LOGP_MAX_TOP + kMoreTop];
   const int lanes = 1 << shift, lane = threadIdx.x & (lanes - 1);
   const size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) >> shift;
   if (row >= (size_t)b.m) return;             // whole groups leave together
@@ -238,33 +276,49 @@ __global__ __launch_bounds__(256) void logp_narrow_fwd(LogpFwd b, int shift,
     if (b.logp) b.logp[row] = target_logp(r, zr, b.targets ? b.targets[row] : -1, b.classes);
   }
   if (!b.top) return;
-  uint32_t order[E];
+  // Logit and class in one number, the class in its lowest bits: no two are equal, and the next
+  // best is what lies closest below the last one.  A bf16 logit has room beside a class; an
+  // fp32 one loses bits, so two more than `top` are taken and ranked by all they have.  Where
+  // the last of them does not lie below the best ones in the bits that are left, the wave
+  // takes the slow way (one such wave and the launch would wait for it).
+  constexpr bool whole = std::is_same<T, u16>::value;
+  const uint32_t mask = whole ? 0xffffu : (uint32_t)(E * lanes) - 1;
+  const int taken = whole ? b.top : min(b.top + kMoreTop, b.classes);
+  uint32_t key[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e)
-    order[e] = class_at<T>(0, lane, lanes, e) < b.classes ? order_of(v[e]) : 0;
-  uint64_t kept = 0;                          // by lane j: the best class j of those at hand
-  for (int k = 0; k < b.top; ++k) {
-    uint32_t best = order[0];
+  for (int e = 0; e < E; ++e)                 // (past the row: -inf behind any class of it)
+    key[e] = (order_of(v[e]) & ~mask) | (mask - class_at<T>(0, lane, lanes, e));
+  uint64_t* list = lists[threadIdx.x >> shift];
+  uint32_t last = 0, kept = 0;                // by lane j: the best class j of those at hand
+  for (int k = 0; k < taken; ++k) {
+    uint32_t most = key[0] - last;            // (first: all of them are above 0)
 #pragma unroll
-    for (int e = 1; e < E; ++e) best = max(best, order[e]);
-    int at = 0;                               // the first of them: classes grow with e
-#pragma unroll
-    for (int e = E - 1; e >= 0; --e) at = order[e] == best ? e : at;
-    const uint64_t key = best ? key_of(best, class_at<T>(0, lane, lanes, at)) : 0;
-    const uint64_t most = group_max(key, lanes);
-    const int gone = key == most ? at : -1;
-#pragma unroll
-    for (int e = 0; e < E; ++e) order[e] = e == gone ? 0 : order[e];
+    for (int e = 1; e < E; ++e) most = max(most, key[e] - last);
+    last += group_max(most, lanes);
     const int j = k & (lanes - 1);
-    if (lane == j) kept = most;
-    if (j != lanes - 1 && k != b.top - 1) continue;
+    if (lane == j) kept = last;
+    if (j != lanes - 1 && k != taken - 1) continue;
     if (lane <= j) {
-      const size_t to = row * b.top + k - j + lane;
-      const float lp = row_logp(r, value_of((uint32_t)(kept >> 32)));
-      b.top_ids[to] = (int32_t)class_of(kept);
-      b.top_values[to] = b.probs ? expf(lp) : lp;
+      const uint32_t c = mask - (kept & mask);
+      const uint64_t full = key_of(order_of(Elem<T>::load(zr, c)), c);
+      if constexpr (whole) give_top(b, r, row, k - j + lane, full);
+      else list[k - j + lane] = full;
     }
   }
+  if constexpr (whole) return;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  bool sure = true;
+  for (int i = lane; i < taken; i += lanes) {
+    const uint64_t mine = list[i];
+    int rank = 0;
+    for (int j = 0; j < taken; ++j) rank += list[j] > mine ? 1 : 0;
+    if (rank < b.top) give_top(b, r, row, rank, mine);
+    if (rank == b.top - 1)
+      sure = taken == b.classes || ((uint32_t)(mine >> 32) & ~mask) > (last & ~mask);
+  }
+  if (__all(sure)) return;
+  narrow_top_exact(b, r, zr, row, lane, lanes);
 }
 
 // ---------------------------------------------------------------- long rows --
@@ -420,14 +474,6 @@ __device__ __forceinline__ void stretch(const LogpFwd& b, const T* zr, int first
     part[2] = s;
   }
   if (b.top) stretch_top<T, P>(b, zr, p, best, lm, plain, first, lane, list, keys);
-}
-
-// Outputs of one of a row's best classes.
-__device__ __forceinline__ void give_top(const LogpFwd& b, const RowSums& r, size_t row, int rank,
-                                         uint64_t key) {
-  const float lp = row_logp(r, value_of((uint32_t)(key >> 32)));
-  b.top_ids[row * b.top + rank] = (int32_t)class_of(key);
-  b.top_values[row * b.top + rank] = b.probs ? expf(lp) : lp;
 }
 
 // One wave joins a row's stretches.  A stretch's list is in order: with d = `depth` and q
