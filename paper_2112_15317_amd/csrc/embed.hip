@@ -89,7 +89,7 @@ __device__ __forceinline__ int slot_from(const EmbedBwd& b, uint32_t key, int lo
 // Zeros in those of the kAbsent rows from v0 on that have no token; one wave.
 constexpr int kAbsent = 64;
 __device__ __forceinline__ void fill_absent(const EmbedBwd& b, int v0, int lane) {
-  const int v1 = min(b.vocab, v0 + kAbsent);
+  const int rows = min(b.vocab - v0, kAbsent);
   uint32_t lo = 0, hi = 0;                          // a bit for each row with a token
   for (int j = slot_from(b, v0, 0, lane); j < b.n;) {
     const uint32_t key = j + lane < b.n ? b.slots[j + lane].x : ~0u;
@@ -103,18 +103,17 @@ __device__ __forceinline__ void fill_absent(const EmbedBwd& b, int v0, int lane)
     lo |= l;
     hi |= h;
     const uint32_t first = __shfl((int)key, 0, 64), last = __shfl((int)key, 63, 64);
-    if (last >= (uint32_t)v1) break;
+    if (last - v0 >= (uint32_t)rows) break;
     j = first == last ? slot_from(b, first + 1, j + 64, lane) : j + 64;
   }
   const int pieces = cdiv(b.width, 4);
   const int shift = pieces >= 64 ? 6 : 32 - __clz((pieces - 1) | 1);    // lanes of a row
-  for (int v = v0 + (lane >> shift); v < v1; v += 64 >> shift) {
-    const int at = v - v0;
+  for (int at = lane >> shift; at < rows; at += 64 >> shift) {
     if ((at < 32 ? lo >> at : hi >> (at - 32)) & 1) continue;
     for (int c = lane & ((1 << shift) - 1); c < pieces; c += 1 << shift) {
       Piece<float> p;
       p.raw = u4{0, 0, 0, 0};
-      p.store(b.dtable + (size_t)v * b.width + c * 4, b.width - c * 4);
+      p.store(b.dtable + (size_t)(v0 + at) * b.width + c * 4, b.width - c * 4);
     }
   }
 }

@@ -34,7 +34,7 @@ constexpr int kMoreTop = 2;            // fp32 classes there that are ranked bes
 template <typename T> constexpr int kNarrowPieces = kNarrowElems / Piece<T>::N;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLeastPower = -1000.f; // in place of masked elements' -inf: 0 times it is 0
-constexpr float kLeastPlain = -1e30f;  // smaller maxima take the careful sums
+constexpr float kMostPlain = 1e30f;    // larger maxima, of either sign, take the careful sums
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -318,6 +318,7 @@ __global__ __launch_bounds__(256) void logp_narrow_fwd(LogpFwd b, int shift,
       sure = taken == b.classes || ((uint32_t)(mine >> 32) & ~mask) > (last & ~mask);
   }
   if (__all(sure)) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // it writes there again
   narrow_top_exact(b, r, zr, row, lane, lanes);
 }
 
@@ -456,7 +457,7 @@ __device__ __forceinline__ void stretch(const LogpFwd& b, const T* zr, int first
     asm volatile("" : "+v"(p[u].raw));
   }
   const float mx = group_max(lm, 64);
-  const bool plain = mx > kLeastPlain && mx < INFINITY;    // not where a NaN is
+  const bool plain = fabsf(mx) < kMostPlain;       // not where a NaN is
   float o, s;
   if (plain) {
     stretch_sums<T, P>(p, mx, lm, lane, reinterpret_cast<u4*>(list), o, s);
@@ -670,7 +671,7 @@ struct PlainGrad {
 
 // Whether a row takes PlainGrad: ordinary stats and no target past the classes.
 __device__ __forceinline__ bool is_plain(const RowGrad& r) {
-  return fabsf(r.mx) < -kLeastPlain && r.ls == r.ls && !r.bad;
+  return fabsf(r.mx) < kMostPlain && r.ls == r.ls && !r.bad;
 }
 // N elements of such a row, or of any other one.
 template <int N, typename T>

@@ -23,7 +23,8 @@ SHAPES = [(1, 1, 0, 0, 1, False, "normal"), (3, 2, 1, 1, 2, True, "normal"), (70
           (3, 50001, 7, 1, 32, False, "masked"), (2, 4096, 0, 0, 20, True, "equal"), (6, 4097, 0, 0, 32, False, "ties"),
           (530, 5000, 0, 0, 3, False, "sure"), (1100, 4200, 0, 1, 0, False, "masked"), (2, 300000, 0, 0, 32, False, "ties"),
           (1, 1 << 20, 0, 0, 9, False, "normal"), (8, 2500, 0, 0, 32, False, "rising"), (4, 33000, 0, 0, 32, False, "falling"),
-          (4100, 1040, 8, 0, 2, True, "normal"), (1300, 9000, 0, 0, 32, False, "wide")]
+          (65, 128, 0, 0, 8, True, "close"), (13, 700, 3, 1, 32, False, "close"), (6, 6000, 0, 0, 20, False, "close"),
+          (9, 30, 0, 0, 29, True, "close"), (4100, 1040, 8, 0, 2, True, "normal"), (1300, 9000, 0, 0, 32, False, "wide")]
 
 
 def _logits(kind, r, m, n):
@@ -42,6 +43,8 @@ def _logits(kind, r, m, n):
         z = np.linspace(-5, 5, n) + np.zeros((m, 1))
     elif kind == "falling":
         z = np.linspace(5, -5, n) + np.zeros((m, 1))
+    elif kind == "close":                       # fp32's last bits decide
+        z = 1.0 + r.integers(0, 4000, (m, n)) * 2.0 ** -23
     elif kind == "wide":                        # the type's ends as masks
         z[:, ::3] = -3.38e38
         z[::5] -= 60.0
@@ -209,8 +212,10 @@ def test_special_rows(n, dtype):
     z[8, :] = -np.inf
     z[8, 7] = np.nan
     z[9, 5] = z[9, n - 2] = np.inf
-    t = np.array([3, n - 1, 4, 5, 5, 0, 9, -1, 2, 5, n, 2 ** 31 - 1])
-    c = Case(dtype, 12, n, 0, 0, 6, False, None, z=z, targets=t)
+    z = np.concatenate([z, np.full((2, n), 3.38e38, np.float32)])      # all the same, and largest but one half
+    z[13, ::2] = 1e30
+    t = np.array([3, n - 1, 4, 5, 5, 0, 9, -1, 2, 5, n, 2 ** 31 - 1, 8, 1])
+    c = Case(dtype, 14, n, 0, 0, 6, False, None, z=z, targets=t)
     c.fwd()
     c.bwd()
     torch.cuda.synchronize()
@@ -222,8 +227,8 @@ def test_special_rows(n, dtype):
         assert np.array_equal(np.isnan(got), np.isnan(ref)), (k, np.argwhere(np.isnan(got) != np.isnan(ref))[:4])
         assert np.array_equal(got == -np.inf, ref == -np.inf), k
     # What is finite in those rows is as everywhere.
-    keep = [0, 1, 5, 6, 7]
-    s = Case(dtype, 5, n, 0, 0, 6, False, None, z=z[keep], targets=t[keep])
+    keep = [0, 1, 5, 6, 7, 12, 13]
+    s = Case(dtype, 7, n, 0, 0, 6, False, None, z=z[keep], targets=t[keep])
     s.fwd()
     s.bwd()
     s.check(FWD + ("top_ids", "dz"))
