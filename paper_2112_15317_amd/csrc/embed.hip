@@ -9,15 +9,19 @@
 // The gradient sorts the tokens by id (slot_sort.hpp), so that each row of the table
 // is summed by one lane group in the tokens' order: no atomics, the same result in
 // every run.  Words in use are few and some of them are in every sentence, so the
-// work is split by sorted tokens, not by rows of the table: a group takes kRun
+// work is split by sorted tokens, not by rows of the table: a group takes 8 to 64
 // tokens in a row; an id's tokens that go past a group's end leave partial sums
-// (fp32, at most two a group), which a last launch joins in order.  Rows without a
-// token are zeroed beside the sort where that is one launch (and every row is), beside
-// the sums else: 65536 tokens of a table of 131072 x 2048 name a quarter of its rows, and
-// zeroing these too would be a sixth of all traffic.
+// (fp32, at most two a group), which a last launch joins in order.  Rows are zeroed beside
+// a sort of one launch (the first 48 MB, which the sort of 4099 ids does not wait for), and
+// beside the sums those of the others that have no token: 65536 tokens of a table of 131072 x
+// 2048 name a quarter of its rows, and zeroing these too would be a sixth of all traffic.
+//
+// Up to kFewTokens tokens it is one launch without a sort: a wave has a token's columns,
+// compares its id with all others, and where it is the first with that id sums all of them.
 #include "rows.hpp"
 #include "slot_sort.hpp"
 
+#include <algorithm>
 #include <cmath>
 
 namespace sb {
@@ -65,6 +69,7 @@ struct EmbedBwd {
   int n, vocab, width, ldy;
   int run, runs;               // sorted tokens of a group; groups along them
   int sum_blocks;
+  int absent0;                 // first of the rows that are zeroed beside the sums
   float scale;
   int accumulate;
   float* dtable;
@@ -86,30 +91,22 @@ __device__ __forceinline__ int slot_from(const EmbedBwd& b, uint32_t key, int lo
   return lo;
 }
 
-// Zeros in those of the kAbsent rows from v0 on that have no token; one wave.
-constexpr int kAbsent = 64;
-__device__ __forceinline__ void fill_absent(const EmbedBwd& b, int v0, int lane) {
-  const int rows = min(b.vocab - v0, kAbsent);
-  uint32_t lo = 0, hi = 0;                          // a bit for each row with a token
-  for (int j = slot_from(b, v0, 0, lane); j < b.n;) {
-    const uint32_t key = j + lane < b.n ? b.slots[j + lane].x : ~0u;
-    const uint32_t at = key - v0;
-    uint32_t l = at < 32 ? 1u << at : 0, h = at - 32 < 32 ? 1u << (at - 32) : 0;
+// A bit for each of the kAbsent rows that a lane's `at` names, over the wave.  (Sixteen: a
+// wave with 64 rows of 741 held up a launch of 8 us for 26.)
+constexpr int kAbsent = 16;
+__device__ __forceinline__ uint32_t named_rows(uint32_t at) {
+  uint32_t bits = at < kAbsent ? 1u << at : 0;
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-      l |= __shfl_xor((int)l, o, 64);
-      h |= __shfl_xor((int)h, o, 64);
-    }
-    lo |= l;
-    hi |= h;
-    const uint32_t first = __shfl((int)key, 0, 64), last = __shfl((int)key, 63, 64);
-    if (last - v0 >= (uint32_t)rows) break;
-    j = first == last ? slot_from(b, first + 1, j + 64, lane) : j + 64;
-  }
-  const int pieces = cdiv(b.width, 4);
+  for (int o = 1; o < 64; o *= 2) bits |= __shfl_xor((int)bits, o, 64);
+  return bits;
+}
+
+// Zeros in those of the kAbsent rows from v0 on that are not named; one wave.
+__device__ __forceinline__ void zero_rows(const EmbedBwd& b, int v0, uint32_t named, int lane) {
+  const int rows = min(b.vocab - v0, kAbsent), pieces = cdiv(b.width, 4);
   const int shift = pieces >= 64 ? 6 : 32 - __clz((pieces - 1) | 1);    // lanes of a row
   for (int at = lane >> shift; at < rows; at += 64 >> shift) {
-    if ((at < 32 ? lo >> at : hi >> (at - 32)) & 1) continue;
+    if (named >> at & 1) continue;
     for (int c = lane & ((1 << shift) - 1); c < pieces; c += 1 << shift) {
       Piece<float> p;
       p.raw = u4{0, 0, 0, 0};
@@ -118,12 +115,101 @@ __device__ __forceinline__ void fill_absent(const EmbedBwd& b, int v0, int lane)
   }
 }
 
+__device__ __forceinline__ void fill_absent(const EmbedBwd& b, int v0, int lane) {
+  const int rows = min(b.vocab - v0, kAbsent);
+  uint32_t named = 0;
+  for (int j = slot_from(b, v0, 0, lane); j < b.n;) {
+    const uint32_t key = j + lane < b.n ? b.slots[j + lane].x : ~0u;
+    named |= named_rows(key - v0);
+    const uint32_t first = __shfl((int)key, 0, 64), last = __shfl((int)key, 63, 64);
+    if (last - v0 >= (uint32_t)rows) break;
+    j = first == last ? slot_from(b, first + 1, j + 64, lane) : j + 64;
+  }
+  zero_rows(b, v0, named, lane);
+}
+
+// N columns of a row of the gradient from their sum.
+template <int N>
+__device__ __forceinline__ void give_row(const EmbedBwd& b, float* out, int left, const float* acc) {
+#pragma unroll
+  for (int q = 0; q < N; q += 4) {
+    Piece<float> o;
+    if (b.accumulate) o.load(out + q, left - q);
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      v[e] = b.accumulate ? fmaf(acc[q + e], b.scale, o.get(e)) : acc[q + e] * b.scale;
+    o.set(v);
+    o.store(out + q, left - q);
+  }
+}
+
+// Few tokens: waves 0 .. n * segs - 1 have a token's columns each, the others rows to zero.
+constexpr int kFewTokens = 128;
+template <typename T>
+__global__ __launch_bounds__(256) void embed_few_kernel(EmbedBwd b, int first, int segs,
+                                                        const int32_t* __restrict__ ids,
+                                                        const T* __restrict__ dy) {
+  constexpr int N = Piece<T>::N, AHEAD = 4;
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  uint32_t key[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int j = h * 64 + lane, id = j < b.n ? ids[j] : -1;
+    key[h] = id >= first && (uint32_t)(id - first) < (uint32_t)b.vocab ? id - first : ~0u;
+  }
+  const int64_t zeros = unit - (int64_t)b.n * segs;
+  if (zeros >= 0) {
+    const int64_t v0 = zeros * kAbsent;
+    if (b.accumulate || v0 >= b.vocab) return;
+    zero_rows(b, (int)v0, named_rows(key[0] - (uint32_t)v0) | named_rows(key[1] - (uint32_t)v0), lane);
+    return;
+  }
+  const int i = (int)(unit / segs), c = (int)(unit - (int64_t)i * segs) * 64 + lane;
+  const int left = b.width - c * N;
+  const uint32_t mine = __shfl((int)(i < 64 ? key[0] : key[1]), i & 63, 64);
+  if (mine == ~0u) return;
+  uint64_t same[2] = {__ballot(key[0] == mine), __ballot(key[1] == mine)};
+  const int head = same[0] ? __ffsll((unsigned long long)same[0]) - 1
+                           : 63 + __ffsll((unsigned long long)same[1]);
+  if (head != i) return;
+  float acc[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] = 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint64_t left_over = same[h];
+    while (left_over) {
+      Piece<T> p[AHEAD];
+      int j[AHEAD];
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        j[a] = left_over ? h * 64 + __ffsll((unsigned long long)left_over) - 1 : -1;
+        left_over &= left_over - 1;
+      }
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        p[a].raw = u4{0, 0, 0, 0};
+        if (j[a] >= 0 && left > 0) p[a].load(dy + (size_t)j[a] * b.ldy + (size_t)c * N, left);
+      }
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a)
+        if (j[a] >= 0)
+#pragma unroll
+          for (int e = 0; e < N; ++e) acc[e] += p[a].get(e);
+    }
+  }
+  if (left > 0) give_row<N>(b, b.dtable + (size_t)mine * b.width + (size_t)c * N, left, acc);
+}
+
 // Sums of one group's tokens, N columns a lane; the blocks behind these zero rows.
 template <typename T>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __restrict__ dy) {
   constexpr int N = Piece<T>::N, AHEAD = 8;
   if (blockIdx.x >= (unsigned)b.sum_blocks) {
-    const int64_t v0 = ((int64_t)(blockIdx.x - b.sum_blocks) * 4 + (threadIdx.x >> 6)) * kAbsent;
+    const int64_t v0 =
+        b.absent0 + ((int64_t)(blockIdx.x - b.sum_blocks) * 4 + (threadIdx.x >> 6)) * kAbsent;
     if (v0 < b.vocab) fill_absent(b, (int)v0, threadIdx.x & 63);
     return;
   }
@@ -167,19 +253,16 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __r
       const uint32_t next = last ? behind : a + 1 < AHEAD ? s[(a + 1) % AHEAD].x : ahead[0].x;
       if (next == key && !last) continue;
       const bool on = next == key;                  // goes on in the next group
-      const bool whole = !head && !on;
-      float* out = (whole ? b.dtable + (size_t)key * b.width
-                          : b.part + ((size_t)g * 2 + (head ? 0 : 1)) * b.width) + (size_t)c * N;
+      if (!head && !on) {
+        give_row<N>(b, b.dtable + (size_t)key * b.width + (size_t)c * N, left, acc);
+      } else {
+        float* out = b.part + ((size_t)g * 2 + (head ? 0 : 1)) * b.width + (size_t)c * N;
 #pragma unroll
-      for (int q = 0; q < N; q += 4) {
-        Piece<float> o;
-        if (whole && b.accumulate) o.load(out + q, left - q);
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[e] = !whole ? acc[q + e] : b.accumulate ? fmaf(acc[q + e], b.scale, o.get(e)) : acc[q + e] * b.scale;
-        o.set(v);
-        o.store(out + q, left - q);
+        for (int q = 0; q < N; q += 4) {
+          Piece<float> o;
+          o.set(acc + q);
+          o.store(out + q, left - q);
+        }
       }
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] = 0.f;
@@ -247,6 +330,8 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd b) {
 
 namespace {
 
+constexpr size_t kBesideBytes = (size_t)48 << 20;       // zeroed beside a sort of one launch
+
 // Sorted tokens of a lane group: long ones leave few partial sums, short ones fill the chip.
 int embed_run(const sb::RowPlan& rp, int n) {
   int run = 8;
@@ -266,6 +351,7 @@ EmbedSpace embed_space(const sb_embed_desc* d) {
   const sb::SortIn s = sb::sort_plan(nullptr, d->first, d->vocab, d->tokens);
   const int run = embed_run(embed_rows(d), d->tokens);
   EmbedSpace e{};
+  if (d->tokens <= sb::kFewTokens) return e;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -363,16 +449,32 @@ extern "C" sb_status sb_embed_bwd(const sb_embed_desc* d, const int32_t* ids, co
   b.accumulate = accumulate;
   b.dtable = dtable;
   b.part = (float*)(ws + at.part);
+  if (d->tokens <= sb::kFewTokens) {
+    const int segs = sb::cdiv(d->width, 64 * 16 / (int)e);
+    const size_t waves = (size_t)d->tokens * segs +
+                         (accumulate ? 0 : ((size_t)d->vocab + sb::kAbsent - 1) / sb::kAbsent);
+    const unsigned blocks = (unsigned)((waves + 3) / 4);
+    if (d->dtype == SB_BF16)
+      sb::embed_few_kernel<sb::u16><<<blocks, 256, 0, st>>>(b, d->first, segs, ids,
+                                                            (const sb::u16*)dy);
+    else
+      sb::embed_few_kernel<float><<<blocks, 256, 0, st>>>(b, d->first, segs, ids, (const float*)dy);
+    return sbh::launch_status();
+  }
   const size_t sums = (((size_t)b.runs * b.rp.segs << b.rp.shift) + 255) / 256;
-  const size_t fills = in.tiles && !accumulate ? ((size_t)d->vocab + 4 * sb::kAbsent - 1) / (4 * sb::kAbsent) : 0;
-  const size_t blocks = sums + fills;
+  const int beside = accumulate || in.tiles
+                         ? 0
+                         : (int)std::min<size_t>(d->vocab, kBesideBytes / ((size_t)d->width * 4));
+  b.absent0 = beside;
+  const size_t absent = accumulate ? 0 : (size_t)(d->vocab - beside);
+  const size_t blocks = sums + (absent + 4 * sb::kAbsent - 1) / (4 * sb::kAbsent);
   if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
   b.sum_blocks = (int)sums;
   b.slots = sbh::sort_slots(in, nullptr, nullptr, (uint2*)(ws + at.a), (uint2*)(ws + at.b),
                             (uint32_t*)(ws + at.counts),
-                            sb::Fill{dtable, accumulate || in.tiles ? 0 : table}, st);
+                            sb::Fill{dtable, (size_t)beside * d->width}, st);
   s = sbh::launch_status();
-  if (s != SB_OK || d->tokens == 0) return s;
+  if (s != SB_OK) return s;
   if (d->dtype == SB_BF16)
     sb::embed_sum_kernel<sb::u16><<<(unsigned)blocks, 256, 0, st>>>(b, (const sb::u16*)dy);
   else
