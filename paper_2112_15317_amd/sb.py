@@ -171,6 +171,8 @@ class SBError(RuntimeError):
 def load():
     """Load libsb.so (raises if it has not been built)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -226,21 +228,28 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+_torch = _get_device = _raw_stream = None      # of torch, once a call has needed them
+
+
 def _stream_for(t, stream):
     """The stream of a call on t's device, which has to be the current one.  (Where torch
     has it, by its number alone: a Stream object takes 2.5 of the 9 us of a small call.)"""
-    import torch
+    global _torch, _get_device, _raw_stream
+    if _torch is None:
+        import torch
+        _get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda dev: torch.cuda.current_stream().cuda_stream)
+        _torch = torch                       # last: other threads look at it
     on = getattr(t, "device", None)          # of a tensor; None and addresses have none
-    if stream is not None and on is None:
-        return _stream(stream)
-    dev = (torch.cuda.current_device if on is None else
-           getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device))()
-    if on is not None and on.index != dev:
+    if on is None:
+        if stream is not None:
+            return _stream(stream)
+        return _raw_stream(_torch.cuda.current_device())
+    dev = _get_device()
+    if on.index != dev:
         raise ValueError("tensors on %s, current device %d" % (on, dev))
-    if stream is None:
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return raw(dev) if raw else torch.cuda.current_stream().cuda_stream
-    return _stream(stream)
+    return _raw_stream(dev) if stream is None else _stream(stream)
 
 
 def _ws(ws):
@@ -682,7 +691,8 @@ def sb_embed_fwd(desc, table, ids, y, stream=None):
     """ids: int32."""
     row, i32, _ = _kinds(desc)
     _check("sb_embed_fwd", load().sb_embed_fwd(
-        ctypes.byref(desc), _at(table, row), _at(ids, i32), _at(y, row), _stream_for(table, stream)))
+        ctypes.byref(desc), _at(table, row), _at(ids, i32), _at(y, row),
+        _stream_for(table, stream)))
 
 
 def sb_embed_bwd(desc, ids, dy, dtable, accumulate=False, ws=None, stream=None):

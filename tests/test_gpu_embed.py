@@ -19,6 +19,7 @@ SHAPES = [(0, 7, 5, 0, 0, "any"), (1, 1, 1, 0, 0, "any"), (1, 300, 64, 0, 0, "an
           (8, 1000, 1024, 0, 0, "any"), (9, 4, 129, 3, 3, "one"), (64, 33, 8, 0, 0, "one"), (65, 33, 9, 0, 1, "pad"),
           (128, 700, 65, 0, 1, "zipf"), (129, 700, 65, 0, 0, "zipf"), (128, 9, 2100, 0, 0, "one"),
           (100, 64, 130, 0, 3, "out"), (5000, 30000, 300, 0, 0, "zipf"), (6000, 8000, 1030, 0, 0, "far"),
+          (16384, 700, 33, 0, 0, "zipf"), (16385, 700, 33, 0, 0, "zipf"),
           (300, 50, 520, 8, 0, "out"), (511, 2000, 100, 0, 0, "zipf"), (1000, 3, 260, 0, 2, "zipf"),
           (2047, 1025, 65, 1, 0, "far"), (8192, 700, 33, 0, 0, "zipf"), (8193, 700, 33, 0, 0, "zipf"),
           (20000, 1023, 24, 0, 1, "one"), (33000, 5000, 17, 0, 0, "far"), (270000, 2100, 4, 0, 0, "zipf"),

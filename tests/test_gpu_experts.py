@@ -21,7 +21,7 @@ SHAPES = [(1, 1, 1, 1, 0, 1, 0, 0, 0, "any"), (1, 2, 8, 8, 0, 1024, 0, 0, 0, "an
           (33, 1, 5, 5, 0, 65, 0, 0, 3, "one"), (70, 2, 3, 9, 6, 130, 4, 0, 0, "any"),
           (100, 4, 6, 12, 3, 512, 0, 8, 0, "none"), (257, 8, 300, 512, 100, 40, 0, 0, 0, "any"),
           (300, 2, 512, 512, 0, 33, 1, 2, 2, "any"), (1365, 3, 11, 22, 11, 741, 0, 0, 0, "any"),
-          (4096, 2, 7, 7, 0, 16, 0, 0, 0, "twice"), (4097, 2, 8, 8, 0, 24, 0, 0, 0, "any"),
+          (2048, 3, 7, 7, 0, 16, 0, 0, 0, "twice"), (2049, 3, 8, 8, 0, 24, 0, 0, 0, "any"),
           (30000, 3, 40, 60, 0, 9, 0, 0, 1, "any"), (90000, 3, 2, 2, 0, 4, 0, 0, 0, "twice"),
           (60, 5, 6, 6, 0, 4200, 8, 0, 0, "any"), (40, 12, 16, 16, 0, 2049, 0, 0, 0, "any")]
 
@@ -49,7 +49,8 @@ class Case:
             self.h = {k: torch.from_numpy(a).bfloat16().float().numpy() for k, a in self.h.items()}
         self.desc = sb.expert_desc(n, top, experts, width, CODE[dtype], first, self.ldx, self.ldr)
         self.d = {k: self.put(torch.from_numpy(a).to(TYPES[dtype])) for k, a in self.h.items()}
-        self.d["ids"], self.d["weights"] = self.put(torch.from_numpy(self.ids)), self.put(torch.from_numpy(self.weights))
+        self.d["ids"] = self.put(torch.from_numpy(self.ids))
+        self.d["weights"] = self.put(torch.from_numpy(self.weights))
         self.whole = {}
         for k, shape, kind in (("place", (n, top), torch.int32), ("offsets", (experts + 1,), torch.int32),
                                ("xs", (n * top, self.ldr), TYPES[dtype]), ("y", (n, self.ldx), TYPES[dtype]),
