@@ -134,19 +134,23 @@ __device__ __forceinline__ uint32_t sort_before(uint32_t v, SortShared& h) {
   return start + incl - v;
 }
 
-// The wave's lanes that are live and have this lane's digit.
-__device__ __forceinline__ uint64_t sort_same(uint32_t d, bool live, int bits) {
-  const uint64_t all = __ballot(live);
-  uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
+// For each round: the wave's lanes that are live and have this lane's digit.
+__device__ __forceinline__ void sort_same(const uint32_t* d, const bool* live, int bits,
+                                          uint64_t* same) {
+#pragma unroll
+  for (int r = 0; r < kSortRounds; ++r) same[r] = __ballot(live[r]);
 #pragma unroll 1
   for (int b = 0; b < bits; ++b) {
-    const uint32_t one = d >> b & 1;
-    const uint64_t ones = __ballot(one != 0);
-    const uint32_t zero = one - 1;                  // all bits where this lane's is 0
-    lo &= (uint32_t)ones ^ zero;
-    hi &= (uint32_t)(ones >> 32) ^ zero;
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r) {         // (side by side: one after another waits)
+      const uint32_t one = d[r] >> b & 1;
+      const uint64_t ones = __ballot(one != 0);
+      const uint32_t zero = one - 1;                // all bits where this lane's is 0
+      const uint32_t lo = (uint32_t)same[r] & ((uint32_t)ones ^ zero);
+      const uint32_t hi = (uint32_t)(same[r] >> 32) & ((uint32_t)(ones >> 32) ^ zero);
+      same[r] = (uint64_t)hi << 32 | lo;
+    }
   }
-  return (uint64_t)hi << 32 | lo;
 }
 // The slot's rank among the wave's slots with its digit: those of this round before it, and
 // those counted in `count` (where its own are added).
@@ -198,11 +202,14 @@ __device__ __forceinline__ void sort_move(const SortIn& s, const SortPass& p, in
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r) live[r] = first + r * 64 < i1;
+    uint32_t d[kSortRounds];
+    uint64_t same[kSortRounds];
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-      const uint32_t d = v[r].x >> p.shift & (bins - 1);
-      rank[r] = sort_rank(h.count[wave], d, live[r], sort_same(d, live[r], s.digit), lane);
-    }
+    for (int r = 0; r < kSortRounds; ++r) d[r] = v[r].x >> p.shift & (bins - 1);
+    sort_same(d, live, s.digit, same);
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r)
+      rank[r] = sort_rank(h.count[wave], d[r], live[r], same[r], lane);
     __syncthreads();
     uint32_t total = 0;
     if (threadIdx.x < bins) total = sort_share(h);
@@ -210,8 +217,7 @@ __device__ __forceinline__ void sort_move(const SortIn& s, const SortPass& p, in
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r) {
       if (!live[r]) continue;
-      const uint32_t d = v[r].x >> p.shift & (bins - 1);
-      const uint32_t to = h.base[d] + h.count[wave][d] + rank[r];
+      const uint32_t to = h.base[d[r]] + h.count[wave][d[r]] + rank[r];
       if (p.out) p.out[to] = v[r];
       else p.place[v[r].y] = v[r].x < s.keys ? (int32_t)to : -1;
     }
