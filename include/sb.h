@@ -655,8 +655,10 @@ sb_status sb_embed_fwd(const sb_embed_desc *desc, const void *table,
  * with ids[i] = first + v.  Sums are fp32 and their order is fixed: repeated
  * calls give bit-identical results.  With accumulate rows without a token are
  * not touched.  The workspace starts at a multiple of 16.  Arguments are checked
- * as above, the workspace must not overlap a tensor; 2^30 tokens and more, or rows
- * of 2^23 and more, are SB_ERR_UNSUPPORTED (the query: (size_t)-1). */
+ * as above, the workspace must not overlap a tensor.  SB_ERR_UNSUPPORTED (the query:
+ * (size_t)-1) for 2^29 rows of the table, 2^30 tokens, rows of 2^23 elements and more
+ * of each, and where the rows come to 2^32 lanes (a row has 8 or a larger power of two,
+ * from 64 on multiples of it, for one or two of its 16-byte pieces each). */
 size_t sb_embed_workspace_bytes(const sb_embed_desc *desc);
 sb_status sb_embed_bwd(const sb_embed_desc *desc, const int32_t *ids,
                        const void *dy, float *dtable, int accumulate,
@@ -684,7 +686,9 @@ sb_status sb_embed_bwd(const sb_embed_desc *desc, const int32_t *ids,
  * tokens may be 0.  The calls below return SB_ERR_INVALID_ARG for bad
  * descriptors, NULL pointers, pointers that are not multiples of their elements'
  * size and outputs that overlap inputs or each other, SB_ERR_UNSUPPORTED for 2^30 slots
- * and more or rows of 2^24 and more.  Places outside the rows count as none.
+ * and more, rows of 2^24 and more, and tokens whose rows come to 2^32 lanes (a row has 8
+ * or a larger power of two, from 64 on multiples of it, for one or two of its 16-byte
+ * pieces each).  Places outside the rows count as none.
  * ---------------------------------------------------------------------- */
 enum { SB_MAX_EXPERTS = 512 };
 typedef struct {
@@ -766,7 +770,8 @@ size_t sb_token_logp_workspace_bytes(const sb_token_logp_desc *desc);
  * are needed where top > 0.  SB_ERR_INVALID_ARG for bad descriptors, NULL
  * pointers, pointers that are not multiples of their elements' size and
  * outputs or a workspace that overlap an input or each other; SB_ERR_UNSUPPORTED for more
- * than 2^20 classes or 2^30 rows and more. */
+ * than 2^20 classes, 2^30 rows and more, or rows that come to 2^32 lanes (one has a lane
+ * for 16 classes at most, 8 lanes at least). */
 sb_status sb_token_logp_fwd(const sb_token_logp_desc *desc, const void *z,
                             const int32_t *targets, float *logp, float *entropy,
                             float *stats, int32_t *top_ids, float *top_values,

@@ -377,13 +377,18 @@ EmbedSpace embed_space(const sb_embed_desc* d) {
   return e;
 }
 
+constexpr int kFwdUnits = 2;           // pieces of a row that a lane has at once
+
 sb_status embed_check(const sb_embed_desc* d) {
   if (!d || d->tokens < 0 || d->vocab < 1 || d->width < 1 || d->first < 0 || d->ldy < d->width)
     return SB_ERR_INVALID_ARG;
   if (d->dtype != SB_F32 && d->dtype != SB_BF16) return SB_ERR_INVALID_ARG;
   if (!std::isfinite(d->scale) || d->first > INT32_MAX - d->vocab) return SB_ERR_INVALID_ARG;
-  if (d->tokens >= 1 << 30 || d->width >= 1 << 23) return SB_ERR_UNSUPPORTED;
-  return SB_OK;
+  if (d->tokens >= 1 << 30 || d->width >= 1 << 23 || d->vocab >= 1 << 29) return SB_ERR_UNSUPPORTED;
+  // The forward has the most lanes: the gradient's sums have at least 8 tokens a group, and the
+  // rows that it zeroes are four lanes each.
+  const sb::RowPlan rp = sb::row_plan<kFwdUnits>(d->width, 16 / (int)sbh::dsize(d->dtype));
+  return sb::row_lanes(rp, d->tokens) < sb::kLaunchLanes - 256 ? SB_OK : SB_ERR_UNSUPPORTED;
 }
 
 size_t embed_out_bytes(const sb_embed_desc* d) {
@@ -393,10 +398,9 @@ size_t embed_out_bytes(const sb_embed_desc* d) {
 template <typename T>
 sb_status embed_fwd(const sb_embed_desc* d, const T* table, const int32_t* ids, T* y,
                     hipStream_t stream) {
-  constexpr int U = 2;
+  constexpr int U = kFwdUnits;
   const sb::RowPlan rp = sb::row_plan<U>(d->width, sb::Piece<T>::N);
-  const size_t lanes = (size_t)d->tokens * rp.segs << rp.shift, blocks = (lanes + 255) / 256;
-  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
+  const size_t blocks = (sb::row_lanes(rp, d->tokens) + 255) / 256;
   sb::embed_fwd_kernel<T, U><<<(unsigned)blocks, 256, 0, stream>>>(
       rp, d->tokens, d->first, d->vocab, d->width, d->ldy, d->scale, table, ids, y);
   return sbh::launch_status();
@@ -472,14 +476,13 @@ extern "C" sb_status sb_embed_bwd(const sb_embed_desc* d, const int32_t* ids, co
       sb::embed_few_kernel<float><<<blocks, 256, 0, st>>>(b, d->first, segs, ids, (const float*)dy);
     return sbh::launch_status();
   }
-  const size_t sums = (((size_t)b.runs * b.rp.segs << b.rp.shift) + 255) / 256;
+  const size_t sums = (sb::row_lanes(b.rp, b.runs) + 255) / 256;
   const int beside = accumulate || in.tiles
                          ? 0
                          : (int)std::min<size_t>(d->vocab, kBesideBytes / ((size_t)d->width * 4));
   b.absent0 = beside;
   const size_t absent = accumulate ? 0 : (size_t)(d->vocab - beside);
   const size_t blocks = sums + (absent + 4 * sb::kAbsent - 1) / (4 * sb::kAbsent);
-  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
   b.sum_blocks = (int)sums;
   b.slots = sbh::sort_slots(in, nullptr, nullptr, (uint2*)(ws + at.a), (uint2*)(ws + at.b),
                             (uint32_t*)(ws + at.counts),

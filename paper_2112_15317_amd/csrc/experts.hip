@@ -189,6 +189,8 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(
 
 namespace {
 
+constexpr int kUnits = 2, kBwdUnits = 4;      // pieces of a row that a lane has at once
+
 sb_status expert_check(const sb_expert_desc* d) {
   if (!d || d->tokens < 0 || d->top < 1 || d->experts < 1 || d->first < 0 || d->width < 1 ||
       d->ldx < d->width || d->ldr < d->width)
@@ -196,7 +198,8 @@ sb_status expert_check(const sb_expert_desc* d) {
   if (d->dtype != SB_F32 && d->dtype != SB_BF16) return SB_ERR_INVALID_ARG;
   if (d->experts > SB_MAX_EXPERTS || d->first > INT32_MAX - d->experts) return SB_ERR_INVALID_ARG;
   if ((int64_t)d->tokens * d->top >= 1 << 30 || d->width >= 1 << 24) return SB_ERR_UNSUPPORTED;
-  return SB_OK;
+  const sb::RowPlan rp = sb::row_plan<kUnits>(d->width, 16 / (int)sbh::dsize(d->dtype));
+  return sb::row_lanes(rp, d->tokens) < sb::kLaunchLanes - 256 ? SB_OK : SB_ERR_UNSUPPORTED;
 }
 
 size_t token_bytes(const sb_expert_desc* d) {
@@ -238,13 +241,11 @@ sb::ExpertRows expert_rows(const sb_expert_desc* d) {
   return b;
 }
 
-// Blocks of `groups` lane groups; 0: more than a launch has.
-unsigned blocks_of(const sb::RowPlan& rp, size_t groups) {
-  const size_t blocks = ((groups << rp.shift) + 255) / 256;
-  return blocks < 1ull << 31 ? (unsigned)blocks : 0;
+// Blocks of `rows` rows' groups; a group of the backward has all stretches of its row.
+unsigned blocks_of(const sb::RowPlan& rp, size_t rows, bool whole = false) {
+  return (unsigned)(((whole ? rows << rp.shift : sb::row_lanes(rp, rows)) + 255) / 256);
 }
 
-constexpr int kUnits = 2, kBwdUnits = 4;      // pieces of a row that a lane has at once
 // Rows of more than the last cache holds are read past the caches by the combining kernel:
 // 1 GB in 209 us, 225 as other loads; 67 MB that lie there take 18.1 and 16.9.
 constexpr size_t kFarBytes = (size_t)256 << 20;
@@ -289,8 +290,7 @@ extern "C" sb_status sb_expert_gather(const sb_expert_desc* d, const void* x, co
   const Span out{xs, row_bytes(d)};
   if (meets(&out, 1, in, 2)) return SB_ERR_INVALID_ARG;
   const sb::ExpertRows b = expert_rows<kUnits>(d);
-  const unsigned blocks = blocks_of(b.rp, (size_t)d->tokens * b.rp.segs);
-  if (!blocks) return SB_ERR_UNSUPPORTED;
+  const unsigned blocks = blocks_of(b.rp, d->tokens);
   hipStream_t st = sbh::stream_of(stream);
   if (d->dtype == SB_BF16)
     sb::expert_gather_kernel<sb::u16, kUnits><<<blocks, 256, 0, st>>>(b, (const sb::u16*)x, place,
@@ -316,8 +316,7 @@ extern "C" sb_status sb_expert_combine(const sb_expert_desc* d, const void* ys,
   const Span out{y, token_bytes(d)};
   if (meets(&out, 1, in, 4)) return SB_ERR_INVALID_ARG;
   const sb::ExpertRows b = expert_rows<kUnits>(d);
-  const unsigned blocks = blocks_of(b.rp, (size_t)d->tokens * b.rp.segs);
-  if (!blocks) return SB_ERR_UNSUPPORTED;
+  const unsigned blocks = blocks_of(b.rp, d->tokens);
   hipStream_t st = sbh::stream_of(stream);
   const bool far = row_bytes(d) >= kFarBytes;
   auto launch = [&](auto e, auto f) {
@@ -350,8 +349,7 @@ extern "C" sb_status sb_expert_combine_bwd(const sb_expert_desc* d, const void* 
   const Span out[2] = {{dys, row_bytes(d)}, {dweights, slot_bytes(d)}};
   if (meets(out, 2, in, 4)) return SB_ERR_INVALID_ARG;
   const sb::ExpertRows b = expert_rows<kBwdUnits>(d);
-  const unsigned blocks = blocks_of(b.rp, (size_t)d->tokens);
-  if (!blocks) return SB_ERR_UNSUPPORTED;
+  const unsigned blocks = blocks_of(b.rp, d->tokens, true);
   hipStream_t st = sbh::stream_of(stream);
   if (d->dtype == SB_BF16)
     sb::expert_combine_bwd_kernel<sb::u16, kBwdUnits><<<blocks, 256, 0, st>>>(

@@ -106,4 +106,8 @@ inline RowPlan row_plan(int width, int n_per_piece) {
   return p;
 }
 
+// Lanes of `rows` rows' groups.  A launch has fewer than 2^32 (kLaunchLanes).
+constexpr size_t kLaunchLanes = (size_t)1 << 32;
+inline size_t row_lanes(const RowPlan& p, size_t rows) { return rows * p.segs << p.shift; }
+
 }  // namespace sb

@@ -31,8 +31,8 @@ __global__ __launch_bounds__(kSortThreads) void slot_sort_count(SortIn s, SortPa
   if (threadIdx.x < bins) p.counts[((size_t)tile << s.digit) + threadIdx.x] = h.base[threadIdx.x];
 }
 
-// 5.4 us for 16384 slots of 8 experts, 8 to 9 for 65536 ids (9 bits) and 262144 slots: the chain
-// of counts, keys, ranks and stores.
+// 5.2 us for 16384 slots of 8 experts, 8 for 65536 ids (9 bits) and 262144 slots: the chain of
+// counts, keys, ranks and stores.
 __global__ __launch_bounds__(kSortThreads) void slot_sort_move(SortIn s, SortPass p) {
   __shared__ SortShared h;
   const int tile = blockIdx.x;

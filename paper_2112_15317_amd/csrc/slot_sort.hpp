@@ -25,7 +25,7 @@ constexpr int kSortStep = kSortThreads * kSortRounds;      // slots a block rank
 constexpr int kSortBins = 1024;
 constexpr int kSortTiles = 64;
 // Slots up to which pairs are counted, with digits to sort by in two passes and more, and in
-// one: 16384 ids of 15 bits take 21 us that way, the four launches 24 and what lies between
+// one: 16384 ids of 15 bits take 21 us that way, the four launches 21 and what lies between
 // them; 8192 slots of 8 experts 11, the two launches 7.8, 5331 slots 6.6.
 constexpr int kSortSmall = 16384, kSortSmallOnePass = 6144;
 

@@ -21,6 +21,7 @@
 // (many equal logits) or a NaN is about, the slow way takes one after another.
 #include "rows.hpp"
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 
@@ -816,16 +817,6 @@ __global__ __launch_bounds__(256) void logp_stretch_bwd(LogpBwd b, const T* z, T
 
 namespace {
 
-sb_status logp_check(const sb_token_logp_desc* d) {
-  if (!d || d->m < 0 || d->classes < 1 || d->ldz < d->classes || d->top < 0 ||
-      d->top > SB_LOGP_MAX_TOP || d->top > d->classes)
-    return SB_ERR_INVALID_ARG;
-  if ((d->dtype != SB_F32 && d->dtype != SB_BF16) || (d->flags & ~SB_TOP_PROBS))
-    return SB_ERR_INVALID_ARG;
-  if (d->classes > 1 << 20 || d->m >= 1 << 30) return SB_ERR_UNSUPPORTED;
-  return SB_OK;
-}
-
 // 16-byte pieces of a row that a lane holds, stretches of a row, and in the forward the
 // waves of a row's block (0: stretches anywhere, joined by a second launch).
 struct LogpPlan {
@@ -866,6 +857,20 @@ int narrow_shift(const sb_token_logp_desc* d) {
   return s;
 }
 
+sb_status logp_check(const sb_token_logp_desc* d) {
+  if (!d || d->m < 0 || d->classes < 1 || d->ldz < d->classes || d->top < 0 ||
+      d->top > SB_LOGP_MAX_TOP || d->top > d->classes)
+    return SB_ERR_INVALID_ARG;
+  if ((d->dtype != SB_F32 && d->dtype != SB_BF16) || (d->flags & ~SB_TOP_PROBS))
+    return SB_ERR_INVALID_ARG;
+  if (d->classes > 1 << 20 || d->m >= 1 << 30) return SB_ERR_UNSUPPORTED;
+  const size_t lanes =
+      narrow(d) ? (size_t)d->m << narrow_shift(d)
+                : (size_t)d->m * 64 *
+                      std::max(logp_plan(d, true).stretches, logp_plan(d, false).stretches);
+  return lanes < sb::kLaunchLanes - 256 ? SB_OK : SB_ERR_UNSUPPORTED;
+}
+
 size_t logp_part_bytes(const sb_token_logp_desc* d, const LogpPlan& p) {
   return sb::round_up((size_t)d->m * p.stretches * 3 * 4, 256);
 }
@@ -893,7 +898,6 @@ sb_status logp_fwd(const sb_token_logp_desc* d, const sb::LogpFwd& b, const Logp
     return sbh::launch_status();
   }
   const size_t blocks = ((size_t)d->m * p.stretches + 3) / 4;
-  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
   switch (p.pieces) {
     case 8: sb::logp_stretch_fwd<T, 8><<<(unsigned)blocks, 256, 0, st>>>(b, z); break;
     case 4: sb::logp_stretch_fwd<T, 4><<<(unsigned)blocks, 256, 0, st>>>(b, z); break;
@@ -914,7 +918,6 @@ sb_status logp_bwd(const sb_token_logp_desc* d, const sb::LogpBwd& b, const Logp
     return sbh::launch_status();
   }
   const size_t blocks = ((size_t)d->m * p.stretches + 3) / 4;
-  if (blocks >= 1ull << 31) return SB_ERR_UNSUPPORTED;
   switch (p.pieces) {
     case 8: sb::logp_stretch_bwd<T, 8><<<(unsigned)blocks, 256, 0, st>>>(b, z, dz); break;
     case 4: sb::logp_stretch_bwd<T, 4><<<(unsigned)blocks, 256, 0, st>>>(b, z, dz); break;

@@ -88,6 +88,30 @@ def test_sizes_past_what_is_provided(name, over):
         assert CALLS[name][5](d) == sb.SIZE_MAX
 
 
+# A launch has fewer than 2^32 lanes: 8 at least for a row, one for 16 of its bytes or more.
+@pytest.mark.parametrize("name,over", [
+    ("sb_embed_fwd", dict(tokens=1 << 29)), ("sb_embed_fwd", dict(tokens=1 << 26, width=512, ldy=512)),
+    ("sb_embed_bwd", dict(vocab=1 << 29)), ("sb_embed_bwd", dict(tokens=1 << 29)),
+    ("sb_expert_gather", dict(tokens=1 << 29, top=1)), ("sb_expert_combine", dict(tokens=1 << 29, top=1)),
+    ("sb_expert_combine_bwd", dict(tokens=1 << 26, top=2, width=512, ldx=512, ldr=512)),
+    ("sb_token_logp_fwd", dict(m=1 << 29, classes=8, ldz=8)), ("sb_token_logp_bwd", dict(m=1 << 29, classes=8, ldz=8)),
+    ("sb_token_logp_fwd", dict(m=1 << 26, classes=1025)), ("sb_token_logp_bwd", dict(m=1 << 26, classes=1025)),
+    ("sb_token_logp_fwd", dict(m=1 << 26, classes=1000)), ("sb_token_logp_bwd", dict(m=1 << 23, classes=1 << 15))])
+def test_rows_past_the_lanes_of_a_launch(name, over):
+    d = _desc(name, **over)
+    assert _call(name, d) == NO
+    if CALLS[name][5]:
+        assert CALLS[name][5](d) == sb.SIZE_MAX
+
+
+@pytest.mark.parametrize("name,over", [
+    ("sb_embed_bwd", dict(tokens=(1 << 29) - 64)), ("sb_embed_bwd", dict(vocab=(1 << 29) - 1)),
+    ("sb_expert_sort", dict(tokens=(1 << 29) - 64, top=1)), ("sb_token_logp_fwd", dict(m=(1 << 29) - 64, classes=8, ldz=8)),
+    ("sb_token_logp_fwd", dict(m=(1 << 26) - 64, classes=1025))])
+def test_rows_up_to_the_lanes_of_a_launch(name, over):
+    assert CALLS[name][5](_desc(name, **over)) != sb.SIZE_MAX
+
+
 @pytest.mark.parametrize("name", NAMES)
 def test_null_descriptor(name):
     _, order, _, _, acc, size = CALLS[name]
