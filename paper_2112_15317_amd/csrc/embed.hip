@@ -16,7 +16,7 @@
 // beside the sums those of the others that have no token: 65536 tokens of a table of 131072 x
 // 2048 name a quarter of its rows, and zeroing these too would be a sixth of all traffic.
 //
-// Up to kFewTokens tokens it is one launch without a sort: a wave has a token's columns,
+// Up to kFewTokens tokens it is one launch without a sort: a block has a token's columns,
 // compares its id with all others, and where it is the first with that id sums all of them.
 #include "rows.hpp"
 #include "slot_sort.hpp"
@@ -50,12 +50,13 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(RowPlan rp, int n, int f
   for (int u = 0; u < U; ++u) {
     const int c = c0 + (u << rp.shift);
     p[u].raw = u4{0, 0, 0, 0};
-    if (inside && c < rp.pieces) p[u].load(src + (size_t)c * N, width - c * N);
+    if (inside && c < rp.pieces) p[u].load(src + (size_t)c * N, width - c * N, width);
   }
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = c0 + (u << rp.shift);
     if (c >= rp.pieces) continue;
+    if (inside) p[u].settle(width - c * N, width);
     if (inside && scale != 1.f) {
       float v[N];
 #pragma unroll
@@ -97,11 +98,13 @@ __device__ __forceinline__ int slot_from(const EmbedBwd& b, uint32_t key, int lo
 // A bit for each of the kAbsent rows that a lane's `at` names, over the wave.  (Sixteen: a
 // wave with 64 rows of 741 held up a launch of 8 us for 26.)
 constexpr int kAbsent = 16;
-__device__ __forceinline__ uint32_t named_rows(uint32_t at) {
-  uint32_t bits = at < kAbsent ? 1u << at : 0;
+__device__ __forceinline__ uint32_t all_bits(uint32_t bits) {
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) bits |= __shfl_xor((int)bits, o, 64);
   return bits;
+}
+__device__ __forceinline__ uint32_t named_rows(uint32_t at) {
+  return all_bits(at < kAbsent ? 1u << at : 0);
 }
 
 // Zeros in those of the kAbsent rows from v0 on that are not named; one wave.
@@ -138,7 +141,10 @@ __device__ __forceinline__ void give_row(const EmbedBwd& b, float* out, int left
 #pragma unroll
   for (int q = 0; q < N; q += 4) {
     Piece<float> o;
-    if (b.accumulate) o.load(out + q, left - q);
+    if (b.accumulate && left > q) {
+      o.load(out + q, left - q, b.width);
+      o.settle(left - q, b.width);
+    }
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -148,45 +154,66 @@ __device__ __forceinline__ void give_row(const EmbedBwd& b, float* out, int left
   }
 }
 
-// Few tokens: waves 0 .. n * segs - 1 have a token's columns each, the others rows to zero.
-// Latency bounds it (three launches took 12 us and more); a batch of one token repeated is
-// summed four rows at a time.
-constexpr int kFewTokens = 128;
-template <typename T>
+// Few tokens, up to 64 H: a block has a token's columns, the blocks behind those rows to zero.
+// Every wave compares the token's id with all; where it is the first with that id, the waves
+// take the others by sixteens in turn, eight rows on their way at once, and the first adds up.
+// Latency bounds it; added to a table of 32000 x 2048, 128 tokens of bf16 take 3.4 us, as many of
+// one id 7.9.  256 tokens of different ids of 741 columns 4.7 us, of one id 15; by sorting, in
+// three launches, 17 and 16.  (512 take 5.6 and 26, by sorting 17 and 19.)
+constexpr int kFewTokens = 256;
+template <typename T, int H>
 __global__ __launch_bounds__(256) void embed_few_kernel(EmbedBwd b, int first, int segs,
                                                         const int32_t* __restrict__ ids,
                                                         const T* __restrict__ dy) {
-  constexpr int N = Piece<T>::N, AHEAD = 4;
-  const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  uint32_t key[2];
+  constexpr int N = Piece<T>::N, AHEAD = 8;
+  __shared__ f4 quarter[3][N / 4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int units = b.n * segs;
+  int id[H];
+  uint32_t key[H];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int j = h * 64 + lane, id = j < b.n ? ids[j] : -1;
-    key[h] = id >= first && (uint32_t)(id - first) < (uint32_t)b.vocab ? id - first : ~0u;
+  for (int h = 0; h < H; ++h) id[h] = b.n > 0 ? ids[min(h * 64 + lane, b.n - 1)] : -1;
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    const bool inside = id[h] >= first && (uint32_t)(id[h] - first) < (uint32_t)b.vocab;
+    key[h] = inside && h * 64 + lane < b.n ? id[h] - first : ~0u;
   }
-  const int64_t zeros = unit - (int64_t)b.n * segs;
-  if (zeros >= 0) {
-    const int64_t v0 = zeros * kAbsent;
-    if (b.accumulate || v0 >= b.vocab) return;
-    const uint32_t named = named_rows(key[0] - (uint32_t)v0) | named_rows(key[1] - (uint32_t)v0);
-    zero_rows(b, (int)v0, named, lane);
+  if ((int64_t)blockIdx.x >= units) {
+    const int64_t v0 = (((int64_t)blockIdx.x - units) * 4 + wave) * kAbsent;
+    if (v0 >= b.vocab) return;
+    uint32_t named = 0;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const uint32_t at = key[h] - (uint32_t)v0;
+      named |= at < kAbsent ? 1u << at : 0;
+    }
+    zero_rows(b, (int)v0, all_bits(named), lane);
     return;
   }
-  const int i = (int)(unit / segs), c = (int)(unit - (int64_t)i * segs) * 64 + lane;
+  const int i = blockIdx.x / segs, c = (int)(blockIdx.x - i * segs) * 64 + lane;
   const int left = b.width - c * N;
-  const uint32_t mine = __shfl((int)(i < 64 ? key[0] : key[1]), i & 63, 64);
+  uint32_t own = 0;
+#pragma unroll
+  for (int h = 0; h < H; ++h) own = i >> 6 == h ? key[h] : own;
+  const uint32_t mine = __builtin_amdgcn_readlane(own, i & 63);
   if (mine == ~0u) return;
-  uint64_t same[2] = {__ballot(key[0] == mine), __ballot(key[1] == mine)};
-  const int head = same[0] ? __ffsll((unsigned long long)same[0]) - 1
-                           : 63 + __ffsll((unsigned long long)same[1]);
-  if (head != i) return;
+  uint64_t same[H];
+  int head = 0, others = -1;                        // (the block's waves all find the same)
+  bool found = false;
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    same[h] = __ballot(key[h] == mine);
+    if (!found && same[h]) head = h * 64 + __ffsll((unsigned long long)same[h]) - 1;
+    found = found || same[h] != 0;
+    others += __popcll(same[h]);
+  }
+  if (head != i || (others == 0 && wave)) return;
   float acc[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) acc[e] = 0.f;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    uint64_t left_over = same[h];
+  for (int h = 0; h < H; ++h) {
+    uint64_t left_over = others ? same[h] & 0xffffull << 16 * wave : same[h];
     while (left_over) {
       Piece<T> p[AHEAD];
       int j[AHEAD];
@@ -198,14 +225,29 @@ __global__ __launch_bounds__(256) void embed_few_kernel(EmbedBwd b, int first, i
 #pragma unroll
       for (int a = 0; a < AHEAD; ++a) {
         p[a].raw = u4{0, 0, 0, 0};
-        if (j[a] >= 0 && left > 0) p[a].load(dy + (size_t)j[a] * b.ldy + (size_t)c * N, left);
+        if (j[a] >= 0 && left > 0) p[a].load(dy + (size_t)j[a] * b.ldy + (size_t)c * N, left, b.width);
       }
 #pragma unroll
       for (int a = 0; a < AHEAD; ++a)
-        if (j[a] >= 0)
+        if (j[a] >= 0) {
+          p[a].settle(left, b.width);
 #pragma unroll
           for (int e = 0; e < N; ++e) acc[e] += p[a].get(e);
+        }
     }
+  }
+  if (others) {
+    if (wave)
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q)
+        quarter[wave - 1][q][lane] =
+            f4{acc[q * 4], acc[q * 4 + 1], acc[q * 4 + 2], acc[q * 4 + 3]};
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int e = 0; e < N; ++e) acc[e] += quarter[w][e / 4][lane][e % 4];
   }
   if (left > 0) give_row<N>(b, b.dtable + (size_t)mine * b.width + (size_t)c * N, left, acc);
 }
@@ -252,11 +294,12 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedBwd b, const T* __r
     for (int a = 0; a < AHEAD; ++a) {
       p[a].raw = u4{0, 0, 0, 0};
       if (j + a < j1 && s[a].x != none && left > 0)
-        p[a].load(dy + (size_t)s[a].y * b.ldy + (size_t)c * N, left);
+        p[a].load(dy + (size_t)s[a].y * b.ldy + (size_t)c * N, left, b.width);
     }
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       if (j + a >= j1 || key == none) break;
+      p[a].settle(left, b.width);
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] += p[a].get(e);
       const bool last = j + a + 1 >= j1;
@@ -312,7 +355,8 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd b) {
 #pragma unroll 8
     for (int h = h0; h < h1; ++h) {
       Piece<float> p;
-      p.load(b.part + (size_t)h * 2 * b.width + c, left);
+      p.load(b.part + (size_t)h * 2 * b.width + c, left, b.width);
+      p.settle(left, b.width);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += p.get(e);
     }
@@ -321,10 +365,14 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedBwd b) {
   __syncthreads();
   if (wave || left <= 0) return;
   Piece<float> p;
-  p.load(b.part + ((size_t)g * 2 + 1) * b.width + c, left);
+  p.load(b.part + ((size_t)g * 2 + 1) * b.width + c, left, b.width);
   float* o = b.dtable + (size_t)key * b.width + c;
   Piece<float> old;
-  if (b.accumulate) old.load(o, left);
+  if (b.accumulate) {
+    old.load(o, left, b.width);
+    old.settle(left, b.width);
+  }
+  p.settle(left, b.width);
   float sum[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -358,11 +406,19 @@ sb::RowPlan embed_rows(const sb_embed_desc* d) {
   return sb::row_plan<1>(d->width, 16 / (int)sbh::dsize(d->dtype));
 }
 
+// Stretches of a row that a wave has each, and whether the gradient is one launch.
+int few_segs(const sb_embed_desc* d) {
+  return sb::cdiv(d->width, 64 * 16 / (int)sbh::dsize(d->dtype));
+}
+bool embed_few(const sb_embed_desc* d) {
+  return d->tokens <= sb::kFewTokens && (int64_t)d->tokens * few_segs(d) <= 1 << 20;
+}
+
 EmbedSpace embed_space(const sb_embed_desc* d) {
   const sb::SortIn s = sb::sort_plan(nullptr, d->first, d->vocab, d->tokens);
   const int run = embed_run(embed_rows(d), d->tokens);
   EmbedSpace e{};
-  if (d->tokens <= sb::kFewTokens) return e;
+  if (embed_few(d)) return e;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -464,16 +520,22 @@ extern "C" sb_status sb_embed_bwd(const sb_embed_desc* d, const int32_t* ids, co
   b.accumulate = accumulate;
   b.dtable = dtable;
   b.part = (float*)(ws + at.part);
-  if (d->tokens <= sb::kFewTokens) {
-    const int segs = sb::cdiv(d->width, 64 * 16 / (int)e);
-    const size_t waves = (size_t)d->tokens * segs +
-                         (accumulate ? 0 : ((size_t)d->vocab + sb::kAbsent - 1) / sb::kAbsent);
-    const unsigned blocks = (unsigned)((waves + 3) / 4);
-    if (d->dtype == SB_BF16)
-      sb::embed_few_kernel<sb::u16><<<blocks, 256, 0, st>>>(b, d->first, segs, ids,
-                                                            (const sb::u16*)dy);
-    else
-      sb::embed_few_kernel<float><<<blocks, 256, 0, st>>>(b, d->first, segs, ids, (const float*)dy);
+  if (embed_few(d)) {
+    const int segs = few_segs(d);
+    const size_t zeros = accumulate ? 0 : ((size_t)d->vocab + sb::kAbsent - 1) / sb::kAbsent;
+    const unsigned blocks = (unsigned)((size_t)d->tokens * segs + (zeros + 3) / 4);
+    if (blocks == 0) return SB_OK;
+    auto launch = [&](auto t, auto h) {
+      using T = decltype(t);
+      sb::embed_few_kernel<T, decltype(h)::value>
+          <<<blocks, 256, 0, st>>>(b, d->first, segs, ids, (const T*)dy);
+    };
+    auto for_type = [&](auto h) {
+      if (d->dtype == SB_BF16) launch(sb::u16(), h);
+      else launch(float(), h);
+    };
+    if (d->tokens <= 128) for_type(std::integral_constant<int, 2>());
+    else for_type(std::integral_constant<int, 4>());
     return sbh::launch_status();
   }
   const size_t sums = (sb::row_lanes(b.rp, b.runs) + 255) / 256;

@@ -40,8 +40,10 @@ __global__ __launch_bounds__(256) void expert_gather_kernel(ExpertRows b, const 
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int c = c0 + (u << b.rp.shift);
-    if (c < b.rp.pieces) p[u].load(x + t * (size_t)b.ldx + (size_t)c * N, b.width - c * N);
+    if (c < b.rp.pieces) p[u].load(x + t * (size_t)b.ldx + (size_t)c * N, b.width - c * N, b.width);
   }
+#pragma unroll
+  for (int u = 0; u < U; ++u) p[u].settle(b.width - (c0 + (u << b.rp.shift)) * N, b.width);
   for (int j = 0; j < b.top; ++j) {
     const uint32_t to = (uint32_t)place[t * b.top + j];
     if (to >= b.rows) continue;
@@ -73,7 +75,10 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
     const int c = c0 + (u << b.rp.shift);
     Piece<T> p;
     p.raw = u4{0, 0, 0, 0};
-    if (add && c < b.rp.pieces) p.load(add + t * (size_t)b.ldx + (size_t)c * N, b.width - c * N);
+    if (add && c < b.rp.pieces) {
+      p.load(add + t * (size_t)b.ldx + (size_t)c * N, b.width - c * N, b.width);
+      p.settle(b.width - c * N, b.width);
+    }
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[u][e] = p.get(e);
   }
@@ -93,16 +98,19 @@ __global__ __launch_bounds__(256) void expert_combine_kernel(ExpertRows b,
       for (int u = 0; u < U; ++u) {
         const int c = c0 + (u << b.rp.shift);
         if (from[j] < b.rows && c < b.rp.pieces)
-          p[j][u].template load<FAR>(ys + from[j] * (size_t)b.ldr + (size_t)c * N, b.width - c * N);
+          p[j][u].template load<FAR>(ys + from[j] * (size_t)b.ldr + (size_t)c * N, b.width - c * N,
+                                     b.width);
       }
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       if (from[j] >= b.rows) continue;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u) {
+        p[j][u].settle(b.width - (c0 + (u << b.rp.shift)) * N, b.width);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[u][e] = fmaf(w[j], p[j][u].get(e), acc[u][e]);
+      }
     }
   }
 #pragma unroll
@@ -133,7 +141,11 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(
   for (int u = 0; u < U; ++u) {
     const int c = lane + (u << b.rp.shift);
     g[u].raw = u4{0, 0, 0, 0};
-    if (c < b.rp.pieces) g[u].load(from + (size_t)c * N, b.width - c * N);
+    if (c < b.rp.pieces) g[u].load(from + (size_t)c * N, b.width - c * N, b.width);
+  }
+  if (b.rp.segs == 1) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) g[u].settle(b.width - (lane + (u << b.rp.shift)) * N, b.width);
   }
   for (int j0 = 0; j0 < b.top; j0 += AHEAD) {
     uint32_t row[AHEAD];
@@ -151,11 +163,16 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(
       for (int u = 0; u < U; ++u) {
         const int c = lane + ((s * U + u) << b.rp.shift), left = b.width - c * N;
         if (c >= b.rp.pieces) continue;
-        if (b.rp.segs > 1) g[u].load(from + (size_t)c * N, left);
+        if (b.rp.segs > 1) g[u].load(from + (size_t)c * N, left, b.width);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j)
           if (dweights && row[j] < b.rows)
-            o[j][u].load(ys + row[j] * (size_t)b.ldr + (size_t)c * N, left);
+            o[j][u].load(ys + row[j] * (size_t)b.ldr + (size_t)c * N, left, b.width);
+      }
+      if (b.rp.segs > 1) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          g[u].settle(b.width - (lane + ((s * U + u) << b.rp.shift)) * N, b.width);
       }
 #pragma unroll
       for (int j = 0; j < AHEAD; ++j) {
@@ -164,6 +181,7 @@ __global__ __launch_bounds__(256) void expert_combine_bwd_kernel(
         for (int u = 0; u < U; ++u) {
           const int c = lane + ((s * U + u) << b.rp.shift);
           if (c >= b.rp.pieces) continue;
+          if (dweights) o[j][u].settle(b.width - c * N, b.width);
           float v[N];
 #pragma unroll
           for (int e = 0; e < N; ++e) {

@@ -183,21 +183,26 @@ __device__ __forceinline__ void load_row(const T* row, int classes, int first, i
   constexpr int N = Piece<T>::N;
   if (first + P * N * lanes <= classes) {
 #pragma unroll
-    for (int u = 0; u < P; ++u) p[u].load(row + first + (lane + u * lanes) * N, N);
+    for (int u = 0; u < P; ++u) p[u].load(row + first + (lane + u * lanes) * N, N, N);
     return;
+  }
+  const uint32_t none = minus_inf<T>();
+#pragma unroll
+  for (int u = 0; u < P; ++u) {
+    const int left = classes - (first + (lane + u * lanes) * N);
+    p[u].raw = u4{none, none, none, none};
+    if (left > 0) p[u].load(row + classes - left, left, classes);
   }
 #pragma unroll
   for (int u = 0; u < P; ++u) {
     const int left = classes - (first + (lane + u * lanes) * N);
-    const uint32_t none = minus_inf<T>();
-    p[u].raw = u4{none, none, none, none};
-    if (left >= N) {
-      p[u].load(row + classes - left, N);
-    } else if (left > 0) {
+    if (left <= 0 || left >= N) continue;
+    if (classes >= N) {
+      p[u].settle(left, classes, none);
+    } else {
       float v[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e)
-        v[e] = e < left ? Elem<T>::load(row, classes - left + e) : -INFINITY;
+      for (int e = 0; e < N; ++e) v[e] = e < left ? p[u].get(e) : -INFINITY;
       p[u].set(v);
     }
   }

@@ -23,7 +23,9 @@ SHAPES = [(0, 7, 5, 0, 0, "any"), (1, 1, 1, 0, 0, "any"), (1, 300, 64, 0, 0, "an
           (300, 50, 520, 8, 0, "out"), (511, 2000, 100, 0, 0, "zipf"), (1000, 3, 260, 0, 2, "zipf"),
           (2047, 1025, 65, 1, 0, "far"), (8192, 700, 33, 0, 0, "zipf"), (8193, 700, 33, 0, 0, "zipf"),
           (20000, 1023, 24, 0, 1, "one"), (33000, 5000, 17, 0, 0, "far"), (270000, 2100, 4, 0, 0, "zipf"),
-          (4100, 70000, 3, 0, 0, "far"), (9000, 1 << 21, 1, 0, 0, "far"), (600, 40, 2300, 0, 0, "zipf")]
+          (4100, 70000, 3, 0, 0, "far"), (256, 700, 741, 0, 0, "zipf"), (256, 33, 129, 3, 1, "one"),
+          (257, 33, 741, 0, 0, "one"), (200, 12, 12, 0, 1, "pad"),
+          (9000, 1 << 21, 1, 0, 0, "far"), (600, 40, 2300, 0, 0, "zipf")]
 
 
 def _ids(kind, r, n, vocab, first):
@@ -151,7 +153,8 @@ def test_long_sums_of_one_sign_do_not_drift():
     assert torch.equal(c.dtable, want)
 
 
-@pytest.mark.parametrize("shape", [(5000, 900, 129, 0, 0, "zipf"), (20000, 3000, 40, 0, 0, "zipf")])
+@pytest.mark.parametrize("shape", [(5000, 900, 129, 0, 0, "zipf"), (20000, 3000, 40, 0, 0, "zipf"),
+                                   (200, 90, 129, 0, 0, "zipf")])
 def test_repeats_streams_and_graphs_agree(shape):
     print_case("embed repeats", shape=shape)
     c = Case("bf16", *shape)
