@@ -36,7 +36,12 @@ constexpr int kMoreTop = 2;            // fp32 classes there that are ranked bes
 template <typename T> constexpr int kNarrowPieces = kNarrowElems / Piece<T>::N;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLeastPower = -1000.f; // in place of masked elements' -inf: 0 times it is 0
-constexpr float kMostPlain = 1e30f;    // larger maxima, of either sign, take the careful sums
+// Largest magnitude of a maximum M whose sums take powers of 2 against M log2 e rounded: that is
+// off by 2^-4 at most, which a factor puts right.  (From 1.5e9 on it is off by up to 128, and a
+// power, or the factor, is infinite or 0.)
+constexpr float kMostSums = 0x1p20f;
+// The same for M itself taken from the logits, in the best classes and the gradient.
+constexpr float kMostPlain = 1e30f;
 
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -406,11 +411,11 @@ __device__ __forceinline__ void stretch_top(const LogpFwd& b, const T* row, cons
   }
 }
 
-// Sums of a stretch without its largest element, for a maximum that is an ordinary
-// number.  Powers of 2: exp(z - M) = 2^(z log2 e - c) * fix, c = M log2 e rounded and
-// fix its error's power, so that an element costs one fused product.  Every lane sums all
-// it has; the first lane that has the maximum does not count, and its elements are summed
-// by all lanes once more, without the maximum.
+// Sums of a stretch without its largest element, for a maximum M of up to kMostSums.
+// Powers of 2: exp(z - M) = 2^(z log2 e - c) * fix, c = M log2 e rounded and fix its
+// error's power, so that an element costs one fused product.  Every lane sums all it has; the
+// first lane that has the maximum does not count, and its elements are summed by all lanes
+// once more, without the maximum.
 template <typename T, int P>
 __device__ __forceinline__ void stretch_sums(const Piece<T>* p, float mx, float lm, int lane,
                                              u4* share, float& o, float& s) {
@@ -468,7 +473,7 @@ __device__ __forceinline__ void stretch(const LogpFwd& b, const T* zr, int first
   const float mx = group_max(lm, 64);
   const bool plain = fabsf(mx) < kMostPlain;       // not where a NaN is
   float o, s;
-  if (plain) {
+  if (fabsf(mx) <= kMostSums) {
     stretch_sums<T, P>(p, mx, lm, lane, reinterpret_cast<u4*>(list), o, s);
   } else {
     int equal;
