@@ -404,7 +404,8 @@ __device__ __forceinline__ void stretch_top(const LogpFwd& b, const T* row, cons
 #pragma unroll 1
     for (int c = first + lane; c < end; c += 64) {
       const uint64_t key = key_of(order_of(Elem<T>::load(row, c)), c);
-      if (key < last && key > most) most = key;
+      // (A NaN in class 0 has the largest key there is.)
+      if ((k == 0 || key < last) && key > most) most = key;
     }
     last = group_max(most, 64);
     if (lane == 0) out[k] = last;

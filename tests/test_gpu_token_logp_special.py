@@ -1,13 +1,12 @@
 """GPU parity of the token log-probabilities where single numbers decide: logits and
-masks of any magnitude, over whole stretches of a row and alone.  The shapes reach what
-tests/test_gpu_token_logp.py leaves: stretches of the longest and the shortest kind,
-many blocks of the joining launch."""
+masks of any magnitude, over whole stretches of a row and alone; NaN in a row's first
+class.  The shapes reach what tests/test_gpu_token_logp.py leaves: stretches of the
+longest and the shortest kind, many blocks of the joining launch."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import token_logp as L
-from paper_2112_15317_amd import sb
 from tests.helpers import print_case
 from tests.test_gpu_token_logp import FWD, Case
 
@@ -42,7 +41,7 @@ def _large(m, n, dtype):
 
 
 # fp32 pieces of a lane's stretch / bf16: 84 x 1025 to 8192 a block a row, 84 x 50001 stretches
-# of 4 / 13 of 8 in a block, 6 x 70000 of 1 / 1, 6 x 140000 of 2 / 1, 460 x 33000 of 4 / 8.
+# of 4 / 13 of 8 in a block, 6 x 70000 of 1 / 1, 6 x 140000 of 2 / 1, 460 x 33000 of 8 / 8.
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("m,n,top", [(84, 700, 8), (84, 1025, 8), (84, 5000, 20), (84, 8192, 8), (84, 50001, 20),
                                      (6, 70000, 8), (6, 140000, 20), (460, 33000, 8)])
@@ -75,3 +74,25 @@ def test_stretches_ruled_out_whole(m, n, top, dtype):
     c.bwd()
     c.check(FWD + ("top_ids", "dz"))
     c.untouched()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [300, 1025, 5000, 50001, 70000])
+def test_nan_in_the_first_class(n, dtype):
+    """NaN ranks above all classes, in class 0 too, and lower classes come first among equal ones."""
+    print_case("token_logp first class", n=n, dtype=dtype)
+    r = np.random.default_rng(n)
+    z = r.normal(size=(6, n)).astype(np.float32)
+    z[0, 0] = np.nan
+    z[1] = np.nan
+    z[2, [0, n // 2, n - 1]] = np.nan
+    z[3, :] = -np.inf
+    z[3, 0] = -np.nan
+    z[4, 0] = np.inf
+    z[4, 1] = np.nan
+    c = Case(dtype, 6, n, 0, 0, 6, False, None, z=z)
+    c.fwd()
+    torch.cuda.synchronize()
+    f = L.forward(c.z, None, 6)
+    assert np.array_equal(c.d["top_ids"].cpu().numpy(), f["top_ids"])
+    assert np.array_equal(torch.isnan(c.d["top_values"]).cpu().numpy(), np.isnan(f["top_values"]))
