@@ -662,9 +662,9 @@ struct LogpBwd {
   const float *top_values, *dtop;
 };
 
-// What a row's gradient needs: logp = z - mx - ls; all = the sum of g, and dH H.
+// What a row's gradient needs: logp = z - mx - ls; dhh = dH H, all = the sum of g.
 struct RowGrad {
-  float mx, ls, dh, all;
+  float mx, ls, dh, dhh, all;
   int target;
   float g;                     // at the target
   bool bad;                    // a target past the classes: a row of NaN
@@ -674,11 +674,11 @@ __device__ __forceinline__ RowGrad row_grad(const LogpBwd& b, size_t row) {
   r.mx = b.stats[row * 2];
   r.ls = b.stats[row * 2 + 1];
   r.dh = b.dentropy ? b.dentropy[row] : 0.f;
-  r.all = b.dentropy ? r.dh * b.entropy[row] : 0.f;
+  r.dhh = b.dentropy ? r.dh * b.entropy[row] : 0.f;
   r.target = b.dlogp ? b.targets[row] : -1;
   r.g = r.target >= 0 ? b.dlogp[row] : 0.f;
   r.bad = r.target >= b.classes;
-  r.all += r.g;
+  r.all = r.g;
   return r;
 }
 // Gradient of a row's k-th alternative on its log-probability; its class in id.
@@ -690,11 +690,12 @@ __device__ __forceinline__ float top_grad(const LogpBwd& b, size_t row, int k, i
   const float p = b.top_values[row * b.top + k];
   return p == 0.f ? 0.f : d * p;
 }
-// dz of a class that has the gradient g itself (0 for most).
-__device__ __forceinline__ float class_grad(const RowGrad& r, float z, float g) {
+// dz of a class that has the gradient g itself (0 for most) and the others `others` in all.  (As
+// all - g they lose what is small beside g, and a sure row has little else.)
+__device__ __forceinline__ float class_grad(const RowGrad& r, float z, float g, float others) {
   const float lp = (z - r.mx) - r.ls;
   const float p = exp2_hw(lp * kLog2e);
-  const float d = p > 0.f ? p * (r.all - g + r.dh * lp) : p == 0.f ? 0.f : p;
+  const float d = p > 0.f ? p * (others + fmaf(r.dh, lp, r.dhh)) : p == 0.f ? 0.f : p;
   return (g != 0.f ? -g * expm1f(lp) : 0.f) - d;
 }
 
@@ -704,7 +705,7 @@ __device__ __forceinline__ float class_grad(const RowGrad& r, float z, float g) 
 struct PlainGrad {
   float mx, l, a, dh;
   __device__ __forceinline__ explicit PlainGrad(const RowGrad& r)
-      : mx(r.mx), l(r.ls * kLog2e), a(fmaf(-r.dh, r.ls, r.all)), dh(r.dh) {}
+      : mx(r.mx), l(r.ls * kLog2e), a(r.all + fmaf(-r.dh, r.ls, r.dhh)), dh(r.dh) {}
   __device__ __forceinline__ float operator()(float z) const {
     const float t = fmaxf(z - mx, kLeastPower);
     return -exp2_hw(fmaf(t, kLog2e, -l)) * fmaf(dh, t, a);
@@ -726,7 +727,7 @@ __device__ __forceinline__ Piece<T> grad_piece(const RowGrad& r, const PlainGrad
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      d[e] = r.bad ? NAN : r.ls == -INFINITY ? 0.f : class_grad(r, z.get(e), 0.f);
+      d[e] = r.bad ? NAN : r.ls == -INFINITY ? 0.f : class_grad(r, z.get(e), 0.f, r.all);
   }
   Piece<T> q;
   q.set(d);
@@ -772,9 +773,12 @@ __global__ __launch_bounds__(256) void logp_narrow_bwd(LogpBwd b, int shift, con
     if (k >= entries) break;
     const int c = id[k];
     const float z0 = c >= 0 && c < b.classes ? Elem<T>::load(zr, c) : 0.f;
-    float sum = 0.f;                            // of all that name this class
-    for (int j = 0; j < entries; ++j) sum += id[j] == c ? g[j] : 0.f;
-    special[i] = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum);
+    float sum = 0.f, others = 0.f;              // of all that name this class, and of the rest
+    for (int j = 0; j < entries; ++j) {
+      sum += id[j] == c ? g[j] : 0.f;
+      others += id[j] == c ? 0.f : g[j];
+    }
+    special[i] = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum, others);
   }
   const bool plain = __all(is_plain(r));
   const PlainGrad grad(r);
@@ -826,12 +830,14 @@ __global__ __launch_bounds__(256) void logp_stretch_bwd(LogpBwd b, const T* z, T
   float special = 0.f;
   if (any) {
     const float z0 = mine ? Elem<T>::load(zr, id) : 0.f;
-    float sum = 0.f;                            // of all that name this class
+    float sum = 0.f, others = 0.f;              // of all that name this class, and of the rest
     for (int k = 0; k <= tops; ++k) {
       const float gk = __shfl(g, k, 64);
-      sum += __shfl(id, k, 64) == id ? gk : 0.f;
+      const bool same = __shfl(id, k, 64) == id;
+      sum += same ? gk : 0.f;
+      others += same ? 0.f : gk;
     }
-    special = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum);
+    special = r.ls == -INFINITY ? 0.f : class_grad(r, z0, sum, others);
   }
   const bool plain = is_plain(r);
   const PlainGrad grad(r);

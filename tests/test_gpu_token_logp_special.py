@@ -1,7 +1,8 @@
 """GPU parity of the token log-probabilities where single numbers decide: logits and
 masks of any magnitude, over whole stretches of a row and alone; NaN in a row's first
-class.  The shapes reach what tests/test_gpu_token_logp.py leaves: stretches of the
-longest and the shortest kind, many blocks of the joining launch."""
+class; the gradient of rows that are sure of their token.  The shapes reach what
+tests/test_gpu_token_logp.py leaves: stretches of the longest and the shortest kind,
+many blocks of the joining launch."""
 import numpy as np
 import pytest
 import torch
@@ -12,6 +13,7 @@ from tests.test_gpu_token_logp import FWD, Case
 
 pytestmark = pytest.mark.gpu
 
+U = 2.0 ** -24                         # half a step of fp32
 # Magnitudes on both sides of every limit that a kernel might draw, of both signs.
 VALUES = [s * v for v in (9e5, 1.2e6, 1e8, 1e9, 1e10, 1e20, 9e29) for s in (1, -1)]
 KINDS = 6
@@ -96,3 +98,41 @@ def test_nan_in_the_first_class(n, dtype):
     f = L.forward(c.z, None, 6)
     assert np.array_equal(c.d["top_ids"].cpu().numpy(), f["top_ids"])
     assert np.array_equal(torch.isnan(c.d["top_values"]).cpu().numpy(), np.isnan(f["top_values"]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [200, 2000, 50001])
+@pytest.mark.parametrize("lead", [15, 22, 25, 28, 40])
+def test_gradient_of_sure_rows(lead, n, dtype):
+    """dz of a class `lead` ahead of the others: what is left where its own gradient g nearly cancels.
+    With t = z - M < 0 of the others, x = exp(t), O = sum x and W = -sum x t: 1 - p = O / (1 + O), H + log p =
+    W / (1 + O), so dz = (g O - others - dH W / (1 + O)) / (1 + O), without a difference of near numbers.
+
+    Errors: of O and W as in the oracle's bounds (3 |t| + 5 + 92 roundings of a term), log1p, expm1 and the
+    power 4 each, products and sums 8 more, each of its own term; bf16 results are rounded once more."""
+    print_case("token_logp sure", lead=lead, n=n, dtype=dtype)
+    r = np.random.default_rng(lead + n)
+    z = (r.integers(-8, 9, (6, n)) / 8).astype(np.float32)
+    z[:, 17] = lead
+    z[:, 3] = 1.125                             # the next best
+    c = Case(dtype, 6, n, 0, 0, 2, True, None, z=z, targets=[17, 17, 17, 17, -1, -1])
+    dl, dh = np.array([1, -1, 1, 0.7, 0, 0], np.float32), np.array([0.5, 0.1, 0, -0.3, 0.25, 0], np.float32)
+    dt = np.array([[0, 0], [0, 0], [0, 0.6], [0.9, -0.7], [0, 0], [1, 0.4]], np.float32)
+    for k, a in (("dlogp", dl), ("dentropy", dh), ("dtop", dt)):
+        c.d[k].copy_(torch.from_numpy(a))
+    c.fwd()
+    c.bwd()
+    torch.cuda.synchronize()
+    got = c.d["dz"][:, 17].double().cpu().numpy()
+    t = np.delete(z.astype(np.float64), 17, 1) - lead
+    O, W = np.exp(t).sum(1), -(np.exp(t) * t).sum(1)
+    ls = np.log1p(O)
+    p = 1 / (1 + O)
+    g = dl.astype(np.float64) * (np.arange(6) < 4) + dt[:, 0] * p
+    others = dt[:, 1] * np.exp(1.125 - lead) * p
+    want = p * (g * O - others - dh * W * p)
+    rel = (3 * (lead + 1) + 5 + 92 + 12 + 8) * U
+    lim = rel * p * (np.abs(g) * O + np.abs(others) + np.abs(dh) * (W * p + 2 * ls))
+    if dtype == "bf16":
+        lim = lim + L.HALF16 * (np.abs(want) + lim)
+    assert np.all(np.abs(got - want) <= lim + L.TINY), (got, want, lim)
