@@ -153,7 +153,7 @@ __device__ __forceinline__ void lane_sums(const Piece<T>* p, float mx, float& o,
 
 // What a row gives once its maximum M, O = S - 1 and the weighted sum are known.
 struct RowSums {
-  float mx, ls, h;
+  float mx, sum, ls, h;
 };
 __device__ __forceinline__ RowSums row_sums(float mx, float o, float s) {
   RowSums r;
@@ -161,11 +161,17 @@ __device__ __forceinline__ RowSums row_sums(float mx, float o, float s) {
   // Nothing is left of a row of -inf alone: probabilities 0, entropy 0, log S -inf.
   const bool none = mx == -INFINITY && o == o;
   r.ls = none ? -INFINITY : mx == INFINITY ? NAN : log1pf(o);
-  r.h = none ? 0.f : r.ls - s / (1.f + o);
+  r.sum = mx == INFINITY ? NAN : 1.f + o;
+  r.h = none ? 0.f : r.ls - s / r.sum;
   return r;
 }
 __device__ __forceinline__ float row_logp(const RowSums& r, float z) {
   return z == -INFINITY && r.ls == r.ls ? -INFINITY : (z - r.mx) - r.ls;
+}
+
+// exp(row_logp), without the logarithm's rounding: that is 2^-20 of a probability of 1e-8.
+__device__ __forceinline__ float row_prob(const RowSums& r, float z) {
+  return z == -INFINITY && r.ls == r.ls ? 0.f : expf(z - r.mx) / r.sum;
 }
 
 template <typename T>
@@ -221,9 +227,9 @@ __device__ __forceinline__ int class_at(int first, int lane, int lanes, int e) {
 // Outputs of one of a row's best classes.
 __device__ __forceinline__ void give_top(const LogpFwd& b, const RowSums& r, size_t row, int rank,
                                          uint64_t key) {
-  const float lp = row_logp(r, value_of((uint32_t)(key >> 32)));
+  const float z = value_of((uint32_t)(key >> 32));
   b.top_ids[row * b.top + rank] = (int32_t)class_of(key);
-  b.top_values[row * b.top + rank] = b.probs ? expf(lp) : lp;
+  b.top_values[row * b.top + rank] = b.probs ? row_prob(r, z) : row_logp(r, z);
 }
 
 // ------------------------------------------------------------- narrow rows --

@@ -1,8 +1,8 @@
 """GPU parity of the token log-probabilities where single numbers decide: logits and
 masks of any magnitude, over whole stretches of a row and alone; NaN in a row's first
-class; the gradient of rows that are sure of their token.  The shapes reach what
-tests/test_gpu_token_logp.py leaves: stretches of the longest and the shortest kind,
-many blocks of the joining launch."""
+class; the gradient of rows that are sure of their token; probabilities far below 1.
+The shapes reach what tests/test_gpu_token_logp.py leaves: stretches of the longest
+and the shortest kind, many blocks of the joining launch."""
 import numpy as np
 import pytest
 import torch
@@ -136,3 +136,39 @@ def test_gradient_of_sure_rows(lead, n, dtype):
     if dtype == "bf16":
         lim = lim + L.HALF16 * (np.abs(want) + lim)
     assert np.all(np.abs(got - want) <= lim + L.TINY), (got, want, lim)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [2, 64, 1500, 70000])
+def test_small_probabilities(n, dtype):
+    """Probabilities of two classes t apart, t to 20 in eighths, the others ruled out: exp(z - M) / S with z - M
+    exact.  The power is off by 2 U of itself, the sum by U, its own power (at most 1.4 U, and fix and its product
+    1.5) and the quotient by U: 7, and 1 for what these leave out."""
+    print_case("token_logp small probabilities", n=n, dtype=dtype)
+    t = np.arange(161) / 8.0
+    z = np.full((161, n), -np.inf, np.float32)
+    z[:, n - 1], z[:, 0] = 0.5, 0.5 - t
+    c = Case(dtype, 161, n, 0, 0, 2, True, None, z=z)
+    c.fwd()
+    torch.cuda.synchronize()
+    got, x = c.d["top_values"].double().cpu().numpy(), np.exp(-t)
+    want = np.stack([1 / (1 + x), x / (1 + x)], 1)
+    far = np.abs(got - want) / (U * want)
+    assert np.all(far <= 8), (np.argwhere(far > 8)[:4], far.max())
+
+
+@pytest.mark.parametrize("n", [8, 1500, 70000])
+def test_probabilities_of_special_rows(n):
+    z = np.zeros((5, n), np.float32)
+    z[0] = -np.inf
+    z[1, 3] = np.nan
+    z[2, 4] = np.inf
+    z[3, 2:] = -np.inf
+    z[4, 2] = -3.38e38
+    c = Case("f32", 5, n, 0, 0, 8, True, None, z=z)
+    c.fwd()
+    torch.cuda.synchronize()
+    f = L.forward(z, None, 8, True)
+    got = c.d["top_values"].double().cpu().numpy()
+    assert np.array_equal(c.d["top_ids"].cpu().numpy(), f["top_ids"])
+    np.testing.assert_allclose(got, f["top_values"], rtol=8 * U, atol=0)
