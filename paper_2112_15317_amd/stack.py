@@ -51,11 +51,13 @@ def _plain(key, fn, *args):
 
 def _on(stream):
     """A context in which ``stream`` (a torch stream, a hipStream_t's number or None) is
-    torch's current one."""
+    torch's current one.  (ExternalStream(0) is a new stream and not the default one.)"""
     if stream is None:
         return contextlib.nullcontext()
-    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream)
-                             else torch.cuda.ExternalStream(stream))
+    if not isinstance(stream, torch.cuda.Stream):
+        number = sb._stream(stream)
+        stream = torch.cuda.ExternalStream(number) if number else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 def capture_graph(step_fn, steps=1):
