@@ -748,7 +748,8 @@ sb_status sb_expert_combine_bwd(const sb_expert_desc *desc, const void *dy,
  *   top_values  [m][top]       their log-probabilities, with SB_TOP_PROBS their
  *                              probabilities
  * All but z and dz fp32.  A logit of -inf is ruled out: probability 0, log-
- * probability -inf.  A row of -inf alone has stats (-inf, -inf), entropy 0,
+ * probability -inf; its dz is 0, or the gradient on its own log-probability where it
+ * has one.  A row of -inf alone has stats (-inf, -inf), entropy 0,
  * log-probabilities -inf, and dz 0.  A NaN or +inf in a row makes its
  * results NaN; NaN ranks above all classes.  m may be 0.
  * Sums run in a fixed order: repeated calls give bit-identical results.

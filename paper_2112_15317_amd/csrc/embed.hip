@@ -157,9 +157,10 @@ __device__ __forceinline__ void give_row(const EmbedBwd& b, float* out, int left
 // Few tokens, up to 64 H: a block has a token's columns, the blocks behind those rows to zero.
 // Every wave compares the token's id with all; where it is the first with that id, the waves
 // take the others by sixteens in turn, eight rows on their way at once, and the first adds up.
-// Latency bounds it; added to a table of 32000 x 2048, 128 tokens of bf16 take 3.4 us, as many of
-// one id 7.9.  256 tokens of different ids of 741 columns 4.7 us, of one id 15; by sorting, in
-// three launches, 17 and 16.  (512 take 5.6 and 26, by sorting 17 and 19.)
+// Latency bounds it; added to a table of 32000 x 2048, 128 tokens of bf16 take 3.2 us, as many of
+// one id 7.4.  256 tokens of 741 columns of bf16 4.0 us where their ids differ, 15 where they are
+// one; 257, by sorting in three launches, 15 and 13.  With a table of 12501 rows written whole 10
+// and 18.5, and 17 and 17.  (512 added at once take 5.6 and 26, by sorting 17 and 19.)
 constexpr int kFewTokens = 256;
 template <typename T, int H>
 __global__ __launch_bounds__(256) void embed_few_kernel(EmbedBwd b, int first, int segs,

@@ -38,7 +38,8 @@ constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 constexpr float kLeastPower = -1000.f; // in place of masked elements' -inf: 0 times it is 0
 // Largest magnitude of a maximum M whose sums take powers of 2 against M log2 e rounded: that is
 // off by 2^-4 at most, which a factor puts right.  (From 1.5e9 on it is off by up to 128, and a
-// power, or the factor, is infinite or 0.)
+// power, or the factor, is infinite or 0.  Larger ones take the sums against M itself: 2048 x
+// 32000 bf16 without alternatives 29.6 us below, 31.2 above.)
 constexpr float kMostSums = 0x1p20f;
 // The same for M itself taken from the logits, in the best classes and the gradient.
 constexpr float kMostPlain = 1e30f;
@@ -262,7 +263,7 @@ __device__ __forceinline__ void narrow_top_exact(const LogpFwd& b, const RowSums
 }
 
 // Instructions and the chain of a wave's steps bound it (4096 waves, four on a SIMD): 32768 x
-// 128 fp32 7.4 us without alternatives, 12.5 with the best eight.
+// 128 fp32 5 to 6 us without alternatives, 12.2 with the best eight, 9.8 of bf16.
 template <typename T>
 __global__ __launch_bounds__(256) void logp_narrow_fwd(LogpFwd b, int shift,
                                                        const T* __restrict__ z) {
